@@ -289,7 +289,101 @@ typedef struct { char name[48]; int64_t launches; double total_ms; double flops;
 HADFL_API hadfl_status hadfl_profile_enable(hadfl_ctx *ctx, int32_t on);
 HADFL_API hadfl_status hadfl_profile_read(hadfl_ctx *ctx, hadfl_kernel_time *out, int32_t cap, int32_t *n);
 
-HADFL_API const char *hadfl_last_error(const hadfl_ctx *ctx);   /* ctx may be NULL: error of the last failed init on this thread */
+/* ---- operators of a language model's head ------------------------------------------------------------------------
+ * For rows of parameters that the caller trains itself (HADFL_NET_NONE): layer norm, activation checkpoints in 8 bits and
+ * the softmax cross entropy over a large vocabulary, each with its gradient and grouped over replicas.  They need no
+ * context: sizes in a small host struct, device tensors of the caller, working memory of the size that the operator's
+ * _workspace call gives.  They enqueue on `stream` and return without waiting; nothing is allocated, kept between calls or
+ * read back.  Errors: EINVAL (text in hadfl_last_error(NULL)) for null or misaligned pointers, sizes and strides out of
+ * range; EDEVICE if a launch fails.  A workspace may serve one call at a time.
+ *
+ * A tensor is given as hadfl_rows: element (replica k, row t, column j) lies at data + k*replica_stride + t*row_stride + j,
+ * counted in elements; columns are contiguous.  Strides are non-negative; an input's may be zero (one tensor for all
+ * replicas, one row for all rows), an output's elements must be distinct (row_stride >= columns, replica_stride >=
+ * (rows - 1) * row_stride + columns).  For a vector per replica the row stride is ignored.  data needs the alignment of its
+ * element; 16-byte aligned tensors with strides of whole 16 bytes are read faster.
+ *   bf16 = 0: tensors of 32-bit floats; 1: the tensors marked (t) hold bf16, all others 32-bit floats.
+ * Limits: n_replicas in [1, 1024], n_rows in [0, 2^20], columns (features, inputs, outputs) in [1, 2^17],
+ * n_classes in [1, 2^20], n_replicas * n_rows at most 2^24. */
+typedef struct { void *data; int64_t replica_stride, row_stride; } hadfl_rows;
+
+/* Layer norm of every row: mean and variance over the n_features values, rstd = 1 / sqrt(variance + eps),
+ *   y = (x - mean) * rstd * gamma + beta.
+ * The gradient, with xh = (x - mean) * rstd and g = dy * gamma:
+ *   dx = rstd * (g - mean_j(g) - xh * mean_j(g * xh)),  dgamma = sum_t dy * xh,  dbeta = sum_t dy.
+ * All sums are in 32 bits, in an order that depends on the sizes alone.
+ *   x, y, dy, dx (t)     dev, [n_replicas][n_rows][n_features]; y may be x, dx may be dy (the same rows)
+ *   gamma, beta          dev, [n_replicas][n_features] floats
+ *   mean, rstd           dev, [n_replicas][n_rows] floats; outputs of the forward call (there both may be NULL), inputs
+ *                        of the gradient
+ *   packed               dev or NULL; the gradient call takes x from this 8-bit checkpoint (hadfl_pack_rows of the same
+ *                        n_replicas, n_rows, n_features) instead of from x, which may then be NULL
+ *   dgamma, dbeta        dev out, [n_replicas][n_features] floats
+ *   work                 dev, 256-byte aligned, the gradient's working memory */
+typedef struct { int32_t n_replicas, n_rows, n_features, bf16; float eps; } hadfl_norm;
+HADFL_API hadfl_status hadfl_norm_workspace(const hadfl_norm *norm, size_t *bytes);
+HADFL_API hadfl_status hadfl_norm_forward(const hadfl_norm *norm, const hadfl_rows *x, const hadfl_rows *gamma,
+                                          const hadfl_rows *beta, const hadfl_rows *y, float *mean, float *rstd, void *stream);
+HADFL_API hadfl_status hadfl_norm_backward(const hadfl_norm *norm, const hadfl_rows *dy, const hadfl_rows *x, const void *packed,
+                                           const hadfl_rows *gamma, const float *mean, const float *rstd,
+                                           const hadfl_rows *dx, const hadfl_rows *dgamma, const hadfl_rows *dbeta,
+                                           void *work, void *stream);
+
+/* Activation checkpoints in 8 bits.  Groups of 32 consecutive values of a row share a power of two 2^e, the least with
+ * max|x| <= 127 * 2^e (e >= -126), and every value becomes the nearest multiple q * 2^e, ties to even.  q * 2^e has at most
+ * eight significant bits: it is exact in bf16 and in fp32.  A group that holds an infinity or a NaN stands for NaNs.
+ * Layout of the checkpoint: q as int8 [n_replicas][n_rows][F], F = n_features rounded up to 32 (the surplus is zero), then
+ * at the next multiple of 256 bytes e + 127 as uint8 [n_replicas][n_rows][F / 32]; 255 marks a group of NaNs.
+ *   x (t)      dev, [n_replicas][n_rows][n_features]
+ *   packed     dev, 256-byte aligned, the bytes that hadfl_packed_bytes gives
+ *   out (t)    dev out, the values that the checkpoint stands for */
+typedef struct { int32_t n_replicas, n_rows, n_features, bf16; } hadfl_pack;
+HADFL_API hadfl_status hadfl_packed_bytes(const hadfl_pack *pack, size_t *bytes);
+HADFL_API hadfl_status hadfl_pack_rows(const hadfl_pack *pack, const hadfl_rows *x, void *packed, void *stream);
+HADFL_API hadfl_status hadfl_unpack_rows(const hadfl_pack *pack, const void *packed, const hadfl_rows *out, void *stream);
+
+/* The parameter gradients of a dense layer y = x W + b whose input was kept in 8 bits:
+ *   dW = x^T dy  ([n_in][n_out], the layout of a dense layer here),  db = sum_t dy,
+ * x the values that the checkpoint stands for.  Products of bf16 operands on the matrix cores, sums in 32 bits; a 32-bit dy
+ * enters as three bf16 parts, which hold it whole.
+ *   packed     dev, checkpoint of [n_replicas][n_rows][n_in]
+ *   dy (t)     dev, [n_replicas][n_rows][n_out]
+ *   dw         dev out, [n_replicas][n_in][n_out] floats
+ *   db         dev out or NULL, [n_replicas][n_out] floats
+ *   work       dev, 256-byte aligned */
+typedef struct { int32_t n_replicas, n_rows, n_in, n_out, bf16; } hadfl_dense;
+HADFL_API hadfl_status hadfl_dense_workspace(const hadfl_dense *dense, size_t *bytes);
+HADFL_API hadfl_status hadfl_dense_grad_packed(const hadfl_dense *dense, const void *packed, const hadfl_rows *dy,
+                                               const hadfl_rows *dw, const hadfl_rows *db, void *work, void *stream);
+
+/* Softmax cross entropy of a last dense layer over many classes, without its logits ever being kept: they are formed
+ * a piece of the vocabulary at a time, once for the loss and once more for the gradient.  With z = x W + b,
+ *   row_loss_t = log sum_v exp(z_tv) - z_t,label(t);   loss = mean of row_loss over the replica's labelled rows.
+ * A row whose label lies outside [0, n_classes) has no label: its row_loss is zero, it adds nothing to any gradient
+ * (whatever its x holds), and its dx is zero.  A replica without labelled rows has loss zero and zero gradients.  A bias of
+ * -inf takes a class out.  With G = (softmax(z) - onehot(label)) / (number of labelled rows):
+ *   dx = G W^T,  dW = x^T G,  db = sum_t G.
+ * fp32: operands enter the matrix products as three bf16 parts (six products), which keeps 32-bit accuracy for
+ * magnitudes below 2^104.  bf16: softmax(z) - onehot is rounded to bf16 for the two products, db is formed before that.
+ *   x (t)                 dev, [n_replicas][n_rows][n_features]
+ *   w (t)                 dev, [n_replicas][n_features][n_classes], the layout of a dense layer here
+ *   bias                  dev or NULL, [n_replicas][n_classes] floats
+ *   labels                dev, [n_replicas][n_rows] int32
+ *   loss                  dev out, [n_replicas] floats
+ *   row_loss              dev out or NULL, [n_replicas][n_rows] floats
+ *   dx (t), dw (t), db    dev out, like x, w, bias; each may be NULL and is then not computed
+ *   work                  dev, 256-byte aligned; hadfl_loss_workspace, grad = 1 for hadfl_loss_grad */
+typedef struct { int32_t n_replicas, n_rows, n_features, n_classes, bf16; } hadfl_loss;
+HADFL_API hadfl_status hadfl_loss_workspace(const hadfl_loss *shape, int32_t grad, size_t *bytes);
+HADFL_API hadfl_status hadfl_loss_forward(const hadfl_loss *shape, const hadfl_rows *x, const hadfl_rows *w,
+                                          const hadfl_rows *bias, const int32_t *labels, float *loss, float *row_loss,
+                                          void *work, void *stream);
+HADFL_API hadfl_status hadfl_loss_grad(const hadfl_loss *shape, const hadfl_rows *x, const hadfl_rows *w,
+                                       const hadfl_rows *bias, const int32_t *labels, float *loss, float *row_loss,
+                                       const hadfl_rows *dx, const hadfl_rows *dw, const hadfl_rows *db,
+                                       void *work, void *stream);
+
+HADFL_API const char *hadfl_last_error(const hadfl_ctx *ctx);   /* ctx may be NULL: error of the last failed call without a context on this thread */
 HADFL_API void hadfl_destroy(hadfl_ctx *ctx);                   /* frees host state only; NULL is a no-op */
 
 #ifdef __cplusplus

@@ -135,6 +135,12 @@ template <typename F> hadfl_status guard(hadfl_ctx* ctx, F&& body) noexcept
     }
 }
 
+}  // namespace
+
+hadfl_status hadfl::fail_call(hadfl_status st, const std::string& msg) { return fail(nullptr, st, msg); }
+
+namespace {
+
 #define HIP_TRY(ctx, expr) do { hipError_t e_ = (expr); if (e_ != hipSuccess) return hip_fail((ctx), e_, #expr); } while (0)
 
 // one replica's row <-> a dense host vector, segment by segment (the row pads every layer's slice to 256 bytes)

@@ -37,6 +37,9 @@ struct NetPlan {
     std::vector<Seg> segs;
 };
 
+// status and text of a call without a context, for hadfl_last_error(NULL) on this thread
+hadfl_status fail_call(hadfl_status st, const std::string& msg);
+
 hadfl_status build_plan(const hadfl_config& cfg, NetPlan& plan, std::string& err);
 
 }  // namespace hadfl

@@ -1,0 +1,133 @@
+// Activation checkpoints in 8 bits.  A group of 32 values x of a row shares 2^e, the least power of two with
+// max|x| <= 127 * 2^e: with max|x| = f * 2^k, f in [1/2, 1), that is e = k - 7, or k - 6 where f > 127/128 -- read off the
+// float's bits.  x * 2^-e is exact (e >= -126), so rounding it to the nearest integer, ties to even, is the only
+// rounding.  A power of two instead of max|x| / 127 costs up to one of the seven bits but makes q * 2^e a bf16 and an fp32
+// number, so that what reads the checkpoint need not round again.
+// Memory bound: 16 values a lane, two lanes a group; values and exponents are written once.
+#include "head.h"
+
+namespace hadfl {
+namespace head {
+
+namespace {
+
+constexpr int kLane = 16;          // values a lane packs
+
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void pack_rows_kernel(const T* x, long long rep, long long row, int rows, int cols, int chunks,
+                                                        long long total, int8_t* q, uint8_t* exps)
+{
+    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;          // (replica, row, chunk of 16)
+    const bool live = at < total;
+    const long long line = live ? at / chunks : 0;
+    const int c = live ? (int)(at - line * chunks) * kLane : 0;
+    const int k = (int)(line / rows), t = (int)(line - (long long)k * rows);
+    const T* src = x + k * rep + t * row + c;
+    float v[kLane];
+#pragma unroll
+    for (int i = 0; i < kLane; ++i) v[i] = 0.f;
+    if (live) {
+        if (VEC) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (c + 8 * h < cols) load8(src + 8 * h, v + 8 * h);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLane; ++i)
+                if (c + i < cols) v[i] = up(src[i]);
+        }
+    }
+    unsigned top = 0;                                                        // of |x|'s bits: orders like |x|, NaN above all
+#pragma unroll
+    for (int i = 0; i < kLane; ++i) top = max(top, __builtin_bit_cast(unsigned, v[i]) & 0x7fffffffu);
+    top = max(top, (unsigned)__shfl_xor((int)top, 1));
+    // biased exponent b: max|x| = 1.f * 2^(b - 127) = f * 2^(b - 126); e + 127 = b - 6, one more where 1.f > 127/64
+    const unsigned b = top >> 23;
+    int byte = (int)b - 6 + ((top & 0x7fffffu) > 0x7e0000u ? 1 : 0);
+    byte = max(byte, 1);
+    const bool poison = b == 255;
+    const float scale = __builtin_bit_cast(float, (unsigned)(254 - byte) << 23);
+    tiles::u4 out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        unsigned w = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int r = poison ? 0 : (int)__builtin_rintf(v[4 * i + j] * scale);
+            w |= (unsigned)(r & 255) << (8 * j);
+        }
+        out[i] = w;
+    }
+    if (!live) return;
+    *(tiles::u4*)(q + at * kLane) = out;
+    if ((threadIdx.x & 1) == 0) exps[at >> 1] = poison ? 255 : (uint8_t)byte;
+}
+
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void unpack_rows_kernel(Packed src, int rows, int cols, int chunks, long long total, T* out,
+                                                          long long rep, long long row)
+{
+    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (at >= total) return;
+    const long long line = at / chunks;
+    const int c = (int)(at - line * chunks) * kLane;
+    const int k = (int)(line / rows), t = (int)(line - (long long)k * rows);
+    T* dst = out + k * rep + t * row + c;
+    const tiles::u4 w = *(const tiles::u4*)(src.q + at * kLane);
+    const float unit = group_unit(src.e[at >> 1]);
+    float v[kLane];
+#pragma unroll
+    for (int i = 0; i < kLane; ++i) v[i] = (float)(int)(int8_t)(w[i / 4] >> (8 * (i % 4))) * unit;
+    if (VEC) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (c + 8 * h < cols) store8(dst + 8 * h, v + 8 * h);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kLane; ++i)
+            if (c + i < cols) dst[i] = (T)v[i];
+    }
+}
+
+}  // namespace
+
+hipError_t launch_pack(int n, int rows, int cols, int bf16, const Rows& x, void* packed, hipStream_t s)
+{
+    const Packed p = packed_of(packed, (long long)n * rows, cols);
+    const int chunks = (int)(p.cols / kLane);
+    const long long total = (long long)n * rows * chunks;
+    if (total == 0) return hipSuccess;
+    const unsigned grid = (unsigned)((total + 255) / 256);
+    const bool vec = chunked(x, bf16, cols);
+    int8_t* q = const_cast<int8_t*>(p.q);
+    uint8_t* e = const_cast<uint8_t*>(p.e);
+    if (bf16) {
+        auto* kernel = vec ? pack_rows_kernel<__bf16, true> : pack_rows_kernel<__bf16, false>;
+        kernel<<<grid, 256, 0, s>>>((const __bf16*)x.p, x.rep, x.row, rows, cols, chunks, total, q, e);
+    } else {
+        auto* kernel = vec ? pack_rows_kernel<float, true> : pack_rows_kernel<float, false>;
+        kernel<<<grid, 256, 0, s>>>((const float*)x.p, x.rep, x.row, rows, cols, chunks, total, q, e);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_unpack(int n, int rows, int cols, int bf16, const void* packed, const Rows& out, hipStream_t s)
+{
+    const Packed p = packed_of(packed, (long long)n * rows, cols);
+    const int chunks = (int)(p.cols / kLane);
+    const long long total = (long long)n * rows * chunks;
+    if (total == 0) return hipSuccess;
+    const unsigned grid = (unsigned)((total + 255) / 256);
+    const bool vec = chunked(out, bf16, cols);
+    if (bf16) {
+        auto* kernel = vec ? unpack_rows_kernel<__bf16, true> : unpack_rows_kernel<__bf16, false>;
+        kernel<<<grid, 256, 0, s>>>(p, rows, cols, chunks, total, (__bf16*)out.p, out.rep, out.row);
+    } else {
+        auto* kernel = vec ? unpack_rows_kernel<float, true> : unpack_rows_kernel<float, false>;
+        kernel<<<grid, 256, 0, s>>>(p, rows, cols, chunks, total, (float*)out.p, out.rep, out.row);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace head
+}  // namespace hadfl

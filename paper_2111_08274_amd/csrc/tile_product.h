@@ -1,0 +1,306 @@
+// Tiled matrix product on the matrix cores for operands as a caller has them: any size, stride and alignment, 32-bit floats,
+// bf16 or an 8-bit checkpoint.  C[m][n] = sum_k A(m, k) B(n, k), what becomes of C is up to an epilogue.
+//
+// An operand is a source of chunks of eight consecutive values; "along" says whether the contraction runs along a source's
+// rows (chunk = eight k of one m) or across them (chunk = eight m of one k).  Chunks go through registers, where what lies
+// outside becomes zero and floats become three bf16 planes, to LDS as they are; an operand across its rows is transposed by
+// the LDS read.  One slab of the contraction is in flight in registers while the one before is multiplied.
+#pragma once
+#include "head.h"
+
+namespace hadfl {
+namespace head {
+
+using namespace tiles;
+
+// rows without a label take no part, whatever they hold
+struct Labelled {
+    const int32_t* labels;         // null: every row does
+    int classes;
+    __device__ __forceinline__ bool at(int t) const { return !labels || (unsigned)labels[t] < (unsigned)classes; }
+};
+
+struct SourceF32 {
+    static constexpr int kPlanes = 3;
+    struct Raw { f4 a, b; };
+    const float* p;
+    long long rep, row;
+    int rows, cols;
+    bool vec;
+    Labelled live;
+    __device__ __forceinline__ void bind(int k) { p += k * rep; if (live.labels) live.labels += (long long)k * rows; }
+    __device__ __forceinline__ Raw load(int r, int c) const
+    {
+        Raw v = {};
+        if (r >= rows || c >= cols || !live.at(r)) return v;
+        const float* s = p + r * row + c;
+        if (vec) { v.a = *(const f4*)s; v.b = *(const f4*)(s + 4); return v; }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) if (c + e < cols) { if (e < 4) v.a[e] = s[e]; else v.b[e - 4] = s[e]; }
+        return v;
+    }
+    static __device__ __forceinline__ void planes(const Raw& v, u4 (&out)[3])
+    {
+        u2 h[2], m[2], l[2];
+        split3(v.a, h[0], m[0], l[0]);
+        split3(v.b, h[1], m[1], l[1]);
+        out[0] = join8(h[0], h[1]); out[1] = join8(m[0], m[1]); out[2] = join8(l[0], l[1]);
+    }
+};
+
+struct SourceBf16 {
+    static constexpr int kPlanes = 1;
+    struct Raw { u4 a; };
+    const __bf16* p;
+    long long rep, row;
+    int rows, cols;
+    bool vec;
+    Labelled live;
+    __device__ __forceinline__ void bind(int k) { p += k * rep; if (live.labels) live.labels += (long long)k * rows; }
+    __device__ __forceinline__ Raw load(int r, int c) const
+    {
+        Raw v = {};
+        if (r >= rows || c >= cols || !live.at(r)) return v;
+        const unsigned short* s = (const unsigned short*)(p + r * row + c);
+        if (vec) { v.a = *(const u4*)s; return v; }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) if (c + e < cols) v.a[e / 2] |= (unsigned)s[e] << (16 * (e % 2));
+        return v;
+    }
+    static __device__ __forceinline__ void planes(const Raw& v, u4 (&out)[1]) { out[0] = v.a; }
+};
+
+struct SourcePacked {              // rows and columns of one replica; the surplus columns of the checkpoint are zero
+    static constexpr int kPlanes = 1;
+    struct Raw { u2 q; unsigned e; };
+    Packed p;
+    int rows, cols;
+    __device__ __forceinline__ void bind(int k)
+    {
+        p.q += (long long)k * rows * p.cols;
+        p.e += (long long)k * rows * (p.cols / kGroup);
+    }
+    __device__ __forceinline__ Raw load(int r, int c) const
+    {
+        Raw v = {};
+        if (r >= rows || c >= p.cols) return v;
+        v.q = *(const u2*)(p.q + r * p.cols + c);
+        v.e = p.e[r * (p.cols / kGroup) + c / kGroup];
+        return v;
+    }
+    static __device__ __forceinline__ void planes(const Raw& v, u4 (&out)[1])
+    {
+        const float unit = group_unit(v.e);                    // q * 2^e has eight significant bits: exact in bf16
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = (float)(int)(int8_t)(v.q[e / 4] >> (8 * (e % 4))) * unit;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[0][e] = to_bf16x2(f[2 * e], f[2 * e + 1]);
+    }
+};
+
+// LDS image of one slab of an operand, one plane: along: [BR rows][KS + 8] (rows 16 bytes off a multiple of 32 banks' width),
+// across: [KS][BR] with rows 64 bytes apart modulo 256, so that the transposing read of 4 rows x 32 columns meets every
+// bank once
+template <bool ALONG, int BR, int KS> struct Image {
+    static constexpr unsigned kPitch = ALONG ? KS * 2 + 16 : BR * 2 + (64 + 256 - BR * 2 % 256) % 256;
+    static constexpr unsigned kPlane = ALONG ? BR * kPitch : KS * kPitch;
+    static constexpr int kAcross = ALONG ? KS / 8 : BR / 8;    // chunks in an image row
+    static constexpr int kChunks = BR * KS / 8;
+    // operand of the 32 rows from r0 and the 16 k of step ks
+    static __device__ __forceinline__ bf16x8 read(const char* plane, int r0, int ks, int lane)
+    {
+        if (ALONG) return *(const bf16x8*)(plane + (r0 + (lane & 31)) * kPitch + (ks * 16 + (lane >> 5) * 8) * 2);
+        const unsigned off = (ks * 16 + (lane >> 5) * 8 + (lane & 15) / 4) * kPitch + (r0 + ((lane >> 4) & 1) * 16 + 4 * (lane & 3)) * 2;
+        return lds_read_tr8(plane, off, kPitch);
+    }
+};
+
+// A wave's part of the tile, as an epilogue gets it.  LANE_M: a lane holds one m (m0 + 32 * tm + lane % 32) and the n
+// n0 + 32 * tn + 8 * (i / 4) + 4 * (lane / 32) + i % 4 of acc[tm][tn][i]; else n and m change places.
+template <int TM, int TN> struct Tile {
+    f16 acc[TM][TN];
+    int rep, split, m0, n0, lane;
+};
+
+template <class SA, bool A_ALONG, class SB, bool B_ALONG, int BM, int BN, int WM, int WN, int KS, int NBUF, bool LANE_M, class Epi>
+__global__ __launch_bounds__(WM * WN * 64) void product_kernel(SA a, SB b, int K, int tiles_m, int tiles_n, int splits, int split_len,
+                                                               int total, Epi epi)
+{
+    constexpr int NT = WM * WN * 64, TM = BM / WM / 32, TN = BN / WN / 32, PA = SA::kPlanes, PB = SB::kPlanes;
+    typedef Image<A_ALONG, BM, KS> IA;
+    typedef Image<B_ALONG, BN, KS> IB;
+    constexpr int NA = (IA::kChunks + NT - 1) / NT, NB = (IB::kChunks + NT - 1) / NT;
+    constexpr unsigned kBuf = PA * IA::kPlane + PB * IB::kPlane;
+    __shared__ __attribute__((aligned(16))) char smem[NBUF * kBuf];
+
+    const unsigned item = logical_block();
+    if (item >= (unsigned)total) return;
+    const int tm_i = item % tiles_m, r1 = item / tiles_m, tn_i = r1 % tiles_n, r2 = r1 / tiles_n;
+    Tile<TM, TN> t;
+    t.split = r2 % splits;
+    t.rep = r2 / splits;
+    a.bind(t.rep);
+    b.bind(t.rep);
+    const int tid = threadIdx.x, wave = tid / 64;
+    t.lane = tid & 63;
+    const int bm = tm_i * BM, bn = tn_i * BN, wm = (wave % WM) * TM * 32, wn = (wave / WM) * TN * 32;
+    t.m0 = bm + wm;
+    t.n0 = bn + wn;
+    const int k_begin = t.split * split_len, k_end = min(K, k_begin + split_len);
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) t.acc[i][j] = f16{};
+
+    typename SA::Raw ra[NA];
+    typename SB::Raw rb[NB];
+    auto fetch = [&](int k0) {
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const int id = tid + i * NT, r = id / IA::kAcross, c = id % IA::kAcross * 8;
+            if (IA::kChunks % NT == 0 || id < IA::kChunks) ra[i] = A_ALONG ? a.load(bm + r, k0 + c) : a.load(k0 + r, bm + c);
+        }
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const int id = tid + i * NT, r = id / IB::kAcross, c = id % IB::kAcross * 8;
+            if (IB::kChunks % NT == 0 || id < IB::kChunks) rb[i] = B_ALONG ? b.load(bn + r, k0 + c) : b.load(k0 + r, bn + c);
+        }
+    };
+    auto store = [&](char* buf) {
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const int id = tid + i * NT, r = id / IA::kAcross, c = id % IA::kAcross;
+            if (IA::kChunks % NT == 0 || id < IA::kChunks) {
+                u4 p[PA];
+                SA::planes(ra[i], p);
+#pragma unroll
+                for (int s = 0; s < PA; ++s) *(u4*)(buf + s * IA::kPlane + r * IA::kPitch + c * 16) = p[s];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const int id = tid + i * NT, r = id / IB::kAcross, c = id % IB::kAcross;
+            if (IB::kChunks % NT == 0 || id < IB::kChunks) {
+                u4 p[PB];
+                SB::planes(rb[i], p);
+#pragma unroll
+                for (int s = 0; s < PB; ++s) *(u4*)(buf + PA * IA::kPlane + s * IB::kPlane + r * IB::kPitch + c * 16) = p[s];
+            }
+        }
+    };
+    auto multiply = [&](const char* buf) {
+#pragma unroll
+        for (int ks = 0; ks < KS / 16; ++ks) {
+            bf16x8 fa[TM][PA], fb[TN][PB];
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int s = 0; s < PA; ++s) fa[i][s] = IA::read(buf + s * IA::kPlane, wm + 32 * i, ks, t.lane);
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int s = 0; s < PB; ++s) fb[j][s] = IB::read(buf + PA * IA::kPlane + s * IB::kPlane, wn + 32 * j, ks, t.lane);
+            // planes i and j with i + j <= 2: what is left out is below 2^-24 of the product
+#pragma unroll
+            for (int sum = 2; sum >= 0; --sum)                  // the small products first
+#pragma unroll
+                for (int s = 0; s < PA; ++s) {
+                    if (sum - s < 0 || sum - s >= PB) continue;
+#pragma unroll
+                    for (int i = 0; i < TM; ++i)
+#pragma unroll
+                        for (int j = 0; j < TN; ++j)
+                            t.acc[i][j] = LANE_M ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j][sum - s], fa[i][s], t.acc[i][j], 0, 0, 0)
+                                                 : __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i][s], fb[j][sum - s], t.acc[i][j], 0, 0, 0);
+                }
+        }
+    };
+
+    if (k_begin < k_end) fetch(k_begin);
+    for (int k0 = k_begin, n = 0; k0 < k_end; k0 += KS, ++n) {
+        char* buf = smem + (NBUF == 2 ? (n & 1) * kBuf : 0);
+        if (NBUF == 1 && n) __syncthreads();                   // the slab before has been read
+        store(buf);
+        __syncthreads();
+        if (k0 + KS < k_end) fetch(k0 + KS);
+        multiply(buf);
+    }
+    constexpr float kScale = (PA == 3 ? 0x1p-24f : 1.f) * (PB == 3 ? 0x1p-24f : 1.f);
+    if (kScale != 1.f) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) t.acc[i][j] *= kScale;
+    }
+    epi(t);
+}
+
+// ---- epilogues that only store ---------------------------------------------------------------------------------
+// C to a tensor, times a factor per replica (lanes along n)
+template <typename T> struct StoreTile {
+    static constexpr bool kLaneM = false;
+    T* p;
+    long long rep, row;
+    const float* factor;           // [replicas] or null
+    int M, N;
+    template <int TM, int TN> __device__ __forceinline__ void operator()(const Tile<TM, TN>& t) const
+    {
+        const float f = factor ? factor[t.rep] : 1.f;
+        T* out = p + t.rep * rep;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const int n = t.n0 + 32 * j + (t.lane & 31);
+                if (n >= N) continue;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int m = t.m0 + 32 * i + 8 * (e / 4) + 4 * (t.lane >> 5) + e % 4;
+                    if (m < M) out[m * row + n] = (T)(t.acc[i][j][e] * f);
+                }
+            }
+    }
+};
+// C into [split][replica][M][ld] floats, over or onto what is there
+struct StoreShare {
+    static constexpr bool kLaneM = false;
+    float* p;
+    int M, N, ld, replicas;
+    bool onto;
+    template <int TM, int TN> __device__ __forceinline__ void operator()(const Tile<TM, TN>& t) const
+    {
+        float* out = p + ((long long)t.split * replicas + t.rep) * M * ld;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const int n = t.n0 + 32 * j + (t.lane & 31);
+                if (n >= N) continue;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int m = t.m0 + 32 * i + 8 * (e / 4) + 4 * (t.lane >> 5) + e % 4;
+                    if (m >= M) continue;
+                    float* q = out + (long long)m * ld + n;
+                    *q = onto ? *q + t.acc[i][j][e] : t.acc[i][j][e];
+                }
+            }
+    }
+};
+
+template <int BM, int BN, int WM, int WN, bool A_ALONG, bool B_ALONG, class SA, class SB, class Epi>
+hipError_t launch_product(const SA& a, const SB& b, int replicas, int M, int N, int K, int splits, int split_len, const Epi& epi, hipStream_t s)
+{
+    constexpr bool wide = SA::kPlanes == 3 || SB::kPlanes == 3;
+    constexpr int KS = BM == 32 && !wide ? 64 : 32, NBUF = wide ? 1 : 2;
+    const int tm = (M + BM - 1) / BM, tn = (N + BN - 1) / BN;
+    const long long total = (long long)replicas * splits * tm * tn;
+    if (total == 0) return hipSuccess;
+    if (total > 0x7fffff00ll) return hipErrorInvalidValue;
+    product_kernel<SA, A_ALONG, SB, B_ALONG, BM, BN, WM, WN, KS, NBUF, Epi::kLaneM, Epi>
+        <<<die_grid(total), WM * WN * 64, 0, s>>>(a, b, K, tm, tn, splits, split_len, (int)total, epi);
+    return hipGetLastError();
+}
+
+}  // namespace head
+}  // namespace hadfl

@@ -40,6 +40,26 @@ class HadflKernelTime(ctypes.Structure):
                 ("flops", ctypes.c_double), ("bytes", ctypes.c_double)]
 
 
+class HadflRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("replica_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64)]
+
+
+class HadflNorm(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_replicas", "n_rows", "n_features", "bf16")] + [("eps", ctypes.c_float)]
+
+
+class HadflPack(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_replicas", "n_rows", "n_features", "bf16")]
+
+
+class HadflDense(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_replicas", "n_rows", "n_in", "n_out", "bf16")]
+
+
+class HadflLoss(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_replicas", "n_rows", "n_features", "n_classes", "bf16")]
+
+
 OPT_SIDE_STREAM, OPT_TILE_HINT = 0, 1
 
 EXPORTS = ("hadfl_param_count", "hadfl_param_layout", "hadfl_workspace_bytes", "hadfl_init_replicas",
@@ -49,7 +69,10 @@ EXPORTS = ("hadfl_param_count", "hadfl_param_layout", "hadfl_workspace_bytes", "
            "hadfl_select_group", "hadfl_aggregate_group", "hadfl_predict_versions",
            "hadfl_select_real", "hadfl_get_predicted", "hadfl_get_steps", "hadfl_get_versions",
            "hadfl_get_selected", "hadfl_get_params", "hadfl_get_losses", "hadfl_profile_enable",
-           "hadfl_profile_read", "hadfl_last_error", "hadfl_destroy")
+           "hadfl_profile_read", "hadfl_last_error", "hadfl_destroy",
+           "hadfl_norm_workspace", "hadfl_norm_forward", "hadfl_norm_backward", "hadfl_packed_bytes", "hadfl_pack_rows",
+           "hadfl_unpack_rows", "hadfl_dense_workspace", "hadfl_dense_grad_packed", "hadfl_loss_workspace",
+           "hadfl_loss_forward", "hadfl_loss_grad")
 
 _lib = None
 
@@ -100,6 +123,19 @@ def lib():
         L.hadfl_get_losses.argtypes = [vp, vp]
         L.hadfl_profile_enable.argtypes = [vp, i32]
         L.hadfl_profile_read.argtypes = [vp, ctypes.POINTER(HadflKernelTime), i32, ctypes.POINTER(i32)]
+        sizep, rowsp = ctypes.POINTER(ctypes.c_size_t), ctypes.POINTER(HadflRows)
+        normp, packp, densep, lossp = (ctypes.POINTER(t) for t in (HadflNorm, HadflPack, HadflDense, HadflLoss))
+        L.hadfl_norm_workspace.argtypes = [normp, sizep]
+        L.hadfl_norm_forward.argtypes = [normp, rowsp, rowsp, rowsp, rowsp, vp, vp, vp]
+        L.hadfl_norm_backward.argtypes = [normp, rowsp, rowsp, vp, rowsp, vp, vp, rowsp, rowsp, rowsp, vp, vp]
+        L.hadfl_packed_bytes.argtypes = [packp, sizep]
+        L.hadfl_pack_rows.argtypes = [packp, rowsp, vp, vp]
+        L.hadfl_unpack_rows.argtypes = [packp, vp, rowsp, vp]
+        L.hadfl_dense_workspace.argtypes = [densep, sizep]
+        L.hadfl_dense_grad_packed.argtypes = [densep, vp, rowsp, rowsp, rowsp, vp, vp]
+        L.hadfl_loss_workspace.argtypes = [lossp, i32, sizep]
+        L.hadfl_loss_forward.argtypes = [lossp, rowsp, rowsp, rowsp, vp, vp, vp, vp, vp]
+        L.hadfl_loss_grad.argtypes = [lossp, rowsp, rowsp, rowsp, vp, vp, vp, rowsp, rowsp, rowsp, vp, vp]
         L.hadfl_last_error.argtypes = [vp]
         L.hadfl_last_error.restype = ctypes.c_char_p
         L.hadfl_destroy.argtypes = [vp]
@@ -353,3 +389,173 @@ class Context:
         _check(lib().hadfl_profile_read(self.h, rows, 4096, ctypes.byref(n)), self.h)
         return {rows[i].name.decode(): dict(launches=rows[i].launches, ms=rows[i].total_ms, flops=rows[i].flops,
                                             bytes=rows[i].bytes) for i in range(min(n.value, 4096))}
+
+
+# ---- operators of a language model's head ----------------------------------------------------------------------------
+class _Operator:
+    """Sizes, types and working memory of one operator on the current torch device.  Its tensors are torch device tensors
+    [replica, row, column] (or [replica, column] for vectors) whose columns are contiguous; other strides are free.  Calls go
+    to `stream` or to the current one, and the tensors have to be ready there; calls of one object share its working memory
+    and must not overlap in time.  Outputs that are not given are allocated."""
+
+    def __init__(self, desc, bf16, workspace=None):
+        import torch
+        self.torch, self.desc = torch, desc
+        self.device = torch.device("cuda", torch.cuda.current_device())
+        self.dtype = torch.bfloat16 if bf16 else torch.float32
+        self._ref = ctypes.byref(desc)
+        self._names = {}
+        self.work = None
+        if workspace is not None:
+            self.work = self._bytes(workspace)
+
+    def _bytes(self, query):
+        n = ctypes.c_size_t()
+        _check(query(self._ref, ctypes.byref(n)))
+        return self.torch.empty(n.value, dtype=self.torch.uint8, device=self.device)
+
+    def _rows(self, name, t, shape, dtype):
+        """The hadfl_rows of a tensor, checked; None stays None."""
+        if t is None:
+            return None
+        if t.dtype != dtype or t.device != self.device or tuple(t.shape) != shape:
+            raise HadflError(EINVAL, "%s must be %s %s on %s, not %s %s on %s" % (name, dtype, shape, self.device, t.dtype, tuple(t.shape), t.device))
+        st = t.stride()
+        if shape[-1] > 1 and st[-1] != 1:
+            raise HadflError(EINVAL, "%s: the columns must be contiguous" % name)
+        r = self._names.get(name)
+        if r is None:
+            r = self._names[name] = HadflRows()
+        r.data, r.replica_stride, r.row_stride = t.data_ptr() or None, st[0], (st[1] if len(shape) == 3 else 0)
+        return r
+
+    def _plain(self, name, t, shape, dtype):
+        """The address of a contiguous tensor, checked."""
+        if t is None:
+            return None
+        if t.dtype != dtype or t.device != self.device or tuple(t.shape) != shape or not t.is_contiguous():
+            raise HadflError(EINVAL, "%s must be contiguous %s %s on %s" % (name, dtype, shape, self.device))
+        return t.data_ptr() or None
+
+    def _out(self, t, shape, dtype):
+        return self.torch.empty(shape, dtype=dtype, device=self.device) if t is None else t
+
+    def _stream(self, stream):
+        return (self.torch.cuda.current_stream(self.device) if stream is None else stream).cuda_stream
+
+
+class LayerNorm(_Operator):
+    """Layer norm of [n_replicas, n_rows, n_features] with gamma, beta [n_replicas, n_features] (32-bit), and its gradient.
+    forward() leaves the rows' statistics in `mean` and `rstd` for backward()."""
+
+    def __init__(self, n_replicas, n_rows, n_features, bf16=0, eps=1e-5):
+        super().__init__(HadflNorm(int(n_replicas), int(n_rows), int(n_features), int(bf16), float(eps)), bf16, lib().hadfl_norm_workspace)
+        self.shape, self.vector = (int(n_replicas), int(n_rows), int(n_features)), (int(n_replicas), int(n_features))
+        f32 = self.torch.float32
+        self.mean = self.torch.empty(self.shape[:2], dtype=f32, device=self.device)
+        self.rstd = self.torch.empty(self.shape[:2], dtype=f32, device=self.device)
+
+    def forward(self, x, gamma, beta, y=None, stream=None):
+        f32 = self.torch.float32
+        y = self._out(y, self.shape, self.dtype)
+        _check(lib().hadfl_norm_forward(self._ref, self._rows("x", x, self.shape, self.dtype), self._rows("gamma", gamma, self.vector, f32),
+                                        self._rows("beta", beta, self.vector, f32), self._rows("y", y, self.shape, self.dtype),
+                                        self.mean.data_ptr() or None, self.rstd.data_ptr() or None, self._stream(stream)))
+        return y
+
+    def backward(self, dy, x, gamma, dx=None, dgamma=None, dbeta=None, stream=None):
+        """x: the tensor given to forward() or the PackedRows that holds it.  -> dx, dgamma, dbeta"""
+        f32 = self.torch.float32
+        dx, dgamma, dbeta = self._out(dx, self.shape, self.dtype), self._out(dgamma, self.vector, f32), self._out(dbeta, self.vector, f32)
+        packed = None
+        if isinstance(x, PackedRows):
+            if x.shape != self.shape:
+                raise HadflError(EINVAL, "the checkpoint holds %s, not %s" % (x.shape, self.shape))
+            x, packed = None, x.data.data_ptr()
+        _check(lib().hadfl_norm_backward(self._ref, self._rows("dy", dy, self.shape, self.dtype), self._rows("x", x, self.shape, self.dtype),
+                                         packed, self._rows("gamma", gamma, self.vector, f32), self.mean.data_ptr() or None,
+                                         self.rstd.data_ptr() or None, self._rows("dx", dx, self.shape, self.dtype),
+                                         self._rows("dgamma", dgamma, self.vector, f32), self._rows("dbeta", dbeta, self.vector, f32),
+                                         self.work.data_ptr(), self._stream(stream)))
+        return dx, dgamma, dbeta
+
+
+class PackedRows(_Operator):
+    """An activation checkpoint in 8 bits of [n_replicas, n_rows, n_features]; bf16: the type that pack() reads and unpack()
+    writes."""
+
+    def __init__(self, n_replicas, n_rows, n_features, bf16=0):
+        super().__init__(HadflPack(int(n_replicas), int(n_rows), int(n_features), int(bf16)), bf16)
+        self.shape = (int(n_replicas), int(n_rows), int(n_features))
+        self.data = self._bytes(lib().hadfl_packed_bytes)
+
+    def pack(self, x, stream=None):
+        _check(lib().hadfl_pack_rows(self._ref, self._rows("x", x, self.shape, self.dtype), self.data.data_ptr(), self._stream(stream)))
+        return self
+
+    def unpack(self, out=None, stream=None):
+        out = self._out(out, self.shape, self.dtype)
+        _check(lib().hadfl_unpack_rows(self._ref, self.data.data_ptr(), self._rows("out", out, self.shape, self.dtype), self._stream(stream)))
+        return out
+
+
+class DenseGrad(_Operator):
+    """dW [n_replicas, n_in, n_out] and db [n_replicas, n_out] (32-bit) of a dense layer from its input's PackedRows and dy
+    [n_replicas, n_rows, n_out]."""
+
+    def __init__(self, n_replicas, n_rows, n_in, n_out, bf16=0):
+        super().__init__(HadflDense(int(n_replicas), int(n_rows), int(n_in), int(n_out), int(bf16)), bf16, lib().hadfl_dense_workspace)
+        self.n, self.rows, self.n_in, self.n_out = int(n_replicas), int(n_rows), int(n_in), int(n_out)
+
+    def backward(self, packed, dy, dw=None, db=None, bias=True, stream=None):
+        """-> dw, db; bias=False leaves db out (None)"""
+        f32 = self.torch.float32
+        if packed.shape != (self.n, self.rows, self.n_in):
+            raise HadflError(EINVAL, "the checkpoint holds %s, not %s" % (packed.shape, (self.n, self.rows, self.n_in)))
+        dw = self._out(dw, (self.n, self.n_in, self.n_out), f32)
+        db = self._out(db, (self.n, self.n_out), f32) if bias else None
+        _check(lib().hadfl_dense_grad_packed(self._ref, packed.data.data_ptr(), self._rows("dy", dy, (self.n, self.rows, self.n_out), self.dtype),
+                                             self._rows("dw", dw, (self.n, self.n_in, self.n_out), f32),
+                                             self._rows("db", db, (self.n, self.n_out), f32), self.work.data_ptr(), self._stream(stream)))
+        return dw, db
+
+
+class ClassLoss(_Operator):
+    """Softmax cross entropy of a last dense layer over many classes, the logits never kept: x [n_replicas, n_rows,
+    n_features], w [n_replicas, n_features, n_classes], bias [n_replicas, n_classes] (32-bit) or None, labels [n_replicas,
+    n_rows] int32; a label outside [0, n_classes) marks a row that takes no part."""
+
+    def __init__(self, n_replicas, n_rows, n_features, n_classes, bf16=0, grad=True):
+        desc = HadflLoss(int(n_replicas), int(n_rows), int(n_features), int(n_classes), int(bf16))
+        query = lib().hadfl_loss_workspace
+        super().__init__(desc, bf16, lambda ref, out: query(ref, int(bool(grad)), out))
+        self.n, self.rows, self.features, self.classes, self.with_grad = int(n_replicas), int(n_rows), int(n_features), int(n_classes), bool(grad)
+
+    def _inputs(self, x, w, labels, bias, row_loss, loss):
+        f32, i32 = self.torch.float32, self.torch.int32
+        return (self._ref, self._rows("x", x, (self.n, self.rows, self.features), self.dtype),
+                self._rows("w", w, (self.n, self.features, self.classes), self.dtype), self._rows("bias", bias, (self.n, self.classes), f32),
+                self._plain("labels", labels, (self.n, self.rows), i32), self._plain("loss", loss, (self.n,), f32),
+                self._plain("row_loss", row_loss, (self.n, self.rows), f32))
+
+    def loss(self, x, w, labels, bias=None, loss=None, row_loss=None, stream=None):
+        """-> loss [n_replicas] (mean over the labelled rows), row_loss [n_replicas, n_rows]"""
+        f32 = self.torch.float32
+        loss, row_loss = self._out(loss, (self.n,), f32), self._out(row_loss, (self.n, self.rows), f32)
+        _check(lib().hadfl_loss_forward(*self._inputs(x, w, labels, bias, row_loss, loss), self.work.data_ptr(), self._stream(stream)))
+        return loss, row_loss
+
+    def grad(self, x, w, labels, bias=None, loss=None, row_loss=None, dx=None, dw=None, db=None, want=("dx", "dw", "db"), stream=None):
+        """-> loss, row_loss, dx, dw, db of the mean losses; what `want` leaves out, and db without a bias, is None"""
+        if not self.with_grad:
+            raise HadflError(ESTATE, "this ClassLoss was made with grad=False")
+        f32 = self.torch.float32
+        loss, row_loss = self._out(loss, (self.n,), f32), self._out(row_loss, (self.n, self.rows), f32)
+        dx = self._out(dx, (self.n, self.rows, self.features), self.dtype) if "dx" in want else None
+        dw = self._out(dw, (self.n, self.features, self.classes), self.dtype) if "dw" in want else None
+        db = self._out(db, (self.n, self.classes), f32) if "db" in want and bias is not None else None
+        _check(lib().hadfl_loss_grad(*self._inputs(x, w, labels, bias, row_loss, loss),
+                                     self._rows("dx", dx, (self.n, self.rows, self.features), self.dtype),
+                                     self._rows("dw", dw, (self.n, self.features, self.classes), self.dtype),
+                                     self._rows("db", db, (self.n, self.classes), f32), self.work.data_ptr(), self._stream(stream)))
+        return loss, row_loss, dx, dw, db

@@ -1,0 +1,426 @@
+"""Layer norm, 8-bit checkpoints, a dense layer's gradient from them and the loss over a large vocabulary on the GPU against
+the same in 64 bits (head_ref.py).  Tensors lie inside larger buffers: inputs between NaNs, outputs between marks that must
+survive, at offsets and strides that divide by nothing or by 16 bytes.  Bounds are worst cases of 32-bit sums and single
+roundings to bf16, from the sizes and the operands' magnitudes alone."""
+import numpy as np
+import pytest
+
+from paper_2111_08274_amd import hadfl
+from tests import head_ref as ref
+
+pytestmark = pytest.mark.gpu
+MARK = 77.0
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _dtype(bf16):
+    return _torch().bfloat16 if bf16 else _torch().float32
+
+
+class Inside:
+    """A tensor [n][rows][cols] (or [n][cols]) as a view into a larger buffer: "whole" contiguous, "padded" with aligned strides,
+    "odd" at an odd element with odd strides."""
+
+    def __init__(self, shape, dtype, layout, fill):
+        torch = _torch()
+        n, cols = shape[0], shape[-1]
+        rows = shape[1] if len(shape) == 3 else 1
+        row, off, gap = {"whole": (cols, 0, 0), "padded": (-(-cols // 8) * 8 + 16, 32, 64), "odd": (cols + 3, 5, 7)}[layout]
+        rep = rows * row + gap
+        self.flat = torch.full((off + n * rep + 64,), fill, dtype=dtype, device="cuda")
+        strides = (rep, row, 1) if len(shape) == 3 else (rep, 1)
+        self.t = self.flat.as_strided(shape, strides, off)
+        self.own = torch.zeros(self.flat.shape, dtype=torch.bool, device="cuda")
+        self.own.as_strided(shape, strides, off).fill_(True)
+
+    def put(self, values):
+        self.t.copy_(_torch().as_tensor(np.ascontiguousarray(values)).to(self.t.dtype))
+        return self.t
+
+    def get(self):
+        return self.t.double().cpu().numpy()
+
+    def untouched(self):
+        return bool((self.flat[~self.own] == MARK).all())
+
+
+def _in(values, bf16, layout):
+    values = np.asarray(values)
+    return Inside(values.shape, _dtype(bf16), layout, float("nan")).put(values)
+
+
+def _out(shape, bf16, layout):
+    return Inside(shape, _dtype(bf16), layout, MARK)
+
+
+def _values(t):
+    return t.double().cpu().numpy()
+
+
+def _check(got, want, bound, what):
+    assert np.isfinite(got).all(), what
+    off = np.abs(got - want) - bound
+    assert (off <= 0).all(), "%s: off by %.3g where %.3g is allowed" % (what, np.abs(got - want).flat[off.argmax()], np.broadcast_to(bound, got.shape).flat[off.argmax()])
+
+
+# ---- layer norm --------------------------------------------------------------------------------------------------------
+NORM = [(1, 1, 1), (1, 1, 512), (2, 3, 7), (3, 17, 33), (2, 40, 128), (2, 41, 129), (3, 70, 512), (1, 130, 520), (2, 9, 1111), (2, 5, 2048),
+        (1, 6, 2056), (2, 3, 4096), (1, 3, 5001), (1, 2, 8192), (2, 3, 8193), (1, 2, 10007), (5, 300, 64)]
+
+
+def _norm_case(n, rows, cols, bf16, layout, seed=0):
+    rng = np.random.default_rng(seed)
+    x = rng.normal(size=(n, rows, cols)) * rng.uniform(0.1, 3, size=(n, rows, 1)) + rng.normal(size=(n, rows, 1))
+    if rows > 1:
+        x[0, 1] = 1.5                                   # a constant row: variance zero
+    return dict(x=_in(x, bf16, layout), dy=_in(rng.normal(size=x.shape), bf16, layout),
+                gamma=_in(rng.normal(size=(n, cols)) * 0.3 + 1, 0, layout), beta=_in(rng.normal(size=(n, cols)), 0, layout))
+
+
+def _norm_bounds(c, x, mean, rstd, cols, rows, bf16):
+    """x: what the backward pass sees"""
+    e, out = ref.EPS32, ref.HALF_BF16 if bf16 else ref.EPS32
+    gamma, beta, dy = (np.abs(_values(c[k])) for k in ("gamma", "beta", "dy"))
+    gamma, beta = gamma[:, None], beta[:, None]
+    xf = np.abs(_values(c["x"]))
+    # the mean of cols values is off by (cols + 16) roundings of the mean magnitude at most, the spread likewise
+    merr = (cols + 16) * e * xf.mean(-1, keepdims=True)
+    rrel = (cols + 16) * e + merr ** 2 * rstd ** 2 + merr * rstd * (cols + 16) * e + 4 * e
+    xh = np.abs((x - mean) * rstd)
+    xherr = (merr + e * (np.abs(x) + np.abs(mean))) * rstd + xh * (rrel + 4 * e)
+    g = dy * gamma
+    y = gamma * xherr + 4 * e * (gamma * xh + beta)
+    m1, m2 = (cols + 16) * e * g.mean(-1, keepdims=True), ((cols + 16) * e * g * xh + g * xherr).mean(-1, keepdims=True)
+    both = g.mean(-1, keepdims=True) + xh * (g * xh).mean(-1, keepdims=True)
+    dx = rstd * (m1 + xh * m2 + xherr * (g * xh).mean(-1, keepdims=True) + 8 * e * (g + both)) + rrel * rstd * (g + both)
+    return dict(y=y, dx=dx, out=out, dgamma=((rows + 16) * e * dy * xh + dy * xherr).sum(1), dbeta=((rows + 16) * e * dy).sum(1))
+
+
+@pytest.mark.parametrize("layout", ["whole", "padded", "odd"])
+@pytest.mark.parametrize("bf16", [0, 1])
+@pytest.mark.parametrize("n,rows,cols", NORM)
+@pytest.mark.parametrize("packed", [False, True])
+def test_layer_norm_and_its_gradient(n, rows, cols, bf16, layout, packed):
+    c = _norm_case(n, rows, cols, bf16, layout)
+    plan = hadfl.LayerNorm(n, rows, cols, bf16=bf16)
+    y, dx = _out((n, rows, cols), bf16, layout), _out((n, rows, cols), bf16, layout)
+    dg, db = _out((n, cols), 0, layout), _out((n, cols), 0, layout)
+    plan.forward(c["x"], c["gamma"], c["beta"], y=y.t)
+    kept = hadfl.PackedRows(n, rows, cols, bf16=bf16).pack(c["x"]) if packed else c["x"]
+    plan.backward(c["dy"], kept, c["gamma"], dx=dx.t, dgamma=dg.t, dbeta=db.t)
+    x, gamma, beta, dy = (_values(c[k]) for k in ("x", "gamma", "beta", "dy"))
+    want_y, mean, rstd = ref.layer_norm(x, gamma[:, None], beta[:, None], np.float32(1e-5))
+    seen = ref.checkpoint(x)[0] if packed else x
+    want_dx, want_dg, want_db = ref.layer_norm_grad(dy, seen, gamma[:, None], mean, rstd)
+    b = _norm_bounds(c, seen, mean, rstd, cols, rows, bf16)
+    _check(y.get(), want_y, b["y"] + b["out"] * np.abs(want_y), "y")
+    _check(dx.get(), want_dx, b["dx"] + b["out"] * np.abs(want_dx), "dx")
+    _check(dg.get(), want_dg, b["dgamma"], "dgamma")
+    _check(db.get(), want_db, b["dbeta"], "dbeta")
+    assert all(o.untouched() for o in (y, dx, dg, db))
+
+
+def test_layer_norm_in_place_and_without_rows():
+    torch = _torch()
+    for bf16 in (0, 1):
+        for cols in (512, 9001):
+            c = _norm_case(2, 33, cols, bf16, "whole")
+            plan = hadfl.LayerNorm(2, 33, cols, bf16=bf16)
+            y = plan.forward(c["x"], c["gamma"], c["beta"])
+            dx, dg, db = plan.backward(c["dy"], c["x"], c["gamma"])
+            dy = c["dy"].clone()
+            again = plan.backward(dy, c["x"], c["gamma"], dx=dy)
+            assert all(torch.equal(p, q) for p, q in zip((dx, dg, db), again))
+            x = c["x"].clone()
+            assert torch.equal(plan.forward(x, c["gamma"], c["beta"], y=x), y)
+    empty = torch.empty((2, 0, 64), device="cuda")
+    plan = hadfl.LayerNorm(2, 0, 64)
+    g = torch.ones((2, 64), device="cuda")
+    assert plan.forward(empty, g, g).shape == (2, 0, 64)
+    for kept in (empty, hadfl.PackedRows(2, 0, 64).pack(empty)):
+        _, dg, db = plan.backward(empty, kept, g)
+        assert not dg.any() and not db.any()
+
+
+def test_layer_norm_of_one_row_for_all_and_a_row_of_nans():
+    torch = _torch()
+    c = _norm_case(2, 5, 200, 0, "whole")
+    plan = hadfl.LayerNorm(2, 5, 200)
+    shared = c["x"][:1, :1].expand(2, 5, 200)                     # strides of zero
+    assert torch.equal(plan.forward(shared, c["gamma"], c["beta"]), plan.forward(shared.contiguous(), c["gamma"], c["beta"]))
+    y = plan.forward(c["x"], c["gamma"], c["beta"])
+    x = c["x"].clone()
+    x[1, 2, 17] = float("nan")
+    x[0, 4, 3] = float("inf")
+    z = plan.forward(x, c["gamma"], c["beta"])
+    hit = torch.zeros((2, 5), dtype=torch.bool, device="cuda")
+    hit[1, 2] = hit[0, 4] = True
+    assert torch.isnan(z[hit]).all() and torch.equal(z[~hit], y[~hit])
+
+
+def test_layer_norm_gradient_against_differences():
+    # d/dh of sum(y * dy) along a direction: central differences of 32-bit forward passes summed in 64 bits.  With h = 2^-8 the
+    # third-order term is of the order h^2 = 1.5e-5 and the roundings of two passes over 2h are of the order 3e-5 of the gradient's
+    # length along the direction; 1e-3 is allowed
+    c = _norm_case(2, 12, 96, 0, "whole", seed=5)
+    c["x"][0, 1] += _torch().randn(96, device="cuda")
+    plan = hadfl.LayerNorm(2, 12, 96)
+    value = lambda x, g, b: float((plan.forward(x, g, b).double() * c["dy"].double()).sum())  # noqa: E731
+    plan.forward(c["x"], c["gamma"], c["beta"])
+    grads = dict(zip(("x", "gamma", "beta"), plan.backward(c["dy"], c["x"], c["gamma"])))
+    for k, name in enumerate(("x", "gamma", "beta")):
+        v = _torch().randn(c[name].shape, device="cuda", generator=_torch().Generator(device="cuda").manual_seed(k))
+        h = 2.0 ** -8
+        args = lambda s: [c[q] + (s * h * v if q == name else 0) for q in ("x", "gamma", "beta")]  # noqa: E731
+        got = (value(*args(1)) - value(*args(-1))) / (2 * h)
+        want = float((grads[name].double() * v.double()).sum())
+        assert abs(got - want) <= 1e-3 * float((grads[name].double() * v.double()).norm()), name
+
+
+# ---- 8-bit checkpoints ---------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("layout", ["whole", "padded", "odd"])
+@pytest.mark.parametrize("bf16", [0, 1])
+@pytest.mark.parametrize("n,rows,cols", [(1, 1, 1), (2, 3, 31), (1, 5, 32), (3, 7, 33), (2, 9, 64), (1, 3, 784), (2, 4, 1000), (1, 2, 4104)])
+def test_checkpoints_are_what_their_definition_says_bit_for_bit(n, rows, cols, bf16, layout):
+    torch = _torch()
+    rng = np.random.default_rng(7)
+    x = rng.normal(size=(n, rows, cols)) * 2.0 ** rng.integers(-20, 20, size=(n, rows, cols))
+    x[0, 0] = 0
+    if cols >= 32:
+        x[-1, -1, :32] = 127 * 2.0 ** -3                     # exactly the largest value of an exponent, and just above it
+        x[-1, -1, 5] = np.float32(127 * 2.0 ** -3) * (1 + 2.0 ** -7)
+        x[-1, 0, :32] = np.arange(32) + 0.5                  # ties
+    if rows > 2:
+        x[0, 1] *= 2.0 ** -126                               # subnormal groups
+        x[0, 2] = rng.choice([-1, 1], size=cols) * 3.0e38
+    t = _in(x.astype(np.float32), bf16, layout)
+    p = hadfl.PackedRows(n, rows, cols, bf16=bf16).pack(t)
+    out = _out((n, rows, cols), bf16, layout)
+    p.unpack(out.t)
+    v, q, e = ref.checkpoint(t.float().cpu().numpy())
+    f = q.shape[-1]
+    raw = p.data.cpu().numpy()
+    assert np.array_equal(raw[:q.size].view(np.int8).reshape(q.shape), q)
+    at = -(-q.size // 256) * 256
+    assert np.array_equal(raw[at:at + e.size].reshape(e.shape), e) and e.shape[-1] == f // 32
+    assert np.array_equal(out.get(), v) and out.untouched()
+    full = torch.empty((n, rows, cols), device="cuda", dtype=_dtype(bf16))
+    assert torch.equal(p.unpack(full), out.t)
+
+
+def test_a_group_with_an_infinity_or_a_nan_stands_for_nans_and_no_other():
+    torch = _torch()
+    for bf16 in (0, 1):
+        x = torch.randn((1, 2, 96), device="cuda").to(_dtype(bf16))
+        y = x.clone()
+        y[0, 0, 40], y[0, 1, 3], y[0, 1, 95] = float("inf"), float("nan"), float("-inf")
+        p, z = hadfl.PackedRows(1, 2, 96, bf16=bf16), None
+        clean = p.pack(x).unpack()
+        z = p.pack(y).unpack()
+        bad = torch.zeros((1, 2, 96), dtype=torch.bool, device="cuda")
+        bad[0, 0, 32:64] = bad[0, 1, :32] = bad[0, 1, 64:] = True
+        assert torch.isnan(z[bad]).all() and torch.equal(z[~bad], clean[~bad])
+
+
+# ---- a dense layer's gradient from a checkpoint ----------------------------------------------------------------------------
+DENSE = [(1, 0, 5, 9), (1, 1, 1, 1), (2, 3, 33, 7), (4, 32, 784, 128), (2, 65, 130, 257), (1, 257, 129, 120), (3, 100, 512, 512), (1, 1000, 48, 96),
+         (1, 2049, 256, 256), (2, 640, 264, 520)]
+
+
+@pytest.mark.parametrize("layout", ["whole", "padded", "odd"])
+@pytest.mark.parametrize("bf16", [0, 1])
+@pytest.mark.parametrize("n,rows,i,o", DENSE)
+def test_dense_gradient_from_a_checkpoint(n, rows, i, o, bf16, layout):
+    rng = np.random.default_rng(11)
+    x, dy = rng.normal(size=(n, rows, i)).clip(0), rng.normal(size=(n, rows, o)) * 2.0 ** rng.integers(-8, 8, size=(n, rows, 1))
+    x, dy = _in(x, bf16, layout), _in(dy, bf16, layout)
+    plan = hadfl.DenseGrad(n, rows, i, o, bf16=bf16)
+    packed = hadfl.PackedRows(n, rows, i, bf16=bf16).pack(x)
+    dw, db = _out((n, i, o), 0, layout), _out((n, o), 0, layout)
+    plan.backward(packed, dy, dw=dw.t, db=db.t)
+    v, d = ref.checkpoint(x.float().cpu().numpy())[0], _values(dy)
+    _check(dw.get(), v.transpose(0, 2, 1) @ d, (rows + 16) * ref.EPS32 * (np.abs(v).transpose(0, 2, 1) @ np.abs(d)), "dw")
+    _check(db.get(), d.sum(1), (rows + 16) * ref.EPS32 * np.abs(d).sum(1), "db")
+    assert dw.untouched() and db.untouched()
+    only, none = plan.backward(packed, dy, bias=False)
+    assert none is None and _torch().equal(only, dw.t)
+
+
+# ---- loss over a large vocabulary ------------------------------------------------------------------------------------------
+LOSS = [(1, 1, 1, 1), (1, 1, 64, 1000), (2, 3, 7, 5), (1, 1, 513, 4099), (4, 32, 128, 1007), (3, 33, 65, 300), (2, 100, 200, 129), (1, 257, 136, 2056),
+        (2, 130, 64, 5003), (1, 31, 1030, 256), (1, 300, 512, 1536)]
+
+
+def _loss_case(n, rows, d, v, bf16, layout, bias, seed=3):
+    rng = np.random.default_rng(seed)
+    x, w = rng.normal(size=(n, rows, d)), rng.normal(size=(n, d, v)) * 1.5 / np.sqrt(d)
+    y = rng.integers(0, v, size=(n, rows)).astype(np.int32)
+    b = rng.normal(size=(n, v)) if bias else None
+    if rows > 2:
+        y[:, 1] = -1
+        y[0, 2], y[-1, 0] = v, -2 ** 31                      # outside on either side
+        x[:, 1] = np.nan                                     # what a row without a label holds must not matter
+        x[0, 2, d // 2] = np.inf
+    if bias and v > 8:
+        b[:, 3] = -np.inf                                    # classes taken out
+        b[0, v // 2] = np.finfo(np.float32).min
+        y[(y == 3) | (y == v // 2)] = 0
+    t = _torch()
+    return dict(x=_in(x, bf16, layout), w=_in(w, bf16, layout), bias=None if b is None else _in(b, 0, layout), y=t.as_tensor(y).cuda(), yh=y)
+
+
+def _loss_reference(c, k, bf16):
+    x, w = _values(c["x"])[k], _values(c["w"])[k]
+    b = None if c["bias"] is None else _values(c["bias"])[k]
+    r = ref.class_loss(x, w, b, c["yh"][k].astype(np.int64))
+    return r, ref.class_loss_bounds(r, w, b, bf16)
+
+
+@pytest.mark.parametrize("layout", ["whole", "padded", "odd"])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("bf16", [0, 1])
+@pytest.mark.parametrize("n,rows,d,v", LOSS)
+def test_loss_over_many_classes_and_its_gradient(n, rows, d, v, bf16, bias, layout):
+    torch = _torch()
+    c = _loss_case(n, rows, d, v, bf16, layout, bias)
+    plan = hadfl.ClassLoss(n, rows, d, v, bf16=bf16)
+    dx, dw, db = _out((n, rows, d), bf16, layout), _out((n, d, v), bf16, layout), _out((n, v), 0, layout)
+    loss, row = plan.grad(c["x"], c["w"], c["y"], c["bias"], dx=dx.t, dw=dw.t, db=db.t if bias else None)[:2]
+    for k in range(n):
+        r, b = _loss_reference(c, k, bf16)
+        _check(_values(row)[k], r["row_loss"], b["row_loss"], "row_loss")
+        _check(_values(loss)[k], r["loss"], b["loss"], "loss")
+        _check(dx.get()[k], r["dx"], b["dx"], "dx")
+        _check(dw.get()[k], r["dw"], b["dw"], "dw")
+        if bias:
+            _check(db.get()[k], r["db"], b["db"], "db")
+        assert not row[k][torch.as_tensor(~r["live"]).cuda()].any() and not dx.t[k][torch.as_tensor(~r["live"]).cuda()].any()
+    assert all(o.untouched() for o in (dx, dw))
+    assert not bias or db.untouched()
+    # the loss alone, with a plan that has no room for gradients
+    alone = hadfl.ClassLoss(n, rows, d, v, bf16=bf16, grad=False).loss(c["x"], c["w"], c["y"], c["bias"])
+    assert torch.equal(alone[0], loss) and torch.equal(alone[1], row)
+
+
+def test_each_gradient_alone_is_the_same_and_repeats_bit_for_bit():
+    torch = _torch()
+    for bf16, rows in ((0, 40), (1, 40), (0, 5), (1, 200)):
+        c = _loss_case(2, rows, 96, 777, bf16, "whole", True)
+        plan = hadfl.ClassLoss(2, rows, 96, 777, bf16=bf16)
+        whole = plan.grad(c["x"], c["w"], c["y"], c["bias"])
+        for _ in range(2):
+            assert all(torch.equal(p, q) for p, q in zip(whole, plan.grad(c["x"], c["w"], c["y"], c["bias"])))
+        for i, name in enumerate(("dx", "dw", "db")):
+            got = plan.grad(c["x"], c["w"], c["y"], c["bias"], want=(name,))
+            assert [g is None for g in got[2:]] == [name != q for q in ("dx", "dw", "db")]
+            assert torch.equal(got[2 + i], whole[2 + i])
+
+
+def test_replicas_without_any_label_or_row():
+    torch = _torch()
+    for bf16 in (0, 1):
+        for rows in (5, 70):
+            c = _loss_case(2, rows, 72, 130, bf16, "whole", True)
+            c["y"][1] = -1
+            out = hadfl.ClassLoss(2, rows, 72, 130, bf16=bf16).grad(c["x"], c["w"], c["y"], c["bias"])
+            assert all(not o[1].any() for o in out) and all(bool(torch.isfinite(o).all()) for o in out)
+        empty = torch.empty((2, 0, 72), device="cuda", dtype=_dtype(bf16))
+        out = hadfl.ClassLoss(2, 0, 72, 130, bf16=bf16).grad(empty, c["w"], c["y"][:, :0].contiguous(), c["bias"])
+        assert all(not o.any() for o in out) and out[3].shape == (2, 72, 130)
+
+
+def test_one_x_or_one_w_for_all_replicas():
+    torch = _torch()
+    for bf16, rows in ((0, 20), (1, 140)):
+        c = _loss_case(3, rows, 64, 512, bf16, "whole", False)
+        plan = hadfl.ClassLoss(3, rows, 64, 512, bf16=bf16)
+        y = c["y"][:1].expand(3, rows).contiguous()
+        x, w = c["x"][:1].expand(3, rows, 64), c["w"][:1].expand(3, 64, 512)
+        a, b = plan.grad(x, w, y), plan.grad(x.contiguous(), w.contiguous(), y)
+        assert all(torch.equal(p, q) for p, q in zip(a, b) if p is not None)
+
+
+def test_large_logits_and_a_label_that_is_out():
+    # logits of thousands: no overflow on the way to a loss that is itself large; a label whose class is out has loss infinity
+    torch = _torch()
+    for bf16 in (0, 1):
+        for rows in (4, 130):
+            g = torch.Generator(device="cuda").manual_seed(1)
+            x = torch.randn((1, rows, 64), device="cuda", generator=g).to(_dtype(bf16)) * 50
+            w = torch.randn((1, 64, 300), device="cuda", generator=g).to(_dtype(bf16)) * 20
+            y = torch.randint(0, 300, (1, rows), device="cuda", generator=g, dtype=torch.int32)
+            plan = hadfl.ClassLoss(1, rows, 64, 300, bf16=bf16)
+            out = plan.grad(x, w, y)
+            c = dict(x=x, w=w, bias=None, yh=y.cpu().numpy())
+            r, b = _loss_reference(c, 0, bf16)
+            _check(_values(out[1])[0], r["row_loss"], b["row_loss"], "row_loss")
+            assert bool(torch.isfinite(out[2]).all()) and bool(torch.isfinite(out[3]).all())
+            bias = torch.zeros((1, 300), device="cuda")
+            bias[0, int(y[0, 0])] = float("-inf")
+            row = plan.loss(x, w, y, bias)[1][0]
+            hit = y[0] == y[0, 0]
+            assert torch.isinf(row[hit]).all() and torch.isfinite(row[~hit]).all()
+
+
+def test_loss_gradient_against_differences():
+    # central differences of the mean loss along a direction, 32-bit passes; |h| = 2^-6, errors as for the norm's
+    torch = _torch()
+    c = _loss_case(2, 24, 48, 400, 0, "whole", True, seed=9)
+    c["bias"] = torch.randn((2, 400), device="cuda", generator=torch.Generator(device="cuda").manual_seed(2))
+    c["x"] = torch.nan_to_num(c["x"], nan=0.5, posinf=0.5)
+    plan = hadfl.ClassLoss(2, 24, 48, 400)
+    grads = dict(zip(("x", "w", "bias"), plan.grad(c["x"], c["w"], c["y"], c["bias"])[2:]))
+    value = lambda a: float(plan.loss(a["x"], a["w"], c["y"], a["bias"])[0].double().sum())  # noqa: E731
+    for k, name in enumerate(("x", "w", "bias")):
+        v = torch.sign(grads[name]) * torch.rand(grads[name].shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(k))
+        v = v / v.norm()
+        h = 2.0 ** -6
+        a, b = dict(c), dict(c)
+        a[name], b[name] = c[name] + h * v, c[name] - h * v
+        want = float((grads[name].double() * v.double()).sum())
+        assert abs((value(a) - value(b)) / (2 * h) - want) <= 1e-2 * abs(want), name
+
+
+def test_head_operators_on_a_stream_of_their_own():
+    torch = _torch()
+    c = _loss_case(2, 50, 128, 1024, 1, "whole", True)
+    plan, norm = hadfl.ClassLoss(2, 50, 128, 1024, bf16=1), hadfl.LayerNorm(2, 50, 128, bf16=1)
+    x = torch.nan_to_num(c["x"], nan=0.25, posinf=0.25)
+    gamma = torch.ones((2, 128), device="cuda")
+    want = plan.grad(norm.forward(x, gamma, gamma), c["w"], c["y"], c["bias"])
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = plan.grad(norm.forward(x, gamma, gamma, stream=s), c["w"], c["y"], c["bias"], stream=s)
+    s.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(want, got))
+
+
+def test_head_operators_replayed_from_a_graph():
+    torch = _torch()
+    n, rows, d, v = 2, 40, 128, 1000
+    c = _loss_case(n, rows, d, v, 0, "whole", True)
+    x = torch.nan_to_num(c["x"], nan=0.25, posinf=0.25).contiguous()
+    norm, loss, packed, dense = hadfl.LayerNorm(n, rows, d), hadfl.ClassLoss(n, rows, d, v), hadfl.PackedRows(n, rows, d), hadfl.DenseGrad(n, rows, d, d)
+    gamma = torch.ones((n, d), device="cuda")
+
+    def step():
+        y = norm.forward(x, gamma, gamma)
+        out = loss.grad(y, c["w"], c["y"], c["bias"])
+        packed.pack(x)
+        return out + norm.backward(out[2], packed, gamma) + dense.backward(packed, out[2])
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for seed in range(3):
+        x.copy_(torch.randn(x.shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed)))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [o.clone() for o in out]
+        assert all(torch.equal(p, q) for p, q in zip(got, step()))
