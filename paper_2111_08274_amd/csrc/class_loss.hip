@@ -1,11 +1,12 @@
 // Softmax cross entropy of a last dense layer over many classes, and its gradient, in pieces of the vocabulary.
 //   1. logits' statistics: z = x W + b a tile at a time; a tile leaves, per row, its largest logit and the sum of exp of the
 //      distances to it, and the label's logit where the tile holds it.  Nothing of z is stored.
-//   2. per row: the tiles' pairs joined, lse = max + log(sum); row losses, their mean and 1 / (labelled rows).
-//   3. for every piece of the vocabulary: z again, G = exp(z - lse) - onehot into a buffer of [rows][piece], then
+//   2. per row: the tiles' pairs joined to its max and sum; row losses max - z_label + log(sum), their mean and 1 / (labelled
+//      rows).
+//   3. for every piece of the vocabulary: z again, G = exp(z - max) / sum - onehot into a buffer of [rows][piece], then
 //      dx += G W^T (shares of the contraction side by side, added in a fixed order) and dW = x^T G.
 // A row without a label has G = 0 and its x is read as zeros.
-#include "tile_product.h"
+#include "direct_product.h"
 
 namespace hadfl {
 namespace head {
@@ -25,71 +26,103 @@ template <bool EXACT> __device__ __forceinline__ float exp_down(float t)
     return __builtin_fmaf(p, rest * kLn2, p);
 }
 
+// logits z of a wave's block of 32 rows (lanes along m), with the bias, -inf beyond the classes; n0: the first column's class
+template <int TM, int TN>
+__device__ __forceinline__ void logits_of(const Tile<TM, TN>& t, int i, int n0, int classes, const float* bias, float (&z)[TN][16])
+{
+    if (!bias && n0 + 32 * TN <= classes) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) z[j][e] = t.acc[i][j][e];
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int c = n0 + 32 * j + 8 * (e / 4) + 4 * (t.lane >> 5) + e % 4;
+            z[j][e] = c < classes ? t.acc[i][j][e] + (bias ? bias[c] : 0.f) : -INFINITY;
+        }
+}
+// f(j, e) for the column of class y, in the lane that holds it; few waves hold any of their rows' labels
+template <int TN, class F> __device__ __forceinline__ void at_label(int lane, int n0, int y, F&& f)
+{
+    if (!__any(y >= n0 && y < n0 + 32 * TN)) return;
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            if (y == n0 + 32 * j + 8 * (e / 4) + 4 * (lane >> 5) + e % 4) f(j, e);
+}
+
 // the statistics of a wave's columns
 template <bool EXACT> struct Statistics {
-    static constexpr bool kLaneM = true;
+    static constexpr bool kLaneM = true, kStaged = false;
     const float* bias;
     long long bias_rep;
     const int32_t* labels;
     float2* part;                  // [replicas][parts][rows]
     float* z_label;                // [replicas][rows]
-    int rows, classes, parts;
+    int rows, c0, classes, parts;  // column 0 is class c0
     template <int TM, int TN> __device__ __forceinline__ void operator()(const Tile<TM, TN>& t) const
     {
         const float* b = bias ? bias + t.rep * bias_rep : nullptr;
+        const int n0 = c0 + t.n0;
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             const int m = t.m0 + 32 * i + (t.lane & 31);
             const int y = m < rows ? labels[(long long)t.rep * rows + m] : -1;
             float z[TN][16], top = -INFINITY;
+            logits_of(t, i, n0, classes, b, z);
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int n = t.n0 + 32 * j + 8 * (e / 4) + 4 * (t.lane >> 5) + e % 4;
-                    z[j][e] = n < classes ? t.acc[i][j][e] + (b ? b[n] : 0.f) : -INFINITY;
-                    top = z[j][e] > top || z[j][e] != z[j][e] ? z[j][e] : top;
-                    if (n == y && n < classes) z_label[(long long)t.rep * rows + m] = z[j][e];
-                }
-            const float other = __shfl_xor(top, 32);
-            top = other > top || other != other ? other : top;
+                for (int e = 0; e < 16; ++e) top = __builtin_fmaxf(top, z[j][e]);          // NaNs show in the sum
+            at_label<TN>(t.lane, n0, y < classes ? y : -1, [&](int j, int e) { z_label[(long long)t.rep * rows + m] = z[j][e]; });
+            top = __builtin_fmaxf(top, __shfl_xor(top, 32));
             float sum = 0.f;
+            const float base = top == -INFINITY ? 0.f : top;   // a row of -inf alone: every term is zero
+            if (EXACT || b) {
 #pragma unroll
-            for (int j = 0; j < TN; ++j)
+                for (int j = 0; j < TN; ++j)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) sum += top == -INFINITY ? 0.f : exp_down<EXACT>(z[j][e] - top);
+                    for (int e = 0; e < 16; ++e) sum += exp_down<EXACT>(z[j][e] - base);
+            } else {
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][e], kLog2e, -base * kLog2e));
+            }
             sum += __shfl_xor(sum, 32);
-            if (t.lane < 32 && m < rows) part[((long long)t.rep * parts + t.n0 / (32 * TN)) * rows + m] = float2{top, sum};
+            if (t.lane < 32 && m < rows) part[((long long)t.rep * parts + n0 / (32 * TN)) * rows + m] = float2{top, sum};
         }
     }
 };
 
 // the pairs of a row's tiles joined: `shares` threads a row, in ascending order of the tiles within a share and of the shares
+__device__ __forceinline__ void join(float2& have, const float2& v)
+{
+    const float top = fmaxf(have.x, v.x);
+    if (top == -INFINITY) { have.y += v.y; return; }           // nothing yet: zero, or a NaN that stays
+    have = float2{top, have.y * expf(have.x - top) + v.y * expf(v.x - top)};
+}
 __global__ __launch_bounds__(256) void row_loss_kernel(const float2* part, const float* z_label, const int32_t* labels, int rows, int classes,
-                                                       int parts, int shares, float* lse, float* row_loss)
+                                                       int parts, int shares, float2* norm, float* row_loss)
 {
     __shared__ float2 got[256];
     const int per = 256 / shares, r = threadIdx.x % per, share = threadIdx.x / per, k = blockIdx.y, t = blockIdx.x * per + r;
     const float2* src = part + (long long)k * parts * rows + t;
-    float top = -INFINITY, sum = 0.f;
+    float2 have{-INFINITY, 0.f};
     if (t < rows)
-        for (int p = share; p < parts; p += shares) {
-            const float2 v = src[(long long)p * rows];
-            const float m = v.x > top || v.x != v.x ? v.x : top;
-            if (m != -INFINITY) { sum = sum * expf(top - m) + v.y * expf(v.x - m); top = m; }
-        }
-    got[threadIdx.x] = float2{top, sum};
+        for (int p = share; p < parts; p += shares) join(have, src[(long long)p * rows]);
+    got[threadIdx.x] = have;
     __syncthreads();
     if (share || t >= rows) return;
-    for (int q = 1; q < shares; ++q) {
-        const float2 v = got[q * per + r];
-        const float m = v.x > top || v.x != v.x ? v.x : top;
-        if (m != -INFINITY) { sum = sum * expf(top - m) + v.y * expf(v.x - m); top = m; }
-    }
+    for (int q = 1; q < shares; ++q) join(have, got[q * per + r]);
     const long long at = (long long)k * rows + t;
-    const float l = top + logf(sum);
-    lse[at] = l;
-    row_loss[at] = (unsigned)labels[at] < (unsigned)classes ? l - z_label[at] : 0.f;
+    norm[at] = have;
+    row_loss[at] = (unsigned)labels[at] < (unsigned)classes ? (have.x - z_label[at]) + logf(have.y) : 0.f;
 }
 
 // a replica's mean loss and the factor 1 / (labelled rows), 0 without any
@@ -117,45 +150,38 @@ __global__ __launch_bounds__(256) void mean_loss_kernel(const float* row_loss, c
 }
 
 // G of a piece, unscaled, and its column sums over a wave's rows
-template <bool EXACT, typename T> struct Gradient {
-    static constexpr bool kLaneM = true;
+template <bool EXACT> struct Softmax {
     const float* bias;
     long long bias_rep;
     const int32_t* labels;
-    const float* lse;
-    T* g;                          // [replicas][rows][ld], all ld columns are written
+    const float2* norm;            // a row's largest logit and the sum of the exp of the distances to it
     float* sums;                   // [replicas][row blocks][ld] or null
-    int rows, c0, classes, ld, blocks;          // the piece holds the classes from c0
-    template <int TM, int TN> __device__ __forceinline__ void operator()(const Tile<TM, TN>& t) const
+    int rows, c0, classes, ld, blocks;          // the piece holds the classes from c0; ld: its columns, rounded up
+    // of the wave's block i of 32 rows; zero in rows that take no part and beyond the classes
+    template <int TM, int TN> __device__ __forceinline__ void block(const Tile<TM, TN>& t, int i, float (&v)[TN][16]) const
     {
-        const float* b = bias ? bias + t.rep * bias_rep : nullptr;
-        float column[TN][16] = {};
-#pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            const int m = t.m0 + 32 * i + (t.lane & 31);
-            const int y = m < rows ? labels[(long long)t.rep * rows + m] : -1;
-            const bool live = (unsigned)y < (unsigned)classes;
-            const float l = live ? lse[(long long)t.rep * rows + m] : 0.f;
+        const int m = t.m0 + 32 * i + (t.lane & 31), n0 = c0 + t.n0;
+        const int y = m < rows ? labels[(long long)t.rep * rows + m] : -1;
+        const bool live = (unsigned)y < (unsigned)classes;
+        const float2 l = live ? norm[(long long)t.rep * rows + m] : float2{0.f, 1.f};
+        logits_of(t, i, n0, classes, bias ? bias + t.rep * bias_rep : nullptr, v);
+        if (EXACT || bias) {
+            const float inv = 1.f / l.y;
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int n = t.n0 + 32 * j + 8 * q + 4 * (t.lane >> 5);
-                    if (n >= ld) continue;
-                    float v[4];
+                for (int e = 0; e < 16; ++e) v[j][e] = live ? exp_down<EXACT>(v[j][e] - l.x) * inv : 0.f;
+        } else {
+            const float shift = -l.x * kLog2e - __builtin_amdgcn_logf(l.y);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int c = c0 + n + e;
-                        v[e] = live && c < classes ? exp_down<EXACT>(t.acc[i][j][4 * q + e] + (b ? b[c] : 0.f) - l) - (c == y ? 1.f : 0.f) : 0.f;
-                        column[j][4 * q + e] += v[e];
-                    }
-                    if (m >= rows) continue;
-                    T* out = g + ((long long)t.rep * rows + m) * ld + n;
-                    if (sizeof(T) == 4) *(f4*)out = f4{v[0], v[1], v[2], v[3]};
-                    else *(u2*)out = u2{to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3])};
-                }
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[j][e] = live ? __builtin_amdgcn_exp2f(__builtin_fmaf(v[j][e], kLog2e, shift)) : 0.f;
         }
-        if (!sums) return;
+        at_label<TN>(t.lane, n0, live ? y : -1, [&](int j, int e) { v[j][e] -= 1.f; });
+    }
+    template <int TM, int TN> __device__ __forceinline__ void store_sums(const Tile<TM, TN>& t, const float (&column)[TN][16]) const
+    {
         float* out = sums + ((long long)t.rep * blocks + t.m0 / (32 * TM)) * ld;
 #pragma unroll
         for (int j = 0; j < TN; ++j)
@@ -167,6 +193,79 @@ template <bool EXACT, typename T> struct Gradient {
                 const int n = t.n0 + 32 * j + 8 * (e / 4) + 4 * (t.lane >> 5) + e % 4;
                 if ((t.lane & 31) == 0 && n < ld) out[n] = v;
             }
+    }
+};
+// into [replicas][rows][ld] of the operands' type, for the general product
+template <bool EXACT, typename T> struct Gradient {
+    static constexpr bool kLaneM = true, kStaged = false;
+    Softmax<EXACT> soft;
+    T* g;
+    template <int TM, int TN> __device__ __forceinline__ void operator()(const Tile<TM, TN>& t) const
+    {
+        float column[TN][16] = {};
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const int m = t.m0 + 32 * i + (t.lane & 31);
+            float v[TN][16];
+            soft.block(t, i, v);
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int n = t.n0 + 32 * j + 8 * q + 4 * (t.lane >> 5);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) column[j][4 * q + e] += v[j][4 * q + e];
+                    if (m >= soft.rows || n >= soft.ld) continue;
+                    T* out = g + ((long long)t.rep * soft.rows + m) * soft.ld + n;
+                    if (sizeof(T) == 4) *(f4*)out = f4{v[j][4 * q], v[j][4 * q + 1], v[j][4 * q + 2], v[j][4 * q + 3]};
+                    else *(u2*)out = u2{to_bf16x2(v[j][4 * q], v[j][4 * q + 1]), to_bf16x2(v[j][4 * q + 2], v[j][4 * q + 3])};
+                }
+        }
+        if (soft.sums) soft.store_sums(t, column);
+    }
+};
+// into bf16 planes [PL][replicas][rows][ld] for the direct product
+template <int PL> struct GradientRows {
+    static constexpr bool kLaneM = true, kStaged = true;
+    template <int TN> static constexpr int stage_bytes() { return RowStage<TN>::kBytes; }
+    Softmax<PL == 3> soft;
+    __bf16* g;
+    long long plane;
+    template <int TM, int TN> __device__ __forceinline__ void operator()(const Tile<TM, TN>& t, char* lds) const
+    {
+        float column[TN][16] = {};
+        const RowStage<TN> stage{lds};
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            float v[TN][16];
+            soft.block(t, i, v);
+            if (soft.sums) {
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) column[j][e] += v[j][e];
+            }
+            u2 part[PL][TN][4];
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if (PL == 3) split3(f4{v[j][4 * q], v[j][4 * q + 1], v[j][4 * q + 2], v[j][4 * q + 3]}, part[0][j][q], part[PL / 2][j][q], part[PL - 1][j][q]);
+                    else part[0][j][q] = u2{to_bf16x2(v[j][4 * q], v[j][4 * q + 1]), to_bf16x2(v[j][4 * q + 2], v[j][4 * q + 3])};
+                }
+#pragma unroll
+            for (int s = 0; s < PL; ++s) {
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) stage.put(t.lane, j, q, part[s][j][q]);
+                stage.take(t.lane, [&](int r, int c, const u4& w) {
+                    const int m = t.m0 + 32 * i + r, n = t.n0 + c;
+                    if (m < soft.rows && n < soft.ld) *(u4*)(g + s * plane + ((long long)t.rep * soft.rows + m) * soft.ld + n) = w;
+                });
+            }
+        }
+        if (soft.sums) soft.store_sums(t, column);
     }
 };
 
@@ -194,39 +293,56 @@ __global__ __launch_bounds__(256) void input_grad_kernel(const float* share, int
     dx[k * rep + t * row + c] = (T)(live.at(t) ? v * factor[k] : 0.f);
 }
 
+// Which kernels, the piece of the vocabulary and the working memory, from the sizes alone.
+//   few rows (at most 64)   the products through registers read W as it is, 32 x 128 or 128 x 128 tiles: W is read once or twice
+//                           per pass, laying it out first would cost as much again
+//   more                    products straight from memory to LDS; x (unlabelled rows as zeros) and a W of 32-bit or unaligned values are
+//                           laid out first
 struct Plan {
-    bool small;                    // 32 x 128 tiles instead of 128 x 128
-    int parts, piece, pieces, blocks, splits, split_len, ldx;
-    size_t lse, z_label, row_loss, factor, part, g, sums, share, total;
+    bool direct, small;            // small: 32 or (direct) 128 rows a tile
+    int bm, wave_m, wave_n, parts, piece, pieces, blocks, splits, split_len, ldx, planes;
+    size_t norm, z_label, row_loss, factor, part, g, sums, share, x, w, total;
 };
-constexpr long long kPieceBytes = 256ll << 20;
+constexpr long long kPieceBytes = 256ll << 20;       // of G, and of a laid-out piece of W
 
 int up_to(long long v, int unit) { return (int)((v + unit - 1) / unit * unit); }
 
 Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
 {
     Plan p{};
-    p.small = rows <= 32;
-    const int bm = p.small ? 32 : 128, wave_n = p.small ? 32 : 64, wave_m = p.small ? 32 : 64;
-    p.parts = up_to(classes, 128) / wave_n;
-    p.blocks = up_to(rows, bm) / wave_m;
-    const long long lines = (long long)n * rows, es = bf16 ? 2 : 4;
-    const long long most = std::max<long long>(1024, kPieceBytes / std::max<long long>(1, lines * es) / 128 * 128);
+    p.direct = rows > 64;
+    p.small = p.direct ? rows <= 128 : rows <= 32;
+    p.bm = p.direct ? (p.small ? 128 : 256) : p.small ? 32 : 128;
+    const int bn = p.direct ? 256 : 128;
+    p.wave_m = p.direct ? p.bm / 2 : p.small ? 32 : 64;
+    p.wave_n = p.direct || !p.small ? 64 : 32;
+    p.planes = p.direct && !bf16 ? 3 : 1;
+    p.parts = up_to(classes, bn) / p.wave_n;
+    p.blocks = up_to(rows, p.bm) / p.wave_m;
+    const long long lines = (long long)n * rows, es = bf16 ? 2 : p.direct ? 6 : 4;
+    long long most = grad ? kPieceBytes / std::max<long long>(1, lines * es) : classes;
+    if (p.direct) most = std::min(most, kPieceBytes / ((long long)n * features * 2 * p.planes));
+    most = std::max<long long>(1024, most / bn * bn);
     p.pieces = (int)((classes + most - 1) / most);
-    p.piece = up_to((classes + p.pieces - 1) / p.pieces, 128);
+    p.piece = up_to((classes + p.pieces - 1) / p.pieces, bn);
     p.pieces = (classes + p.piece - 1) / p.piece;
-    p.ldx = up_to(features, 4);
-    const long long tiles = (long long)n * ((rows + bm - 1) / bm) * ((features + 127) / 128);
-    p.splits = (int)std::max<long long>(1, std::min<long long>(512 / std::max<long long>(1, tiles), p.piece / 512));
+    p.ldx = up_to(features, 8);
+    const int bd = p.direct ? 256 : 128;                 // columns of dx a tile
+    const long long tiles = (long long)n * ((rows + p.bm - 1) / p.bm) * ((features + bd - 1) / bd);
+    p.splits = (int)std::max<long long>(1, std::min<long long>((p.direct ? 256 : 512) / std::max<long long>(1, tiles), p.piece / 512));
     p.split_len = up_to((p.piece + p.splits - 1) / p.splits, 128);
     p.splits = (p.piece + p.split_len - 1) / p.split_len;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += align256(bytes); return o; };
-    p.lse = take((size_t)lines * 4);
+    p.norm = take((size_t)lines * 8);
     p.z_label = take((size_t)lines * 4);
     p.row_loss = take((size_t)lines * 4);
     p.factor = take((size_t)n * 4);
     p.part = take((size_t)lines * p.parts * 8);
+    if (p.direct) {
+        p.x = take((size_t)lines * p.ldx * 2 * p.planes);
+        p.w = take((size_t)n * features * p.piece * 2 * p.planes);
+    }
     if (grad) {
         p.g = take((size_t)lines * p.piece * es);
         p.sums = take((size_t)n * p.blocks * p.piece * 4);
@@ -242,69 +358,148 @@ template <class S> S source(const Rows& r, int rows, int cols, bool vec, Labelle
     return S{(P)r.p, r.rep, r.row, rows, cols, vec, live};
 }
 
-template <class S, typename T, int BM, int BN, int WM, int WN> hipError_t run(const LossArgs& a, const Plan& p, hipStream_t s)
+// the pointers into the working memory
+struct Work {
+    float *z_label, *factor, *row_loss, *sums, *share;
+    float2 *norm, *part;
+    char* g;
+    __bf16 *x, *w;
+    Work(const LossArgs& a, const Plan& p)
+    {
+        char* at = (char*)a.work;
+        norm = (float2*)(at + p.norm); z_label = (float*)(at + p.z_label); factor = (float*)(at + p.factor);
+        row_loss = a.row_loss ? a.row_loss : (float*)(at + p.row_loss);
+        sums = (float*)(at + p.sums); share = (float*)(at + p.share); part = (float2*)(at + p.part);
+        g = at + p.g; x = (__bf16*)(at + p.x); w = (__bf16*)(at + p.w);
+    }
+};
+
+hipError_t join_rows(const LossArgs& a, const Plan& p, const Work& w, hipStream_t s)
 {
-    constexpr bool exact = sizeof(T) == 4;
-    char* work = (char*)a.work;
-    float *lse = (float*)(work + p.lse), *z_label = (float*)(work + p.z_label), *factor = (float*)(work + p.factor);
-    float* row_loss = a.row_loss ? a.row_loss : (float*)(work + p.row_loss);
-    float2* part = (float2*)(work + p.part);
     hipError_t e = hipSuccess;
-    const S x = source<S>(a.x, a.rows, a.features, chunked(a.x, a.bf16, a.features));
-    const S w = source<S>(a.w, a.features, a.classes, chunked(a.w, a.bf16, a.classes));
-    const float* bias = (const float*)a.bias.p;
     if (a.rows) {
-        const Statistics<exact> stats{bias, a.bias.rep, a.labels, part, z_label, a.rows, a.classes, p.parts};
-        e = launch_product<BM, BN, WM, WN, true, false>(x, w, a.n, a.rows, a.classes, a.features, 1, a.features, stats, s);
-        if (e != hipSuccess) return e;
         int per = 256;
         while (per > 4 && per / 2 >= a.rows) per /= 2;
         while (per > 32 && p.parts >= 512 / per) per /= 2;
-        const int shares = 256 / per;
-        row_loss_kernel<<<dim3((unsigned)((a.rows + per - 1) / per), (unsigned)a.n), 256, 0, s>>>(part, z_label, a.labels, a.rows, a.classes, p.parts,
-                                                                                               shares, lse, row_loss);
+        row_loss_kernel<<<dim3((unsigned)((a.rows + per - 1) / per), (unsigned)a.n), 256, 0, s>>>(w.part, w.z_label, a.labels, a.rows, a.classes, p.parts,
+                                                                                               256 / per, w.norm, w.row_loss);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    mean_loss_kernel<<<(unsigned)a.n, 256, 0, s>>>(row_loss, a.labels, a.rows, a.classes, a.loss, factor);
-    if ((e = hipGetLastError()) != hipSuccess || !a.grad) return e;
-    T* g = (T*)(work + p.g);
-    float *sums = (float*)(work + p.sums), *share = (float*)(work + p.share);
+    mean_loss_kernel<<<(unsigned)a.n, 256, 0, s>>>(w.row_loss, a.labels, a.rows, a.classes, a.loss, w.factor);
+    return hipGetLastError();
+}
+hipError_t bias_grad(const LossArgs& a, const Plan& p, const Work& w, int ld, int c0, int cols, hipStream_t s)
+{
+    if (!a.db.p) return hipSuccess;
+    bias_grad_kernel<<<dim3((unsigned)((cols + 255) / 256), (unsigned)a.n), 256, 0, s>>>(w.sums, a.rows ? p.blocks : 0, ld, c0, cols, w.factor,
+                                                                                          (float*)a.db.p, a.db.rep);
+    return hipGetLastError();
+}
+template <typename T> hipError_t input_grad(const LossArgs& a, const Plan& p, const Work& w, hipStream_t s)
+{
+    if (!a.dx.p || !a.rows) return hipSuccess;
+    input_grad_kernel<T><<<dim3((unsigned)a.rows, (unsigned)((a.features + 255) / 256), (unsigned)a.n), 256, 0, s>>>(
+        w.share, p.splits, a.n, a.rows, a.features, p.ldx, Labelled{a.labels, a.classes}, w.factor, (T*)a.dx.p, a.dx.rep, a.dx.row);
+    return hipGetLastError();
+}
+
+// few rows: everything through registers
+template <class S, typename T, int BM, int WM, int WN> hipError_t run_general(const LossArgs& a, const Plan& p, hipStream_t s)
+{
+    constexpr bool exact = sizeof(T) == 4;
+    const Work k(a, p);
+    hipError_t e = hipSuccess;
+    const S x = source<S>(a.x, a.rows, a.features, chunked(a.x, a.bf16, a.features));
+    const float* bias = (const float*)a.bias.p;
+    if (a.rows) {
+        const S w = source<S>(a.w, a.features, a.classes, chunked(a.w, a.bf16, a.classes));
+        const Statistics<exact> stats{bias, a.bias.rep, a.labels, k.part, k.z_label, a.rows, 0, a.classes, p.parts};
+        e = launch_product<BM, 128, WM, WN, true, false>(x, w, a.n, a.rows, a.classes, a.features, 1, a.features, stats, s);
+        if (e != hipSuccess) return e;
+    }
+    if ((e = join_rows(a, p, k, s)) != hipSuccess || !a.grad) return e;
     const Labelled live{a.labels, a.classes};
     for (int i = 0; i < p.pieces; ++i) {
         const int c0 = i * p.piece, cols = std::min(p.piece, a.classes - c0), ld = up_to(cols, 128);
         Rows wr = a.w;
         wr.p = (T*)a.w.p + c0;
-        const S wp = source<S>(wr, a.features, cols, chunked(wr, a.bf16, cols));
-        const Rows gr{g, (long long)a.rows * ld, ld};
-        const S gs = source<S>(gr, a.rows, ld, true);          // zero beyond cols
+        const S w = source<S>(wr, a.features, cols, chunked(wr, a.bf16, cols));
+        const S g = source<S>(Rows{k.g, (long long)a.rows * ld, ld}, a.rows, ld, true);              // zero beyond cols
         if (a.rows) {
-            const Gradient<exact, T> grad{bias, a.bias.rep, a.labels, lse, g, a.db.p ? sums : nullptr, a.rows, c0, a.classes, ld, p.blocks};
-            e = launch_product<BM, BN, WM, WN, true, false>(x, wp, a.n, a.rows, cols, a.features, 1, a.features, grad, s);
+            const Softmax<exact> soft{bias, a.bias.rep, a.labels, k.norm, a.db.p ? k.sums : nullptr, a.rows, c0, a.classes, ld, p.blocks};
+            e = launch_product<BM, 128, WM, WN, true, false>(x, w, a.n, a.rows, cols, a.features, 1, a.features, Gradient<exact, T>{soft, (T*)k.g}, s);
             if (e != hipSuccess) return e;
         }
         if (a.dx.p && a.rows) {
-            const StoreShare store{share, a.rows, a.features, p.ldx, a.n, i > 0};
-            e = launch_product<BM, BN, WM, WN, true, true>(gs, wp, a.n, a.rows, a.features, cols, p.splits, p.split_len, store, s);
+            const StoreShare store{k.share, a.rows, a.features, p.ldx, a.n, i > 0};
+            e = launch_product<BM, 128, WM, WN, true, true>(g, w, a.n, a.rows, a.features, cols, p.splits, p.split_len, store, s);
             if (e != hipSuccess) return e;
         }
         if (a.dw.p) {
-            const StoreTile<T> store{(T*)a.dw.p + c0, a.dw.rep, a.dw.row, factor, a.features, cols};
+            const StoreTile<T> store{(T*)a.dw.p + c0, a.dw.rep, a.dw.row, k.factor, a.features, cols};
             const S xl = source<S>(a.x, a.rows, a.features, x.vec, live);
-            e = launch_product<128, 128, 2, 2, false, false>(xl, gs, a.n, a.features, cols, a.rows, 1, std::max(1, a.rows), store, s);
+            e = launch_product<128, 128, 2, 2, false, false>(xl, g, a.n, a.features, cols, a.rows, 1, std::max(1, a.rows), store, s);
             if (e != hipSuccess) return e;
         }
-        if (a.db.p) {
-            bias_grad_kernel<<<dim3((unsigned)((cols + 255) / 256), (unsigned)a.n), 256, 0, s>>>(sums, a.rows ? p.blocks : 0, ld, c0, cols, factor,
-                                                                                                  (float*)a.db.p, a.db.rep);
-            if ((e = hipGetLastError()) != hipSuccess) return e;
+        if ((e = bias_grad(a, p, k, ld, c0, cols, s)) != hipSuccess) return e;
+    }
+    return input_grad<T>(a, p, k, s);
+}
+
+// more rows: operands straight from memory to LDS
+template <typename T, int BM> hipError_t run_direct(const LossArgs& a, const Plan& p, hipStream_t s)
+{
+    constexpr int PL = sizeof(T) == 4 ? 3 : 1;
+    const Work k(a, p);
+    const float* bias = (const float*)a.bias.p;
+    hipError_t e = lay_out<T>(a.n, a.rows, a.features, p.ldx, a.x, Labelled{a.labels, a.classes}, k.x, s);
+    if (e != hipSuccess) return e;
+    const Plane3 x{k.x, (long long)a.rows * p.ldx, (long long)a.n * a.rows * p.ldx, p.ldx, a.rows, p.ldx};
+    // W as it is, or laid out a piece at a time
+    const bool as_is = PL == 1 && chunked(a.w, 1, a.classes) && direct_pitch(a.w.row);
+    auto weights = [&](int c0, int cols, bool there, Plane3& w) -> hipError_t {
+        if (as_is) { w = Plane3{(const __bf16*)a.w.p + c0, a.w.rep, 0, (int)a.w.row, a.features, cols}; return hipSuccess; }
+        const int ld = up_to(cols, 8);
+        w = Plane3{k.w, (long long)a.features * ld, (long long)a.n * a.features * ld, ld, a.features, ld};
+        if (there) return hipSuccess;
+        return lay_out<T>(a.n, a.features, cols, ld, Rows{(T*)a.w.p + c0, a.w.rep, a.w.row}, Labelled{nullptr, 0}, k.w, s);
+    };
+    Plane3 w;
+    const int step = as_is ? a.classes : p.piece;
+    for (int c0 = 0; c0 < a.classes; c0 += step) {
+        const int cols = std::min(step, a.classes - c0);
+        if ((e = weights(c0, cols, false, w)) != hipSuccess) return e;
+        const Statistics<PL == 3> stats{bias, a.bias.rep, a.labels, k.part, k.z_label, a.rows, c0, a.classes, p.parts};
+        e = launch_direct<PL, PL, BM, 256, 2, 4, true, false>(x, w, a.n, a.rows, cols, a.features, 1, a.features, stats, s);
+        if (e != hipSuccess) return e;
+    }
+    if ((e = join_rows(a, p, k, s)) != hipSuccess || !a.grad) return e;
+    for (int i = 0; i < p.pieces; ++i) {
+        const int c0 = i * p.piece, cols = std::min(p.piece, a.classes - c0), ld = up_to(cols, 256);
+        if ((e = weights(c0, cols, p.pieces == 1, w)) != hipSuccess) return e;
+        const Plane3 g{(const __bf16*)k.g, (long long)a.rows * ld, (long long)a.n * a.rows * ld, ld, a.rows, ld};
+        const Softmax<PL == 3> soft{bias, a.bias.rep, a.labels, k.norm, a.db.p ? k.sums : nullptr, a.rows, c0, a.classes, ld, p.blocks};
+        e = launch_direct<PL, PL, BM, 256, 2, 4, true, false>(x, w, a.n, a.rows, cols, a.features, 1, a.features, GradientRows<PL>{soft, (__bf16*)k.g, g.plane}, s);
+        if (e != hipSuccess) return e;
+        if (a.dx.p) {
+            const StoreShare store{k.share, a.rows, a.features, p.ldx, a.n, i > 0};
+            e = launch_direct<PL, PL, BM, 256, 2, 4, true, true>(g, w, a.n, a.rows, a.features, w.cols, p.splits, p.split_len, store, s);
+            if (e != hipSuccess) return e;
         }
+        if (a.dw.p) {
+            if (PL == 1) {
+                const Rows out{(__bf16*)a.dw.p + c0, a.dw.rep, a.dw.row};
+                const StoreRows store{(__bf16*)out.p, out.rep, out.row, k.factor, a.features, cols, chunked(out, 1, 8)};
+                e = launch_direct<PL, PL, 256, 256, 2, 4, false, false>(x, g, a.n, a.features, cols, a.rows, 1, a.rows, store, s);
+            } else {
+                const StoreTile<float> store{(float*)a.dw.p + c0, a.dw.rep, a.dw.row, k.factor, a.features, cols};
+                e = launch_direct<PL, PL, 256, 256, 2, 4, false, false>(x, g, a.n, a.features, cols, a.rows, 1, a.rows, store, s);
+            }
+            if (e != hipSuccess) return e;
+        }
+        if ((e = bias_grad(a, p, k, ld, c0, cols, s)) != hipSuccess) return e;
     }
-    if (a.dx.p && a.rows) {
-        input_grad_kernel<T><<<dim3((unsigned)a.rows, (unsigned)((a.features + 255) / 256), (unsigned)a.n), 256, 0, s>>>(
-            share, p.splits, a.n, a.rows, a.features, p.ldx, live, factor, (T*)a.dx.p, a.dx.rep, a.dx.row);
-        e = hipGetLastError();
-    }
-    return e;
+    return input_grad<T>(a, p, k, s);
 }
 
 }  // namespace
@@ -317,8 +512,12 @@ size_t loss_work_bytes(int n, int rows, int features, int classes, int bf16, boo
 hipError_t launch_loss(const LossArgs& a, hipStream_t s)
 {
     const Plan p = plan_of(a.n, a.rows, a.features, a.classes, a.bf16, a.grad);
-    if (a.bf16) return p.small ? run<SourceBf16, __bf16, 32, 128, 1, 4>(a, p, s) : run<SourceBf16, __bf16, 128, 128, 2, 2>(a, p, s);
-    return p.small ? run<SourceF32, float, 32, 128, 1, 4>(a, p, s) : run<SourceF32, float, 128, 128, 2, 2>(a, p, s);
+    if (p.direct) {
+        if (a.bf16) return p.small ? run_direct<__bf16, 128>(a, p, s) : run_direct<__bf16, 256>(a, p, s);
+        return p.small ? run_direct<float, 128>(a, p, s) : run_direct<float, 256>(a, p, s);
+    }
+    if (a.bf16) return p.small ? run_general<SourceBf16, __bf16, 32, 1, 4>(a, p, s) : run_general<SourceBf16, __bf16, 128, 2, 2>(a, p, s);
+    return p.small ? run_general<SourceF32, float, 32, 1, 4>(a, p, s) : run_general<SourceF32, float, 128, 2, 2>(a, p, s);
 }
 
 }  // namespace head

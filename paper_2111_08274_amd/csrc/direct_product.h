@@ -1,0 +1,277 @@
+// Tiled matrix product on the matrix cores for operands that lie as the matrix cores take them: bf16 (a 32-bit operand as
+// three bf16 planes), rows on 16 bytes, whole chunks of eight values.  C[m][n] = sum_k A(m, k) B(n, k).
+//
+// Slabs of 64 k go from memory to LDS without passing registers (buffer loads that write LDS), one slab ahead of the one
+// being multiplied, one barrier a slab.  The LDS image is the slab itself with its 16-byte chunks exchanged within a row, so
+// that the operand reads meet every bank once (a load that writes LDS puts the chunks of a wave one after the other: the exchange is in
+// the addresses it reads from):
+//   along   the contraction runs along the source's rows: [rows][64 k], chunk c of row r at c ^ (r & 7)
+//   across  it runs across them: [64 k][columns], chunk c of row k at c ^ 4 (k & 3); the operand read transposes
+// 256 x 256 tiles of eight waves hold 128 x 64 each: 1.5 KiB of LDS reads a matrix instruction of 32 cycles a wave.
+#pragma once
+#include "tile_product.h"
+
+namespace hadfl {
+namespace head {
+
+constexpr int kSlab = 64;
+
+struct Plane3 {                    // an operand: source rows `lines` of `cols` values, `ld` apart
+    const __bf16* p;
+    long long rep, plane;
+    int ld, lines, cols;
+};
+// what the kernel's 32-bit offsets within a tile reach
+inline bool direct_pitch(long long ld) { return ld <= (1ll << 22); }
+
+typedef __attribute__((address_space(3))) void LdsVoid;
+
+template <bool ALONG, int BR, int NT> struct Loader {
+    static constexpr int kBytes = BR * kSlab * 2, kAcross = ALONG ? 8 : BR / 8, kLoads = kBytes / 16 / NT;
+    static constexpr int kStep = NT / kAcross;                 // image rows between a thread's chunks
+    unsigned off, step;            // of this thread's first chunk, and to its next one
+    int kc;                        // along: the chunk's first k
+    __device__ __forceinline__ void init(int tid, int ld)
+    {
+        const int r = tid / kAcross, c = tid % kAcross;
+        const int from = ALONG ? c ^ (r & 7) : c ^ ((r & 3) << 2);           // kStep is a multiple of 8: the same for all its rows
+        off = (unsigned)(r * ld + from * 8) * 2;
+        step = (unsigned)(kStep * ld) * 2;
+        kc = from * 8;
+    }
+    // r0: the tile's first row (along) or column (across)
+    __device__ __forceinline__ void issue(const Plane3& s, const __bf16* base, int r0, int k0, int wave, char* image) const
+    {
+        static_assert(kStep % 8 == 0 && kLoads >= 1, "");
+        const long long first = ALONG ? (long long)r0 * s.ld : (long long)k0 * s.ld + r0;
+        const long long rest = ALONG ? (long long)(s.lines - r0 - 1) * s.ld + s.cols : (long long)(s.lines - k0 - 1) * s.ld + s.cols - r0;
+        const Buffer b = buffer(base + first, (unsigned)min(rest * 2, 0xffffffe0ll));
+        const bool in = !ALONG || k0 + kc < s.cols;
+        unsigned at = off + (ALONG ? (unsigned)k0 * 2 : 0u);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (LdsVoid*)(image + (i * NT + wave * 64) * 16), 16, (int)(in ? at : kOutside), 0, 0, 0);
+            at += step;
+        }
+    }
+    // operand of the 32 rows from r0 and the 16 k of step ks
+    static __device__ __forceinline__ bf16x8 read(const char* image, int r0, int ks, int lane)
+    {
+        if (ALONG) {
+            const int r = r0 + (lane & 31);
+            return *(const bf16x8*)(image + r * 128 + (((ks * 2 + (lane >> 5)) ^ (lane & 7)) * 16));
+        }
+        const int k = ks * 16 + (lane >> 5) * 8 + ((lane & 15) >> 2), c = r0 + ((lane >> 4) & 1) * 16 + 4 * (lane & 3);
+        return lds_read_tr8(image, (unsigned)(k * BR * 2 + ((c >> 3) ^ ((k & 3) << 2)) * 16 + (c & 7) * 2), BR * 2);
+    }
+};
+
+// pairs of planes whose products are kept, the small ones first
+template <int PA, int PB> struct Pairs;
+template <> struct Pairs<1, 1> { static constexpr int kCount = 1; static __device__ int a(int) { return 0; } static __device__ int b(int) { return 0; } };
+template <> struct Pairs<1, 3> { static constexpr int kCount = 3; static __device__ int a(int) { return 0; } static __device__ int b(int s) { return 2 - s; } };
+template <> struct Pairs<3, 3> {
+    static constexpr int kCount = 6;                           // (0,2) (1,1) (2,0) (0,1) (1,0) (0,0)
+    static __device__ int a(int s) { return s == 1 || s == 4 ? 1 : s == 2 ? 2 : 0; }
+    static __device__ int b(int s) { return s == 0 ? 2 : s == 1 || s == 3 ? 1 : 0; }
+};
+
+// a tile's place: groups of eight tiles down m, so that the 32 compute units of a die work on about 8 x 4 tiles that share operands
+__device__ __forceinline__ void place_tile(int at, int tiles_m, int tiles_n, int& m, int& n)
+{
+    constexpr int G = 8;
+    const int per = G * tiles_n, g = at / per, in = at - g * per, rows = min(G, tiles_m - g * G);
+    n = in / rows;
+    m = g * G + in - n * rows;
+}
+
+template <bool A_ALONG, bool B_ALONG, int PA, int PB, int BM, int BN, int WM, int WN, class Epi>
+__global__ __launch_bounds__(WM * WN * 64) void direct_kernel(Plane3 a, Plane3 b, int K, int tiles_m, int tiles_n, int splits, int split_len,
+                                                              int total, Epi epi)
+{
+    constexpr int NT = WM * WN * 64, TM = BM / WM / 32, TN = BN / WN / 32;
+    typedef Loader<A_ALONG, BM, NT> LA;
+    typedef Loader<B_ALONG, BN, NT> LB;
+    typedef Pairs<PA, PB> P;
+    // two objects: the compiler then sees that a load into one does not touch the other
+    __shared__ __attribute__((aligned(16))) char image0[LA::kBytes + LB::kBytes];
+    __shared__ __attribute__((aligned(16))) char image1[LA::kBytes + LB::kBytes];
+
+    const unsigned item = logical_block();
+    if (item >= (unsigned)total) return;
+    const int per = tiles_m * tiles_n, r = item / per;
+    int tm_i, tn_i;
+    place_tile(item - r * per, tiles_m, tiles_n, tm_i, tn_i);
+    Tile<TM, TN> t;
+    t.split = r % splits;
+    t.rep = r / splits;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+    t.lane = tid & 63;
+    const int bm = tm_i * BM, bn = tn_i * BN, wm = (wave % WM) * TM * 32, wn = (wave / WM) * TN * 32;
+    t.m0 = bm + wm;
+    t.n0 = bn + wn;
+    const __bf16 *pa = a.p + t.rep * a.rep, *pb = b.p + t.rep * b.rep;
+    const int k_begin = t.split * split_len, k_end = min(K, k_begin + split_len);
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) t.acc[i][j] = f16{};
+    LA la;
+    LB lb;
+    la.init(tid, a.ld);
+    lb.init(tid, b.ld);
+
+    int pair = 0, k0 = k_begin;                                // of the next slab to load
+    auto issue = [&](char* image) {
+        la.issue(a, pa + P::a(pair) * a.plane, bm, k0, wave, image);
+        lb.issue(b, pb + P::b(pair) * b.plane, bn, k0, wave, image + LA::kBytes);
+        k0 += kSlab;
+        if (k0 >= k_end) { k0 = k_begin; ++pair; }
+    };
+    auto multiply = [&](const char* image) {
+#pragma unroll
+        for (int ks = 0; ks < kSlab / 16; ++ks) {
+            bf16x8 fa[TM], fb[TN];
+#pragma unroll
+            for (int i = 0; i < TM; ++i) fa[i] = LA::read(image, wm + 32 * i, ks, t.lane);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) fb[j] = LB::read(image + LA::kBytes, wn + 32 * j, ks, t.lane);
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+                    t.acc[i][j] = Epi::kLaneM ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], t.acc[i][j], 0, 0, 0)
+                                              : __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], t.acc[i][j], 0, 0, 0);
+        }
+    };
+    const int slabs = k_begin < k_end ? P::kCount * ((k_end - k_begin + kSlab - 1) / kSlab) : 0;
+    if (slabs) issue(image0);
+    for (int s = 0; s < slabs; s += 2) {
+        __syncthreads();                                       // image 0 has arrived, image 1 has been read
+        if (s + 1 < slabs) issue(image1);
+        multiply(image0);
+        if (s + 1 < slabs) {
+            __syncthreads();
+            if (s + 2 < slabs) issue(image0);
+            multiply(image1);
+        }
+    }
+    constexpr float kScale = (PA == 3 ? 0x1p-24f : 1.f) * (PB == 3 ? 0x1p-24f : 1.f);
+    if (kScale != 1.f) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) t.acc[i][j] *= kScale;
+    }
+    if constexpr (Epi::kStaged) {
+        __syncthreads();                                       // the images are free: a part for every wave
+        epi(t, image0 + wave * Epi::template stage_bytes<TN>());
+    } else epi(t);
+}
+
+template <int PA, int PB, int BM, int BN, int WM, int WN, bool A_ALONG, bool B_ALONG, class Epi>
+hipError_t launch_direct(const Plane3& a, const Plane3& b, int replicas, int M, int N, int K, int splits, int split_len, const Epi& epi, hipStream_t s)
+{
+    const int tm = (M + BM - 1) / BM, tn = (N + BN - 1) / BN;
+    const long long total = (long long)replicas * splits * tm * tn;
+    if (total == 0) return hipSuccess;
+    if (total > 0x7fffff00ll) return hipErrorInvalidValue;
+    direct_kernel<A_ALONG, B_ALONG, PA, PB, BM, BN, WM, WN, Epi>
+        <<<die_grid(total), WM * WN * 64, 0, s>>>(a, b, K, tm, tn, splits, split_len, (int)total, epi);
+    return hipGetLastError();
+}
+
+// ---- laying operands out ---------------------------------------------------------------------------------------------
+// x [replicas][rows][cols] -> bf16 [planes][replicas][rows][ld], zero beyond cols and in rows that take no part
+template <typename T>
+__global__ __launch_bounds__(256) void lay_out_kernel(const T* x, long long rep, long long row, int rows, int cols, int ld, long long total, long long plane,
+                                                      bool vec, Labelled live, __bf16* out)
+{
+    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;          // chunk of eight
+    if (at >= total) return;
+    const int chunks = ld / 8;
+    const long long line = at / chunks;
+    const int c = (int)(at - line * chunks) * 8, k = (int)(line / rows), t = (int)(line - (long long)k * rows);
+    if (live.labels) live.labels += (long long)k * rows;
+    const T* src = x + k * rep + t * row + c;
+    float v[8] = {};
+    if (live.at(t)) {
+        if (vec) { if (c < cols) load8(src, v); }
+        else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) if (c + e < cols) v[e] = up(src[e]);
+        }
+    }
+    if (sizeof(T) == 2) { store8(out + at * 8, v); return; }
+    u2 h[2], m[2], l[2];
+    split3(f4{v[0], v[1], v[2], v[3]}, h[0], m[0], l[0]);
+    split3(f4{v[4], v[5], v[6], v[7]}, h[1], m[1], l[1]);
+    *(u4*)(out + at * 8) = join8(h[0], h[1]);
+    *(u4*)(out + plane + at * 8) = join8(m[0], m[1]);
+    *(u4*)(out + 2 * plane + at * 8) = join8(l[0], l[1]);
+}
+template <typename T>
+hipError_t lay_out(int n, int rows, int cols, int ld, const Rows& x, Labelled live, __bf16* out, hipStream_t s)
+{
+    const long long plane = (long long)n * rows * ld, total = plane / 8;
+    if (total == 0) return hipSuccess;
+    lay_out_kernel<T><<<(unsigned)((total + 255) / 256), 256, 0, s>>>((const T*)x.p, x.rep, x.row, rows, cols, ld, total, plane,
+                                                                       chunked(x, sizeof(T) == 2, cols), live, out);
+    return hipGetLastError();
+}
+
+// ---- a wave's tile to bf16 rows, through LDS -----------------------------------------------------------------------------
+// One block of 32 rows of 32 * TN columns (lanes along m) at a time: a lane writes its four consecutive n, then eight lanes take a row of
+// 128 bytes to memory (straight from the registers a store would touch 32 rows, eight bytes each).
+template <int TN> struct RowStage {
+    static constexpr int kPitch = TN * 64 + 16, kBytes = 32 * kPitch;
+    char* p;
+    __device__ __forceinline__ void put(int lane, int j, int q, const u2& v) const { *(u2*)(p + (lane & 31) * kPitch + (32 * j + 8 * q + 4 * (lane >> 5)) * 2) = v; }
+    // store(row, first column, chunk) for every chunk of eight
+    template <class F> __device__ __forceinline__ void take(int lane, F&& store) const
+    {
+        constexpr int kAcross = TN * 4;
+#pragma unroll
+        for (int i = 0; i < 32 * kAcross / 64; ++i) {
+            const int id = i * 64 + lane, r = id / kAcross, c = id % kAcross;
+            store(r, c * 8, *(const u4*)(p + r * kPitch + c * 16));
+        }
+    }
+};
+// C times a factor per replica to a bf16 tensor
+struct StoreRows {
+    static constexpr bool kLaneM = true, kStaged = true;
+    template <int TN> static constexpr int stage_bytes() { return RowStage<TN>::kBytes; }
+    __bf16* p;
+    long long rep, row;
+    const float* factor;
+    int M, N;
+    bool vec;
+    template <int TM, int TN> __device__ __forceinline__ void operator()(const Tile<TM, TN>& t, char* lds) const
+    {
+        const float f = factor[t.rep];
+        __bf16* out = p + t.rep * rep;
+        const RowStage<TN> stage{lds};
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    stage.put(t.lane, j, q, u2{to_bf16x2(t.acc[i][j][4 * q] * f, t.acc[i][j][4 * q + 1] * f),
+                                               to_bf16x2(t.acc[i][j][4 * q + 2] * f, t.acc[i][j][4 * q + 3] * f)});
+            stage.take(t.lane, [&](int r, int c, const u4& v) {
+                const int m = t.m0 + 32 * i + r, n = t.n0 + c;
+                if (m >= M || n >= N) return;
+                __bf16* q = out + m * row + n;
+                if (vec && n + 8 <= N) { *(u4*)q = v; return; }
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (n + e < N) ((unsigned short*)q)[e] = (unsigned short)(v[e / 2] >> (16 * (e % 2)));
+            });
+        }
+    }
+};
+
+}  // namespace head
+}  // namespace hadfl

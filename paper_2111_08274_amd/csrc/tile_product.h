@@ -239,7 +239,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(SA a, SB b, int K
 // ---- epilogues that only store ---------------------------------------------------------------------------------
 // C to a tensor, times a factor per replica (lanes along n)
 template <typename T> struct StoreTile {
-    static constexpr bool kLaneM = false;
+    static constexpr bool kLaneM = false, kStaged = false;
     T* p;
     long long rep, row;
     const float* factor;           // [replicas] or null
@@ -264,7 +264,7 @@ template <typename T> struct StoreTile {
 };
 // C into [split][replica][M][ld] floats, over or onto what is there
 struct StoreShare {
-    static constexpr bool kLaneM = false;
+    static constexpr bool kLaneM = false, kStaged = false;
     float* p;
     int M, N, ld, replicas;
     bool onto;

@@ -366,6 +366,29 @@ def test_large_logits_and_a_label_that_is_out():
             assert torch.isinf(row[hit]).all() and torch.isfinite(row[~hit]).all()
 
 
+def test_a_row_whose_mask_leaves_nothing():
+    # every class masked by the type's lowest value: the logits are equal, so the loss is log(classes) and the gradient's rows
+    # are 1 / classes but for the label's; a row of -inf alone has no softmax, and its neighbours keep theirs
+    torch = _torch()
+    for bf16 in (0, 1):
+        for rows in (3, 100):
+            g = torch.Generator(device="cuda").manual_seed(4)
+            x = torch.randn((2, rows, 32), device="cuda", generator=g).to(_dtype(bf16))
+            w = torch.randn((2, 32, 500), device="cuda", generator=g).to(_dtype(bf16))
+            y = torch.randint(0, 500, (2, rows), device="cuda", generator=g, dtype=torch.int32)
+            bias = torch.full((2, 500), torch.finfo(torch.float32).min, device="cuda")
+            bias[1] = 0
+            plan = hadfl.ClassLoss(2, rows, 32, 500, bf16=bf16)
+            loss, row, dx, dw, db = plan.grad(x, w, y, bias)
+            assert (row[0] - float(np.log(500))).abs().max() < 1e-5 and bool(torch.isfinite(row).all())
+            want = torch.full((500,), rows / 500.0, dtype=torch.float64) - torch.bincount(y[0].cpu().long(), minlength=500)
+            assert (db[0].double().cpu() * rows - want).abs().max() < 1e-4
+            assert all(bool(torch.isfinite(t).all()) for t in (dx, dw, db))
+            bias[0] = float("-inf")
+            out = plan.grad(x, w, y, bias)
+            assert torch.isnan(out[1][0]).all() and all(torch.equal(p[1], q[1]) for p, q in zip(out, (loss, row, dx, dw, db)))
+
+
 def test_loss_gradient_against_differences():
     # central differences of the mean loss along a direction, 32-bit passes; |h| = 2^-6, errors as for the norm's
     torch = _torch()
