@@ -56,73 +56,131 @@ template <int TN, class F> __device__ __forceinline__ void at_label(int lane, in
             if (y == n0 + 32 * j + 8 * (e / 4) + 4 * (lane >> 5) + e % 4) f(j, e);
 }
 
-// the statistics of a wave's columns
-template <bool EXACT> struct Statistics {
-    static constexpr bool kLaneM = true, kStaged = false;
+__device__ __forceinline__ void join(float2& have, const float2& v)
+{
+    const float top = fmaxf(have.x, v.x);
+    if (top == -INFINITY) { have.y += v.y; return; }           // nothing yet: zero, or a NaN that stays
+    have = float2{top, have.y * exp_down<true>(have.x - top) + v.y * exp_down<true>(v.x - top)};
+}
+
+// The statistics of a tile: per wave and row, then joined over the WN waves that share rows.  z: the logits too (few rows), or null.
+template <bool EXACT, int BM, int BN, int WN> struct Statistics {
+    static constexpr bool kLaneM = true, kStaged = true;
     const float* bias;
     long long bias_rep;
     const int32_t* labels;
     float2* part;                  // [replicas][parts][rows]
     float* z_label;                // [replicas][rows]
-    int rows, c0, classes, parts;  // column 0 is class c0
-    template <int TM, int TN> __device__ __forceinline__ void operator()(const Tile<TM, TN>& t) const
+    float* z;                      // [replicas][rows][ld]
+    int rows, c0, classes, parts, ld;           // column 0 is class c0
+    template <int TM, int TN> __device__ __forceinline__ void operator()(const Tile<TM, TN>& t, char* lds) const
     {
         const float* b = bias ? bias + t.rep * bias_rep : nullptr;
         const int n0 = c0 + t.n0;
+        float2* got = (float2*)lds;                            // [WN][BM]
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             const int m = t.m0 + 32 * i + (t.lane & 31);
             const int y = m < rows ? labels[(long long)t.rep * rows + m] : -1;
-            float z[TN][16], top = -INFINITY;
-            logits_of(t, i, n0, classes, b, z);
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) top = __builtin_fmaxf(top, z[j][e]);          // NaNs show in the sum
-            at_label<TN>(t.lane, n0, y < classes ? y : -1, [&](int j, int e) { z_label[(long long)t.rep * rows + m] = z[j][e]; });
-            top = __builtin_fmaxf(top, __shfl_xor(top, 32));
-            float sum = 0.f;
-            const float base = top == -INFINITY ? 0.f : top;   // a row of -inf alone: every term is zero
-            if (EXACT || b) {
+            float v[TN][16], top = -INFINITY;
+            logits_of(t, i, n0, classes, b, v);
+            if (z && m < rows) {
 #pragma unroll
                 for (int j = 0; j < TN; ++j)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) sum += exp_down<EXACT>(z[j][e] - base);
+                    for (int q = 0; q < 4; ++q)
+                        *(f4*)(z + ((long long)t.rep * rows + m) * ld + n0 + 32 * j + 8 * q + 4 * (t.lane >> 5)) =
+                            f4{v[j][4 * q], v[j][4 * q + 1], v[j][4 * q + 2], v[j][4 * q + 3]};
+            }
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) top = __builtin_fmaxf(top, v[j][e]);          // NaNs show in the sum
+            at_label<TN>(t.lane, n0, y < classes ? y : -1, [&](int j, int e) { z_label[(long long)t.rep * rows + m] = v[j][e]; });
+            top = __builtin_fmaxf(top, __shfl_xor(top, 32));
+            float sum = 0.f;
+            const float base = top == -INFINITY ? 0.f : top;   // a row of -inf alone: every term is zero
+            if (EXACT || b) {                                  // the difference first: a bias may be the type's lowest value
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sum += exp_down<EXACT>(v[j][e] - base);
             } else {
 #pragma unroll
                 for (int j = 0; j < TN; ++j)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][e], kLog2e, -base * kLog2e));
+                    for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(v[j][e], kLog2e, -base * kLog2e));
             }
             sum += __shfl_xor(sum, 32);
-            if (t.lane < 32 && m < rows) part[((long long)t.rep * parts + n0 / (32 * TN)) * rows + m] = float2{top, sum};
+            if (t.lane < 32) got[(t.n0 - t.bn) / (32 * TN) * BM + m - t.bm] = float2{top, sum};
         }
+        __syncthreads();
+        const int m = t.bm + threadIdx.x;
+        if (threadIdx.x >= BM || m >= rows) return;
+        float2 have = got[threadIdx.x];
+#pragma unroll
+        for (int w = 1; w < WN; ++w) join(have, got[w * BM + threadIdx.x]);
+        part[((long long)t.rep * parts + (c0 + t.bn) / BN) * rows + m] = have;
     }
 };
 
-// the pairs of a row's tiles joined: `shares` threads a row, in ascending order of the tiles within a share and of the shares
-__device__ __forceinline__ void join(float2& have, const float2& v)
+// The pairs of a row's tiles joined: `shares` threads a row, each its tiles in ascending order, eight loads in flight; then the
+// shares pairwise.  Where one workgroup has all rows of a replica it also takes their mean (loss, factor; else null).
+__device__ __forceinline__ void mean_of_rows(float sum, int count, float* sums, int* counts, float* loss, float* factor)
 {
-    const float top = fmaxf(have.x, v.x);
-    if (top == -INFINITY) { have.y += v.y; return; }           // nothing yet: zero, or a NaN that stays
-    have = float2{top, have.y * expf(have.x - top) + v.y * expf(v.x - top)};
+    __syncthreads();
+    sums[threadIdx.x] = sum;
+    counts[threadIdx.x] = count;
+    for (int d = 128; d > 0; d /= 2) {
+        __syncthreads();
+        if (threadIdx.x < d) { sums[threadIdx.x] += sums[threadIdx.x + d]; counts[threadIdx.x] += counts[threadIdx.x + d]; }
+    }
+    if (threadIdx.x == 0) {
+        *factor = counts[0] ? 1.f / (float)counts[0] : 0.f;
+        *loss = counts[0] ? sums[0] / (float)counts[0] : 0.f;
+    }
 }
 __global__ __launch_bounds__(256) void row_loss_kernel(const float2* part, const float* z_label, const int32_t* labels, int rows, int classes,
-                                                       int parts, int shares, float2* norm, float* row_loss)
+                                                       int parts, int shares, float2* norm, float* row_loss, float* loss, float* factor)
 {
+    constexpr int U = 8;
     __shared__ float2 got[256];
     const int per = 256 / shares, r = threadIdx.x % per, share = threadIdx.x / per, k = blockIdx.y, t = blockIdx.x * per + r;
     const float2* src = part + (long long)k * parts * rows + t;
     float2 have{-INFINITY, 0.f};
     if (t < rows)
-        for (int p = share; p < parts; p += shares) join(have, src[(long long)p * rows]);
+        for (int p = share; p < parts; p += U * shares) {
+            float2 v[U];
+            float top = have.x;
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = p + u * shares < parts ? src[(long long)(p + u * shares) * rows] : float2{-INFINITY, 0.f};
+#pragma unroll
+            for (int u = 0; u < U; ++u) top = fmaxf(top, v[u].x);
+            const float base = top == -INFINITY ? 0.f : top;
+            have.y *= exp_down<true>(have.x - base);
+#pragma unroll
+            for (int u = 0; u < U; ++u) have.y += v[u].y * exp_down<true>(v[u].x - base);
+            have.x = top;
+            // all -inf so far: the sums are zero or NaN, and exp(-inf) took a NaN along: 0 * NaN
+        }
     got[threadIdx.x] = have;
-    __syncthreads();
-    if (share || t >= rows) return;
-    for (int q = 1; q < shares; ++q) join(have, got[q * per + r]);
-    const long long at = (long long)k * rows + t;
-    norm[at] = have;
-    row_loss[at] = (unsigned)labels[at] < (unsigned)classes ? (have.x - z_label[at]) + logf(have.y) : 0.f;
+    for (int d = shares / 2; d > 0; d /= 2) {
+        __syncthreads();
+        if (share < d) { join(have, got[threadIdx.x + d * per]); got[threadIdx.x] = have; }
+    }
+    float value = 0.f;
+    int live = 0;
+    if (share == 0 && t < rows) {
+        const long long at = (long long)k * rows + t;
+        norm[at] = have;
+        live = (unsigned)labels[at] < (unsigned)classes;
+        value = live ? (have.x - z_label[at]) + logf(have.y) : 0.f;
+        row_loss[at] = value;
+    }
+    if (!loss) return;
+    __shared__ float sums[256];
+    __shared__ int counts[256];
+    mean_of_rows(value, live, sums, counts, loss + k, factor + k);
 }
 
 // a replica's mean loss and the factor 1 / (labelled rows), 0 without any
@@ -133,20 +191,45 @@ __global__ __launch_bounds__(256) void mean_loss_kernel(const float* row_loss, c
     const long long base = (long long)blockIdx.x * rows;
     float sum = 0.f;
     int count = 0;
+#pragma unroll 4
     for (int t = threadIdx.x; t < rows; t += 256) {
         sum += row_loss[base + t];
         count += (unsigned)labels[base + t] < (unsigned)classes;
     }
-    sums[threadIdx.x] = sum;
-    counts[threadIdx.x] = count;
-    for (int d = 128; d > 0; d /= 2) {
-        __syncthreads();
-        if (threadIdx.x < d) { sums[threadIdx.x] += sums[threadIdx.x + d]; counts[threadIdx.x] += counts[threadIdx.x + d]; }
+    mean_of_rows(sum, count, sums, counts, loss + blockIdx.x, factor + blockIdx.x);
+}
+
+// Few rows: G of the whole vocabulary from its logits, four columns a thread, and db.  32-bit G takes the logits' place.
+template <bool EXACT, typename T>
+__global__ __launch_bounds__(256) void gradient_columns_kernel(const float* z, const int32_t* labels, const float2* norm, int rows, int classes, int ld,
+                                                               T* g, const float* factor, float* db, long long db_rep)
+{
+    const int c = (blockIdx.x * 256 + threadIdx.x) * 4, k = blockIdx.y;
+    if (c >= ld) return;
+    const long long first = (long long)k * rows;
+    float sum[4] = {};
+#pragma unroll 4
+    for (int t = 0; t < rows; ++t) {
+        const int y = labels[first + t];
+        const bool live = (unsigned)y < (unsigned)classes;
+        const float2 l = norm[first + t];
+        const float inv = 1.f / l.y;
+        const f4 v = *(const f4*)(z + (first + t) * ld + c);
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            p[e] = live && c + e < classes ? exp_down<EXACT>(v[e] - l.x) * inv - (c + e == y ? 1.f : 0.f) : 0.f;
+            sum[e] += p[e];
+        }
+        T* out = g + (first + t) * ld + c;
+        if (sizeof(T) == 4) *(f4*)out = f4{p[0], p[1], p[2], p[3]};
+        else *(u2*)out = u2{to_bf16x2(p[0], p[1]), to_bf16x2(p[2], p[3])};
     }
-    if (threadIdx.x == 0) {
-        factor[blockIdx.x] = counts[0] ? 1.f / (float)counts[0] : 0.f;
-        loss[blockIdx.x] = counts[0] ? sums[0] / (float)counts[0] : 0.f;
-    }
+    if (!db) return;
+    const float f = factor[k];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (c + e < classes) db[k * db_rep + c + e] = sum[e] * f;
 }
 
 // G of a piece, unscaled, and its column sums over a wave's rows
@@ -227,14 +310,13 @@ template <bool EXACT, typename T> struct Gradient {
 // into bf16 planes [PL][replicas][rows][ld] for the direct product
 template <int PL> struct GradientRows {
     static constexpr bool kLaneM = true, kStaged = true;
-    template <int TN> static constexpr int stage_bytes() { return RowStage<TN>::kBytes; }
     Softmax<PL == 3> soft;
     __bf16* g;
     long long plane;
     template <int TM, int TN> __device__ __forceinline__ void operator()(const Tile<TM, TN>& t, char* lds) const
     {
         float column[TN][16] = {};
-        const RowStage<TN> stage{lds};
+        const RowStage<TN> stage{lds + t.wave * RowStage<TN>::kBytes};
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             float v[TN][16];
@@ -279,18 +361,27 @@ __global__ __launch_bounds__(256) void bias_grad_kernel(const float* sums, int b
     db[k * rep + c0 + c] = v * factor[k];
 }
 
-// dx: the shares of the contraction in ascending order; zero for a row without a label
+// dx: the shares of the contraction in ascending order, eight columns a thread; zero for a row without a label
 template <typename T>
-__global__ __launch_bounds__(256) void input_grad_kernel(const float* share, int splits, int replicas, int rows, int cols, int ld, Labelled live,
-                                                         const float* factor, T* dx, long long rep, long long row)
+__global__ __launch_bounds__(256) void input_grad_kernel(const float* share, int splits, long long step, int rows, int cols, int ld, long long total,
+                                                         Labelled live, const float* factor, T* dx, long long rep, long long row)
 {
-    const int k = blockIdx.z, t = blockIdx.x, c = blockIdx.y * 256 + threadIdx.x;
-    if (c >= cols) return;
-    const long long at = ((long long)k * rows + t) * ld + c, step = (long long)replicas * rows * ld;
-    float v = 0.f;
-    for (int s = 0; s < splits; ++s) v += share[s * step + at];
+    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (at >= total) return;
+    const int chunks = ld / 8;
+    const long long line = at / chunks;
+    const int c = (int)(at - line * chunks) * 8, k = (int)(line / rows), t = (int)(line - (long long)k * rows);
+    f4 a = {}, b = {};
+    const float* src = share + at * 8;
+#pragma unroll 8
+    for (int s = 0; s < splits; ++s) { a += *(const f4*)(src + s * step); b += *(const f4*)(src + s * step + 4); }
     live.labels += (long long)k * rows;
-    dx[k * rep + t * row + c] = (T)(live.at(t) ? v * factor[k] : 0.f);
+    const float f = factor[k];
+    const bool on = live.at(t);
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { v[e] = on ? a[e] * f : 0.f; v[4 + e] = on ? b[e] * f : 0.f; }
+    store_chunk(dx + k * rep + t * row + c, cols - c, v);
 }
 
 // Which kernels, the piece of the vocabulary and the working memory, from the sizes alone.
@@ -300,8 +391,8 @@ __global__ __launch_bounds__(256) void input_grad_kernel(const float* share, int
 //                           laid out first
 struct Plan {
     bool direct, small;            // small: 32 or (direct) 128 rows a tile
-    int bm, wave_m, wave_n, parts, piece, pieces, blocks, splits, split_len, ldx, planes;
-    size_t norm, z_label, row_loss, factor, part, g, sums, share, x, w, total;
+    int bm, wave_m, parts, piece, pieces, blocks, splits, split_len, ldx, planes;
+    size_t norm, z_label, row_loss, factor, part, g, z, sums, share, x, w, total;
 };
 constexpr long long kPieceBytes = 256ll << 20;       // of G, and of a laid-out piece of W
 
@@ -315,11 +406,10 @@ Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
     p.bm = p.direct ? (p.small ? 128 : 256) : p.small ? 32 : 128;
     const int bn = p.direct ? 256 : 128;
     p.wave_m = p.direct ? p.bm / 2 : p.small ? 32 : 64;
-    p.wave_n = p.direct || !p.small ? 64 : 32;
     p.planes = p.direct && !bf16 ? 3 : 1;
-    p.parts = up_to(classes, bn) / p.wave_n;
+    p.parts = up_to(classes, bn) / bn;
     p.blocks = up_to(rows, p.bm) / p.wave_m;
-    const long long lines = (long long)n * rows, es = bf16 ? 2 : p.direct ? 6 : 4;
+    const long long lines = (long long)n * rows, es = p.direct ? (bf16 ? 2 : 6) : bf16 ? 6 : 4;      // of G and, few rows, the logits
     long long most = grad ? kPieceBytes / std::max<long long>(1, lines * es) : classes;
     if (p.direct) most = std::min(most, kPieceBytes / ((long long)n * features * 2 * p.planes));
     most = std::max<long long>(1024, most / bn * bn);
@@ -329,7 +419,7 @@ Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
     p.ldx = up_to(features, 8);
     const int bd = p.direct ? 256 : 128;                 // columns of dx a tile
     const long long tiles = (long long)n * ((rows + p.bm - 1) / p.bm) * ((features + bd - 1) / bd);
-    p.splits = (int)std::max<long long>(1, std::min<long long>((p.direct ? 256 : 512) / std::max<long long>(1, tiles), p.piece / 512));
+    p.splits = (int)std::max<long long>(1, std::min<long long>((p.direct ? 256 : 512) / std::max<long long>(1, tiles), p.piece / (p.direct ? 512 : 128)));
     p.split_len = up_to((p.piece + p.splits - 1) / p.splits, 128);
     p.splits = (p.piece + p.split_len - 1) / p.split_len;
     size_t at = 0;
@@ -344,7 +434,8 @@ Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
         p.w = take((size_t)n * features * p.piece * 2 * p.planes);
     }
     if (grad) {
-        p.g = take((size_t)lines * p.piece * es);
+        p.g = take((size_t)lines * p.piece * (p.direct ? es : bf16 ? 2 : 4));
+        p.z = !p.direct && bf16 ? take((size_t)lines * p.piece * 4) : p.g;
         p.sums = take((size_t)n * p.blocks * p.piece * 4);
         p.share = take((size_t)p.splits * lines * p.ldx * 4);
     }
@@ -352,15 +443,9 @@ Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
     return p;
 }
 
-template <class S> S source(const Rows& r, int rows, int cols, bool vec, Labelled live = {nullptr, 0})
-{
-    typedef decltype(S::p) P;
-    return S{(P)r.p, r.rep, r.row, rows, cols, vec, live};
-}
-
 // the pointers into the working memory
 struct Work {
-    float *z_label, *factor, *row_loss, *sums, *share;
+    float *z_label, *factor, *row_loss, *z, *sums, *share;
     float2 *norm, *part;
     char* g;
     __bf16 *x, *w;
@@ -370,20 +455,21 @@ struct Work {
         norm = (float2*)(at + p.norm); z_label = (float*)(at + p.z_label); factor = (float*)(at + p.factor);
         row_loss = a.row_loss ? a.row_loss : (float*)(at + p.row_loss);
         sums = (float*)(at + p.sums); share = (float*)(at + p.share); part = (float2*)(at + p.part);
-        g = at + p.g; x = (__bf16*)(at + p.x); w = (__bf16*)(at + p.w);
+        g = at + p.g; z = (float*)(at + p.z); x = (__bf16*)(at + p.x); w = (__bf16*)(at + p.w);
     }
 };
 
 hipError_t join_rows(const LossArgs& a, const Plan& p, const Work& w, hipStream_t s)
 {
-    hipError_t e = hipSuccess;
+    int per = 256;                                             // rows a workgroup
+    while (per > 4 && per / 2 >= a.rows) per /= 2;
+    while (per > 32 && p.parts >= 2048 / per) per /= 2;
+    const bool alone = a.rows <= per;
     if (a.rows) {
-        int per = 256;
-        while (per > 4 && per / 2 >= a.rows) per /= 2;
-        while (per > 32 && p.parts >= 512 / per) per /= 2;
-        row_loss_kernel<<<dim3((unsigned)((a.rows + per - 1) / per), (unsigned)a.n), 256, 0, s>>>(w.part, w.z_label, a.labels, a.rows, a.classes, p.parts,
-                                                                                               256 / per, w.norm, w.row_loss);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+        row_loss_kernel<<<dim3((unsigned)((a.rows + per - 1) / per), (unsigned)a.n), 256, 0, s>>>(
+            w.part, w.z_label, a.labels, a.rows, a.classes, p.parts, 256 / per, w.norm, w.row_loss, alone ? a.loss : nullptr, w.factor);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess || alone) return e;
     }
     mean_loss_kernel<<<(unsigned)a.n, 256, 0, s>>>(w.row_loss, a.labels, a.rows, a.classes, a.loss, w.factor);
     return hipGetLastError();
@@ -398,38 +484,42 @@ hipError_t bias_grad(const LossArgs& a, const Plan& p, const Work& w, int ld, in
 template <typename T> hipError_t input_grad(const LossArgs& a, const Plan& p, const Work& w, hipStream_t s)
 {
     if (!a.dx.p || !a.rows) return hipSuccess;
-    input_grad_kernel<T><<<dim3((unsigned)a.rows, (unsigned)((a.features + 255) / 256), (unsigned)a.n), 256, 0, s>>>(
-        w.share, p.splits, a.n, a.rows, a.features, p.ldx, Labelled{a.labels, a.classes}, w.factor, (T*)a.dx.p, a.dx.rep, a.dx.row);
+    const long long lines = (long long)a.n * a.rows, total = lines * (p.ldx / 8);
+    input_grad_kernel<T><<<(unsigned)((total + 255) / 256), 256, 0, s>>>(w.share, p.splits, lines * p.ldx, a.rows, a.features, p.ldx, total,
+                                                                          Labelled{a.labels, a.classes}, w.factor, (T*)a.dx.p, a.dx.rep, a.dx.row);
     return hipGetLastError();
 }
 
-// few rows: everything through registers
-template <class S, typename T, int BM, int WM, int WN> hipError_t run_general(const LossArgs& a, const Plan& p, hipStream_t s)
+// few rows: everything through registers.  Where one piece holds the whole vocabulary its logits stay in it for the gradient.
+template <typename T, int BM, int WM, int WN> hipError_t run_general(const LossArgs& a, const Plan& p, hipStream_t s)
 {
     constexpr bool exact = sizeof(T) == 4;
     const Work k(a, p);
+    const bool once = a.grad && p.pieces == 1;
     hipError_t e = hipSuccess;
-    const S x = source<S>(a.x, a.rows, a.features, chunked(a.x, a.bf16, a.features));
+    const Source<T> x = source<T>(a.x, a.rows, a.features);
     const float* bias = (const float*)a.bias.p;
     if (a.rows) {
-        const S w = source<S>(a.w, a.features, a.classes, chunked(a.w, a.bf16, a.classes));
-        const Statistics<exact> stats{bias, a.bias.rep, a.labels, k.part, k.z_label, a.rows, 0, a.classes, p.parts};
-        e = launch_product<BM, 128, WM, WN, true, false>(x, w, a.n, a.rows, a.classes, a.features, 1, a.features, stats, s);
+        const Statistics<exact, BM, 128, WN> stats{bias, a.bias.rep, a.labels, k.part, k.z_label, once ? k.z : nullptr, a.rows, 0, a.classes, p.parts, p.piece};
+        e = launch_product<BM, 128, WM, WN, true, false>(x, source<T>(a.w, a.features, a.classes), a.n, a.rows, a.classes, a.features, 1, a.features, stats, s);
         if (e != hipSuccess) return e;
     }
     if ((e = join_rows(a, p, k, s)) != hipSuccess || !a.grad) return e;
     const Labelled live{a.labels, a.classes};
     for (int i = 0; i < p.pieces; ++i) {
         const int c0 = i * p.piece, cols = std::min(p.piece, a.classes - c0), ld = up_to(cols, 128);
-        Rows wr = a.w;
-        wr.p = (T*)a.w.p + c0;
-        const S w = source<S>(wr, a.features, cols, chunked(wr, a.bf16, cols));
-        const S g = source<S>(Rows{k.g, (long long)a.rows * ld, ld}, a.rows, ld, true);              // zero beyond cols
-        if (a.rows) {
+        const Source<T> w = source<T>(Rows{(T*)a.w.p + c0, a.w.rep, a.w.row}, a.features, cols);
+        const Source<T> g = source<T>(Rows{k.g, (long long)a.rows * ld, ld}, a.rows, ld);            // zero beyond cols
+        if (once) {
+            gradient_columns_kernel<exact, T><<<dim3((unsigned)((ld / 4 + 255) / 256), (unsigned)a.n), 256, 0, s>>>(
+                k.z, a.labels, k.norm, a.rows, a.classes, ld, (T*)k.g, k.factor, (float*)a.db.p, a.db.rep);
+            e = hipGetLastError();
+        } else if (a.rows) {
             const Softmax<exact> soft{bias, a.bias.rep, a.labels, k.norm, a.db.p ? k.sums : nullptr, a.rows, c0, a.classes, ld, p.blocks};
             e = launch_product<BM, 128, WM, WN, true, false>(x, w, a.n, a.rows, cols, a.features, 1, a.features, Gradient<exact, T>{soft, (T*)k.g}, s);
-            if (e != hipSuccess) return e;
+            if (e == hipSuccess) e = bias_grad(a, p, k, ld, c0, cols, s);
         }
+        if (e != hipSuccess) return e;
         if (a.dx.p && a.rows) {
             const StoreShare store{k.share, a.rows, a.features, p.ldx, a.n, i > 0};
             e = launch_product<BM, 128, WM, WN, true, true>(g, w, a.n, a.rows, a.features, cols, p.splits, p.split_len, store, s);
@@ -437,11 +527,10 @@ template <class S, typename T, int BM, int WM, int WN> hipError_t run_general(co
         }
         if (a.dw.p) {
             const StoreTile<T> store{(T*)a.dw.p + c0, a.dw.rep, a.dw.row, k.factor, a.features, cols};
-            const S xl = source<S>(a.x, a.rows, a.features, x.vec, live);
-            e = launch_product<128, 128, 2, 2, false, false>(xl, g, a.n, a.features, cols, a.rows, 1, std::max(1, a.rows), store, s);
+            e = launch_product<128, 128, 2, 2, false, false>(source<T>(a.x, a.rows, a.features, live), g, a.n, a.features, cols, a.rows, 1,
+                                                             std::max(1, a.rows), store, s);
             if (e != hipSuccess) return e;
         }
-        if ((e = bias_grad(a, p, k, ld, c0, cols, s)) != hipSuccess) return e;
     }
     return input_grad<T>(a, p, k, s);
 }
@@ -469,7 +558,7 @@ template <typename T, int BM> hipError_t run_direct(const LossArgs& a, const Pla
     for (int c0 = 0; c0 < a.classes; c0 += step) {
         const int cols = std::min(step, a.classes - c0);
         if ((e = weights(c0, cols, false, w)) != hipSuccess) return e;
-        const Statistics<PL == 3> stats{bias, a.bias.rep, a.labels, k.part, k.z_label, a.rows, c0, a.classes, p.parts};
+        const Statistics<PL == 3, BM, 256, 4> stats{bias, a.bias.rep, a.labels, k.part, k.z_label, nullptr, a.rows, c0, a.classes, p.parts, 0};
         e = launch_direct<PL, PL, BM, 256, 2, 4, true, false>(x, w, a.n, a.rows, cols, a.features, 1, a.features, stats, s);
         if (e != hipSuccess) return e;
     }
@@ -489,7 +578,7 @@ template <typename T, int BM> hipError_t run_direct(const LossArgs& a, const Pla
         if (a.dw.p) {
             if (PL == 1) {
                 const Rows out{(__bf16*)a.dw.p + c0, a.dw.rep, a.dw.row};
-                const StoreRows store{(__bf16*)out.p, out.rep, out.row, k.factor, a.features, cols, chunked(out, 1, 8)};
+                const StoreRows store{(__bf16*)out.p, out.rep, out.row, k.factor, a.features, cols};
                 e = launch_direct<PL, PL, 256, 256, 2, 4, false, false>(x, g, a.n, a.features, cols, a.rows, 1, a.rows, store, s);
             } else {
                 const StoreTile<float> store{(float*)a.dw.p + c0, a.dw.rep, a.dw.row, k.factor, a.features, cols};
@@ -516,8 +605,8 @@ hipError_t launch_loss(const LossArgs& a, hipStream_t s)
         if (a.bf16) return p.small ? run_direct<__bf16, 128>(a, p, s) : run_direct<__bf16, 256>(a, p, s);
         return p.small ? run_direct<float, 128>(a, p, s) : run_direct<float, 256>(a, p, s);
     }
-    if (a.bf16) return p.small ? run_general<SourceBf16, __bf16, 32, 1, 4>(a, p, s) : run_general<SourceBf16, __bf16, 128, 2, 2>(a, p, s);
-    return p.small ? run_general<SourceF32, float, 32, 1, 4>(a, p, s) : run_general<SourceF32, float, 128, 2, 2>(a, p, s);
+    if (a.bf16) return p.small ? run_general<__bf16, 32, 1, 4>(a, p, s) : run_general<__bf16, 128, 2, 2>(a, p, s);
+    return p.small ? run_general<float, 32, 1, 4>(a, p, s) : run_general<float, 128, 2, 2>(a, p, s);
 }
 
 }  // namespace head

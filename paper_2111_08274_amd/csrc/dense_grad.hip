@@ -44,7 +44,7 @@ size_t dense_work_bytes(int n, int rows, int, int out, int)
     return align256((size_t)n * shares_of(n, rows, out) * out * sizeof(float));
 }
 
-template <class S, typename T> static hipError_t run(const DenseArgs& a, hipStream_t s)
+template <typename T> static hipError_t run(const DenseArgs& a, hipStream_t s)
 {
     hipError_t e;
     if (a.db.p) {
@@ -57,15 +57,14 @@ template <class S, typename T> static hipError_t run(const DenseArgs& a, hipStre
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     const SourcePacked x{a.x, a.rows, a.in};
-    typedef decltype(S::p) P;
-    const S dy{(P)a.dy.p, a.dy.rep, a.dy.row, a.rows, a.out, chunked(a.dy, a.bf16, a.out), {nullptr, 0}};
+    const Source<T> dy = source<T>(a.dy, a.rows, a.out);
     const StoreTile<float> store{(float*)a.dw.p, a.dw.rep, a.dw.row, nullptr, a.in, a.out};
     return launch_product<128, 128, 2, 2, false, false>(x, dy, a.n, a.in, a.out, a.rows, 1, std::max(1, a.rows), store, s);
 }
 
 hipError_t launch_dense_grad(const DenseArgs& a, hipStream_t s)
 {
-    return a.bf16 ? run<SourceBf16, __bf16>(a, s) : run<SourceF32, float>(a, s);
+    return a.bf16 ? run<__bf16>(a, s) : run<float>(a, s);
 }
 
 }  // namespace head

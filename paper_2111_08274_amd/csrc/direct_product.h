@@ -107,7 +107,8 @@ __global__ __launch_bounds__(WM * WN * 64) void direct_kernel(Plane3 a, Plane3 b
     t.rep = r / splits;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     t.lane = tid & 63;
-    const int bm = tm_i * BM, bn = tn_i * BN, wm = (wave % WM) * TM * 32, wn = (wave / WM) * TN * 32;
+    t.wave = wave;
+    const int bm = t.bm = tm_i * BM, bn = t.bn = tn_i * BN, wm = (wave % WM) * TM * 32, wn = (wave / WM) * TN * 32;
     t.m0 = bm + wm;
     t.n0 = bn + wn;
     const __bf16 *pa = a.p + t.rep * a.rep, *pb = b.p + t.rep * b.rep;
@@ -164,8 +165,8 @@ __global__ __launch_bounds__(WM * WN * 64) void direct_kernel(Plane3 a, Plane3 b
             for (int j = 0; j < TN; ++j) t.acc[i][j] *= kScale;
     }
     if constexpr (Epi::kStaged) {
-        __syncthreads();                                       // the images are free: a part for every wave
-        epi(t, image0 + wave * Epi::template stage_bytes<TN>());
+        __syncthreads();                                       // the images are free
+        epi(t, image0);
     } else epi(t);
 }
 
@@ -185,7 +186,7 @@ hipError_t launch_direct(const Plane3& a, const Plane3& b, int replicas, int M, 
 // x [replicas][rows][cols] -> bf16 [planes][replicas][rows][ld], zero beyond cols and in rows that take no part
 template <typename T>
 __global__ __launch_bounds__(256) void lay_out_kernel(const T* x, long long rep, long long row, int rows, int cols, int ld, long long total, long long plane,
-                                                      bool vec, Labelled live, __bf16* out)
+                                                      Labelled live, __bf16* out)
 {
     const long long at = (long long)blockIdx.x * 256 + threadIdx.x;          // chunk of eight
     if (at >= total) return;
@@ -194,29 +195,22 @@ __global__ __launch_bounds__(256) void lay_out_kernel(const T* x, long long rep,
     const int c = (int)(at - line * chunks) * 8, k = (int)(line / rows), t = (int)(line - (long long)k * rows);
     if (live.labels) live.labels += (long long)k * rows;
     const T* src = x + k * rep + t * row + c;
-    float v[8] = {};
-    if (live.at(t)) {
-        if (vec) { if (c < cols) load8(src, v); }
-        else {
+    Chunk<T> chunk;
+    chunk.load(src, live.at(t) ? cols - c : 0);
+    if constexpr (sizeof(T) == 2) *(u4*)(out + at * 8) = chunk.a;
+    else {
+        u4 part[3];
+        Source<float>::planes(chunk, part);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) if (c + e < cols) v[e] = up(src[e]);
-        }
+        for (int i = 0; i < 3; ++i) *(u4*)(out + i * plane + at * 8) = part[i];
     }
-    if (sizeof(T) == 2) { store8(out + at * 8, v); return; }
-    u2 h[2], m[2], l[2];
-    split3(f4{v[0], v[1], v[2], v[3]}, h[0], m[0], l[0]);
-    split3(f4{v[4], v[5], v[6], v[7]}, h[1], m[1], l[1]);
-    *(u4*)(out + at * 8) = join8(h[0], h[1]);
-    *(u4*)(out + plane + at * 8) = join8(m[0], m[1]);
-    *(u4*)(out + 2 * plane + at * 8) = join8(l[0], l[1]);
 }
 template <typename T>
 hipError_t lay_out(int n, int rows, int cols, int ld, const Rows& x, Labelled live, __bf16* out, hipStream_t s)
 {
     const long long plane = (long long)n * rows * ld, total = plane / 8;
     if (total == 0) return hipSuccess;
-    lay_out_kernel<T><<<(unsigned)((total + 255) / 256), 256, 0, s>>>((const T*)x.p, x.rep, x.row, rows, cols, ld, total, plane,
-                                                                       chunked(x, sizeof(T) == 2, cols), live, out);
+    lay_out_kernel<T><<<(unsigned)((total + 255) / 256), 256, 0, s>>>((const T*)x.p, x.rep, x.row, rows, cols, ld, total, plane, live, out);
     return hipGetLastError();
 }
 
@@ -241,17 +235,15 @@ template <int TN> struct RowStage {
 // C times a factor per replica to a bf16 tensor
 struct StoreRows {
     static constexpr bool kLaneM = true, kStaged = true;
-    template <int TN> static constexpr int stage_bytes() { return RowStage<TN>::kBytes; }
     __bf16* p;
     long long rep, row;
     const float* factor;
     int M, N;
-    bool vec;
     template <int TM, int TN> __device__ __forceinline__ void operator()(const Tile<TM, TN>& t, char* lds) const
     {
         const float f = factor[t.rep];
         __bf16* out = p + t.rep * rep;
-        const RowStage<TN> stage{lds};
+        const RowStage<TN> stage{lds + t.wave * RowStage<TN>::kBytes};
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
 #pragma unroll
@@ -264,7 +256,7 @@ struct StoreRows {
                 const int m = t.m0 + 32 * i + r, n = t.n0 + c;
                 if (m >= M || n >= N) return;
                 __bf16* q = out + m * row + n;
-                if (vec && n + 8 <= N) { *(u4*)q = v; return; }
+                if (n + 8 <= N) { *(u4any*)q = v; return; }
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
                     if (n + e < N) ((unsigned short*)q)[e] = (unsigned short)(v[e / 2] >> (16 * (e % 2)));

@@ -79,32 +79,72 @@ hipError_t launch_loss(const LossArgs& a, hipStream_t s);
 // ---- device pieces ------------------------------------------------------------------------------------------------
 __device__ __forceinline__ float up(__bf16 v) { return (float)v; }
 __device__ __forceinline__ float up(float v) { return v; }
-
-// eight consecutive values from an address of 16 bytes' alignment
-__device__ __forceinline__ void load8(const float* p, float* v)
-{
-    const tiles::f4 a = *(const tiles::f4*)p, b = *(const tiles::f4*)(p + 4);
+// Eight consecutive values of a row, as they are in memory.  Vector accesses need no alignment of their own on this chip (a chunk
+// across a line's end is two accesses), so rows of any stride are read 16 bytes a lane; only a row's last chunk may hold fewer values.
+typedef unsigned int u4any __attribute__((ext_vector_type(4), aligned(2)));
+template <typename T> struct Chunk;
+// keeps a short chunk's eight comparisons where they are used: hoisted out of a loop over rows they would fill the scalar registers
+__device__ __forceinline__ int here(int left) { asm volatile("" : "+v"(left)); return left; }
+template <> struct Chunk<float> {
+    tiles::u4 a, b;
+    __device__ __forceinline__ void load(const float* p, int left)
+    {
+        if (left >= 8) { a = *(const u4any*)p; b = *(const u4any*)(p + 4); return; }
+        a = b = tiles::u4{0, 0, 0, 0};
+        const unsigned* w = (const unsigned*)p;
+        left = here(left);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
-}
-__device__ __forceinline__ void load8(const __bf16* p, float* v)
-{
-    const tiles::u4 a = *(const tiles::u4*)p;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        v[2 * e] = __builtin_bit_cast(float, a[e] << 16);
-        v[2 * e + 1] = __builtin_bit_cast(float, a[e] & 0xffff0000u);
+        for (int e = 0; e < 8; ++e)
+            if (e < left) { if (e < 4) a[e] = w[e]; else b[e - 4] = w[e]; }
     }
-}
-__device__ __forceinline__ void store8(float* p, const float* v)
+    __device__ __forceinline__ void get(float* v) const
+    {
+        const tiles::f4 low = __builtin_bit_cast(tiles::f4, a), high = __builtin_bit_cast(tiles::f4, b);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { v[e] = low[e]; v[4 + e] = high[e]; }
+    }
+};
+template <> struct Chunk<__bf16> {
+    tiles::u4 a;
+    __device__ __forceinline__ void load(const __bf16* p, int left)
+    {
+        if (left >= 8) { a = *(const u4any*)p; return; }
+        a = tiles::u4{0, 0, 0, 0};
+        const unsigned short* w = (const unsigned short*)p;
+        left = here(left);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < left) a[e / 2] |= (unsigned)w[e] << (16 * (e % 2));
+    }
+    __device__ __forceinline__ void get(float* v) const
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[2 * e] = __builtin_bit_cast(float, a[e] << 16);
+            v[2 * e + 1] = __builtin_bit_cast(float, a[e] & 0xffff0000u);
+        }
+    }
+};
+__device__ __forceinline__ void store_chunk(float* p, int left, const float* v)
 {
-    *(tiles::f4*)p = tiles::f4{v[0], v[1], v[2], v[3]};
-    *(tiles::f4*)(p + 4) = tiles::f4{v[4], v[5], v[6], v[7]};
+    if (left >= 8) {
+        *(u4any*)p = __builtin_bit_cast(tiles::u4, (tiles::f4{v[0], v[1], v[2], v[3]}));
+        *(u4any*)(p + 4) = __builtin_bit_cast(tiles::u4, (tiles::f4{v[4], v[5], v[6], v[7]}));
+        return;
+    }
+    left = here(left);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) if (e < left) p[e] = v[e];
 }
-__device__ __forceinline__ void store8(__bf16* p, const float* v)
+__device__ __forceinline__ void store_chunk(__bf16* p, int left, const float* v)
 {
-    *(tiles::u4*)p = tiles::u4{tiles::to_bf16x2(v[0], v[1]), tiles::to_bf16x2(v[2], v[3]), tiles::to_bf16x2(v[4], v[5]),
-                               tiles::to_bf16x2(v[6], v[7])};
+    if (left >= 8) {
+        *(u4any*)p = tiles::u4{tiles::to_bf16x2(v[0], v[1]), tiles::to_bf16x2(v[2], v[3]), tiles::to_bf16x2(v[4], v[5]), tiles::to_bf16x2(v[6], v[7])};
+        return;
+    }
+    left = here(left);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) if (e < left) p[e] = (__bf16)v[e];
 }
 // 2^e of a group from its stored byte; 255 gives infinity, whose product with the group's zeros is the NaN it stands for
 __device__ __forceinline__ float group_unit(unsigned byte) { return __builtin_bit_cast(float, byte << 23); }

@@ -4,7 +4,8 @@
 //             parameter sums dgamma = sum_t dy * xh, dbeta = sum_t dy stay in registers while a thread walks down its
 //             rows (a thread keeps its columns), and one partial per workgroup is added up by a second, small launch in
 //             ascending order: no atomics, the same bits every time.
-// Memory bound: a row is read once into registers (NL lanes, 8 * CH values a lane), both passes run there.
+// Memory bound: a row is read once into registers (NL lanes, 8 * CH values a lane), both passes run there, and the next row is
+// loaded meanwhile.
 #include "head.h"
 
 namespace hadfl {
@@ -12,72 +13,60 @@ namespace head {
 
 namespace {
 
-// lanes per row and chunks of eight values a lane; VEC: chunks of consecutive values from 16-byte aligned rows, else lane i
-// holds the columns i, i + NL, ... (unaligned rows in whole cache lines all the same)
-template <int NL, bool VEC> __device__ __forceinline__ int column(int lane, int i, int e)
-{
-    return VEC ? (i * NL + lane) * 8 + e : (i * 8 + e) * NL + lane;
-}
+// first column of chunk i of a lane
+template <int NL> __device__ __forceinline__ int column(int lane, int i) { return (i * NL + lane) * 8; }
 
-template <typename T, int NL, int CH, bool VEC>
-__device__ __forceinline__ void load_row(const T* row, int lane, int cols, float (&v)[CH][8])
-{
+// a lane's chunks of a row, as they are in memory: the next row is on its way while one is worked on
+template <typename T, int NL, int CH> struct RowOf {
+    Chunk<T> chunk[CH];
+    __device__ __forceinline__ void load(const T* row, int lane, int cols)
+    {
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-        if (VEC) {
-            if (column<NL, VEC>(lane, i, 0) < cols) load8(row + column<NL, VEC>(lane, i, 0), v[i]);
-            else for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
-        } else {
+        for (int i = 0; i < CH; ++i) chunk[i].load(row + column<NL>(lane, i), cols - column<NL>(lane, i));
+    }
+    __device__ __forceinline__ void get(float (&v)[CH][8]) const
+    {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) { const int c = column<NL, VEC>(lane, i, e); v[i][e] = c < cols ? up(row[c]) : 0.f; }
+        for (int i = 0; i < CH; ++i) chunk[i].get(v[i]);
+    }
+};
+// the same from an 8-bit checkpoint, whose surplus columns are zero
+template <int NL, int CH> struct KeptOf {
+    tiles::u2 q[CH];
+    unsigned e[CH];
+    __device__ __forceinline__ void load(const Packed& kept, long long line, int lane)
+    {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int c = column<NL>(lane, i);
+            q[i] = tiles::u2{0, 0};
+            e[i] = 1;
+            if (c >= kept.cols) continue;
+            q[i] = *(const tiles::u2*)(kept.q + line * kept.cols + c);
+            e[i] = kept.e[line * (kept.cols / kGroup) + c / kGroup];
         }
     }
-}
-template <int NL, int CH, bool VEC>
-__device__ __forceinline__ void load_kept(const Packed& kept, long long line, int lane, int cols, float (&v)[CH][8])
-{
-    const int8_t* q = kept.q + line * kept.cols;
-    const uint8_t* exps = kept.e + line * (kept.cols / kGroup);
+    __device__ __forceinline__ void get(float (&v)[CH][8]) const
+    {
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-        if (VEC) {
-            const int c = column<NL, VEC>(lane, i, 0);
-            if (c < cols) {
-                const tiles::u2 w = *(const tiles::u2*)(q + c);
-                const float unit = group_unit(exps[c / kGroup]);
+        for (int i = 0; i < CH; ++i)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[i][e] = (float)(int)(int8_t)(w[e / 4] >> (8 * (e % 4))) * unit;
-            } else for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int c = column<NL, VEC>(lane, i, e);
-                v[i][e] = c < cols ? (float)(int)q[c] * group_unit(exps[c / kGroup]) : 0.f;
-            }
-        }
+            for (int j = 0; j < 8; ++j) v[i][j] = (float)(int)(int8_t)(q[i][j / 4] >> (8 * (j % 4))) * group_unit(e[i]);
     }
+};
+// gamma, beta: in memory as any row of floats
+template <int NL, int CH>
+__device__ __forceinline__ void load_param(const float* p, int lane, int cols, float (&v)[CH][8])
+{
+    RowOf<float, NL, CH> r;
+    r.load(p, lane, cols);
+    r.get(v);
 }
-template <typename T, int NL, int CH, bool VEC>
+template <typename T, int NL, int CH>
 __device__ __forceinline__ void store_row(T* row, int lane, int cols, const float (&v)[CH][8])
 {
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-        if (VEC) {
-            if (column<NL, VEC>(lane, i, 0) < cols) store8(row + column<NL, VEC>(lane, i, 0), v[i]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) { const int c = column<NL, VEC>(lane, i, e); if (c < cols) row[c] = (T)v[i][e]; }
-        }
-    }
-}
-// parameter vectors have no alignment of their own: gamma may start anywhere in a parameter row
-template <int NL, int CH, bool VEC>
-__device__ __forceinline__ void load_param(const float* p, int lane, int cols, float (&v)[CH][8])
-{
-#pragma unroll
-    for (int i = 0; i < CH; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) { const int c = column<NL, VEC>(lane, i, e); v[i][e] = c < cols ? p[c] : 0.f; }
+    for (int i = 0; i < CH; ++i) store_chunk(row + column<NL>(lane, i), cols - column<NL>(lane, i), v[i]);
 }
 
 // sums of two values over the NL lanes of a row, to all of them; NL = 256: the whole workgroup, through LDS in two slots used
@@ -100,20 +89,25 @@ template <int NL> struct RowSum {
     }
 };
 
-template <typename T, int NL, int CH, bool VEC>
+template <typename T, int NL, int CH>
 __global__ __launch_bounds__(256) void norm_forward_kernel(NormArgs a)
 {
     constexpr int RPB = 256 / NL;                              // rows a workgroup works on at once
     __shared__ float slot[2][4][2];
     const int lane = threadIdx.x % NL, k = blockIdx.y, step = gridDim.x * RPB;
+    const T* x = (const T*)a.x.p + k * a.x.rep;
+    RowOf<T, NL, CH> next;
+    int t = blockIdx.x * RPB + threadIdx.x / NL;
+    if (t < a.rows) next.load(x + t * a.x.row, lane, a.cols);
     float g[CH][8], b[CH][8];
-    load_param<NL, CH, VEC>((const float*)a.gamma.p + k * a.gamma.rep, lane, a.cols, g);
-    load_param<NL, CH, VEC>((const float*)a.beta.p + k * a.beta.rep, lane, a.cols, b);
+    load_param<NL, CH>((const float*)a.gamma.p + k * a.gamma.rep, lane, a.cols, g);
+    load_param<NL, CH>((const float*)a.beta.p + k * a.beta.rep, lane, a.cols, b);
     RowSum<NL> sum{slot};
     const float inv = 1.f / (float)a.cols;
-    for (int t = blockIdx.x * RPB + threadIdx.x / NL; t < a.rows; t += step) {
+    for (; t < a.rows; t += step) {
         float v[CH][8], m = 0.f, q = 0.f, none = 0.f;
-        load_row<T, NL, CH, VEC>((const T*)a.x.p + k * a.x.rep + t * a.x.row, lane, a.cols, v);
+        next.get(v);
+        if (t + step < a.rows) next.load(x + (t + step) * a.x.row, lane, a.cols);
 #pragma unroll
         for (int i = 0; i < CH; ++i)
 #pragma unroll
@@ -124,7 +118,7 @@ __global__ __launch_bounds__(256) void norm_forward_kernel(NormArgs a)
         for (int i = 0; i < CH; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                v[i][e] = column<NL, VEC>(lane, i, e) < a.cols ? v[i][e] - m : 0.f;
+                v[i][e] = column<NL>(lane, i) + e < a.cols ? v[i][e] - m : 0.f;
                 q += v[i][e] * v[i][e];
             }
         sum.add(q, none);
@@ -133,34 +127,48 @@ __global__ __launch_bounds__(256) void norm_forward_kernel(NormArgs a)
         for (int i = 0; i < CH; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[i][e] = v[i][e] * r * g[i][e] + b[i][e];
-        store_row<T, NL, CH, VEC>((T*)a.y.p + k * a.y.rep + t * a.y.row, lane, a.cols, v);
+        store_row<T, NL, CH>((T*)a.y.p + k * a.y.rep + t * a.y.row, lane, a.cols, v);
         if (lane == 0 && a.mean) { a.mean[(long long)k * a.rows + t] = m; a.rstd[(long long)k * a.rows + t] = r; }
     }
 }
 
-template <typename T, bool KEPT, int NL, int CH, bool VEC>
+template <typename T, bool KEPT, int NL, int CH>
 __global__ __launch_bounds__(256) void norm_backward_kernel(NormArgs a, float* partial)
 {
     constexpr int RPB = 256 / NL;
     __shared__ float slot[2][4][2];
     __shared__ float parts[NL == 256 ? 1 : 256][17];           // 17: the sums below read a column of it
     const int lane = threadIdx.x % NL, k = blockIdx.y, step = gridDim.x * RPB;
+    const T *x = (const T*)a.x.p + k * a.x.rep, *dy = (const T*)a.dy.p + k * a.dy.rep;
+    const long long lines = (long long)k * a.rows;
+    RowOf<T, NL, CH> next_d, next_x;
+    KeptOf<NL, CH> next_k;
+    float next_m = 0.f, next_r = 0.f;
+    auto fetch = [&](int t) {
+        next_d.load(dy + t * a.dy.row, lane, a.cols);
+        if (KEPT) next_k.load(a.kept, lines + t, lane);
+        else next_x.load(x + t * a.x.row, lane, a.cols);
+        next_m = a.mean[lines + t];
+        next_r = a.rstd[lines + t];
+    };
+    int t = blockIdx.x * RPB + threadIdx.x / NL;
+    if (t < a.rows) fetch(t);
     float g[CH][8], sg[CH][8] = {}, sb[CH][8] = {};
-    load_param<NL, CH, VEC>((const float*)a.gamma.p + k * a.gamma.rep, lane, a.cols, g);
+    load_param<NL, CH>((const float*)a.gamma.p + k * a.gamma.rep, lane, a.cols, g);
     RowSum<NL> sum{slot};
     const float inv = 1.f / (float)a.cols;
-    for (int t = blockIdx.x * RPB + threadIdx.x / NL; t < a.rows; t += step) {
-        const long long line = (long long)k * a.rows + t;
+    for (; t < a.rows; t += step) {
         float v[CH][8], d[CH][8], m1 = 0.f, m2 = 0.f;
-        load_row<T, NL, CH, VEC>((const T*)a.dy.p + k * a.dy.rep + t * a.dy.row, lane, a.cols, d);
-        if (KEPT) load_kept<NL, CH, VEC>(a.kept, line, lane, a.cols, v);
-        else load_row<T, NL, CH, VEC>((const T*)a.x.p + k * a.x.rep + t * a.x.row, lane, a.cols, v);
-        const float m = a.mean[line], r = a.rstd[line];
+        const float m = next_m, r = next_r;
+        next_d.get(d);
+        if (KEPT) next_k.get(v);
+        else next_x.get(v);
+        if (t + step < a.rows) fetch(t + step);
 #pragma unroll
         for (int i = 0; i < CH; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float xh = column<NL, VEC>(lane, i, e) < a.cols ? (v[i][e] - m) * r : 0.f;
+                const float xh = column<NL>(lane, i) + e < a.cols ? (v[i][e] - m) * r : 0.f;
                 v[i][e] = xh;
                 sg[i][e] += d[i][e] * xh;
                 sb[i][e] += d[i][e];
@@ -175,36 +183,28 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(NormArgs a, float* p
         for (int i = 0; i < CH; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) d[i][e] = r * (d[i][e] - m1 - v[i][e] * m2);
-        store_row<T, NL, CH, VEC>((T*)a.dx.p + k * a.dx.rep + t * a.dx.row, lane, a.cols, d);
+        store_row<T, NL, CH>((T*)a.dx.p + k * a.dx.rep + t * a.dx.row, lane, a.cols, d);
     }
     // the workgroup's sums: to its partial, or straight to the result where it is the replica's only one
     float* og = partial ? partial + ((long long)k * gridDim.x + blockIdx.x) * 2 * a.cols : (float*)a.dgamma.p + k * a.dgamma.rep;
     float* ob = partial ? og + a.cols : (float*)a.dbeta.p + k * a.dbeta.rep;
+    if (RPB == 1) {
+        store_row<float, NL, CH>(og, lane, a.cols, sg);
+        store_row<float, NL, CH>(ob, lane, a.cols, sb);
+        return;
+    }
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-        if (RPB > 1) {
-            __syncthreads();
+    for (int i = 0; i < CH; ++i) {                             // of the rows side by side, in ascending order
+        __syncthreads();
 #pragma unroll
-            for (int e = 0; e < 8; ++e) { parts[threadIdx.x][e] = sg[i][e]; parts[threadIdx.x][8 + e] = sb[i][e]; }
-            __syncthreads();
-        }
-        // sixteen sums a lane of the row: spread over all threads
+        for (int e = 0; e < 8; ++e) { parts[threadIdx.x][e] = sg[i][e]; parts[threadIdx.x][8 + e] = sb[i][e]; }
+        __syncthreads();
         for (int w = threadIdx.x; w < NL * 16; w += 256) {
-            const int l = RPB > 1 ? w / 16 : lane;
-            if (RPB > 1) {
-                const int e = w % 16, c = column<NL, VEC>(l, i, e & 7);
-                float v = 0.f;
+            const int l = w / 16, e = w % 16, c = column<NL>(l, i) + (e & 7);
+            float s = 0.f;
 #pragma unroll
-                for (int j = 0; j < RPB; ++j) v += parts[j * NL + l][e];
-                if (c < a.cols) (e < 8 ? og : ob)[c] = v;
-            }
-        }
-        if (RPB == 1) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int c = column<NL, VEC>(lane, i, e);
-                if (c < a.cols) { og[c] = sg[i][e]; ob[c] = sb[i][e]; }
-            }
+            for (int j = 0; j < RPB; ++j) s += parts[j * NL + l][e];
+            if (c < a.cols) (e < 8 ? og : ob)[c] = s;
         }
     }
 }
@@ -303,7 +303,7 @@ __global__ __launch_bounds__(256) void norm_sums_kernel(const float* partial, in
 
 constexpr int kLongest = 8192;     // columns that a workgroup keeps in registers
 
-int lanes_of(int cols) { return cols <= 128 ? 16 : cols <= 2048 ? 64 : 256; }
+int lanes_of(int cols) { return cols <= 128 ? 16 : cols <= 1024 ? 64 : 256; }
 int chunks_of(int cols) { const int per = lanes_of(cols) * 8; return (cols + per - 1) / per; }
 
 // workgroups per replica: enough to fill the chip four deep, each with whole rows
@@ -314,25 +314,24 @@ int groups_of(int n, int rows, int cols)
     return std::max(1, std::min((rows + rpb - 1) / rpb, std::max(1, 1024 / n)));
 }
 
-template <typename T, bool VEC> hipError_t forward(const NormArgs& a, hipStream_t s)
+template <typename T> hipError_t forward(const NormArgs& a, hipStream_t s)
 {
-    const dim3 grid((unsigned)groups_of(a.n, a.rows, a.cols), (unsigned)a.n);
-#define HADFL_CASE(NL, CH) case NL * 8 + CH: norm_forward_kernel<T, NL, CH, VEC><<<grid, 256, 0, s>>>(a); break;
+    const int rpb = 256 / lanes_of(a.cols);
+    const dim3 grid((unsigned)std::max(1, std::min((a.rows + rpb - 1) / rpb, std::max(1, 2048 / a.n))), (unsigned)a.n);
+#define HADFL_CASE(NL, CH) case NL * 8 + CH: norm_forward_kernel<T, NL, CH><<<grid, 256, 0, s>>>(a); break;
     switch (lanes_of(a.cols) * 8 + chunks_of(a.cols)) {
-        HADFL_CASE(16, 1) HADFL_CASE(64, 1) HADFL_CASE(64, 2) HADFL_CASE(64, 3) HADFL_CASE(64, 4)
-        HADFL_CASE(256, 2) HADFL_CASE(256, 3) HADFL_CASE(256, 4)
+        HADFL_CASE(16, 1) HADFL_CASE(64, 1) HADFL_CASE(64, 2) HADFL_CASE(256, 1) HADFL_CASE(256, 2) HADFL_CASE(256, 3) HADFL_CASE(256, 4)
         default: return hipErrorInvalidValue;
     }
 #undef HADFL_CASE
     return hipGetLastError();
 }
-template <typename T, bool KEPT, bool VEC> hipError_t backward(const NormArgs& a, float* partial, int groups, hipStream_t s)
+template <typename T, bool KEPT> hipError_t backward(const NormArgs& a, float* partial, int groups, hipStream_t s)
 {
     const dim3 grid((unsigned)groups, (unsigned)a.n);
-#define HADFL_CASE(NL, CH) case NL * 8 + CH: norm_backward_kernel<T, KEPT, NL, CH, VEC><<<grid, 256, 0, s>>>(a, partial); break;
+#define HADFL_CASE(NL, CH) case NL * 8 + CH: norm_backward_kernel<T, KEPT, NL, CH><<<grid, 256, 0, s>>>(a, partial); break;
     switch (lanes_of(a.cols) * 8 + chunks_of(a.cols)) {
-        HADFL_CASE(16, 1) HADFL_CASE(64, 1) HADFL_CASE(64, 2) HADFL_CASE(64, 3) HADFL_CASE(64, 4)
-        HADFL_CASE(256, 2) HADFL_CASE(256, 3) HADFL_CASE(256, 4)
+        HADFL_CASE(16, 1) HADFL_CASE(64, 1) HADFL_CASE(64, 2) HADFL_CASE(256, 1) HADFL_CASE(256, 2) HADFL_CASE(256, 3) HADFL_CASE(256, 4)
         default: return hipErrorInvalidValue;
     }
 #undef HADFL_CASE
@@ -349,9 +348,8 @@ template <typename T, bool KEPT> hipError_t backward_any(const NormArgs& a, hipS
         if (a.rows) norm_backward_long_kernel<T, KEPT><<<dim3((unsigned)a.rows, (unsigned)a.n), 256, 0, s>>>(a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     } else {
-        const bool vec = chunked(a.dy, a.bf16, a.cols) && chunked(a.dx, a.bf16, a.cols) && (KEPT || chunked(a.x, a.bf16, a.cols));
         if (groups == 1) partial = nullptr;
-        e = vec ? backward<T, KEPT, true>(a, partial, groups, s) : backward<T, KEPT, false>(a, partial, groups, s);
+        e = backward<T, KEPT>(a, partial, groups, s);
         if (e != hipSuccess || groups == 1) return e;
     }
     norm_sums_kernel<<<dim3((unsigned)((2 * a.cols + 31) / 32), (unsigned)a.n), 256, 0, s>>>(partial, groups, a.cols, a.dgamma, a.dbeta);
@@ -374,9 +372,7 @@ hipError_t launch_norm_forward(const NormArgs& a, hipStream_t s)
         else norm_forward_long_kernel<float><<<grid, 256, 0, s>>>(a);
         return hipGetLastError();
     }
-    const bool vec = chunked(a.x, a.bf16, a.cols) && chunked(a.y, a.bf16, a.cols);
-    if (a.bf16) return vec ? forward<__bf16, true>(a, s) : forward<__bf16, false>(a, s);
-    return vec ? forward<float, true>(a, s) : forward<float, false>(a, s);
+    return a.bf16 ? forward<__bf16>(a, s) : forward<float>(a, s);
 }
 
 hipError_t launch_norm_backward(const NormArgs& a, hipStream_t s)

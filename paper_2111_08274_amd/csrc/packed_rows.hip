@@ -13,7 +13,7 @@ namespace {
 
 constexpr int kLane = 16;          // values a lane packs
 
-template <typename T, bool VEC>
+template <typename T>
 __global__ __launch_bounds__(256) void pack_rows_kernel(const T* x, long long rep, long long row, int rows, int cols, int chunks,
                                                         long long total, int8_t* q, uint8_t* exps)
 {
@@ -27,14 +27,11 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(const T* x, long long re
 #pragma unroll
     for (int i = 0; i < kLane; ++i) v[i] = 0.f;
     if (live) {
-        if (VEC) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                if (c + 8 * h < cols) load8(src + 8 * h, v + 8 * h);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kLane; ++i)
-                if (c + i < cols) v[i] = up(src[i]);
+        for (int h = 0; h < 2; ++h) {
+            Chunk<T> chunk;
+            chunk.load(src + 8 * h, cols - c - 8 * h);
+            chunk.get(v + 8 * h);
         }
     }
     unsigned top = 0;                                                        // of |x|'s bits: orders like |x|, NaN above all
@@ -63,7 +60,7 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(const T* x, long long re
     if ((threadIdx.x & 1) == 0) exps[at >> 1] = poison ? 255 : (uint8_t)byte;
 }
 
-template <typename T, bool VEC>
+template <typename T>
 __global__ __launch_bounds__(256) void unpack_rows_kernel(Packed src, int rows, int cols, int chunks, long long total, T* out,
                                                           long long rep, long long row)
 {
@@ -78,15 +75,8 @@ __global__ __launch_bounds__(256) void unpack_rows_kernel(Packed src, int rows, 
     float v[kLane];
 #pragma unroll
     for (int i = 0; i < kLane; ++i) v[i] = (float)(int)(int8_t)(w[i / 4] >> (8 * (i % 4))) * unit;
-    if (VEC) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-            if (c + 8 * h < cols) store8(dst + 8 * h, v + 8 * h);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kLane; ++i)
-            if (c + i < cols) dst[i] = (T)v[i];
-    }
+    for (int h = 0; h < 2; ++h) store_chunk(dst + 8 * h, cols - c - 8 * h, v + 8 * h);
 }
 
 }  // namespace
@@ -98,15 +88,12 @@ hipError_t launch_pack(int n, int rows, int cols, int bf16, const Rows& x, void*
     const long long total = (long long)n * rows * chunks;
     if (total == 0) return hipSuccess;
     const unsigned grid = (unsigned)((total + 255) / 256);
-    const bool vec = chunked(x, bf16, cols);
     int8_t* q = const_cast<int8_t*>(p.q);
     uint8_t* e = const_cast<uint8_t*>(p.e);
     if (bf16) {
-        auto* kernel = vec ? pack_rows_kernel<__bf16, true> : pack_rows_kernel<__bf16, false>;
-        kernel<<<grid, 256, 0, s>>>((const __bf16*)x.p, x.rep, x.row, rows, cols, chunks, total, q, e);
+        pack_rows_kernel<__bf16><<<grid, 256, 0, s>>>((const __bf16*)x.p, x.rep, x.row, rows, cols, chunks, total, q, e);
     } else {
-        auto* kernel = vec ? pack_rows_kernel<float, true> : pack_rows_kernel<float, false>;
-        kernel<<<grid, 256, 0, s>>>((const float*)x.p, x.rep, x.row, rows, cols, chunks, total, q, e);
+        pack_rows_kernel<float><<<grid, 256, 0, s>>>((const float*)x.p, x.rep, x.row, rows, cols, chunks, total, q, e);
     }
     return hipGetLastError();
 }
@@ -118,13 +105,10 @@ hipError_t launch_unpack(int n, int rows, int cols, int bf16, const void* packed
     const long long total = (long long)n * rows * chunks;
     if (total == 0) return hipSuccess;
     const unsigned grid = (unsigned)((total + 255) / 256);
-    const bool vec = chunked(out, bf16, cols);
     if (bf16) {
-        auto* kernel = vec ? unpack_rows_kernel<__bf16, true> : unpack_rows_kernel<__bf16, false>;
-        kernel<<<grid, 256, 0, s>>>(p, rows, cols, chunks, total, (__bf16*)out.p, out.rep, out.row);
+        unpack_rows_kernel<__bf16><<<grid, 256, 0, s>>>(p, rows, cols, chunks, total, (__bf16*)out.p, out.rep, out.row);
     } else {
-        auto* kernel = vec ? unpack_rows_kernel<float, true> : unpack_rows_kernel<float, false>;
-        kernel<<<grid, 256, 0, s>>>(p, rows, cols, chunks, total, (float*)out.p, out.rep, out.row);
+        unpack_rows_kernel<float><<<grid, 256, 0, s>>>(p, rows, cols, chunks, total, (float*)out.p, out.rep, out.row);
     }
     return hipGetLastError();
 }

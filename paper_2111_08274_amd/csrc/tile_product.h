@@ -20,55 +20,33 @@ struct Labelled {
     __device__ __forceinline__ bool at(int t) const { return !labels || (unsigned)labels[t] < (unsigned)classes; }
 };
 
-struct SourceF32 {
-    static constexpr int kPlanes = 3;
-    struct Raw { f4 a, b; };
-    const float* p;
+template <typename T> struct Source {
+    static constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;
+    typedef Chunk<T> Raw;
+    const T* p;
     long long rep, row;
     int rows, cols;
-    bool vec;
     Labelled live;
     __device__ __forceinline__ void bind(int k) { p += k * rep; if (live.labels) live.labels += (long long)k * rows; }
     __device__ __forceinline__ Raw load(int r, int c) const
     {
-        Raw v = {};
-        if (r >= rows || c >= cols || !live.at(r)) return v;
-        const float* s = p + r * row + c;
-        if (vec) { v.a = *(const f4*)s; v.b = *(const f4*)(s + 4); return v; }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) if (c + e < cols) { if (e < 4) v.a[e] = s[e]; else v.b[e - 4] = s[e]; }
+        Raw v;
+        v.load(p + r * row + c, r < rows && live.at(r) ? cols - c : 0);
         return v;
     }
-    static __device__ __forceinline__ void planes(const Raw& v, u4 (&out)[3])
+    static __device__ __forceinline__ void planes(const Chunk<__bf16>& v, u4 (&out)[1]) { out[0] = v.a; }
+    static __device__ __forceinline__ void planes(const Chunk<float>& v, u4 (&out)[3])
     {
         u2 h[2], m[2], l[2];
-        split3(v.a, h[0], m[0], l[0]);
-        split3(v.b, h[1], m[1], l[1]);
+        split3(__builtin_bit_cast(f4, v.a), h[0], m[0], l[0]);
+        split3(__builtin_bit_cast(f4, v.b), h[1], m[1], l[1]);
         out[0] = join8(h[0], h[1]); out[1] = join8(m[0], m[1]); out[2] = join8(l[0], l[1]);
     }
 };
-
-struct SourceBf16 {
-    static constexpr int kPlanes = 1;
-    struct Raw { u4 a; };
-    const __bf16* p;
-    long long rep, row;
-    int rows, cols;
-    bool vec;
-    Labelled live;
-    __device__ __forceinline__ void bind(int k) { p += k * rep; if (live.labels) live.labels += (long long)k * rows; }
-    __device__ __forceinline__ Raw load(int r, int c) const
-    {
-        Raw v = {};
-        if (r >= rows || c >= cols || !live.at(r)) return v;
-        const unsigned short* s = (const unsigned short*)(p + r * row + c);
-        if (vec) { v.a = *(const u4*)s; return v; }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) if (c + e < cols) v.a[e / 2] |= (unsigned)s[e] << (16 * (e % 2));
-        return v;
-    }
-    static __device__ __forceinline__ void planes(const Raw& v, u4 (&out)[1]) { out[0] = v.a; }
-};
+template <typename T> Source<T> source(const Rows& r, int rows, int cols, Labelled live = {nullptr, 0})
+{
+    return Source<T>{(const T*)r.p, r.rep, r.row, rows, cols, live};
+}
 
 struct SourcePacked {              // rows and columns of one replica; the surplus columns of the checkpoint are zero
     static constexpr int kPlanes = 1;
@@ -120,7 +98,7 @@ template <bool ALONG, int BR, int KS> struct Image {
 // n0 + 32 * tn + 8 * (i / 4) + 4 * (lane / 32) + i % 4 of acc[tm][tn][i]; else n and m change places.
 template <int TM, int TN> struct Tile {
     f16 acc[TM][TN];
-    int rep, split, m0, n0, lane;
+    int rep, split, m0, n0, lane, wave, bm, bn;                 // bm, bn: where the workgroup's tile begins
 };
 
 template <class SA, bool A_ALONG, class SB, bool B_ALONG, int BM, int BN, int WM, int WN, int KS, int NBUF, bool LANE_M, class Epi>
@@ -144,7 +122,8 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(SA a, SB b, int K
     b.bind(t.rep);
     const int tid = threadIdx.x, wave = tid / 64;
     t.lane = tid & 63;
-    const int bm = tm_i * BM, bn = tn_i * BN, wm = (wave % WM) * TM * 32, wn = (wave / WM) * TN * 32;
+    t.wave = wave;
+    const int bm = t.bm = tm_i * BM, bn = t.bn = tn_i * BN, wm = (wave % WM) * TM * 32, wn = (wave / WM) * TN * 32;
     t.m0 = bm + wm;
     t.n0 = bn + wn;
     const int k_begin = t.split * split_len, k_end = min(K, k_begin + split_len);
@@ -233,7 +212,10 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(SA a, SB b, int K
 #pragma unroll
             for (int j = 0; j < TN; ++j) t.acc[i][j] *= kScale;
     }
-    epi(t);
+    if constexpr (Epi::kStaged) {
+        __syncthreads();
+        epi(t, smem);
+    } else epi(t);
 }
 
 // ---- epilogues that only store ---------------------------------------------------------------------------------
@@ -292,7 +274,8 @@ template <int BM, int BN, int WM, int WN, bool A_ALONG, bool B_ALONG, class SA, 
 hipError_t launch_product(const SA& a, const SB& b, int replicas, int M, int N, int K, int splits, int split_len, const Epi& epi, hipStream_t s)
 {
     constexpr bool wide = SA::kPlanes == 3 || SB::kPlanes == 3;
-    constexpr int KS = BM == 32 && !wide ? 64 : 32, NBUF = wide ? 1 : 2;
+    // few rows: memory bound, so more of W on its way at a time and one image, for more workgroups on a compute unit
+    constexpr int KS = BM == 32 ? (wide ? 64 : 128) : 32, NBUF = wide || BM == 32 ? 1 : 2;
     const int tm = (M + BM - 1) / BM, tn = (N + BN - 1) / BN;
     const long long total = (long long)replicas * splits * tm * tn;
     if (total == 0) return hipSuccess;
