@@ -65,7 +65,7 @@ __device__ __forceinline__ void join(float2& have, const float2& v)
 
 // The statistics of a tile: per wave and row, then joined over the WN waves that share rows.  z: the logits too (few rows), or null.
 template <bool EXACT, int BM, int BN, int WN> struct Statistics {
-    static constexpr bool kLaneM = true, kStaged = true;
+    static constexpr bool kLaneM = true, kStaged = true, kSums = false;
     const float* bias;
     long long bias_rep;
     const int32_t* labels;
@@ -160,8 +160,7 @@ __global__ __launch_bounds__(256) void row_loss_kernel(const float2* part, const
             have.y *= exp_down<true>(have.x - base);
 #pragma unroll
             for (int u = 0; u < U; ++u) have.y += v[u].y * exp_down<true>(v[u].x - base);
-            have.x = top;
-            // all -inf so far: the sums are zero or NaN, and exp(-inf) took a NaN along: 0 * NaN
+            have.x = top;                                      // all -inf so far: the sums are zeros, or NaNs that stay
         }
     got[threadIdx.x] = have;
     for (int d = shares / 2; d > 0; d /= 2) {
@@ -199,37 +198,26 @@ __global__ __launch_bounds__(256) void mean_loss_kernel(const float* row_loss, c
     mean_of_rows(sum, count, sums, counts, loss + blockIdx.x, factor + blockIdx.x);
 }
 
-// Few rows: G of the whole vocabulary from its logits, four columns a thread, and db.  32-bit G takes the logits' place.
+// Few rows: G of the whole vocabulary from its logits, a column a thread, and db.  32-bit G takes the logits' place.
 template <bool EXACT, typename T>
 __global__ __launch_bounds__(256) void gradient_columns_kernel(const float* z, const int32_t* labels, const float2* norm, int rows, int classes, int ld,
                                                                T* g, const float* factor, float* db, long long db_rep)
 {
-    const int c = (blockIdx.x * 256 + threadIdx.x) * 4, k = blockIdx.y;
+    const int c = blockIdx.x * 256 + threadIdx.x, k = blockIdx.y;
     if (c >= ld) return;
     const long long first = (long long)k * rows;
-    float sum[4] = {};
-#pragma unroll 4
+    float sum = 0.f;
+#pragma unroll 8
     for (int t = 0; t < rows; ++t) {
         const int y = labels[first + t];
         const bool live = (unsigned)y < (unsigned)classes;
         const float2 l = norm[first + t];
-        const float inv = 1.f / l.y;
-        const f4 v = *(const f4*)(z + (first + t) * ld + c);
-        float p[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            p[e] = live && c + e < classes ? exp_down<EXACT>(v[e] - l.x) * inv - (c + e == y ? 1.f : 0.f) : 0.f;
-            sum[e] += p[e];
-        }
-        T* out = g + (first + t) * ld + c;
-        if (sizeof(T) == 4) *(f4*)out = f4{p[0], p[1], p[2], p[3]};
-        else *(u2*)out = u2{to_bf16x2(p[0], p[1]), to_bf16x2(p[2], p[3])};
+        const float v = z[(first + t) * ld + c];
+        const float p = live && c < classes ? exp_down<EXACT>(v - l.x) * (1.f / l.y) - (c == y ? 1.f : 0.f) : 0.f;
+        sum += p;
+        g[(first + t) * ld + c] = (T)p;
     }
-    if (!db) return;
-    const float f = factor[k];
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (c + e < classes) db[k * db_rep + c + e] = sum[e] * f;
+    if (db && c < classes) db[k * db_rep + c] = sum * factor[k];
 }
 
 // G of a piece, unscaled, and its column sums over a wave's rows
@@ -280,7 +268,7 @@ template <bool EXACT> struct Softmax {
 };
 // into [replicas][rows][ld] of the operands' type, for the general product
 template <bool EXACT, typename T> struct Gradient {
-    static constexpr bool kLaneM = true, kStaged = false;
+    static constexpr bool kLaneM = true, kStaged = false, kSums = false;
     Softmax<EXACT> soft;
     T* g;
     template <int TM, int TN> __device__ __forceinline__ void operator()(const Tile<TM, TN>& t) const
@@ -309,7 +297,7 @@ template <bool EXACT, typename T> struct Gradient {
 };
 // into bf16 planes [PL][replicas][rows][ld] for the direct product
 template <int PL> struct GradientRows {
-    static constexpr bool kLaneM = true, kStaged = true;
+    static constexpr bool kLaneM = true, kStaged = true, kSums = false;
     Softmax<PL == 3> soft;
     __bf16* g;
     long long plane;
@@ -361,20 +349,34 @@ __global__ __launch_bounds__(256) void bias_grad_kernel(const float* sums, int b
     db[k * rep + c0 + c] = v * factor[k];
 }
 
-// dx: the shares of the contraction in ascending order, eight columns a thread; zero for a row without a label
-template <typename T>
+// dx: the shares of the contraction, eight columns a thread; zero for a row without a label.  G threads take the shares of a chunk,
+// each its own in ascending order, and are added in ascending order: with few rows there are many shares and few chunks.
+template <typename T, int G>
 __global__ __launch_bounds__(256) void input_grad_kernel(const float* share, int splits, long long step, int rows, int cols, int ld, long long total,
                                                          Labelled live, const float* factor, T* dx, long long rep, long long row)
 {
-    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+    constexpr int PER = 256 / G;
+    __shared__ __attribute__((aligned(16))) float part[G][G > 1 ? PER * 8 : 8];
+    const int mine = threadIdx.x % PER, group = threadIdx.x / PER;
+    const long long at = (long long)blockIdx.x * PER + mine;
+    f4 a = {}, b = {};
+    if (at < total) {
+        const float* src = share + at * 8;
+#pragma unroll 8
+        for (int s = group; s < splits; s += G) { a += *(const f4*)(src + s * step); b += *(const f4*)(src + s * step + 4); }
+    }
+    if (G > 1) {
+        *(f4*)&part[group][mine * 8] = a;
+        *(f4*)&part[group][mine * 8 + 4] = b;
+        __syncthreads();
+        if (group) return;
+#pragma unroll
+        for (int g = 1; g < G; ++g) { a += *(const f4*)&part[g][mine * 8]; b += *(const f4*)&part[g][mine * 8 + 4]; }
+    }
     if (at >= total) return;
     const int chunks = ld / 8;
     const long long line = at / chunks;
     const int c = (int)(at - line * chunks) * 8, k = (int)(line / rows), t = (int)(line - (long long)k * rows);
-    f4 a = {}, b = {};
-    const float* src = share + at * 8;
-#pragma unroll 8
-    for (int s = 0; s < splits; ++s) { a += *(const f4*)(src + s * step); b += *(const f4*)(src + s * step + 4); }
     live.labels += (long long)k * rows;
     const float f = factor[k];
     const bool on = live.at(t);
@@ -485,8 +487,10 @@ template <typename T> hipError_t input_grad(const LossArgs& a, const Plan& p, co
 {
     if (!a.dx.p || !a.rows) return hipSuccess;
     const long long lines = (long long)a.n * a.rows, total = lines * (p.ldx / 8);
-    input_grad_kernel<T><<<(unsigned)((total + 255) / 256), 256, 0, s>>>(w.share, p.splits, lines * p.ldx, a.rows, a.features, p.ldx, total,
-                                                                          Labelled{a.labels, a.classes}, w.factor, (T*)a.dx.p, a.dx.rep, a.dx.row);
+    auto* kernel = p.splits > 8 ? input_grad_kernel<T, 8> : input_grad_kernel<T, 1>;
+    const int per = p.splits > 8 ? 32 : 256;
+    kernel<<<(unsigned)((total + per - 1) / per), 256, 0, s>>>(w.share, p.splits, lines * p.ldx, a.rows, a.features, p.ldx, total,
+                                                                Labelled{a.labels, a.classes}, w.factor, (T*)a.dx.p, a.dx.rep, a.dx.row);
     return hipGetLastError();
 }
 
@@ -511,7 +515,7 @@ template <typename T, int BM, int WM, int WN> hipError_t run_general(const LossA
         const Source<T> w = source<T>(Rows{(T*)a.w.p + c0, a.w.rep, a.w.row}, a.features, cols);
         const Source<T> g = source<T>(Rows{k.g, (long long)a.rows * ld, ld}, a.rows, ld);            // zero beyond cols
         if (once) {
-            gradient_columns_kernel<exact, T><<<dim3((unsigned)((ld / 4 + 255) / 256), (unsigned)a.n), 256, 0, s>>>(
+            gradient_columns_kernel<exact, T><<<dim3((unsigned)((ld + 255) / 256), (unsigned)a.n), 256, 0, s>>>(
                 k.z, a.labels, k.norm, a.rows, a.classes, ld, (T*)k.g, k.factor, (float*)a.db.p, a.db.rep);
             e = hipGetLastError();
         } else if (a.rows) {
@@ -526,7 +530,7 @@ template <typename T, int BM, int WM, int WN> hipError_t run_general(const LossA
             if (e != hipSuccess) return e;
         }
         if (a.dw.p) {
-            const StoreTile<T> store{(T*)a.dw.p + c0, a.dw.rep, a.dw.row, k.factor, a.features, cols};
+            const StoreTile<T> store{(T*)a.dw.p + c0, a.dw.rep, a.dw.row, k.factor, a.features, cols, nullptr, 0};
             e = launch_product<128, 128, 2, 2, false, false>(source<T>(a.x, a.rows, a.features, live), g, a.n, a.features, cols, a.rows, 1,
                                                              std::max(1, a.rows), store, s);
             if (e != hipSuccess) return e;
@@ -581,7 +585,7 @@ template <typename T, int BM> hipError_t run_direct(const LossArgs& a, const Pla
                 const StoreRows store{(__bf16*)out.p, out.rep, out.row, k.factor, a.features, cols};
                 e = launch_direct<PL, PL, 256, 256, 2, 4, false, false>(x, g, a.n, a.features, cols, a.rows, 1, a.rows, store, s);
             } else {
-                const StoreTile<float> store{(float*)a.dw.p + c0, a.dw.rep, a.dw.row, k.factor, a.features, cols};
+                const StoreTile<float> store{(float*)a.dw.p + c0, a.dw.rep, a.dw.row, k.factor, a.features, cols, nullptr, 0};
                 e = launch_direct<PL, PL, 256, 256, 2, 4, false, false>(x, g, a.n, a.features, cols, a.rows, 1, a.rows, store, s);
             }
             if (e != hipSuccess) return e;

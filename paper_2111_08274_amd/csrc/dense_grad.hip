@@ -1,71 +1,64 @@
-// Parameter gradients of a dense layer whose input was kept in 8 bits: dW = x^T dy with x read straight from the checkpoint,
-// db = sum_t dy.  q * 2^e is exact in bf16, so a bf16 dy needs one product and a 32-bit dy, in three bf16 planes, three.
-#include "tile_product.h"
+// Parameter gradients of a dense layer whose input was kept in 8 bits: dW = x^T dy with x from the checkpoint, db = sum_t dy.
+// q * 2^e is exact in bf16, so a bf16 dy needs one product and a 32-bit dy, in three bf16 planes, three.  db comes from the same
+// operands as one more product, of ones (tile_product.h).
+//   short contractions or few outputs   chunks of the checkpoint become bf16 in registers, on their way to LDS
+//   otherwise                           the checkpoint is laid out as bf16 first (3 bytes a value once, where every column of tiles would
+//                                       convert it again) and both operands go straight from memory to LDS
+#include "direct_product.h"
 
 namespace hadfl {
 namespace head {
 
 namespace {
 
-// column sums of a share of the rows, a thread per column
-template <typename T>
-__global__ __launch_bounds__(256) void column_sums_kernel(const T* x, long long rep, long long row, int rows, int cols, int per, float* part)
+struct Plan {
+    bool direct, big;              // big: 256 x 256 tiles, else 128 x 128
+    int ldx, ldy, planes;
+    size_t x, y, total;
+};
+
+Plan plan_of(int n, int rows, int in, int out, int bf16)
 {
-    const int c = blockIdx.x * 256 + threadIdx.x, k = blockIdx.z;
-    if (c >= cols) return;
-    const int t0 = blockIdx.y * per, t1 = min(rows, t0 + per);
-    const T* src = x + k * rep + c;
-    float v = 0.f;
-#pragma unroll 8
-    for (int t = t0; t < t1; ++t) v += up(src[t * row]);
-    part[((long long)k * gridDim.y + blockIdx.y) * cols + c] = v;
-}
-// and the shares in ascending order
-__global__ __launch_bounds__(256) void add_shares_kernel(const float* part, int shares, int cols, float* out, long long rep)
-{
-    const int c = blockIdx.x * 256 + threadIdx.x, k = blockIdx.y;
-    if (c >= cols) return;
-    float v = 0.f;
-#pragma unroll 8
-    for (int s = 0; s < shares; ++s) v += part[((long long)k * shares + s) * cols + c];
-    out[k * rep + c] = v;
+    Plan p{};
+    p.direct = rows >= 256 && in >= 128 && out >= 128;
+    p.big = (long long)n * ((in + 255) / 256) * ((out + 255) / 256) >= 192;
+    p.ldx = (in + 7) / 8 * 8;
+    p.ldy = (out + 7) / 8 * 8;
+    p.planes = bf16 ? 1 : 3;
+    if (p.direct) {
+        p.x = 0;
+        p.y = align256((size_t)n * rows * p.ldx * 2);
+        p.total = p.y + align256((size_t)n * rows * p.ldy * 2 * p.planes);
+    }
+    return p;
 }
 
-int shares_of(int n, int rows, int cols)
+template <typename T> hipError_t run(const DenseArgs& a, hipStream_t s)
 {
-    const int most = std::max(1, 2048 / (n * ((cols + 255) / 256)));
-    return std::max(1, std::min(most, (rows + 31) / 32));
+    constexpr int PL = sizeof(T) == 4 ? 3 : 1;
+    const Plan p = plan_of(a.n, a.rows, a.in, a.out, a.bf16);
+    const StoreTile<float, true, PL> store{(float*)a.dw.p, a.dw.rep, a.dw.row, nullptr, a.in, a.out, (float*)a.db.p, a.db.rep};
+    if (!p.direct)
+        return launch_product<128, 128, 2, 2, false, false>(SourcePacked{a.x, a.rows, a.in}, source<T>(a.dy, a.rows, a.out), a.n, a.in, a.out, a.rows, 1,
+                                                            std::max(1, a.rows), store, s);
+    __bf16 *wx = (__bf16*)((char*)a.work + p.x), *wy = (__bf16*)((char*)a.work + p.y);
+    hipError_t e = launch_unpack(a.n, a.rows, a.in, 1, a.x.q, Rows{wx, (long long)a.rows * p.ldx, p.ldx}, s);
+    if (e != hipSuccess) return e;
+    const Plane3 x{wx, (long long)a.rows * p.ldx, 0, p.ldx, a.rows, p.ldx};
+    Plane3 dy{(const __bf16*)a.dy.p, a.dy.rep, 0, (int)a.dy.row, a.rows, a.out};
+    if (PL == 3 || !chunked(a.dy, 1, a.out) || !direct_pitch(a.dy.row)) {
+        if ((e = lay_out<T>(a.n, a.rows, a.out, p.ldy, a.dy, Labelled{nullptr, 0}, wy, s)) != hipSuccess) return e;
+        dy = Plane3{wy, (long long)a.rows * p.ldy, (long long)a.n * a.rows * p.ldy, p.ldy, a.rows, p.ldy};
+    }
+    if (p.big) return launch_direct<1, PL, 256, 256, 2, 4, false, false>(x, dy, a.n, a.in, a.out, a.rows, 1, a.rows, store, s);
+    return launch_direct<1, PL, 128, 128, 2, 2, false, false>(x, dy, a.n, a.in, a.out, a.rows, 1, a.rows, store, s);
 }
 
 }  // namespace
 
-size_t dense_work_bytes(int n, int rows, int, int out, int)
-{
-    return align256((size_t)n * shares_of(n, rows, out) * out * sizeof(float));
-}
+size_t dense_work_bytes(int n, int rows, int in, int out, int bf16) { return plan_of(n, rows, in, out, bf16).total; }
 
-template <typename T> static hipError_t run(const DenseArgs& a, hipStream_t s)
-{
-    hipError_t e;
-    if (a.db.p) {
-        const int shares = shares_of(a.n, a.rows, a.out), per = (a.rows + shares - 1) / shares;
-        float* part = (float*)a.work;
-        column_sums_kernel<T><<<dim3((unsigned)((a.out + 255) / 256), (unsigned)shares, (unsigned)a.n), 256, 0, s>>>(
-            (const T*)a.dy.p, a.dy.rep, a.dy.row, a.rows, a.out, per, part);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-        add_shares_kernel<<<dim3((unsigned)((a.out + 255) / 256), (unsigned)a.n), 256, 0, s>>>(part, shares, a.out, (float*)a.db.p, a.db.rep);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
-    const SourcePacked x{a.x, a.rows, a.in};
-    const Source<T> dy = source<T>(a.dy, a.rows, a.out);
-    const StoreTile<float> store{(float*)a.dw.p, a.dw.rep, a.dw.row, nullptr, a.in, a.out};
-    return launch_product<128, 128, 2, 2, false, false>(x, dy, a.n, a.in, a.out, a.rows, 1, std::max(1, a.rows), store, s);
-}
-
-hipError_t launch_dense_grad(const DenseArgs& a, hipStream_t s)
-{
-    return a.bf16 ? run<__bf16>(a, s) : run<float>(a, s);
-}
+hipError_t launch_dense_grad(const DenseArgs& a, hipStream_t s) { return a.bf16 ? run<__bf16>(a, s) : run<float>(a, s); }
 
 }  // namespace head
 }  // namespace hadfl

@@ -117,6 +117,11 @@ __global__ __launch_bounds__(WM * WN * 64) void direct_kernel(Plane3 a, Plane3 b
     for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int j = 0; j < TN; ++j) t.acc[i][j] = f16{};
+    if (Epi::kSums) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) t.sum[j] = f16{};
+    }
+    const bool sums = has_sum(epi, t.m0);
     LA la;
     LB lb;
     la.init(tid, a.ld);
@@ -137,6 +142,10 @@ __global__ __launch_bounds__(WM * WN * 64) void direct_kernel(Plane3 a, Plane3 b
             for (int i = 0; i < TM; ++i) fa[i] = LA::read(image, wm + 32 * i, ks, t.lane);
 #pragma unroll
             for (int j = 0; j < TN; ++j) fb[j] = LB::read(image + LA::kBytes, wn + 32 * j, ks, t.lane);
+            if (Epi::kSums && sums) {
+#pragma unroll
+                for (int j = 0; j < TN; ++j) t.sum[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ones(), fb[j], t.sum[j], 0, 0, 0);
+            }
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -234,7 +243,7 @@ template <int TN> struct RowStage {
 };
 // C times a factor per replica to a bf16 tensor
 struct StoreRows {
-    static constexpr bool kLaneM = true, kStaged = true;
+    static constexpr bool kLaneM = true, kStaged = true, kSums = false;
     __bf16* p;
     long long rep, row;
     const float* factor;

@@ -96,12 +96,26 @@ template <bool ALONG, int BR, int KS> struct Image {
 
 // A wave's part of the tile, as an epilogue gets it.  LANE_M: a lane holds one m (m0 + 32 * tm + lane % 32) and the n
 // n0 + 32 * tn + 8 * (i / 4) + 4 * (lane / 32) + i % 4 of acc[tm][tn][i]; else n and m change places.
+// sum: the columns' sums of B (every row of them the same), in the waves that has_sum() names of an epilogue that asks for them.
 template <int TM, int TN> struct Tile {
     f16 acc[TM][TN];
+    f16 sum[TN];
     int rep, split, m0, n0, lane, wave, bm, bn;                 // bm, bn: where the workgroup's tile begins
 };
 
-template <class SA, bool A_ALONG, class SB, bool B_ALONG, int BM, int BN, int WM, int WN, int KS, int NBUF, bool LANE_M, class Epi>
+// sum_k B(n, k) is one more product, of ones: the first waves of the first row of tiles form it from the operands they hold
+template <class Epi> __device__ __forceinline__ bool has_sum(const Epi& epi, int m0)
+{
+    if constexpr (Epi::kSums) return m0 == 0 && epi.sums;
+    return false;
+}
+__device__ __forceinline__ bf16x8 ones()
+{
+    constexpr unsigned one2 = 0x3f803f80u;
+    return __builtin_bit_cast(bf16x8, (u4{one2, one2, one2, one2}));
+}
+
+template <class SA, bool A_ALONG, class SB, bool B_ALONG, int BM, int BN, int WM, int WN, int KS, int NBUF, class Epi>
 __global__ __launch_bounds__(WM * WN * 64) void product_kernel(SA a, SB b, int K, int tiles_m, int tiles_n, int splits, int split_len,
                                                                int total, Epi epi)
 {
@@ -131,6 +145,11 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(SA a, SB b, int K
     for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int j = 0; j < TN; ++j) t.acc[i][j] = f16{};
+    if (Epi::kSums) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) t.sum[j] = f16{};
+    }
+    const bool sums = has_sum(epi, t.m0);
 
     typename SA::Raw ra[NA];
     typename SB::Raw rb[NB];
@@ -180,6 +199,12 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(SA a, SB b, int K
             for (int j = 0; j < TN; ++j)
 #pragma unroll
                 for (int s = 0; s < PB; ++s) fb[j][s] = IB::read(buf + PA * IA::kPlane + s * IB::kPlane, wn + 32 * j, ks, t.lane);
+            if (Epi::kSums && sums) {
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int s = PB - 1; s >= 0; --s) t.sum[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ones(), fb[j][s], t.sum[j], 0, 0, 0);
+            }
             // planes i and j with i + j <= 2: what is left out is below 2^-24 of the product
 #pragma unroll
             for (int sum = 2; sum >= 0; --sum)                  // the small products first
@@ -190,7 +215,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(SA a, SB b, int K
                     for (int i = 0; i < TM; ++i)
 #pragma unroll
                         for (int j = 0; j < TN; ++j)
-                            t.acc[i][j] = LANE_M ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j][sum - s], fa[i][s], t.acc[i][j], 0, 0, 0)
+                            t.acc[i][j] = Epi::kLaneM ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j][sum - s], fa[i][s], t.acc[i][j], 0, 0, 0)
                                                  : __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i][s], fb[j][sum - s], t.acc[i][j], 0, 0, 0);
                 }
         }
@@ -219,13 +244,15 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(SA a, SB b, int K
 }
 
 // ---- epilogues that only store ---------------------------------------------------------------------------------
-// C to a tensor, times a factor per replica (lanes along n)
-template <typename T> struct StoreTile {
-    static constexpr bool kLaneM = false, kStaged = false;
+// C to a tensor, times a factor per replica (lanes along n); SUMS: and the columns' sums of a B in PB planes
+template <typename T, bool SUMS = false, int PB = 1> struct StoreTile {
+    static constexpr bool kLaneM = false, kStaged = false, kSums = SUMS;
     T* p;
     long long rep, row;
     const float* factor;           // [replicas] or null
     int M, N;
+    float* sums;
+    long long sums_rep;
     template <int TM, int TN> __device__ __forceinline__ void operator()(const Tile<TM, TN>& t) const
     {
         const float f = factor ? factor[t.rep] : 1.f;
@@ -242,11 +269,18 @@ template <typename T> struct StoreTile {
                     if (m < M) out[m * row + n] = (T)(t.acc[i][j][e] * f);
                 }
             }
+        if (SUMS && has_sum(*this, t.m0)) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const int n = t.n0 + 32 * j + t.lane;
+                if (t.lane < 32 && n < N) sums[t.rep * sums_rep + n] = t.sum[j][0] * (PB == 3 ? 0x1p-24f : 1.f);
+            }
+        }
     }
 };
 // C into [split][replica][M][ld] floats, over or onto what is there
 struct StoreShare {
-    static constexpr bool kLaneM = false, kStaged = false;
+    static constexpr bool kLaneM = false, kStaged = false, kSums = false;
     float* p;
     int M, N, ld, replicas;
     bool onto;
@@ -280,7 +314,7 @@ hipError_t launch_product(const SA& a, const SB& b, int replicas, int M, int N, 
     const long long total = (long long)replicas * splits * tm * tn;
     if (total == 0) return hipSuccess;
     if (total > 0x7fffff00ll) return hipErrorInvalidValue;
-    product_kernel<SA, A_ALONG, SB, B_ALONG, BM, BN, WM, WN, KS, NBUF, Epi::kLaneM, Epi>
+    product_kernel<SA, A_ALONG, SB, B_ALONG, BM, BN, WM, WN, KS, NBUF, Epi>
         <<<die_grid(total), WM * WN * 64, 0, s>>>(a, b, K, tm, tn, splits, split_len, (int)total, epi);
     return hipGetLastError();
 }

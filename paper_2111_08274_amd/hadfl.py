@@ -123,19 +123,17 @@ def lib():
         L.hadfl_get_losses.argtypes = [vp, vp]
         L.hadfl_profile_enable.argtypes = [vp, i32]
         L.hadfl_profile_read.argtypes = [vp, ctypes.POINTER(HadflKernelTime), i32, ctypes.POINTER(i32)]
-        sizep, rowsp = ctypes.POINTER(ctypes.c_size_t), ctypes.POINTER(HadflRows)
-        normp, packp, densep, lossp = (ctypes.POINTER(t) for t in (HadflNorm, HadflPack, HadflDense, HadflLoss))
-        L.hadfl_norm_workspace.argtypes = [normp, sizep]
-        L.hadfl_norm_forward.argtypes = [normp, rowsp, rowsp, rowsp, rowsp, vp, vp, vp]
-        L.hadfl_norm_backward.argtypes = [normp, rowsp, rowsp, vp, rowsp, vp, vp, rowsp, rowsp, rowsp, vp, vp]
-        L.hadfl_packed_bytes.argtypes = [packp, sizep]
-        L.hadfl_pack_rows.argtypes = [packp, rowsp, vp, vp]
-        L.hadfl_unpack_rows.argtypes = [packp, vp, rowsp, vp]
-        L.hadfl_dense_workspace.argtypes = [densep, sizep]
-        L.hadfl_dense_grad_packed.argtypes = [densep, vp, rowsp, rowsp, rowsp, vp, vp]
-        L.hadfl_loss_workspace.argtypes = [lossp, i32, sizep]
-        L.hadfl_loss_forward.argtypes = [lossp, rowsp, rowsp, rowsp, vp, vp, vp, vp, vp]
-        L.hadfl_loss_grad.argtypes = [lossp, rowsp, rowsp, rowsp, vp, vp, vp, rowsp, rowsp, rowsp, vp, vp]
+        # descriptors and tensors of the head's operators go by address (_Operator keeps the structs): converting typed
+        # pointers costs about as much as a launch
+        sizep = ctypes.POINTER(ctypes.c_size_t)
+        L.hadfl_norm_workspace.argtypes = L.hadfl_packed_bytes.argtypes = L.hadfl_dense_workspace.argtypes = [vp, sizep]
+        L.hadfl_loss_workspace.argtypes = [vp, i32, sizep]
+        L.hadfl_norm_forward.argtypes = [vp] * 8
+        L.hadfl_norm_backward.argtypes = [vp] * 12
+        L.hadfl_pack_rows.argtypes = L.hadfl_unpack_rows.argtypes = [vp] * 4
+        L.hadfl_dense_grad_packed.argtypes = [vp] * 7
+        L.hadfl_loss_forward.argtypes = [vp] * 9
+        L.hadfl_loss_grad.argtypes = [vp] * 12
         L.hadfl_last_error.argtypes = [vp]
         L.hadfl_last_error.restype = ctypes.c_char_p
         L.hadfl_destroy.argtypes = [vp]
@@ -403,8 +401,10 @@ class _Operator:
         self.torch, self.desc = torch, desc
         self.device = torch.device("cuda", torch.cuda.current_device())
         self.dtype = torch.bfloat16 if bf16 else torch.float32
-        self._ref = ctypes.byref(desc)
-        self._names = {}
+        self._ref = ctypes.addressof(desc)
+        self._structs = {}
+        # the handle itself where torch offers it; the object around it takes longer to make than a kernel to launch
+        self._current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
         self.work = None
         if workspace is not None:
             self.work = self._bytes(workspace)
@@ -415,25 +415,27 @@ class _Operator:
         return self.torch.empty(n.value, dtype=self.torch.uint8, device=self.device)
 
     def _rows(self, name, t, shape, dtype):
-        """The hadfl_rows of a tensor, checked; None stays None."""
+        """The address of the hadfl_rows of a tensor, checked; None stays None."""
         if t is None:
             return None
-        if t.dtype != dtype or t.device != self.device or tuple(t.shape) != shape:
+        if t.dtype != dtype or t.device != self.device or t.shape != shape:
             raise HadflError(EINVAL, "%s must be %s %s on %s, not %s %s on %s" % (name, dtype, shape, self.device, t.dtype, tuple(t.shape), t.device))
         st = t.stride()
-        if shape[-1] > 1 and st[-1] != 1:
+        if st[-1] != 1 and shape[-1] > 1:
             raise HadflError(EINVAL, "%s: the columns must be contiguous" % name)
-        r = self._names.get(name)
-        if r is None:
-            r = self._names[name] = HadflRows()
-        r.data, r.replica_stride, r.row_stride = t.data_ptr() or None, st[0], (st[1] if len(shape) == 3 else 0)
-        return r
+        got = self._structs.get(name)
+        if got is None:
+            r = HadflRows()
+            got = self._structs[name] = (r, ctypes.addressof(r))
+        r = got[0]
+        r.data, r.replica_stride, r.row_stride = t.data_ptr() or None, st[0], (st[1] if len(st) == 3 else 0)
+        return got[1]
 
     def _plain(self, name, t, shape, dtype):
         """The address of a contiguous tensor, checked."""
         if t is None:
             return None
-        if t.dtype != dtype or t.device != self.device or tuple(t.shape) != shape or not t.is_contiguous():
+        if t.dtype != dtype or t.device != self.device or t.shape != shape or not t.is_contiguous():
             raise HadflError(EINVAL, "%s must be contiguous %s %s on %s" % (name, dtype, shape, self.device))
         return t.data_ptr() or None
 
@@ -441,7 +443,7 @@ class _Operator:
         return self.torch.empty(shape, dtype=dtype, device=self.device) if t is None else t
 
     def _stream(self, stream):
-        return (self.torch.cuda.current_stream(self.device) if stream is None else stream).cuda_stream
+        return self._current(self.device.index) if stream is None else stream.cuda_stream
 
 
 class LayerNorm(_Operator):
