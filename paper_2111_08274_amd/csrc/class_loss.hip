@@ -37,12 +37,19 @@ __device__ __forceinline__ void logits_of(const Tile<TM, TN>& t, int i, int n0, 
             for (int e = 0; e < 16; ++e) z[j][e] = t.acc[i][j][e];
         return;
     }
+    float b[TN][16] = {};
+    if (bias) {                    // beyond the classes: the last one's, unused
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) b[j][e] = bias[min(n0 + 32 * j + 8 * (e / 4) + 4 * (t.lane >> 5) + e % 4, classes - 1)];
+    }
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const int c = n0 + 32 * j + 8 * (e / 4) + 4 * (t.lane >> 5) + e % 4;
-            z[j][e] = c < classes ? t.acc[i][j][e] + (bias ? bias[c] : 0.f) : -INFINITY;
+            z[j][e] = c < classes ? t.acc[i][j][e] + b[j][e] : -INFINITY;
         }
 }
 // f(j, e) for the column of class y, in the lane that holds it; few waves hold any of their rows' labels

@@ -1,8 +1,8 @@
 // Tiled matrix product on the matrix cores for operands that lie as the matrix cores take them: bf16 (a 32-bit operand as
 // three bf16 planes), rows on 16 bytes, whole chunks of eight values.  C[m][n] = sum_k A(m, k) B(n, k).
 //
-// Slabs of 64 k go from memory to LDS without passing registers (buffer loads that write LDS), one slab ahead of the one
-// being multiplied, one barrier a slab.  The LDS image is the slab itself with its 16-byte chunks exchanged within a row, so
+// Slabs of 64 k go from memory to LDS without passing registers (buffer loads that write LDS), as many slabs ahead of the one
+// being multiplied as LDS holds (256 x 256 tiles: one, 128 x 256: two, 128 x 128: three), one barrier a slab.  The LDS image is the slab itself with its 16-byte chunks exchanged within a row, so
 // that the operand reads meet every bank once (a load that writes LDS puts the chunks of a wave one after the other: the exchange is in
 // the addresses it reads from):
 //   along   the contraction runs along the source's rows: [rows][64 k], chunk c of row r at c ^ (r & 7)
@@ -25,6 +25,20 @@ struct Plane3 {                    // an operand: source rows `lines` of `cols` 
 inline bool direct_pitch(long long ld) { return ld <= (1ll << 22); }
 
 typedef __attribute__((address_space(3))) void LdsVoid;
+// 16 bytes a lane from b + off to LDS, the wave's lanes one after the other from `at` (the same in all lanes); an offset outside the
+// buffer gives zeros.  It has no result in a register; slab_barrier() waits for it.  Written out because the compiler, which cannot
+// tell the images apart behind the transposing reads, would wait for every load before the next of those.
+__device__ __forceinline__ void load_to_lds(Buffer b, unsigned off, unsigned at)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(at), "v"(off), "s"(b) : "memory", "m0");
+}
+
+// an address that is the same in all lanes, in scalar registers
+__device__ __forceinline__ const __bf16* same(const __bf16* p)
+{
+    const unsigned long long v = (unsigned long long)p;
+    return (const __bf16*)((unsigned long long)__builtin_amdgcn_readfirstlane((unsigned)(v >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((unsigned)v));
+}
 
 template <bool ALONG, int BR, int NT> struct Loader {
     static constexpr int kBytes = BR * kSlab * 2, kAcross = ALONG ? 8 : BR / 8, kLoads = kBytes / 16 / NT;
@@ -45,12 +59,13 @@ template <bool ALONG, int BR, int NT> struct Loader {
         static_assert(kStep % 8 == 0 && kLoads >= 1, "");
         const long long first = ALONG ? (long long)r0 * s.ld : (long long)k0 * s.ld + r0;
         const long long rest = ALONG ? (long long)(s.lines - r0 - 1) * s.ld + s.cols : (long long)(s.lines - k0 - 1) * s.ld + s.cols - r0;
-        const Buffer b = buffer(base + first, (unsigned)min(rest * 2, 0xffffffe0ll));
+        const Buffer b = buffer(same(base + first), __builtin_amdgcn_readfirstlane((unsigned)min(rest * 2, 0xffffffe0ll)));
         const bool in = !ALONG || k0 + kc < s.cols;
+        const unsigned first_byte = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(LdsVoid*)image + wave * 1024);
         unsigned at = off + (ALONG ? (unsigned)k0 * 2 : 0u);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (LdsVoid*)(image + (i * NT + wave * 64) * 16), 16, (int)(in ? at : kOutside), 0, 0, 0);
+            load_to_lds(b, in ? at : kOutside, first_byte + i * NT * 16);
             at += step;
         }
     }
@@ -76,6 +91,16 @@ template <> struct Pairs<3, 3> {
     static __device__ int b(int s) { return s == 0 ? 2 : s == 1 || s == 3 ? 1 : 0; }
 };
 
+// waits for all but the last N loads of this wave and for its LDS reads, then for the other waves
+template <int N> __device__ __forceinline__ void slab_barrier()
+{
+    static_assert(N < 64, "the counter has six bits");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x70);          // vector loads: N, LDS: 0, exports: any
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // a tile's place: groups of eight tiles down m, so that the 32 compute units of a die work on about 8 x 4 tiles that share operands
 __device__ __forceinline__ void place_tile(int at, int tiles_m, int tiles_n, int& m, int& n)
 {
@@ -93,9 +118,8 @@ __global__ __launch_bounds__(WM * WN * 64) void direct_kernel(Plane3 a, Plane3 b
     typedef Loader<A_ALONG, BM, NT> LA;
     typedef Loader<B_ALONG, BN, NT> LB;
     typedef Pairs<PA, PB> P;
-    // two objects: the compiler then sees that a load into one does not touch the other
-    __shared__ __attribute__((aligned(16))) char image0[LA::kBytes + LB::kBytes];
-    __shared__ __attribute__((aligned(16))) char image1[LA::kBytes + LB::kBytes];
+    constexpr int kImage = LA::kBytes + LB::kBytes, IMAGES = kImage > 49152 ? 2 : kImage > 32768 ? 3 : 4, kLoads = LA::kLoads + LB::kLoads;
+    __shared__ __attribute__((aligned(16))) char images[IMAGES * kImage];
 
     const unsigned item = logical_block();
     if (item >= (unsigned)total) return;
@@ -155,16 +179,21 @@ __global__ __launch_bounds__(WM * WN * 64) void direct_kernel(Plane3 a, Plane3 b
         }
     };
     const int slabs = k_begin < k_end ? P::kCount * ((k_end - k_begin + kSlab - 1) / kSlab) : 0;
-    if (slabs) issue(image0);
-    for (int s = 0; s < slabs; s += 2) {
-        __syncthreads();                                       // image 0 has arrived, image 1 has been read
-        if (s + 1 < slabs) issue(image1);
-        multiply(image0);
-        if (s + 1 < slabs) {
-            __syncthreads();
-            if (s + 2 < slabs) issue(image0);
-            multiply(image1);
-        }
+    // Slab i: its loads are done when at most those of the IMAGES - 2 slabs after it are outstanding (loads finish in order);
+    // the barrier says so for all waves, and that all have read the slab before, whose image the next loads take.
+    auto turn = [&](int i, char* image, char* free) {
+        if (i >= slabs) return;
+        if (IMAGES > 2 && i + IMAGES - 2 < slabs) slab_barrier<(IMAGES - 2) * kLoads>();
+        else slab_barrier<0>();
+        if (i + IMAGES - 1 < slabs) issue(free);
+        multiply(image);
+    };
+#pragma unroll
+    for (int i = 0; i < IMAGES - 1; ++i)
+        if (i < slabs) issue(images + i * kImage);
+    for (int i = 0; i < slabs; i += IMAGES) {
+#pragma unroll
+        for (int u = 0; u < IMAGES; ++u) turn(i + u, images + u * kImage, images + (u + IMAGES - 1) % IMAGES * kImage);
     }
     constexpr float kScale = (PA == 3 ? 0x1p-24f : 1.f) * (PB == 3 ? 0x1p-24f : 1.f);
     if (kScale != 1.f) {
@@ -175,7 +204,7 @@ __global__ __launch_bounds__(WM * WN * 64) void direct_kernel(Plane3 a, Plane3 b
     }
     if constexpr (Epi::kStaged) {
         __syncthreads();                                       // the images are free
-        epi(t, image0);
+        epi(t, images);
     } else epi(t);
 }
 

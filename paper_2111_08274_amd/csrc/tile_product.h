@@ -28,12 +28,15 @@ template <typename T> struct Source {
     int rows, cols;
     Labelled live;
     __device__ __forceinline__ void bind(int k) { p += k * rep; if (live.labels) live.labels += (long long)k * rows; }
-    __device__ __forceinline__ Raw load(int r, int c) const
+    // INSIDE: the caller knows that the chunk lies within the source
+    template <bool INSIDE> __device__ __forceinline__ Raw load(int r, int c) const
     {
         Raw v;
-        v.load(p + r * row + c, r < rows && live.at(r) ? cols - c : 0);
+        if (INSIDE) v.load(p + r * row + c, 8);
+        else v.load(p + r * row + c, r < rows && live.at(r) ? cols - c : 0);
         return v;
     }
+    __device__ __forceinline__ bool inside(int r_end, int c_end) const { return r_end <= rows && c_end <= cols && !live.labels; }
     static __device__ __forceinline__ void planes(const Chunk<__bf16>& v, u4 (&out)[1]) { out[0] = v.a; }
     static __device__ __forceinline__ void planes(const Chunk<float>& v, u4 (&out)[3])
     {
@@ -58,10 +61,11 @@ struct SourcePacked {              // rows and columns of one replica; the surpl
         p.q += (long long)k * rows * p.cols;
         p.e += (long long)k * rows * (p.cols / kGroup);
     }
-    __device__ __forceinline__ Raw load(int r, int c) const
+    __device__ __forceinline__ bool inside(int r_end, int c_end) const { return r_end <= rows && c_end <= p.cols; }
+    template <bool INSIDE> __device__ __forceinline__ Raw load(int r, int c) const
     {
         Raw v = {};
-        if (r >= rows || c >= p.cols) return v;
+        if (!INSIDE && (r >= rows || c >= p.cols)) return v;
         v.q = *(const u2*)(p.q + r * p.cols + c);
         v.e = p.e[r * (p.cols / kGroup) + c / kGroup];
         return v;
@@ -115,6 +119,8 @@ __device__ __forceinline__ bf16x8 ones()
     return __builtin_bit_cast(bf16x8, (u4{one2, one2, one2, one2}));
 }
 
+template <bool B> struct Yes { static constexpr bool value = B; };
+
 template <class SA, bool A_ALONG, class SB, bool B_ALONG, int BM, int BN, int WM, int WN, int KS, int NBUF, class Epi>
 __global__ __launch_bounds__(WM * WN * 64) void product_kernel(SA a, SB b, int K, int tiles_m, int tiles_n, int splits, int split_len,
                                                                int total, Epi epi)
@@ -154,16 +160,25 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(SA a, SB b, int K
     typename SA::Raw ra[NA];
     typename SB::Raw rb[NB];
     auto fetch = [&](int k0) {
+        auto all_a = [&](auto inside) {
 #pragma unroll
-        for (int i = 0; i < NA; ++i) {
-            const int id = tid + i * NT, r = id / IA::kAcross, c = id % IA::kAcross * 8;
-            if (IA::kChunks % NT == 0 || id < IA::kChunks) ra[i] = A_ALONG ? a.load(bm + r, k0 + c) : a.load(k0 + r, bm + c);
-        }
+            for (int i = 0; i < NA; ++i) {
+                const int id = tid + i * NT, r = id / IA::kAcross, c = id % IA::kAcross * 8;
+                if (IA::kChunks % NT == 0 || id < IA::kChunks)
+                    ra[i] = A_ALONG ? a.template load<decltype(inside)::value>(bm + r, k0 + c) : a.template load<decltype(inside)::value>(k0 + r, bm + c);
+            }
+        };
+        auto all_b = [&](auto inside) {
 #pragma unroll
-        for (int i = 0; i < NB; ++i) {
-            const int id = tid + i * NT, r = id / IB::kAcross, c = id % IB::kAcross * 8;
-            if (IB::kChunks % NT == 0 || id < IB::kChunks) rb[i] = B_ALONG ? b.load(bn + r, k0 + c) : b.load(k0 + r, bn + c);
-        }
+            for (int i = 0; i < NB; ++i) {
+                const int id = tid + i * NT, r = id / IB::kAcross, c = id % IB::kAcross * 8;
+                if (IB::kChunks % NT == 0 || id < IB::kChunks)
+                    rb[i] = B_ALONG ? b.template load<decltype(inside)::value>(bn + r, k0 + c) : b.template load<decltype(inside)::value>(k0 + r, bn + c);
+            }
+        };
+        // most slabs lie inside: loads without a comparison each, all on their way at once
+        if (B_ALONG ? b.inside(bn + BN, k0 + KS) : b.inside(k0 + KS, bn + BN)) all_b(Yes<true>{}); else all_b(Yes<false>{});
+        if (A_ALONG ? a.inside(bm + BM, k0 + KS) : a.inside(k0 + KS, bm + BM)) all_a(Yes<true>{}); else all_a(Yes<false>{});
     };
     auto store = [&](char* buf) {
 #pragma unroll
@@ -293,12 +308,15 @@ struct StoreShare {
             for (int j = 0; j < TN; ++j) {
                 const int n = t.n0 + 32 * j + (t.lane & 31);
                 if (n >= N) continue;
+                float have[16] = {};
+                if (onto) {                                    // all loads on their way before the first addition
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) have[e] = out[(long long)min(t.m0 + 32 * i + 8 * (e / 4) + 4 * (t.lane >> 5) + e % 4, M - 1) * ld + n];
+                }
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int m = t.m0 + 32 * i + 8 * (e / 4) + 4 * (t.lane >> 5) + e % 4;
-                    if (m >= M) continue;
-                    float* q = out + (long long)m * ld + n;
-                    *q = onto ? *q + t.acc[i][j][e] : t.acc[i][j][e];
+                    if (m < M) out[(long long)m * ld + n] = have[e] + t.acc[i][j][e];
                 }
             }
     }
