@@ -345,7 +345,7 @@ HADFL_API hadfl_status hadfl_unpack_rows(const hadfl_pack *pack, const void *pac
 /* The parameter gradients of a dense layer y = x W + b whose input was kept in 8 bits:
  *   dW = x^T dy  ([n_in][n_out], the layout of a dense layer here),  db = sum_t dy,
  * x the values that the checkpoint stands for.  Products of bf16 operands on the matrix cores, sums in 32 bits; a 32-bit dy
- * enters as three bf16 parts, which hold it whole.
+ * enters as three bf16 parts, which hold it whole for magnitudes from 2^-107 on.
  *   packed     dev, checkpoint of [n_replicas][n_rows][n_in]
  *   dy (t)     dev, [n_replicas][n_rows][n_out]
  *   dw         dev out, [n_replicas][n_in][n_out] floats
@@ -363,8 +363,10 @@ HADFL_API hadfl_status hadfl_dense_grad_packed(const hadfl_dense *dense, const v
  * (whatever its x holds), and its dx is zero.  A replica without labelled rows has loss zero and zero gradients.  A bias of
  * -inf takes a class out.  With G = (softmax(z) - onehot(label)) / (number of labelled rows):
  *   dx = G W^T,  dW = x^T G,  db = sum_t G.
- * fp32: operands enter the matrix products as three bf16 parts (six products), which keeps 32-bit accuracy for
- * magnitudes below 2^104.  bf16: softmax(z) - onehot is rounded to bf16 for the two products, db is formed before that.
+ * fp32: operands enter the matrix products in parts of 16 bits whose products are summed in 32 bits: up to 64 rows three
+ * bf16 parts (six products, whole for magnitudes from 2^-107 on), beyond two fp16 parts (three products) scaled by a power of two to
+ * the replica's largest finite magnitude: a product is off by at most 2^-20 of itself, 2^-23.5 in the mean square, for
+ * magnitudes down to 2^-29 of the largest.  bf16: softmax(z) - onehot is rounded to bf16 for the two products, db is formed before that.
  *   x (t)                 dev, [n_replicas][n_rows][n_features]
  *   w (t)                 dev, [n_replicas][n_features][n_classes], the layout of a dense layer here
  *   bias                  dev or NULL, [n_replicas][n_classes] floats

@@ -212,17 +212,28 @@ __global__ __launch_bounds__(256) void gradient_columns_kernel(const float* z, c
 {
     const int c = blockIdx.x * 256 + threadIdx.x, k = blockIdx.y;
     if (c >= ld) return;
+    constexpr int U = 8;                                       // rows at a time: their loads before the first store, which may be theirs
     const long long first = (long long)k * rows;
     float sum = 0.f;
-#pragma unroll 8
-    for (int t = 0; t < rows; ++t) {
-        const int y = labels[first + t];
-        const bool live = (unsigned)y < (unsigned)classes;
-        const float2 l = norm[first + t];
-        const float v = z[(first + t) * ld + c];
-        const float p = live && c < classes ? exp_down<EXACT>(v - l.x) * (1.f / l.y) - (c == y ? 1.f : 0.f) : 0.f;
-        sum += p;
-        g[(first + t) * ld + c] = (T)p;
+    for (int t0 = 0; t0 < rows; t0 += U) {
+        float v[U];
+        float2 l[U];
+        int y[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long long t = first + min(t0 + u, rows - 1);
+            v[u] = z[t * ld + c];
+            l[u] = norm[t];
+            y[u] = labels[t];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (t0 + u >= rows) break;
+            const bool live = (unsigned)y[u] < (unsigned)classes;
+            const float p = live && c < classes ? exp_down<EXACT>(v[u] - l[u].x) * (1.f / l[u].y) - (c == y[u] ? 1.f : 0.f) : 0.f;
+            sum += p;
+            g[(first + t0 + u) * ld + c] = (T)p;
+        }
     }
     if (db && c < classes) db[k * db_rep + c] = sum * factor[k];
 }
@@ -302,10 +313,10 @@ template <bool EXACT, typename T> struct Gradient {
         if (soft.sums) soft.store_sums(t, column);
     }
 };
-// into bf16 planes [PL][replicas][rows][ld] for the direct product
+// into planes [PL][replicas][rows][ld] for the direct product: bf16, or two fp16 parts (|G| <= 1)
 template <int PL> struct GradientRows {
     static constexpr bool kLaneM = true, kStaged = true, kSums = false;
-    Softmax<PL == 3> soft;
+    Softmax<PL == 2> soft;
     __bf16* g;
     long long plane;
     template <int TM, int TN> __device__ __forceinline__ void operator()(const Tile<TM, TN>& t, char* lds) const
@@ -327,7 +338,7 @@ template <int PL> struct GradientRows {
             for (int j = 0; j < TN; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    if (PL == 3) split3(f4{v[j][4 * q], v[j][4 * q + 1], v[j][4 * q + 2], v[j][4 * q + 3]}, part[0][j][q], part[PL / 2][j][q], part[PL - 1][j][q]);
+                    if (PL == 2) split2(f4{v[j][4 * q], v[j][4 * q + 1], v[j][4 * q + 2], v[j][4 * q + 3]}, up_scale(kOneBits), part[0][j][q], part[PL - 1][j][q]);
                     else part[0][j][q] = u2{to_bf16x2(v[j][4 * q], v[j][4 * q + 1]), to_bf16x2(v[j][4 * q + 2], v[j][4 * q + 3])};
                 }
 #pragma unroll
@@ -401,7 +412,7 @@ __global__ __launch_bounds__(256) void input_grad_kernel(const float* share, int
 struct Plan {
     bool direct, small;            // small: 32 or (direct) 128 rows a tile
     int bm, wave_m, parts, piece, pieces, blocks, splits, split_len, ldx, planes;
-    size_t norm, z_label, row_loss, factor, part, g, z, sums, share, x, w, total;
+    size_t norm, z_label, row_loss, factor, part, g, z, sums, share, x, w, top, total;
 };
 constexpr long long kPieceBytes = 256ll << 20;       // of G, and of a laid-out piece of W
 
@@ -415,10 +426,10 @@ Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
     p.bm = p.direct ? (p.small ? 128 : 256) : p.small ? 32 : 128;
     const int bn = p.direct ? 256 : 128;
     p.wave_m = p.direct ? p.bm / 2 : p.small ? 32 : 64;
-    p.planes = p.direct && !bf16 ? 3 : 1;
+    p.planes = p.direct && !bf16 ? 2 : 1;
     p.parts = up_to(classes, bn) / bn;
     p.blocks = up_to(rows, p.bm) / p.wave_m;
-    const long long lines = (long long)n * rows, es = p.direct ? (bf16 ? 2 : 6) : bf16 ? 6 : 4;      // of G and, few rows, the logits
+    const long long lines = (long long)n * rows, es = p.direct ? (bf16 ? 2 : 4) : bf16 ? 6 : 4;      // of G and, few rows, the logits
     long long most = grad ? kPieceBytes / std::max<long long>(1, lines * es) : classes;
     if (p.direct) most = std::min(most, kPieceBytes / ((long long)n * features * 2 * p.planes));
     most = std::max<long long>(1024, most / bn * bn);
@@ -441,6 +452,7 @@ Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
     if (p.direct) {
         p.x = take((size_t)lines * p.ldx * 2 * p.planes);
         p.w = take((size_t)n * features * p.piece * 2 * p.planes);
+        p.top = take((size_t)n * 8);
     }
     if (grad) {
         p.g = take((size_t)lines * p.piece * (p.direct ? es : bf16 ? 2 : 4));
@@ -458,13 +470,14 @@ struct Work {
     float2 *norm, *part;
     char* g;
     __bf16 *x, *w;
+    unsigned* top;                 // [2][replicas]: of x and of W
     Work(const LossArgs& a, const Plan& p)
     {
         char* at = (char*)a.work;
         norm = (float2*)(at + p.norm); z_label = (float*)(at + p.z_label); factor = (float*)(at + p.factor);
         row_loss = a.row_loss ? a.row_loss : (float*)(at + p.row_loss);
         sums = (float*)(at + p.sums); share = (float*)(at + p.share); part = (float2*)(at + p.part);
-        g = at + p.g; z = (float*)(at + p.z); x = (__bf16*)(at + p.x); w = (__bf16*)(at + p.w);
+        g = at + p.g; z = (float*)(at + p.z); x = (__bf16*)(at + p.x); w = (__bf16*)(at + p.w); top = (unsigned*)(at + p.top);
     }
 };
 
@@ -538,7 +551,7 @@ template <typename T, int BM, int WM, int WN> hipError_t run_general(const LossA
         }
         if (a.dw.p) {
             const StoreTile<T> store{(T*)a.dw.p + c0, a.dw.rep, a.dw.row, k.factor, a.features, cols, nullptr, 0};
-            e = launch_product<128, 128, 2, 2, false, false>(source<T>(a.x, a.rows, a.features, live), g, a.n, a.features, cols, a.rows, 1,
+            e = launch_product<64, 64, 2, 2, false, false>(source<T>(a.x, a.rows, a.features, live), g, a.n, a.features, cols, a.rows, 1,
                                                              std::max(1, a.rows), store, s);
             if (e != hipSuccess) return e;
         }
@@ -549,27 +562,36 @@ template <typename T, int BM, int WM, int WN> hipError_t run_general(const LossA
 // more rows: operands straight from memory to LDS
 template <typename T, int BM> hipError_t run_direct(const LossArgs& a, const Plan& p, hipStream_t s)
 {
-    constexpr int PL = sizeof(T) == 4 ? 3 : 1;
+    constexpr int PL = sizeof(T) == 4 ? 2 : 1;
     const Work k(a, p);
     const float* bias = (const float*)a.bias.p;
-    hipError_t e = lay_out<T>(a.n, a.rows, a.features, p.ldx, a.x, Labelled{a.labels, a.classes}, k.x, s);
+    const Labelled live{a.labels, a.classes};
+    hipError_t e = hipSuccess;
+    const unsigned *top_x = nullptr, *top_w = nullptr;
+    if (PL == 2) {
+        top_x = k.top; top_w = k.top + a.n;
+        for (int i = 0; i < 2 * a.n && e == hipSuccess; i += 1024) { clear_kernel<<<1, 1024, 0, s>>>(k.top + i, std::min(1024, 2 * a.n - i)); e = hipGetLastError(); }
+        if (e == hipSuccess) e = find_largest(a.n, a.rows, a.features, a.x, live, k.top, s);
+        if (e == hipSuccess) e = find_largest(a.n, a.features, a.classes, a.w, Labelled{nullptr, 0}, k.top + a.n, s);
+    }
+    if (e == hipSuccess) e = lay_out<T, PL>(a.n, a.rows, a.features, p.ldx, a.x, live, top_x, k.x, s);
     if (e != hipSuccess) return e;
-    const Plane3 x{k.x, (long long)a.rows * p.ldx, (long long)a.n * a.rows * p.ldx, p.ldx, a.rows, p.ldx};
+    const Plane3 x{k.x, (long long)a.rows * p.ldx, (long long)a.n * a.rows * p.ldx, p.ldx, a.rows, p.ldx, top_x};
     // W as it is, or laid out a piece at a time
     const bool as_is = PL == 1 && chunked(a.w, 1, a.classes) && direct_pitch(a.w.row);
     auto weights = [&](int c0, int cols, bool there, Plane3& w) -> hipError_t {
-        if (as_is) { w = Plane3{(const __bf16*)a.w.p + c0, a.w.rep, 0, (int)a.w.row, a.features, cols}; return hipSuccess; }
+        if (as_is) { w = Plane3{(const __bf16*)a.w.p + c0, a.w.rep, 0, (int)a.w.row, a.features, cols, nullptr}; return hipSuccess; }
         const int ld = up_to(cols, 8);
-        w = Plane3{k.w, (long long)a.features * ld, (long long)a.n * a.features * ld, ld, a.features, ld};
+        w = Plane3{k.w, (long long)a.features * ld, (long long)a.n * a.features * ld, ld, a.features, ld, top_w};
         if (there) return hipSuccess;
-        return lay_out<T>(a.n, a.features, cols, ld, Rows{(T*)a.w.p + c0, a.w.rep, a.w.row}, Labelled{nullptr, 0}, k.w, s);
+        return lay_out<T, PL>(a.n, a.features, cols, ld, Rows{(T*)a.w.p + c0, a.w.rep, a.w.row}, Labelled{nullptr, 0}, top_w, k.w, s);
     };
     Plane3 w;
     const int step = as_is ? a.classes : p.piece;
     for (int c0 = 0; c0 < a.classes; c0 += step) {
         const int cols = std::min(step, a.classes - c0);
         if ((e = weights(c0, cols, false, w)) != hipSuccess) return e;
-        const Statistics<PL == 3, BM, 256, 4> stats{bias, a.bias.rep, a.labels, k.part, k.z_label, nullptr, a.rows, c0, a.classes, p.parts, 0};
+        const Statistics<PL == 2, BM, 256, 4> stats{bias, a.bias.rep, a.labels, k.part, k.z_label, nullptr, a.rows, c0, a.classes, p.parts, 0};
         e = launch_direct<PL, PL, BM, 256, 2, 4, true, false>(x, w, a.n, a.rows, cols, a.features, 1, a.features, stats, s);
         if (e != hipSuccess) return e;
     }
@@ -577,8 +599,8 @@ template <typename T, int BM> hipError_t run_direct(const LossArgs& a, const Pla
     for (int i = 0; i < p.pieces; ++i) {
         const int c0 = i * p.piece, cols = std::min(p.piece, a.classes - c0), ld = up_to(cols, 256);
         if ((e = weights(c0, cols, p.pieces == 1, w)) != hipSuccess) return e;
-        const Plane3 g{(const __bf16*)k.g, (long long)a.rows * ld, (long long)a.n * a.rows * ld, ld, a.rows, ld};
-        const Softmax<PL == 3> soft{bias, a.bias.rep, a.labels, k.norm, a.db.p ? k.sums : nullptr, a.rows, c0, a.classes, ld, p.blocks};
+        const Plane3 g{(const __bf16*)k.g, (long long)a.rows * ld, (long long)a.n * a.rows * ld, ld, a.rows, ld, nullptr};
+        const Softmax<PL == 2> soft{bias, a.bias.rep, a.labels, k.norm, a.db.p ? k.sums : nullptr, a.rows, c0, a.classes, ld, p.blocks};
         e = launch_direct<PL, PL, BM, 256, 2, 4, true, false>(x, w, a.n, a.rows, cols, a.features, 1, a.features, GradientRows<PL>{soft, (__bf16*)k.g, g.plane}, s);
         if (e != hipSuccess) return e;
         if (a.dx.p) {

@@ -37,18 +37,18 @@ template <typename T> hipError_t run(const DenseArgs& a, hipStream_t s)
 {
     constexpr int PL = sizeof(T) == 4 ? 3 : 1;
     const Plan p = plan_of(a.n, a.rows, a.in, a.out, a.bf16);
-    const StoreTile<float, true, PL> store{(float*)a.dw.p, a.dw.rep, a.dw.row, nullptr, a.in, a.out, (float*)a.db.p, a.db.rep};
+    const StoreTile<float, true> store{(float*)a.dw.p, a.dw.rep, a.dw.row, nullptr, a.in, a.out, (float*)a.db.p, a.db.rep};
     if (!p.direct)
-        return launch_product<128, 128, 2, 2, false, false>(SourcePacked{a.x, a.rows, a.in}, source<T>(a.dy, a.rows, a.out), a.n, a.in, a.out, a.rows, 1,
-                                                            std::max(1, a.rows), store, s);
+        return launch_product<64, 64, 2, 2, false, false>(SourcePacked{a.x, a.rows, a.in}, source<T>(a.dy, a.rows, a.out), a.n, a.in, a.out, a.rows, 1,
+                                                          std::max(1, a.rows), store, s);
     __bf16 *wx = (__bf16*)((char*)a.work + p.x), *wy = (__bf16*)((char*)a.work + p.y);
     hipError_t e = launch_unpack(a.n, a.rows, a.in, 1, a.x.q, Rows{wx, (long long)a.rows * p.ldx, p.ldx}, s);
     if (e != hipSuccess) return e;
-    const Plane3 x{wx, (long long)a.rows * p.ldx, 0, p.ldx, a.rows, p.ldx};
-    Plane3 dy{(const __bf16*)a.dy.p, a.dy.rep, 0, (int)a.dy.row, a.rows, a.out};
+    const Plane3 x{wx, (long long)a.rows * p.ldx, 0, p.ldx, a.rows, p.ldx, nullptr};
+    Plane3 dy{(const __bf16*)a.dy.p, a.dy.rep, 0, (int)a.dy.row, a.rows, a.out, nullptr};
     if (PL == 3 || !chunked(a.dy, 1, a.out) || !direct_pitch(a.dy.row)) {
-        if ((e = lay_out<T>(a.n, a.rows, a.out, p.ldy, a.dy, Labelled{nullptr, 0}, wy, s)) != hipSuccess) return e;
-        dy = Plane3{wy, (long long)a.rows * p.ldy, (long long)a.n * a.rows * p.ldy, p.ldy, a.rows, p.ldy};
+        if ((e = lay_out<T, PL>(a.n, a.rows, a.out, p.ldy, a.dy, Labelled{nullptr, 0}, nullptr, wy, s)) != hipSuccess) return e;
+        dy = Plane3{wy, (long long)a.rows * p.ldy, (long long)a.n * a.rows * p.ldy, p.ldy, a.rows, p.ldy, nullptr};
     }
     if (p.big) return launch_direct<1, PL, 256, 256, 2, 4, false, false>(x, dy, a.n, a.in, a.out, a.rows, 1, a.rows, store, s);
     return launch_direct<1, PL, 128, 128, 2, 2, false, false>(x, dy, a.n, a.in, a.out, a.rows, 1, a.rows, store, s);

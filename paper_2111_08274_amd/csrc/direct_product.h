@@ -1,5 +1,15 @@
-// Tiled matrix product on the matrix cores for operands that lie as the matrix cores take them: bf16 (a 32-bit operand as
-// three bf16 planes), rows on 16 bytes, whole chunks of eight values.  C[m][n] = sum_k A(m, k) B(n, k).
+// Tiled matrix product on the matrix cores for operands that lie as the matrix cores take them: planes of 16-bit values, rows
+// on 16 bytes, whole chunks of eight values.  C[m][n] = sum_k A(m, k) B(n, k).
+//
+// A plane holds
+//   bf16 operands            as they are
+//   32-bit operands, 3       three bf16 parts (parts3), against a bf16 operand: three products, nothing is lost
+//   32-bit operands, 2       two fp16 parts: with 2^s the power of two that takes the replica's largest finite magnitude to [2^14, 2^15),
+//                            y = 2^s x, h = fp16(y), l = fp16(2^11 (y - h)).  Products l h' and h l' first, 2^-11 on the sums, then
+//                            h h'; l l', at most 2^-22 of the product, is left out, and l's own rounding is at most 2^-22 of y: a
+//                            product is off by 2^-23.5 in the mean square, which is what a 32-bit sum of a few terms loses.  The factor
+//                            on l keeps it a normal number, so this holds for magnitudes down to 2^-29 of the largest; below, the
+//                            error stays under 2^-50 of the largest.  Three products where three bf16 parts would take six.
 //
 // Slabs of 64 k go from memory to LDS without passing registers (buffer loads that write LDS), as many slabs ahead of the one
 // being multiplied as LDS holds (256 x 256 tiles: one, 128 x 256: two, 128 x 128: three), one barrier a slab.  The LDS image is the slab itself with its 16-byte chunks exchanged within a row, so
@@ -9,6 +19,8 @@
 //   across  it runs across them: [64 k][columns], chunk c of row k at c ^ 4 (k & 3); the operand read transposes
 // 256 x 256 tiles of eight waves hold 128 x 64 each: 1.5 KiB of LDS reads a matrix instruction of 32 cycles a wave.
 #pragma once
+#include <algorithm>
+
 #include "tile_product.h"
 
 namespace hadfl {
@@ -20,7 +32,32 @@ struct Plane3 {                    // an operand: source rows `lines` of `cols` 
     const __bf16* p;
     long long rep, plane;
     int ld, lines, cols;
+    const unsigned* top;           // two fp16 parts: the replicas' largest magnitudes (bits of a float); null: 1
 };
+
+constexpr float kLowScale = 0x1p11f;
+// 2^s and 2^-s of two fp16 parts.  A tensor of magnitudes below 2^-112 is scaled by 2^126, which is still exact.
+__device__ __forceinline__ float up_scale(unsigned top) { return __builtin_bit_cast(float, (unsigned)min(127 + 14 + 127 - (int)(top >> 23), 253) << 23); }
+__device__ __forceinline__ float down_scale(unsigned top) { return __builtin_bit_cast(float, (unsigned)max((int)(top >> 23) - 14, 1) << 23); }
+constexpr unsigned kOneBits = 0x3f800000u;
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ unsigned to_f16x2(float a, float b) { return __builtin_bit_cast(unsigned, (h2{(_Float16)a, (_Float16)b})); }
+__device__ __forceinline__ void split2(const f4& x, float scale, u2& h, u2& l)
+{
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const float a = x[2 * e] * scale, b = x[2 * e + 1] * scale;
+        const h2 top{(_Float16)a, (_Float16)b};
+        h[e] = __builtin_bit_cast(unsigned, top);
+        l[e] = to_f16x2((a - (float)top[0]) * kLowScale, (b - (float)top[1]) * kLowScale);
+    }
+}
+template <bool F16> __device__ __forceinline__ f16 multiply16(const bf16x8& a, const bf16x8& b, const f16& c)
+{
+    if (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
 // what the kernel's 32-bit offsets within a tile reach
 inline bool direct_pitch(long long ld) { return ld <= (1ll << 22); }
 
@@ -85,10 +122,10 @@ template <bool ALONG, int BR, int NT> struct Loader {
 template <int PA, int PB> struct Pairs;
 template <> struct Pairs<1, 1> { static constexpr int kCount = 1; static __device__ int a(int) { return 0; } static __device__ int b(int) { return 0; } };
 template <> struct Pairs<1, 3> { static constexpr int kCount = 3; static __device__ int a(int) { return 0; } static __device__ int b(int s) { return 2 - s; } };
-template <> struct Pairs<3, 3> {
-    static constexpr int kCount = 6;                           // (0,2) (1,1) (2,0) (0,1) (1,0) (0,0)
-    static __device__ int a(int s) { return s == 1 || s == 4 ? 1 : s == 2 ? 2 : 0; }
-    static __device__ int b(int s) { return s == 0 ? 2 : s == 1 || s == 3 ? 1 : 0; }
+template <> struct Pairs<2, 2> {
+    static constexpr int kCount = 3;                           // (1,0) (0,1) (0,0)
+    static __device__ int a(int s) { return s == 0; }
+    static __device__ int b(int s) { return s == 1; }
 };
 
 // waits for all but the last N loads of this wave and for its LDS reads, then for the other waves
@@ -174,10 +211,10 @@ __global__ __launch_bounds__(WM * WN * 64) void direct_kernel(Plane3 a, Plane3 b
             for (int i = 0; i < TM; ++i)
 #pragma unroll
                 for (int j = 0; j < TN; ++j)
-                    t.acc[i][j] = Epi::kLaneM ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], t.acc[i][j], 0, 0, 0)
-                                              : __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], t.acc[i][j], 0, 0, 0);
+                    t.acc[i][j] = Epi::kLaneM ? multiply16<PA == 2>(fb[j], fa[i], t.acc[i][j]) : multiply16<PA == 2>(fa[i], fb[j], t.acc[i][j]);
         }
     };
+    const int low_slabs = 2 * ((k_end - k_begin + kSlab - 1) / kSlab);      // two fp16 parts: those of the products with a low part
     const int slabs = k_begin < k_end ? P::kCount * ((k_end - k_begin + kSlab - 1) / kSlab) : 0;
     // Slab i: its loads are done when at most those of the IMAGES - 2 slabs after it are outstanding (loads finish in order);
     // the barrier says so for all waves, and that all have read the slab before, whose image the next loads take.
@@ -186,6 +223,12 @@ __global__ __launch_bounds__(WM * WN * 64) void direct_kernel(Plane3 a, Plane3 b
         if (IMAGES > 2 && i + IMAGES - 2 < slabs) slab_barrier<(IMAGES - 2) * kLoads>();
         else slab_barrier<0>();
         if (i + IMAGES - 1 < slabs) issue(free);
+        if (PA == 2 && i == low_slabs) {
+#pragma unroll
+            for (int x = 0; x < TM; ++x)
+#pragma unroll
+                for (int y = 0; y < TN; ++y) t.acc[x][y] *= 1.f / kLowScale;
+        }
         multiply(image);
     };
 #pragma unroll
@@ -195,12 +238,12 @@ __global__ __launch_bounds__(WM * WN * 64) void direct_kernel(Plane3 a, Plane3 b
 #pragma unroll
         for (int u = 0; u < IMAGES; ++u) turn(i + u, images + u * kImage, images + (u + IMAGES - 1) % IMAGES * kImage);
     }
-    constexpr float kScale = (PA == 3 ? 0x1p-24f : 1.f) * (PB == 3 ? 0x1p-24f : 1.f);
-    if (kScale != 1.f) {
+    if (PA == 2) {                                             // one after the other: their product may be no float
+        const float sa = down_scale(a.top ? a.top[t.rep] : kOneBits), sb = down_scale(b.top ? b.top[t.rep] : kOneBits);
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) t.acc[i][j] *= kScale;
+            for (int j = 0; j < TN; ++j) t.acc[i][j] = t.acc[i][j] * sa * sb;
     }
     if constexpr (Epi::kStaged) {
         __syncthreads();                                       // the images are free
@@ -221,10 +264,37 @@ hipError_t launch_direct(const Plane3& a, const Plane3& b, int replicas, int M, 
 }
 
 // ---- laying operands out ---------------------------------------------------------------------------------------------
-// x [replicas][rows][cols] -> bf16 [planes][replicas][rows][ld], zero beyond cols and in rows that take no part
-template <typename T>
+// the largest finite magnitude of every replica's x, as a float's bits, joined to what top holds; rows that take no part are left out
+__global__ __launch_bounds__(256) inline void largest_kernel(const float* x, long long rep, long long row, int rows, int cols, Labelled live, unsigned* top)
+{
+    const int k = blockIdx.y, chunks = (cols + 7) / 8;
+    const long long total = (long long)rows * chunks, step = (long long)gridDim.x * 256;
+    if (live.labels) live.labels += (long long)k * rows;
+    unsigned most = 0;
+    for (long long at = (long long)blockIdx.x * 256 + threadIdx.x; at < total; at += step) {
+        const int t = (int)(at / chunks), c = (int)(at - (long long)t * chunks) * 8;
+        Chunk<float> v;
+        v.load(x + k * rep + t * row + c, live.at(t) ? cols - c : 0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const unsigned a = v.a[e] & 0x7fffffffu, b = v.b[e] & 0x7fffffffu;
+            most = max(most, max(a < 0x7f800000u ? a : 0u, b < 0x7f800000u ? b : 0u));
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) most = max(most, (unsigned)__shfl_xor((int)most, d));
+    __shared__ unsigned waves[4];
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x / 64] = most;
+    __syncthreads();
+    // a maximum: the same in any order; one a workgroup, since additions to one address queue up
+    if (threadIdx.x == 0) atomicMax(top + k, max(max(waves[0], waves[1]), max(waves[2], waves[3])));
+}
+__global__ inline void clear_kernel(unsigned* p, int n) { if ((int)threadIdx.x < n) p[threadIdx.x] = 0; }
+
+// x [replicas][rows][cols] -> [planes][replicas][rows][ld], zero beyond cols and in rows that take no part
+template <typename T, int PL>
 __global__ __launch_bounds__(256) void lay_out_kernel(const T* x, long long rep, long long row, int rows, int cols, int ld, long long total, long long plane,
-                                                      Labelled live, __bf16* out)
+                                                      Labelled live, const unsigned* top, __bf16* out)
 {
     const long long at = (long long)blockIdx.x * 256 + threadIdx.x;          // chunk of eight
     if (at >= total) return;
@@ -232,23 +302,34 @@ __global__ __launch_bounds__(256) void lay_out_kernel(const T* x, long long rep,
     const long long line = at / chunks;
     const int c = (int)(at - line * chunks) * 8, k = (int)(line / rows), t = (int)(line - (long long)k * rows);
     if (live.labels) live.labels += (long long)k * rows;
-    const T* src = x + k * rep + t * row + c;
     Chunk<T> chunk;
-    chunk.load(src, live.at(t) ? cols - c : 0);
-    if constexpr (sizeof(T) == 2) *(u4*)(out + at * 8) = chunk.a;
+    chunk.load(x + k * rep + t * row + c, live.at(t) ? cols - c : 0);
+    u4 part[PL];
+    if constexpr (PL == 1) part[0] = chunk.a;
+    else if constexpr (PL == 3) Source<float>::planes(chunk, part);
     else {
-        u4 part[3];
-        Source<float>::planes(chunk, part);
-#pragma unroll
-        for (int i = 0; i < 3; ++i) *(u4*)(out + i * plane + at * 8) = part[i];
+        const float scale = up_scale(top[k]);
+        u2 h[2], l[2];
+        split2(__builtin_bit_cast(f4, chunk.a), scale, h[0], l[0]);
+        split2(__builtin_bit_cast(f4, chunk.b), scale, h[1], l[1]);
+        part[0] = join8(h[0], h[1]);
+        part[1] = join8(l[0], l[1]);
     }
+#pragma unroll
+    for (int i = 0; i < PL; ++i) *(u4*)(out + i * plane + at * 8) = part[i];
 }
-template <typename T>
-hipError_t lay_out(int n, int rows, int cols, int ld, const Rows& x, Labelled live, __bf16* out, hipStream_t s)
+template <typename T, int PL>
+hipError_t lay_out(int n, int rows, int cols, int ld, const Rows& x, Labelled live, const unsigned* top, __bf16* out, hipStream_t s)
 {
     const long long plane = (long long)n * rows * ld, total = plane / 8;
     if (total == 0) return hipSuccess;
-    lay_out_kernel<T><<<(unsigned)((total + 255) / 256), 256, 0, s>>>((const T*)x.p, x.rep, x.row, rows, cols, ld, total, plane, live, out);
+    lay_out_kernel<T, PL><<<(unsigned)((total + 255) / 256), 256, 0, s>>>((const T*)x.p, x.rep, x.row, rows, cols, ld, total, plane, live, top, out);
+    return hipGetLastError();
+}
+inline hipError_t find_largest(int n, int rows, int cols, const Rows& x, Labelled live, unsigned* top, hipStream_t s)
+{
+    const long long blocks = ((long long)rows * ((cols + 7) / 8) + 255) / 256;
+    largest_kernel<<<dim3((unsigned)std::min<long long>(blocks, std::max(8, 1024 / n)), (unsigned)n), 256, 0, s>>>((const float*)x.p, x.rep, x.row, rows, cols, live, top);
     return hipGetLastError();
 }
 

@@ -20,6 +20,22 @@ struct Labelled {
     __device__ __forceinline__ bool at(int t) const { return !labels || (unsigned)labels[t] < (unsigned)classes; }
 };
 
+// Three bf16 parts of a float whose sum is the float: h = bf16(x), m = bf16(x - h), l = x - h - m, both differences exact.  No scale, so
+// that products of any two magnitudes whose product is a float stay floats; l is no normal bf16 below 2^-107, where the float's lowest
+// bits go.
+__device__ __forceinline__ void parts3(const f4& x, u2& h, u2& m, u2& l)
+{
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        float a = x[2 * e], b = x[2 * e + 1];
+        h[e] = to_bf16x2(a, b);
+        a -= __builtin_bit_cast(float, h[e] << 16); b -= __builtin_bit_cast(float, h[e] & 0xffff0000u);
+        m[e] = to_bf16x2(a, b);
+        a -= __builtin_bit_cast(float, m[e] << 16); b -= __builtin_bit_cast(float, m[e] & 0xffff0000u);
+        l[e] = to_bf16x2(a, b);
+    }
+}
+
 template <typename T> struct Source {
     static constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;
     typedef Chunk<T> Raw;
@@ -41,8 +57,8 @@ template <typename T> struct Source {
     static __device__ __forceinline__ void planes(const Chunk<float>& v, u4 (&out)[3])
     {
         u2 h[2], m[2], l[2];
-        split3(__builtin_bit_cast(f4, v.a), h[0], m[0], l[0]);
-        split3(__builtin_bit_cast(f4, v.b), h[1], m[1], l[1]);
+        parts3(__builtin_bit_cast(f4, v.a), h[0], m[0], l[0]);
+        parts3(__builtin_bit_cast(f4, v.b), h[1], m[1], l[1]);
         out[0] = join8(h[0], h[1]); out[1] = join8(m[0], m[1]); out[2] = join8(l[0], l[1]);
     }
 };
@@ -82,10 +98,10 @@ struct SourcePacked {              // rows and columns of one replica; the surpl
 };
 
 // LDS image of one slab of an operand, one plane: along: [BR rows][KS + 8] (rows 16 bytes off a multiple of 32 banks' width),
-// across: [KS][BR] with rows 64 bytes apart modulo 256, so that the transposing read of 4 rows x 32 columns meets every
+// across: [KS][BR] with rows an odd multiple of 64 bytes apart, so that the transposing read of 4 rows x 32 columns meets every
 // bank once
 template <bool ALONG, int BR, int KS> struct Image {
-    static constexpr unsigned kPitch = ALONG ? KS * 2 + 16 : BR * 2 + (64 + 256 - BR * 2 % 256) % 256;
+    static constexpr unsigned kPitch = ALONG ? KS * 2 + 16 : BR * 2 % 128 == 0 ? BR * 2 + 64 : BR * 2;
     static constexpr unsigned kPlane = ALONG ? BR * kPitch : KS * kPitch;
     static constexpr int kAcross = ALONG ? KS / 8 : BR / 8;    // chunks in an image row
     static constexpr int kChunks = BR * KS / 8;
@@ -245,13 +261,6 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(SA a, SB b, int K
         if (k0 + KS < k_end) fetch(k0 + KS);
         multiply(buf);
     }
-    constexpr float kScale = (PA == 3 ? 0x1p-24f : 1.f) * (PB == 3 ? 0x1p-24f : 1.f);
-    if (kScale != 1.f) {
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) t.acc[i][j] *= kScale;
-    }
     if constexpr (Epi::kStaged) {
         __syncthreads();
         epi(t, smem);
@@ -259,8 +268,8 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(SA a, SB b, int K
 }
 
 // ---- epilogues that only store ---------------------------------------------------------------------------------
-// C to a tensor, times a factor per replica (lanes along n); SUMS: and the columns' sums of a B in PB planes
-template <typename T, bool SUMS = false, int PB = 1> struct StoreTile {
+// C to a tensor, times a factor per replica (lanes along n); SUMS: and B's column sums
+template <typename T, bool SUMS = false> struct StoreTile {
     static constexpr bool kLaneM = false, kStaged = false, kSums = SUMS;
     T* p;
     long long rep, row;
@@ -288,7 +297,7 @@ template <typename T, bool SUMS = false, int PB = 1> struct StoreTile {
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
                 const int n = t.n0 + 32 * j + t.lane;
-                if (t.lane < 32 && n < N) sums[t.rep * sums_rep + n] = t.sum[j][0] * (PB == 3 ? 0x1p-24f : 1.f);
+                if (t.lane < 32 && n < N) sums[t.rep * sums_rep + n] = t.sum[j][0];
             }
         }
     }

@@ -366,6 +366,33 @@ def test_large_logits_and_a_label_that_is_out():
             assert torch.isinf(row[hit]).all() and torch.isfinite(row[~hit]).all()
 
 
+@pytest.mark.parametrize("rows", [20, 100, 300])
+@pytest.mark.parametrize("kind", ["columns", "far apart", "outlier"])
+def test_32_bit_operands_of_uneven_magnitude(rows, kind):
+    # what enters the matrix products in parts of 16 bits: features whose x and W differ by opposite powers of two, tensors of extreme
+    # magnitude, and one value 2^20 times the rest.  The bounds are those of 32-bit sums, as everywhere here
+    torch = _torch()
+    rng = np.random.default_rng(12)
+    n, d, v = 2, 96, 700
+    x, w = rng.normal(size=(n, rows, d)), rng.normal(size=(n, d, v)) * 1.5 / np.sqrt(d)
+    if kind == "columns":
+        e = 2.0 ** rng.integers(-10, 11, size=d)
+        x, w = x * e, w / e[:, None]
+    elif kind == "far apart":
+        x, w = x * 2.0 ** 90, w * 2.0 ** -90
+    else:
+        x[0, 3, 5] = 2.0 ** 20
+        w[:, 5] *= 2.0 ** -20
+    y = rng.integers(0, v, size=(n, rows)).astype(np.int32)
+    c = dict(x=_in(x, 0, "whole"), w=_in(w, 0, "whole"), bias=None, y=torch.as_tensor(y).cuda(), yh=y)
+    loss, row, dx, dw, _ = hadfl.ClassLoss(n, rows, d, v).grad(c["x"], c["w"], c["y"])
+    for k in range(n):
+        r, b = _loss_reference(c, k, 0)
+        _check(_values(row)[k], r["row_loss"], b["row_loss"], "row_loss")
+        _check(_values(dx)[k], r["dx"], b["dx"], "dx")
+        _check(_values(dw)[k], r["dw"], b["dw"], "dw")
+
+
 def test_a_row_whose_mask_leaves_nothing():
     # every class masked by the type's lowest value: the logits are equal, so the loss is log(classes) and the gradient's rows
     # are 1 / classes but for the label's; a row of -inf alone has no softmax, and its neighbours keep theirs
