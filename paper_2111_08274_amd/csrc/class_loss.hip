@@ -367,43 +367,6 @@ __global__ __launch_bounds__(256) void bias_grad_kernel(const float* sums, int b
     db[k * rep + c0 + c] = v * factor[k];
 }
 
-// dx: the shares of the contraction, eight columns a thread; zero for a row without a label.  G threads take the shares of a chunk,
-// each its own in ascending order, and are added in ascending order: with few rows there are many shares and few chunks.
-template <typename T, int G>
-__global__ __launch_bounds__(256) void input_grad_kernel(const float* share, int splits, long long step, int rows, int cols, int ld, long long total,
-                                                         Labelled live, const float* factor, T* dx, long long rep, long long row)
-{
-    constexpr int PER = 256 / G;
-    __shared__ __attribute__((aligned(16))) float part[G][G > 1 ? PER * 8 : 8];
-    const int mine = threadIdx.x % PER, group = threadIdx.x / PER;
-    const long long at = (long long)blockIdx.x * PER + mine;
-    f4 a = {}, b = {};
-    if (at < total) {
-        const float* src = share + at * 8;
-#pragma unroll 8
-        for (int s = group; s < splits; s += G) { a += *(const f4*)(src + s * step); b += *(const f4*)(src + s * step + 4); }
-    }
-    if (G > 1) {
-        *(f4*)&part[group][mine * 8] = a;
-        *(f4*)&part[group][mine * 8 + 4] = b;
-        __syncthreads();
-        if (group) return;
-#pragma unroll
-        for (int g = 1; g < G; ++g) { a += *(const f4*)&part[g][mine * 8]; b += *(const f4*)&part[g][mine * 8 + 4]; }
-    }
-    if (at >= total) return;
-    const int chunks = ld / 8;
-    const long long line = at / chunks;
-    const int c = (int)(at - line * chunks) * 8, k = (int)(line / rows), t = (int)(line - (long long)k * rows);
-    live.labels += (long long)k * rows;
-    const float f = factor[k];
-    const bool on = live.at(t);
-    float v[8];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) { v[e] = on ? a[e] * f : 0.f; v[4 + e] = on ? b[e] * f : 0.f; }
-    store_chunk(dx + k * rep + t * row + c, cols - c, v);
-}
-
 // Which kernels, the piece of the vocabulary and the working memory, from the sizes alone.
 //   few rows (at most 64)   the products through registers read W as it is, 32 x 128 or 128 x 128 tiles: W is read once or twice
 //                           per pass, laying it out first would cost as much again
@@ -506,12 +469,7 @@ hipError_t bias_grad(const LossArgs& a, const Plan& p, const Work& w, int ld, in
 template <typename T> hipError_t input_grad(const LossArgs& a, const Plan& p, const Work& w, hipStream_t s)
 {
     if (!a.dx.p || !a.rows) return hipSuccess;
-    const long long lines = (long long)a.n * a.rows, total = lines * (p.ldx / 8);
-    auto* kernel = p.splits > 8 ? input_grad_kernel<T, 8> : input_grad_kernel<T, 1>;
-    const int per = p.splits > 8 ? 32 : 256;
-    kernel<<<(unsigned)((total + per - 1) / per), 256, 0, s>>>(w.share, p.splits, lines * p.ldx, a.rows, a.features, p.ldx, total,
-                                                                Labelled{a.labels, a.classes}, w.factor, (T*)a.dx.p, a.dx.rep, a.dx.row);
-    return hipGetLastError();
+    return join_shares<T>(w.share, p.splits, a.n, a.rows, a.features, p.ldx, Labelled{a.labels, a.classes}, w.factor, a.dx, nullptr, 0, s);
 }
 
 // few rows: everything through registers.  Where one piece holds the whole vocabulary its logits stay in it for the gradient.
@@ -545,7 +503,7 @@ template <typename T, int BM, int WM, int WN> hipError_t run_general(const LossA
         }
         if (e != hipSuccess) return e;
         if (a.dx.p && a.rows) {
-            const StoreShare store{k.share, a.rows, a.features, p.ldx, a.n, i > 0};
+            const StoreShare<> store{k.share, a.rows, a.features, p.ldx, a.rows, a.n, i > 0, false};
             e = launch_product<BM, 128, WM, WN, true, true>(g, w, a.n, a.rows, a.features, cols, p.splits, p.split_len, store, s);
             if (e != hipSuccess) return e;
         }
@@ -604,7 +562,7 @@ template <typename T, int BM> hipError_t run_direct(const LossArgs& a, const Pla
         e = launch_direct<PL, PL, BM, 256, 2, 4, true, false>(x, w, a.n, a.rows, cols, a.features, 1, a.features, GradientRows<PL>{soft, (__bf16*)k.g, g.plane}, s);
         if (e != hipSuccess) return e;
         if (a.dx.p) {
-            const StoreShare store{k.share, a.rows, a.features, p.ldx, a.n, i > 0};
+            const StoreShare<> store{k.share, a.rows, a.features, p.ldx, a.rows, a.n, i > 0, false};
             e = launch_direct<PL, PL, BM, 256, 2, 4, true, true>(g, w, a.n, a.rows, a.features, w.cols, p.splits, p.split_len, store, s);
             if (e != hipSuccess) return e;
         }

@@ -1,7 +1,7 @@
 // Parameter gradients of a dense layer whose input was kept in 8 bits: dW = x^T dy with x from the checkpoint, db = sum_t dy.
 // q * 2^e is exact in bf16, so a bf16 dy needs one product and a 32-bit dy, in three bf16 planes, three.  db comes from the same
 // operands as one more product, of ones (tile_product.h).
-//   short contractions or few outputs   chunks of the checkpoint become bf16 in registers, on their way to LDS
+//   short contractions or few columns   chunks of the checkpoint become bf16 in registers, on their way to LDS
 //   otherwise                           the checkpoint is laid out as bf16 first (3 bytes a value once, where every column of tiles would
 //                                       convert it again) and both operands go straight from memory to LDS
 #include "direct_product.h"
@@ -12,35 +12,40 @@ namespace head {
 namespace {
 
 struct Plan {
-    bool direct, big;              // big: 256 x 256 tiles, else 128 x 128
-    int ldx, ldy, planes;
-    size_t x, y, total;
+    bool direct, big;              // big: 256 x 256 tiles, else 128 x 128; not direct: 64 x 64
+    int ldx, ldy, planes, splits, split_len;
+    size_t x, y, share, total;
 };
 
 Plan plan_of(int n, int rows, int in, int out, int bf16)
 {
     Plan p{};
-    p.direct = rows >= 256 && in >= 128 && out >= 128;
-    p.big = (long long)n * ((in + 255) / 256) * ((out + 255) / 256) >= 192;
+    p.direct = rows >= 256 && in >= 96 && out >= 96;
+    auto tiles = [&](int t) { return (long long)n * ((in + t - 1) / t) * ((out + t - 1) / t); };
+    p.big = tiles(256) >= 192;
     p.ldx = (in + 7) / 8 * 8;
     p.ldy = (out + 7) / 8 * 8;
     p.planes = bf16 ? 1 : 3;
+    // fewer tiles than compute units: the rows in shares, of 256 rows at least, that a second launch adds
+    const long long have = tiles(!p.direct ? 64 : p.big ? 256 : 128);
+    p.splits = (int)std::max<long long>(1, std::min<long long>(256 / have, rows / 256));
+    p.split_len = (((rows + p.splits - 1) / p.splits) + 63) / 64 * 64;
+    p.splits = std::max(1, (rows + p.split_len - 1) / std::max(1, p.split_len));
     if (p.direct) {
         p.x = 0;
         p.y = align256((size_t)n * rows * p.ldx * 2);
-        p.total = p.y + align256((size_t)n * rows * p.ldy * 2 * p.planes);
+        p.share = p.y + align256((size_t)n * rows * p.ldy * 2 * p.planes);
     }
+    p.total = p.share + (p.splits > 1 ? align256((size_t)p.splits * n * (in + 1) * p.ldy * 4) : 0);
     return p;
 }
 
-template <typename T> hipError_t run(const DenseArgs& a, hipStream_t s)
+template <typename T, class Store> hipError_t product(const DenseArgs& a, const Plan& p, const Store& store, hipStream_t s)
 {
     constexpr int PL = sizeof(T) == 4 ? 3 : 1;
-    const Plan p = plan_of(a.n, a.rows, a.in, a.out, a.bf16);
-    const StoreTile<float, true> store{(float*)a.dw.p, a.dw.rep, a.dw.row, nullptr, a.in, a.out, (float*)a.db.p, a.db.rep};
     if (!p.direct)
-        return launch_product<64, 64, 2, 2, false, false>(SourcePacked{a.x, a.rows, a.in}, source<T>(a.dy, a.rows, a.out), a.n, a.in, a.out, a.rows, 1,
-                                                          std::max(1, a.rows), store, s);
+        return launch_product<64, 64, 2, 2, false, false>(SourcePacked{a.x, a.rows, a.in}, source<T>(a.dy, a.rows, a.out), a.n, a.in, a.out, a.rows,
+                                                          p.splits, std::max(1, p.split_len), store, s);
     __bf16 *wx = (__bf16*)((char*)a.work + p.x), *wy = (__bf16*)((char*)a.work + p.y);
     hipError_t e = launch_unpack(a.n, a.rows, a.in, 1, a.x.q, Rows{wx, (long long)a.rows * p.ldx, p.ldx}, s);
     if (e != hipSuccess) return e;
@@ -50,8 +55,20 @@ template <typename T> hipError_t run(const DenseArgs& a, hipStream_t s)
         if ((e = lay_out<T, PL>(a.n, a.rows, a.out, p.ldy, a.dy, Labelled{nullptr, 0}, nullptr, wy, s)) != hipSuccess) return e;
         dy = Plane3{wy, (long long)a.rows * p.ldy, (long long)a.n * a.rows * p.ldy, p.ldy, a.rows, p.ldy, nullptr};
     }
-    if (p.big) return launch_direct<1, PL, 256, 256, 2, 4, false, false>(x, dy, a.n, a.in, a.out, a.rows, 1, a.rows, store, s);
-    return launch_direct<1, PL, 128, 128, 2, 2, false, false>(x, dy, a.n, a.in, a.out, a.rows, 1, a.rows, store, s);
+    if (p.big) return launch_direct<1, PL, 256, 256, 2, 4, false, false>(x, dy, a.n, a.in, a.out, a.rows, p.splits, p.split_len, store, s);
+    return launch_direct<1, PL, 128, 128, 2, 2, false, false>(x, dy, a.n, a.in, a.out, a.rows, p.splits, p.split_len, store, s);
+}
+
+template <typename T> hipError_t run(const DenseArgs& a, hipStream_t s)
+{
+    const Plan p = plan_of(a.n, a.rows, a.in, a.out, a.bf16);
+    if (p.splits == 1) return product<T>(a, p, StoreTile<float, true>{(float*)a.dw.p, a.dw.rep, a.dw.row, nullptr, a.in, a.out, (float*)a.db.p, a.db.rep}, s);
+    float* share = (float*)((char*)a.work + p.share);
+    const bool sums = a.db.p;
+    const int lines = a.in + (sums ? 1 : 0);
+    const hipError_t e = product<T>(a, p, StoreShare<true>{share, a.in, a.out, p.ldy, lines, a.n, false, sums}, s);
+    if (e != hipSuccess) return e;
+    return join_shares<float>(share, p.splits, a.n, lines, a.out, p.ldy, Labelled{nullptr, 0}, nullptr, a.dw, (float*)a.db.p, a.db.rep, s);
 }
 
 }  // namespace

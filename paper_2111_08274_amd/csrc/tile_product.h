@@ -302,15 +302,15 @@ template <typename T, bool SUMS = false> struct StoreTile {
         }
     }
 };
-// C into [split][replica][M][ld] floats, over or onto what is there
-struct StoreShare {
-    static constexpr bool kLaneM = false, kStaged = false, kSums = false;
+// C into [split][replica][lines][ld] floats, over or onto what is there; SUMS: B's column sums into line M (lines = M + 1)
+template <bool SUMS = false> struct StoreShare {
+    static constexpr bool kLaneM = false, kStaged = false, kSums = SUMS;
     float* p;
-    int M, N, ld, replicas;
-    bool onto;
+    int M, N, ld, lines, replicas;
+    bool onto, sums;
     template <int TM, int TN> __device__ __forceinline__ void operator()(const Tile<TM, TN>& t) const
     {
-        float* out = p + ((long long)t.split * replicas + t.rep) * M * ld;
+        float* out = p + ((long long)t.split * replicas + t.rep) * lines * ld;
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -328,8 +328,64 @@ struct StoreShare {
                     if (m < M) out[(long long)m * ld + n] = have[e] + t.acc[i][j][e];
                 }
             }
+        if (SUMS && has_sum(*this, t.m0)) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const int n = t.n0 + 32 * j + t.lane;
+                if (t.lane < 32 && n < N) out[(long long)M * ld + n] = t.sum[j][0];
+            }
+        }
     }
 };
+
+// A tensor from the shares of a contraction, [splits][replicas][lines][ld] floats, eight columns a thread, times a factor per replica (or
+// null); zero in rows that take no part; the last line goes to `last` if that is there.  G threads take the shares of a chunk, each its own in
+// ascending order, and are added in ascending order: where there are many shares there are few chunks.
+template <typename T, int G>
+__global__ __launch_bounds__(256) void join_shares_kernel(const float* share, int splits, long long step, int lines, int cols, int ld, long long total,
+                                                          Labelled live, const float* factor, T* out, long long rep, long long row, T* last, long long last_rep)
+{
+    constexpr int PER = 256 / G;
+    __shared__ __attribute__((aligned(16))) float part[G][G > 1 ? PER * 8 : 8];
+    const int mine = threadIdx.x % PER, group = threadIdx.x / PER;
+    const long long at = (long long)blockIdx.x * PER + mine;
+    f4 a = {}, b = {};
+    if (at < total) {
+        const float* src = share + at * 8;
+#pragma unroll 8
+        for (int s = group; s < splits; s += G) { a += *(const f4*)(src + s * step); b += *(const f4*)(src + s * step + 4); }
+    }
+    if (G > 1) {
+        *(f4*)&part[group][mine * 8] = a;
+        *(f4*)&part[group][mine * 8 + 4] = b;
+        __syncthreads();
+        if (group) return;
+#pragma unroll
+        for (int g = 1; g < G; ++g) { a += *(const f4*)&part[g][mine * 8]; b += *(const f4*)&part[g][mine * 8 + 4]; }
+    }
+    if (at >= total) return;
+    const int chunks = ld / 8;
+    const long long line = at / chunks;
+    const int c = (int)(at - line * chunks) * 8, k = (int)(line / lines), t = (int)(line - (long long)k * lines);
+    if (live.labels) live.labels += (long long)k * lines;
+    const float f = factor ? factor[k] : 1.f;
+    const bool on = live.at(t);
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { v[e] = on ? a[e] * f : 0.f; v[4 + e] = on ? b[e] * f : 0.f; }
+    store_chunk(last && t == lines - 1 ? last + k * last_rep + c : out + k * rep + t * row + c, cols - c, v);
+}
+template <typename T>
+hipError_t join_shares(const float* share, int splits, int replicas, int lines, int cols, int ld, Labelled live, const float* factor, const Rows& out,
+                       T* last, long long last_rep, hipStream_t s)
+{
+    const long long all = (long long)replicas * lines, total = all * (ld / 8);
+    if (total == 0) return hipSuccess;
+    auto* kernel = splits > 8 ? join_shares_kernel<T, 8> : join_shares_kernel<T, 1>;
+    const int per = splits > 8 ? 32 : 256;
+    kernel<<<(unsigned)((total + per - 1) / per), 256, 0, s>>>(share, splits, all * ld, lines, cols, ld, total, live, factor, (T*)out.p, out.rep, out.row, last, last_rep);
+    return hipGetLastError();
+}
 
 template <int BM, int BN, int WM, int WN, bool A_ALONG, bool B_ALONG, class SA, class SB, class Epi>
 hipError_t launch_product(const SA& a, const SB& b, int replicas, int M, int N, int K, int splits, int split_len, const Epi& epi, hipStream_t s)

@@ -228,7 +228,7 @@ def test_a_group_with_an_infinity_or_a_nan_stands_for_nans_and_no_other():
 
 # ---- a dense layer's gradient from a checkpoint ----------------------------------------------------------------------------
 DENSE = [(1, 0, 5, 9), (1, 1, 1, 1), (2, 3, 33, 7), (4, 32, 784, 128), (2, 65, 130, 257), (1, 257, 129, 120), (3, 100, 512, 512), (1, 1000, 48, 96),
-         (1, 2049, 256, 256), (2, 640, 264, 520)]
+         (1, 2049, 256, 256), (2, 640, 264, 520), (1, 3000, 40, 90), (2, 1500, 97, 130), (16, 300, 520, 512)]
 
 
 @pytest.mark.parametrize("layout", ["whole", "padded", "odd"])
