@@ -13,18 +13,10 @@ namespace head {
 
 namespace {
 
-constexpr float kLog2e = 1.44269504088896340736f, kLog2eLow = 1.92596299112661746887e-8f, kLn2 = 0.693147180559945309417f;
+constexpr float kLog2e = 1.44269504088896340736f;
 
-// exp of a number that is not positive.  EXACT: the product with log2(e) in two parts, else its rounding error, |t| * 2^-24,
-// would show in a 32-bit gradient
-template <bool EXACT> __device__ __forceinline__ float exp_down(float t)
-{
-    const float y = t * kLog2e;
-    const float p = __builtin_amdgcn_exp2f(y);
-    if (!EXACT || !(y > -126.f)) return p;
-    const float rest = __builtin_fmaf(t, kLog2e, -y) + t * kLog2eLow;
-    return __builtin_fmaf(p, rest * kLn2, p);
-}
+// exp of a number that is not positive, off by |t| / 2 units in the last place at most: what a rounding of t itself does
+__device__ __forceinline__ float exp_down(float t) { return __builtin_amdgcn_exp2f(t * kLog2e); }
 
 // logits z of a wave's block of 32 rows (lanes along m), with the bias, -inf beyond the classes; n0: the first column's class
 template <int TM, int TN>
@@ -67,7 +59,7 @@ __device__ __forceinline__ void join(float2& have, const float2& v)
 {
     const float top = fmaxf(have.x, v.x);
     if (top == -INFINITY) { have.y += v.y; return; }           // nothing yet: zero, or a NaN that stays
-    have = float2{top, have.y * exp_down<true>(have.x - top) + v.y * exp_down<true>(v.x - top)};
+    have = float2{top, have.y * exp_down(have.x - top) + v.y * exp_down(v.x - top)};
 }
 
 // The statistics of a tile: per wave and row, then joined over the WN waves that share rows.  z: the logits too (few rows), or null.
@@ -111,7 +103,7 @@ template <bool EXACT, int BM, int BN, int WN> struct Statistics {
 #pragma unroll
                 for (int j = 0; j < TN; ++j)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) sum += exp_down<EXACT>(v[j][e] - base);
+                    for (int e = 0; e < 16; ++e) sum += exp_down(v[j][e] - base);
             } else {
 #pragma unroll
                 for (int j = 0; j < TN; ++j)
@@ -164,9 +156,9 @@ __global__ __launch_bounds__(256) void row_loss_kernel(const float2* part, const
 #pragma unroll
             for (int u = 0; u < U; ++u) top = fmaxf(top, v[u].x);
             const float base = top == -INFINITY ? 0.f : top;
-            have.y *= exp_down<true>(have.x - base);
+            have.y *= exp_down(have.x - base);
 #pragma unroll
-            for (int u = 0; u < U; ++u) have.y += v[u].y * exp_down<true>(v[u].x - base);
+            for (int u = 0; u < U; ++u) have.y += v[u].y * exp_down(v[u].x - base);
             have.x = top;                                      // all -inf so far: the sums are zeros, or NaNs that stay
         }
     got[threadIdx.x] = have;
@@ -205,37 +197,41 @@ __global__ __launch_bounds__(256) void mean_loss_kernel(const float* row_loss, c
     mean_of_rows(sum, count, sums, counts, loss + blockIdx.x, factor + blockIdx.x);
 }
 
-// Few rows: G of the whole vocabulary from its logits, a column a thread, and db.  32-bit G takes the logits' place.
-template <bool EXACT, typename T>
+// Few rows: G of the whole vocabulary from its logits, 64 columns a workgroup, every fourth row a wave, and db.  32-bit G takes the
+// logits' place.
+template <typename T>
 __global__ __launch_bounds__(256) void gradient_columns_kernel(const float* z, const int32_t* labels, const float2* norm, int rows, int classes, int ld,
                                                                T* g, const float* factor, float* db, long long db_rep)
 {
-    const int c = blockIdx.x * 256 + threadIdx.x, k = blockIdx.y;
-    if (c >= ld) return;
     constexpr int U = 8;                                       // rows at a time: their loads before the first store, which may be theirs
+    __shared__ float sums[4][64];
+    const int wave = threadIdx.x >> 6, c = blockIdx.x * 64 + (threadIdx.x & 63), k = blockIdx.y;
     const long long first = (long long)k * rows;
     float sum = 0.f;
-    for (int t0 = 0; t0 < rows; t0 += U) {
+    for (int t0 = wave; t0 < rows; t0 += 4 * U) {
         float v[U];
         float2 l[U];
         int y[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const long long t = first + min(t0 + u, rows - 1);
+            const long long t = first + min(t0 + 4 * u, rows - 1);
             v[u] = z[t * ld + c];
             l[u] = norm[t];
             y[u] = labels[t];
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (t0 + u >= rows) break;
+            if (t0 + 4 * u >= rows) break;
             const bool live = (unsigned)y[u] < (unsigned)classes;
-            const float p = live && c < classes ? exp_down<EXACT>(v[u] - l[u].x) * (1.f / l[u].y) - (c == y[u] ? 1.f : 0.f) : 0.f;
+            const float p = live && c < classes ? exp_down(v[u] - l[u].x) * (1.f / l[u].y) - (c == y[u] ? 1.f : 0.f) : 0.f;
             sum += p;
-            g[(first + t0 + u) * ld + c] = (T)p;
+            g[(first + t0 + 4 * u) * ld + c] = (T)p;
         }
     }
-    if (db && c < classes) db[k * db_rep + c] = sum * factor[k];
+    if (!db) return;
+    sums[wave][threadIdx.x & 63] = sum;
+    __syncthreads();
+    if (wave == 0 && c < classes) db[k * db_rep + c] = ((sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x])) * factor[k];
 }
 
 // G of a piece, unscaled, and its column sums over a wave's rows
@@ -259,7 +255,7 @@ template <bool EXACT> struct Softmax {
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) v[j][e] = live ? exp_down<EXACT>(v[j][e] - l.x) * inv : 0.f;
+                for (int e = 0; e < 16; ++e) v[j][e] = live ? exp_down(v[j][e] - l.x) * inv : 0.f;
         } else {
             const float shift = -l.x * kLog2e - __builtin_amdgcn_logf(l.y);
 #pragma unroll
@@ -368,32 +364,33 @@ __global__ __launch_bounds__(256) void bias_grad_kernel(const float* sums, int b
 }
 
 // Which kernels, the piece of the vocabulary and the working memory, from the sizes alone.
-//   few rows (at most 64)   the products through registers read W as it is, 32 x 128 or 128 x 128 tiles: W is read once or twice
-//                           per pass, laying it out first would cost as much again
+//   few rows (at most 64)   the products through registers read W as it is, 32 or 64 x 128 tiles: W is read once per pass, laying
+//                           it out first would cost as much again
 //   more                    products straight from memory to LDS; x (unlabelled rows as zeros) and a W of 32-bit or unaligned values are
 //                           laid out first
 struct Plan {
     bool direct, small;            // small: 32 or (direct) 128 rows a tile
-    int bm, wave_m, parts, piece, pieces, blocks, splits, split_len, ldx, planes;
+    int bm, wave_m, parts, z_splits, z_len, piece, pieces, blocks, splits, split_len, ldx, planes;
     size_t norm, z_label, row_loss, factor, part, g, z, sums, share, x, w, top, total;
 };
 constexpr long long kPieceBytes = 256ll << 20;       // of G, and of a laid-out piece of W
+constexpr long long kSharedW = 48ll << 20;
 
 int up_to(long long v, int unit) { return (int)((v + unit - 1) / unit * unit); }
 
 Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
 {
     Plan p{};
-    p.direct = rows > 64;
+    p.direct = rows > 64 || (rows && std::min(features, classes) < 8);
     p.small = p.direct ? rows <= 128 : rows <= 32;
-    p.bm = p.direct ? (p.small ? 128 : 256) : p.small ? 32 : 128;
+    p.bm = p.direct ? (p.small ? 128 : 256) : p.small ? 32 : 64;
     const int bn = p.direct ? 256 : 128;
-    p.wave_m = p.direct ? p.bm / 2 : p.small ? 32 : 64;
+    p.wave_m = p.direct ? p.bm / 2 : 32;
     p.planes = p.direct && !bf16 ? 2 : 1;
     p.parts = up_to(classes, bn) / bn;
     p.blocks = up_to(rows, p.bm) / p.wave_m;
     const long long lines = (long long)n * rows, es = p.direct ? (bf16 ? 2 : 4) : bf16 ? 6 : 4;      // of G and, few rows, the logits
-    long long most = grad ? kPieceBytes / std::max<long long>(1, lines * es) : classes;
+    long long most = grad ? kPieceBytes / std::max<long long>(1, lines * es) : up_to(classes, bn);
     if (p.direct) most = std::min(most, kPieceBytes / ((long long)n * features * 2 * p.planes));
     most = std::max<long long>(1024, most / bn * bn);
     p.pieces = (int)((classes + most - 1) / most);
@@ -405,6 +402,13 @@ Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
     p.splits = (int)std::max<long long>(1, std::min<long long>((p.direct ? 256 : 512) / std::max<long long>(1, tiles), p.piece / (p.direct ? 512 : 128)));
     p.split_len = up_to((p.piece + p.splits - 1) / p.splits, 128);
     p.splits = (p.piece + p.split_len - 1) / p.split_len;
+    // few rows, a large W in one piece: its contraction in shares of at least 128 features, for some 4096 workgroups
+    p.z_splits = 1;
+    const long long w_tiles = (long long)n * p.parts;
+    if (!p.direct && p.pieces == 1 && (long long)n * features * classes * (bf16 ? 2 : 4) >= kSharedW)
+        p.z_splits = (int)std::max<long long>(1, std::min<long long>(4096 / w_tiles, features / 128));
+    p.z_len = up_to((features + p.z_splits - 1) / p.z_splits, 128);
+    p.z_splits = (features + p.z_len - 1) / p.z_len;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += align256(bytes); return o; };
     p.norm = take((size_t)lines * 8);
@@ -417,9 +421,10 @@ Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
         p.w = take((size_t)n * features * p.piece * 2 * p.planes);
         p.top = take((size_t)n * 8);
     }
+    if (!p.direct && (p.z_splits > 1 || grad) && (bf16 || !grad)) p.z = take((size_t)lines * p.piece * 4 * p.z_splits);
     if (grad) {
-        p.g = take((size_t)lines * p.piece * (p.direct ? es : bf16 ? 2 : 4));
-        p.z = !p.direct && bf16 ? take((size_t)lines * p.piece * 4) : p.g;
+        p.g = take((size_t)lines * p.piece * (p.direct ? es : bf16 ? 2 : 4 * p.z_splits));
+        if (!p.direct && !bf16) p.z = p.g;                // 32-bit G takes the logits' place
         p.sums = take((size_t)n * p.blocks * p.piece * 4);
         p.share = take((size_t)p.splits * lines * p.ldx * 4);
     }
@@ -481,11 +486,15 @@ template <typename T, int BM, int WM, int WN> hipError_t run_general(const LossA
     hipError_t e = hipSuccess;
     const Source<T> x = source<T>(a.x, a.rows, a.features);
     const float* bias = (const float*)a.bias.p;
-    if (a.rows) {
+    if (a.rows && p.z_splits > 1) {
+        const StoreShare<> store{k.z, a.rows, a.classes, p.piece, a.rows, a.n, false, false};
+        e = launch_product<BM, 128, WM, WN, true, false>(x, source<T>(a.w, a.features, a.classes), a.n, a.rows, a.classes, a.features, p.z_splits, p.z_len, store, s);
+        if (e == hipSuccess) e = launch_join_logits(a, k.z, p.z_splits, p.piece, k.part, k.z_label, s);
+    } else if (a.rows) {
         const Statistics<exact, BM, 128, WN> stats{bias, a.bias.rep, a.labels, k.part, k.z_label, once ? k.z : nullptr, a.rows, 0, a.classes, p.parts, p.piece};
         e = launch_product<BM, 128, WM, WN, true, false>(x, source<T>(a.w, a.features, a.classes), a.n, a.rows, a.classes, a.features, 1, a.features, stats, s);
-        if (e != hipSuccess) return e;
     }
+    if (e != hipSuccess) return e;
     if ((e = join_rows(a, p, k, s)) != hipSuccess || !a.grad) return e;
     const Labelled live{a.labels, a.classes};
     for (int i = 0; i < p.pieces; ++i) {
@@ -493,7 +502,7 @@ template <typename T, int BM, int WM, int WN> hipError_t run_general(const LossA
         const Source<T> w = source<T>(Rows{(T*)a.w.p + c0, a.w.rep, a.w.row}, a.features, cols);
         const Source<T> g = source<T>(Rows{k.g, (long long)a.rows * ld, ld}, a.rows, ld);            // zero beyond cols
         if (once) {
-            gradient_columns_kernel<exact, T><<<dim3((unsigned)((ld + 255) / 256), (unsigned)a.n), 256, 0, s>>>(
+            gradient_columns_kernel<T><<<dim3((unsigned)(ld / 64), (unsigned)a.n), 256, 0, s>>>(
                 k.z, a.labels, k.norm, a.rows, a.classes, ld, (T*)k.g, k.factor, (float*)a.db.p, a.db.rep);
             e = hipGetLastError();
         } else if (a.rows) {
@@ -507,9 +516,11 @@ template <typename T, int BM, int WM, int WN> hipError_t run_general(const LossA
             e = launch_product<BM, 128, WM, WN, true, true>(g, w, a.n, a.rows, a.features, cols, p.splits, p.split_len, store, s);
             if (e != hipSuccess) return e;
         }
-        if (a.dw.p) {
+        if (a.dw.p && once && a.rows && a.rows <= 16 && a.classes >= 4) {
+            if ((e = launch_few_weights<T>(a, (const T*)k.g, ld, k.factor, s)) != hipSuccess) return e;
+        } else if (a.dw.p) {
             const StoreTile<T> store{(T*)a.dw.p + c0, a.dw.rep, a.dw.row, k.factor, a.features, cols, nullptr, 0};
-            e = launch_product<64, 64, 2, 2, false, false>(source<T>(a.x, a.rows, a.features, live), g, a.n, a.features, cols, a.rows, 1,
+            e = launch_product<64, 64, 2, 2, false, false>(source<T, true>(a.x, a.rows, a.features, live), g, a.n, a.features, cols, a.rows, 1,
                                                              std::max(1, a.rows), store, s);
             if (e != hipSuccess) return e;
         }
@@ -596,8 +607,8 @@ hipError_t launch_loss(const LossArgs& a, hipStream_t s)
         if (a.bf16) return p.small ? run_direct<__bf16, 128>(a, p, s) : run_direct<__bf16, 256>(a, p, s);
         return p.small ? run_direct<float, 128>(a, p, s) : run_direct<float, 256>(a, p, s);
     }
-    if (a.bf16) return p.small ? run_general<__bf16, 32, 1, 4>(a, p, s) : run_general<__bf16, 128, 2, 2>(a, p, s);
-    return p.small ? run_general<float, 32, 1, 4>(a, p, s) : run_general<float, 128, 2, 2>(a, p, s);
+    if (a.bf16) return p.small ? run_general<__bf16, 32, 1, 4>(a, p, s) : run_general<__bf16, 64, 2, 2>(a, p, s);
+    return p.small ? run_general<float, 32, 1, 4>(a, p, s) : run_general<float, 64, 2, 2>(a, p, s);
 }
 
 }  // namespace head

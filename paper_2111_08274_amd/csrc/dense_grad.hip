@@ -20,7 +20,7 @@ struct Plan {
 Plan plan_of(int n, int rows, int in, int out, int bf16)
 {
     Plan p{};
-    p.direct = rows >= 256 && in >= 96 && out >= 96;
+    p.direct = (rows >= 256 && in >= 96 && out >= 96) || (rows && out < 8);     // the other way takes rows of eight values at least
     auto tiles = [&](int t) { return (long long)n * ((in + t - 1) / t) * ((out + t - 1) / t); };
     p.big = tiles(256) >= 192;
     p.ldx = (in + 7) / 8 * 8;

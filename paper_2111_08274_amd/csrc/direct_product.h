@@ -306,7 +306,7 @@ __global__ __launch_bounds__(256) void lay_out_kernel(const T* x, long long rep,
     chunk.load(x + k * rep + t * row + c, live.at(t) ? cols - c : 0);
     u4 part[PL];
     if constexpr (PL == 1) part[0] = chunk.a;
-    else if constexpr (PL == 3) Source<float>::planes(chunk, part);
+    else if constexpr (PL == 3) Source<float>::split(chunk, part);
     else {
         const float scale = up_scale(top[k]);
         u2 h[2], l[2];

@@ -75,6 +75,11 @@ struct LossArgs {
 };
 size_t loss_work_bytes(int n, int rows, int features, int classes, int bf16, bool grad);
 hipError_t launch_loss(const LossArgs& a, hipStream_t s);
+// few rows: logits [replicas][rows][ld], ld a multiple of 128, from the shares of their contraction (into the first one's place), their
+// statistics per 128 classes (part [replicas][tiles][rows]: the largest logit and the sum of exp of the distances to it), the labels' logits
+hipError_t launch_join_logits(const LossArgs& a, float* share, int splits, int ld, float2* part, float* z_label, hipStream_t s);
+// dW from G [replicas][rows][ld], at most 16 rows, at least four classes
+template <typename T> hipError_t launch_few_weights(const LossArgs& a, const T* g, int ld, const float* factor, hipStream_t s);
 
 // ---- device pieces ------------------------------------------------------------------------------------------------
 __device__ __forceinline__ float up(__bf16 v) { return (float)v; }
@@ -82,6 +87,9 @@ __device__ __forceinline__ float up(float v) { return v; }
 // Eight consecutive values of a row, as they are in memory.  Vector accesses need no alignment of their own on this chip (a chunk
 // across a line's end is two accesses), so rows of any stride are read 16 bytes a lane; only a row's last chunk may hold fewer values.
 typedef unsigned int u4any __attribute__((ext_vector_type(4), aligned(2)));
+// said to be in global memory: a pointer chosen between two would else be loaded through the path that also serves LDS, whose loads are
+// only waited for all together
+__device__ __forceinline__ tiles::u4 load16(const void* p) { return *(const __attribute__((address_space(1))) u4any*)(unsigned long long)p; }
 template <typename T> struct Chunk;
 // keeps a short chunk's eight comparisons where they are used: hoisted out of a loop over rows they would fill the scalar registers
 __device__ __forceinline__ int here(int left) { asm volatile("" : "+v"(left)); return left; }
@@ -89,7 +97,7 @@ template <> struct Chunk<float> {
     tiles::u4 a, b;
     __device__ __forceinline__ void load(const float* p, int left)
     {
-        if (left >= 8) { a = *(const u4any*)p; b = *(const u4any*)(p + 4); return; }
+        if (left >= 8) { a = load16(p); b = load16(p + 4); return; }
         a = b = tiles::u4{0, 0, 0, 0};
         const unsigned* w = (const unsigned*)p;
         left = here(left);
@@ -108,7 +116,7 @@ template <> struct Chunk<__bf16> {
     tiles::u4 a;
     __device__ __forceinline__ void load(const __bf16* p, int left)
     {
-        if (left >= 8) { a = *(const u4any*)p; return; }
+        if (left >= 8) { a = load16(p); return; }
         a = tiles::u4{0, 0, 0, 0};
         const unsigned short* w = (const unsigned short*)p;
         left = here(left);

@@ -4,7 +4,7 @@
 // An operand is a source of chunks of eight consecutive values; "along" says whether the contraction runs along a source's
 // rows (chunk = eight k of one m) or across them (chunk = eight m of one k).  Chunks go through registers, where what lies
 // outside becomes zero and floats become three bf16 planes, to LDS as they are; an operand across its rows is transposed by
-// the LDS read.  One slab of the contraction is in flight in registers while the one before is multiplied.
+// the LDS read.  One or two slabs of the contraction are in flight in registers while the one before is multiplied.
 #pragma once
 #include "head.h"
 
@@ -36,25 +36,53 @@ __device__ __forceinline__ void parts3(const f4& x, u2& h, u2& m, u2& l)
     }
 }
 
-template <typename T> struct Source {
+// A row's last chunk, of fewer than eight values, is loaded as the row's last eight and moved down when it is used; what lies outside
+// is loaded from the source's beginning and taken as zero.  So no load of a slab has a branch before it.  Rows hold eight values at least.
+__device__ __forceinline__ void move_down(Chunk<float>& v, int by)
+{
+    u4 a = v.a, b = v.b;
+    const u4 none{0, 0, 0, 0};
+    if (by & 4) { a = b; b = none; }
+    if (by & 2) { a = u4{a[2], a[3], b[0], b[1]}; b = u4{b[2], b[3], 0, 0}; }
+    if (by & 1) { a = u4{a[1], a[2], a[3], b[0]}; b = u4{b[1], b[2], b[3], 0}; }
+    v.a = a; v.b = b;
+}
+__device__ __forceinline__ void move_down(Chunk<__bf16>& v, int by)
+{
+    u4 a = v.a;
+    if (by & 4) a = u4{a[2], a[3], 0, 0};
+    if (by & 2) a = u4{a[1], a[2], a[3], 0};
+    if (by & 1) a = u4{a[0] >> 16 | a[1] << 16, a[1] >> 16 | a[2] << 16, a[2] >> 16 | a[3] << 16, a[3] >> 16};
+    v.a = a;
+}
+template <typename T, bool LABELLED = false> struct Source {
     static constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;
-    typedef Chunk<T> Raw;
+    struct Raw { Chunk<T> v; int label; bool in; };
     const T* p;
     long long rep, row;
     int rows, cols;
     Labelled live;
-    __device__ __forceinline__ void bind(int k) { p += k * rep; if (live.labels) live.labels += (long long)k * rows; }
-    // INSIDE: the caller knows that the chunk lies within the source
-    template <bool INSIDE> __device__ __forceinline__ Raw load(int r, int c) const
+    __device__ __forceinline__ void bind(int k) { p += k * rep; if (LABELLED) live.labels += (long long)k * rows; }
+    __device__ __forceinline__ Raw load(int r, int c) const
     {
         Raw v;
-        if (INSIDE) v.load(p + r * row + c, 8);
-        else v.load(p + r * row + c, r < rows && live.at(r) ? cols - c : 0);
+        v.in = r < rows && c < cols;
+        v.label = LABELLED ? live.labels[min(r, rows - 1)] : 0;
+        v.v.load(p + (v.in ? r * row + min(c, cols - 8) : 0ll), 8);
         return v;
     }
-    __device__ __forceinline__ bool inside(int r_end, int c_end) const { return r_end <= rows && c_end <= cols && !live.labels; }
-    static __device__ __forceinline__ void planes(const Chunk<__bf16>& v, u4 (&out)[1]) { out[0] = v.a; }
-    static __device__ __forceinline__ void planes(const Chunk<float>& v, u4 (&out)[3])
+    // the chunk at column c, some chunk of its slab reaching beyond the row or not
+    __device__ __forceinline__ bool has_tail(int c_begin, int c_end) const { return (cols & 7) && c_begin < cols && c_end > cols; }
+    __device__ __forceinline__ void planes(Raw v, int c, bool tail, u4 (&out)[kPlanes]) const
+    {
+        if (tail) move_down(v.v, min(max(c + 8 - cols, 0), 7));
+        split(v.v, out);
+        const bool on = v.in && (!LABELLED || (unsigned)v.label < (unsigned)live.classes);
+#pragma unroll
+        for (int s = 0; s < kPlanes; ++s) out[s] = on ? out[s] : u4{0, 0, 0, 0};
+    }
+    static __device__ __forceinline__ void split(const Chunk<__bf16>& v, u4 (&out)[1]) { out[0] = v.a; }
+    static __device__ __forceinline__ void split(const Chunk<float>& v, u4 (&out)[3])
     {
         u2 h[2], m[2], l[2];
         parts3(__builtin_bit_cast(f4, v.a), h[0], m[0], l[0]);
@@ -62,14 +90,14 @@ template <typename T> struct Source {
         out[0] = join8(h[0], h[1]); out[1] = join8(m[0], m[1]); out[2] = join8(l[0], l[1]);
     }
 };
-template <typename T> Source<T> source(const Rows& r, int rows, int cols, Labelled live = {nullptr, 0})
+template <typename T, bool LABELLED = false> Source<T, LABELLED> source(const Rows& r, int rows, int cols, Labelled live = {nullptr, 0})
 {
-    return Source<T>{(const T*)r.p, r.rep, r.row, rows, cols, live};
+    return Source<T, LABELLED>{(const T*)r.p, r.rep, r.row, rows, cols, live};
 }
 
 struct SourcePacked {              // rows and columns of one replica; the surplus columns of the checkpoint are zero
     static constexpr int kPlanes = 1;
-    struct Raw { u2 q; unsigned e; };
+    struct Raw { u2 q; unsigned e; bool in; };
     Packed p;
     int rows, cols;
     __device__ __forceinline__ void bind(int k)
@@ -77,23 +105,24 @@ struct SourcePacked {              // rows and columns of one replica; the surpl
         p.q += (long long)k * rows * p.cols;
         p.e += (long long)k * rows * (p.cols / kGroup);
     }
-    __device__ __forceinline__ bool inside(int r_end, int c_end) const { return r_end <= rows && c_end <= p.cols; }
-    template <bool INSIDE> __device__ __forceinline__ Raw load(int r, int c) const
+    __device__ __forceinline__ bool has_tail(int, int) const { return false; }
+    __device__ __forceinline__ Raw load(int r, int c) const
     {
-        Raw v = {};
-        if (!INSIDE && (r >= rows || c >= p.cols)) return v;
-        v.q = *(const u2*)(p.q + r * p.cols + c);
-        v.e = p.e[r * (p.cols / kGroup) + c / kGroup];
+        Raw v;
+        v.in = r < rows && c < p.cols;
+        const long long at = v.in ? r * p.cols + c : 0;
+        v.q = *(const u2*)(p.q + at);
+        v.e = p.e[at / kGroup];
         return v;
     }
-    static __device__ __forceinline__ void planes(const Raw& v, u4 (&out)[1])
+    __device__ __forceinline__ void planes(const Raw& v, int, bool, u4 (&out)[1]) const
     {
         const float unit = group_unit(v.e);                    // q * 2^e has eight significant bits: exact in bf16
         float f[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] = (float)(int)(int8_t)(v.q[e / 4] >> (8 * (e % 4))) * unit;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) out[0][e] = to_bf16x2(f[2 * e], f[2 * e + 1]);
+        for (int e = 0; e < 4; ++e) out[0][e] = v.in ? to_bf16x2(f[2 * e], f[2 * e + 1]) : 0u;
     }
 };
 
@@ -135,9 +164,7 @@ __device__ __forceinline__ bf16x8 ones()
     return __builtin_bit_cast(bf16x8, (u4{one2, one2, one2, one2}));
 }
 
-template <bool B> struct Yes { static constexpr bool value = B; };
-
-template <class SA, bool A_ALONG, class SB, bool B_ALONG, int BM, int BN, int WM, int WN, int KS, int NBUF, class Epi>
+template <class SA, bool A_ALONG, class SB, bool B_ALONG, int BM, int BN, int WM, int WN, int KS, int NBUF, int AHEAD, class Epi>
 __global__ __launch_bounds__(WM * WN * 64) void product_kernel(SA a, SB b, int K, int tiles_m, int tiles_n, int splits, int split_len,
                                                                int total, Epi epi)
 {
@@ -173,36 +200,28 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(SA a, SB b, int K
     }
     const bool sums = has_sum(epi, t.m0);
 
-    typename SA::Raw ra[NA];
-    typename SB::Raw rb[NB];
-    auto fetch = [&](int k0) {
-        auto all_a = [&](auto inside) {
+    typename SA::Raw ra[AHEAD][NA];
+    typename SB::Raw rb[AHEAD][NB];
+    auto fetch = [&](int k0, int slot) {
 #pragma unroll
-            for (int i = 0; i < NA; ++i) {
-                const int id = tid + i * NT, r = id / IA::kAcross, c = id % IA::kAcross * 8;
-                if (IA::kChunks % NT == 0 || id < IA::kChunks)
-                    ra[i] = A_ALONG ? a.template load<decltype(inside)::value>(bm + r, k0 + c) : a.template load<decltype(inside)::value>(k0 + r, bm + c);
-            }
-        };
-        auto all_b = [&](auto inside) {
+        for (int i = 0; i < NB; ++i) {
+            const int id = tid + i * NT, r = id / IB::kAcross, c = id % IB::kAcross * 8;
+            if (IB::kChunks % NT == 0 || id < IB::kChunks) rb[slot][i] = B_ALONG ? b.load(bn + r, k0 + c) : b.load(k0 + r, bn + c);
+        }
 #pragma unroll
-            for (int i = 0; i < NB; ++i) {
-                const int id = tid + i * NT, r = id / IB::kAcross, c = id % IB::kAcross * 8;
-                if (IB::kChunks % NT == 0 || id < IB::kChunks)
-                    rb[i] = B_ALONG ? b.template load<decltype(inside)::value>(bn + r, k0 + c) : b.template load<decltype(inside)::value>(k0 + r, bn + c);
-            }
-        };
-        // most slabs lie inside: loads without a comparison each, all on their way at once
-        if (B_ALONG ? b.inside(bn + BN, k0 + KS) : b.inside(k0 + KS, bn + BN)) all_b(Yes<true>{}); else all_b(Yes<false>{});
-        if (A_ALONG ? a.inside(bm + BM, k0 + KS) : a.inside(k0 + KS, bm + BM)) all_a(Yes<true>{}); else all_a(Yes<false>{});
+        for (int i = 0; i < NA; ++i) {
+            const int id = tid + i * NT, r = id / IA::kAcross, c = id % IA::kAcross * 8;
+            if (IA::kChunks % NT == 0 || id < IA::kChunks) ra[slot][i] = A_ALONG ? a.load(bm + r, k0 + c) : a.load(k0 + r, bm + c);
+        }
     };
-    auto store = [&](char* buf) {
+    auto store = [&](char* buf, int slot, int k0) {
+        const bool tail_a = A_ALONG ? a.has_tail(k0, k0 + KS) : a.has_tail(bm, bm + BM), tail_b = B_ALONG ? b.has_tail(k0, k0 + KS) : b.has_tail(bn, bn + BN);
 #pragma unroll
         for (int i = 0; i < NA; ++i) {
             const int id = tid + i * NT, r = id / IA::kAcross, c = id % IA::kAcross;
             if (IA::kChunks % NT == 0 || id < IA::kChunks) {
                 u4 p[PA];
-                SA::planes(ra[i], p);
+                a.planes(ra[slot][i], (A_ALONG ? k0 : bm) + c * 8, tail_a, p);
 #pragma unroll
                 for (int s = 0; s < PA; ++s) *(u4*)(buf + s * IA::kPlane + r * IA::kPitch + c * 16) = p[s];
             }
@@ -212,7 +231,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(SA a, SB b, int K
             const int id = tid + i * NT, r = id / IB::kAcross, c = id % IB::kAcross;
             if (IB::kChunks % NT == 0 || id < IB::kChunks) {
                 u4 p[PB];
-                SB::planes(rb[i], p);
+                b.planes(rb[slot][i], (B_ALONG ? k0 : bn) + c * 8, tail_b, p);
 #pragma unroll
                 for (int s = 0; s < PB; ++s) *(u4*)(buf + PA * IA::kPlane + s * IB::kPlane + r * IB::kPitch + c * 16) = p[s];
             }
@@ -252,14 +271,22 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(SA a, SB b, int K
         }
     };
 
-    if (k_begin < k_end) fetch(k_begin);
-    for (int k0 = k_begin, n = 0; k0 < k_end; k0 += KS, ++n) {
-        char* buf = smem + (NBUF == 2 ? (n & 1) * kBuf : 0);
-        if (NBUF == 1 && n) __syncthreads();                   // the slab before has been read
-        store(buf);
-        __syncthreads();
-        if (k0 + KS < k_end) fetch(k0 + KS);
-        multiply(buf);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (k_begin + i * KS < k_end) fetch(k_begin + i * KS, i);
+    constexpr int TURNS = AHEAD * NBUF;
+    for (int k0 = k_begin; k0 < k_end; k0 += TURNS * KS) {
+#pragma unroll
+        for (int u = 0; u < TURNS; ++u) {
+            const int k = k0 + u * KS;
+            if (k >= k_end) break;
+            char* buf = smem + u % NBUF * kBuf;
+            if (NBUF == 1 && k > k_begin) __syncthreads();     // the slab before has been read
+            store(buf, u % AHEAD, k);
+            __syncthreads();
+            if (k + AHEAD * KS < k_end) fetch(k + AHEAD * KS, u % AHEAD);
+            multiply(buf);
+        }
     }
     if constexpr (Epi::kStaged) {
         __syncthreads();
@@ -392,12 +419,12 @@ hipError_t launch_product(const SA& a, const SB& b, int replicas, int M, int N, 
 {
     constexpr bool wide = SA::kPlanes == 3 || SB::kPlanes == 3;
     // few rows: memory bound, so more of W on its way at a time and one image, for more workgroups on a compute unit
-    constexpr int KS = BM == 32 ? (wide ? 64 : 128) : 32, NBUF = wide || BM == 32 ? 1 : 2;
+    constexpr int KS = BM == 32 ? (wide ? 64 : 128) : 32, NBUF = wide || BM == 32 ? 1 : 2, AHEAD = BM == 32 ? 2 : 1;
     const int tm = (M + BM - 1) / BM, tn = (N + BN - 1) / BN;
     const long long total = (long long)replicas * splits * tm * tn;
     if (total == 0) return hipSuccess;
     if (total > 0x7fffff00ll) return hipErrorInvalidValue;
-    product_kernel<SA, A_ALONG, SB, B_ALONG, BM, BN, WM, WN, KS, NBUF, Epi>
+    product_kernel<SA, A_ALONG, SB, B_ALONG, BM, BN, WM, WN, KS, NBUF, AHEAD, Epi>
         <<<die_grid(total), WM * WN * 64, 0, s>>>(a, b, K, tm, tn, splits, split_len, (int)total, epi);
     return hipGetLastError();
 }
