@@ -370,8 +370,8 @@ __global__ __launch_bounds__(256) void bias_grad_kernel(const float* sums, int b
 //                           laid out first
 struct Plan {
     bool direct, small;            // small: 32 or (direct) 128 rows a tile
-    int bm, wave_m, parts, z_splits, z_len, piece, pieces, blocks, splits, split_len, ldx, planes;
-    size_t norm, z_label, row_loss, factor, part, g, z, sums, share, x, w, top, total;
+    int bm, wave_m, parts, z_splits, z_len, piece, pieces, blocks, splits, split_len, w_splits, w_len, ldx, planes;
+    size_t norm, z_label, row_loss, factor, part, g, z, sums, share, w_share, x, w, top, total;
 };
 constexpr long long kPieceBytes = 256ll << 20;       // of G, and of a laid-out piece of W
 constexpr long long kSharedW = 48ll << 20;
@@ -382,7 +382,8 @@ Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
 {
     Plan p{};
     p.direct = rows > 64 || (rows && std::min(features, classes) < 8);
-    p.small = p.direct ? rows <= 128 : rows <= 32;
+    // 128 rows a tile also where 256 would leave half of the chip without a tile
+    p.small = p.direct ? rows <= 128 || (long long)n * ((rows + 255) / 256) * ((classes + 255) / 256) < 128 : rows <= 32;
     p.bm = p.direct ? (p.small ? 128 : 256) : p.small ? 32 : 64;
     const int bn = p.direct ? 256 : 128;
     p.wave_m = p.direct ? p.bm / 2 : 32;
@@ -402,6 +403,11 @@ Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
     p.splits = (int)std::max<long long>(1, std::min<long long>((p.direct ? 256 : 512) / std::max<long long>(1, tiles), p.piece / (p.direct ? 512 : 128)));
     p.split_len = up_to((p.piece + p.splits - 1) / p.splits, 128);
     p.splits = (p.piece + p.split_len - 1) / p.split_len;
+    // dW of a piece with fewer tiles than compute units: the rows in shares of at least 256
+    const long long dw_tiles = (long long)n * ((features + 255) / 256) * (p.piece / 256);
+    p.w_splits = p.direct ? (int)std::max<long long>(1, std::min<long long>(256 / std::max<long long>(1, dw_tiles), rows / 256)) : 1;
+    p.w_len = up_to((rows + p.w_splits - 1) / p.w_splits, 64);
+    if (rows) p.w_splits = (rows + p.w_len - 1) / p.w_len;
     // few rows, a large W in one piece: its contraction in shares of at least 128 features, for some 4096 workgroups
     p.z_splits = 1;
     const long long w_tiles = (long long)n * p.parts;
@@ -427,6 +433,7 @@ Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
         if (!p.direct && !bf16) p.z = p.g;                // 32-bit G takes the logits' place
         p.sums = take((size_t)n * p.blocks * p.piece * 4);
         p.share = take((size_t)p.splits * lines * p.ldx * 4);
+        if (p.w_splits > 1) p.w_share = take((size_t)p.w_splits * n * features * p.piece * 4);
     }
     p.total = at;
     return p;
@@ -434,7 +441,7 @@ Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
 
 // the pointers into the working memory
 struct Work {
-    float *z_label, *factor, *row_loss, *z, *sums, *share;
+    float *z_label, *factor, *row_loss, *z, *sums, *share, *w_share;
     float2 *norm, *part;
     char* g;
     __bf16 *x, *w;
@@ -444,7 +451,7 @@ struct Work {
         char* at = (char*)a.work;
         norm = (float2*)(at + p.norm); z_label = (float*)(at + p.z_label); factor = (float*)(at + p.factor);
         row_loss = a.row_loss ? a.row_loss : (float*)(at + p.row_loss);
-        sums = (float*)(at + p.sums); share = (float*)(at + p.share); part = (float2*)(at + p.part);
+        sums = (float*)(at + p.sums); share = (float*)(at + p.share); w_share = (float*)(at + p.w_share); part = (float2*)(at + p.part);
         g = at + p.g; z = (float*)(at + p.z); x = (__bf16*)(at + p.x); w = (__bf16*)(at + p.w); top = (unsigned*)(at + p.top);
     }
 };
@@ -528,6 +535,13 @@ template <typename T, int BM, int WM, int WN> hipError_t run_general(const LossA
     return input_grad<T>(a, p, k, s);
 }
 
+template <typename T, int PL, class Store>
+hipError_t weight_grad(const Plane3& x, const Plane3& g, const LossArgs& a, int cols, const Plan& p, const Store& store, hipStream_t s)
+{
+    if (a.features <= 128) return launch_direct<PL, PL, 128, 256, 2, 4, false, false>(x, g, a.n, a.features, cols, a.rows, p.w_splits, p.w_len, store, s);
+    return launch_direct<PL, PL, 256, 256, 2, 4, false, false>(x, g, a.n, a.features, cols, a.rows, p.w_splits, p.w_len, store, s);
+}
+
 // more rows: operands straight from memory to LDS
 template <typename T, int BM> hipError_t run_direct(const LossArgs& a, const Plan& p, hipStream_t s)
 {
@@ -574,18 +588,17 @@ template <typename T, int BM> hipError_t run_direct(const LossArgs& a, const Pla
         if (e != hipSuccess) return e;
         if (a.dx.p) {
             const StoreShare<> store{k.share, a.rows, a.features, p.ldx, a.rows, a.n, i > 0, false};
-            e = launch_direct<PL, PL, BM, 256, 2, 4, true, true>(g, w, a.n, a.rows, a.features, w.cols, p.splits, p.split_len, store, s);
+            if (a.features <= 128) e = launch_direct<PL, PL, BM, 128, 4, 2, true, true>(g, w, a.n, a.rows, a.features, w.cols, p.splits, p.split_len, store, s);
+            else e = launch_direct<PL, PL, BM, 256, 2, 4, true, true>(g, w, a.n, a.rows, a.features, w.cols, p.splits, p.split_len, store, s);
             if (e != hipSuccess) return e;
         }
         if (a.dw.p) {
-            if (PL == 1) {
-                const Rows out{(__bf16*)a.dw.p + c0, a.dw.rep, a.dw.row};
-                const StoreRows store{(__bf16*)out.p, out.rep, out.row, k.factor, a.features, cols};
-                e = launch_direct<PL, PL, 256, 256, 2, 4, false, false>(x, g, a.n, a.features, cols, a.rows, 1, a.rows, store, s);
-            } else {
-                const StoreTile<float> store{(float*)a.dw.p + c0, a.dw.rep, a.dw.row, k.factor, a.features, cols, nullptr, 0};
-                e = launch_direct<PL, PL, 256, 256, 2, 4, false, false>(x, g, a.n, a.features, cols, a.rows, 1, a.rows, store, s);
-            }
+            const Rows out{(T*)a.dw.p + c0, a.dw.rep, a.dw.row};
+            if (p.w_splits > 1) {
+                e = weight_grad<T, PL>(x, g, a, cols, p, StoreShare<>{k.w_share, a.features, cols, ld, a.features, a.n, false, false}, s);
+                if (e == hipSuccess) e = join_shares<T>(k.w_share, p.w_splits, a.n, a.features, cols, ld, Labelled{nullptr, 0}, k.factor, out, nullptr, 0, s);
+            } else if constexpr (PL == 1) e = weight_grad<T, PL>(x, g, a, cols, p, StoreRows{(__bf16*)out.p, out.rep, out.row, k.factor, a.features, cols}, s);
+            else e = weight_grad<T, PL>(x, g, a, cols, p, StoreTile<float>{(float*)out.p, out.rep, out.row, k.factor, a.features, cols, nullptr, 0}, s);
             if (e != hipSuccess) return e;
         }
         if ((e = bias_grad(a, p, k, ld, c0, cols, s)) != hipSuccess) return e;
