@@ -280,47 +280,53 @@ __global__ __launch_bounds__(256) void norm_columns_long_kernel(NormArgs a, floa
     out[a.cols + c] = sb;
 }
 
-// dgamma, dbeta: the partials of a replica in ascending order, eight shares of them side by side
-__global__ __launch_bounds__(256) void norm_sums_kernel(const float* partial, int parts, int cols, Rows dgamma, Rows dbeta)
+// dgamma, dbeta: the partials of a replica, S shares of them side by side, each in ascending order
+template <int S> __global__ __launch_bounds__(256) void norm_sums_kernel(const float* partial, int parts, int cols, Rows dgamma, Rows dbeta)
 {
-    __shared__ float share[8][32];
-    const int k = blockIdx.y, c = blockIdx.x * 32 + threadIdx.x % 32, w = threadIdx.x / 32;      // of both vectors, end to end
+    constexpr int C = 256 / S;
+    __shared__ float share[S][C];
+    const int k = blockIdx.y, c = blockIdx.x * C + threadIdx.x % C, w = threadIdx.x / C;         // of both vectors, end to end
     const float* src = partial + (long long)k * parts * 2 * cols + c;
     float v = 0.f;
     if (c < 2 * cols) {
 #pragma unroll 8
-        for (int p = w; p < parts; p += 8) v += src[(long long)p * 2 * cols];
+        for (int p = w; p < parts; p += S) v += src[(long long)p * 2 * cols];
     }
-    share[w][threadIdx.x % 32] = v;
+    share[w][threadIdx.x % C] = v;
     __syncthreads();
     if (w || c >= 2 * cols) return;
     v = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v += share[j][threadIdx.x];
+    for (int j = 0; j < S; ++j) v += share[j][threadIdx.x];
     if (c < cols) ((float*)dgamma.p)[k * dgamma.rep + c] = v;
     else ((float*)dbeta.p)[k * dbeta.rep + c - cols] = v;
 }
 
 constexpr int kLongest = 8192;     // columns that a workgroup keeps in registers
 
-int lanes_of(int cols) { return cols <= 128 ? 16 : cols <= 1024 ? 64 : 256; }
-int chunks_of(int cols) { const int per = lanes_of(cols) * 8; return (cols + per - 1) / per; }
+// Lanes of a row.  A wave per row needs no barrier; the backward pass, which holds seven rows' worth of registers, is faster with a workgroup
+// per row from 1024 columns on (4 x 4096 x 2048 bf16: 41 us against 52), the forward pass from 1536 (4 x 4096 x 1536 bf16: 17.5 against 25.7 the
+// other way).
+int lanes_of(int cols, bool backward) { return cols <= 128 ? 16 : cols <= (backward ? 1024 : 1536) ? 64 : 256; }
+int chunks_of(int cols, int lanes) { return (cols + lanes * 8 - 1) / (lanes * 8); }
 
-// workgroups per replica: enough to fill the chip four deep, each with whole rows
+// Workgroups per replica of the backward pass: four for every compute unit, two where their partials are long (2 x 4096 x 8192 bf16: 86 us
+// against 100; 4 x 4096 x 1536: 34 against 48 the other way), but fewer where a thread would not have four rows to add up, and then at
+// least one for every compute unit.
 int groups_of(int n, int rows, int cols)
 {
     if (cols > kLongest) return std::max(1, std::min((rows + 15) / 16, std::max(1, 4096 / (n * ((cols + 255) / 256)))));
-    const int rpb = 256 / lanes_of(cols);
-    return std::max(1, std::min((rows + rpb - 1) / rpb, std::max(1, 1024 / n)));
+    const int rpb = 256 / lanes_of(cols, true), all = (rows + rpb - 1) / rpb;
+    return std::max(1, std::min(all, std::max(256 / n, std::min((cols > 2048 ? 512 : 1024) / n, all / 4))));
 }
 
 template <typename T> hipError_t forward(const NormArgs& a, hipStream_t s)
 {
-    const int rpb = 256 / lanes_of(a.cols);
+    const int lanes = lanes_of(a.cols, false), rpb = 256 / lanes;
     const dim3 grid((unsigned)std::max(1, std::min((a.rows + rpb - 1) / rpb, std::max(1, 2048 / a.n))), (unsigned)a.n);
 #define HADFL_CASE(NL, CH) case NL * 8 + CH: norm_forward_kernel<T, NL, CH><<<grid, 256, 0, s>>>(a); break;
-    switch (lanes_of(a.cols) * 8 + chunks_of(a.cols)) {
-        HADFL_CASE(16, 1) HADFL_CASE(64, 1) HADFL_CASE(64, 2) HADFL_CASE(256, 1) HADFL_CASE(256, 2) HADFL_CASE(256, 3) HADFL_CASE(256, 4)
+    switch (lanes * 8 + chunks_of(a.cols, lanes)) {
+        HADFL_CASE(16, 1) HADFL_CASE(64, 1) HADFL_CASE(64, 2) HADFL_CASE(64, 3) HADFL_CASE(256, 1) HADFL_CASE(256, 2) HADFL_CASE(256, 3) HADFL_CASE(256, 4)
         default: return hipErrorInvalidValue;
     }
 #undef HADFL_CASE
@@ -330,7 +336,8 @@ template <typename T, bool KEPT> hipError_t backward(const NormArgs& a, float* p
 {
     const dim3 grid((unsigned)groups, (unsigned)a.n);
 #define HADFL_CASE(NL, CH) case NL * 8 + CH: norm_backward_kernel<T, KEPT, NL, CH><<<grid, 256, 0, s>>>(a, partial); break;
-    switch (lanes_of(a.cols) * 8 + chunks_of(a.cols)) {
+    const int lanes = lanes_of(a.cols, true);
+    switch (lanes * 8 + chunks_of(a.cols, lanes)) {
         HADFL_CASE(16, 1) HADFL_CASE(64, 1) HADFL_CASE(64, 2) HADFL_CASE(256, 1) HADFL_CASE(256, 2) HADFL_CASE(256, 3) HADFL_CASE(256, 4)
         default: return hipErrorInvalidValue;
     }
@@ -352,7 +359,12 @@ template <typename T, bool KEPT> hipError_t backward_any(const NormArgs& a, hipS
         e = backward<T, KEPT>(a, partial, groups, s);
         if (e != hipSuccess || groups == 1) return e;
     }
-    norm_sums_kernel<<<dim3((unsigned)((2 * a.cols + 31) / 32), (unsigned)a.n), 256, 0, s>>>(partial, groups, a.cols, a.dgamma, a.dbeta);
+    // whole lines of 32 columns, or half lines and twice the workgroups where those would not fill the chip (1 x 4096 x 768: 14 us for the
+    // backward pass against 21)
+    if ((long long)a.n * 2 * a.cols >= 256 * 32)
+        norm_sums_kernel<8><<<dim3((unsigned)((2 * a.cols + 31) / 32), (unsigned)a.n), 256, 0, s>>>(partial, groups, a.cols, a.dgamma, a.dbeta);
+    else
+        norm_sums_kernel<16><<<dim3((unsigned)((2 * a.cols + 15) / 16), (unsigned)a.n), 256, 0, s>>>(partial, groups, a.cols, a.dgamma, a.dbeta);
     return hipGetLastError();
 }
 
