@@ -369,11 +369,13 @@ __global__ __launch_bounds__(256) void bias_grad_kernel(const float* sums, int b
 //   more                    products straight from memory to LDS; x (unlabelled rows as zeros) and a W of 32-bit or unaligned values are
 //                           laid out first
 struct Plan {
-    bool direct, small;            // small: 32 or (direct) 128 rows a tile
-    int bm, wave_m, parts, z_splits, z_len, piece, pieces, blocks, splits, split_len, w_splits, w_len, ldx, planes;
+    bool direct, small;            // small: 32 rows a tile, not 64
+    int bm, bn, wave_m, parts, z_splits, z_len, piece, pieces, blocks, splits, split_len, w_tile, w_splits, w_len, ldx, planes;
     size_t norm, z_label, row_loss, factor, part, g, z, sums, share, w_share, x, w, top, total;
 };
-constexpr long long kPieceBytes = 256ll << 20;       // of G, and of a laid-out piece of W
+// of G, and of a laid-out piece of W: a 32-bit W of more than one piece is laid out again for the gradient (16 x 699 x 576 x 9056: 2.36 ms
+// with 256 MiB, 2.10 with 512 and 1024; bf16 the same with each)
+constexpr long long kPieceBytes = 512ll << 20;
 constexpr long long kSharedW = 48ll << 20;
 
 int up_to(long long v, int unit) { return (int)((v + unit - 1) / unit * unit); }
@@ -382,10 +384,15 @@ Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
 {
     Plan p{};
     p.direct = rows > 64 || (rows && std::min(features, classes) < 8);
-    // 128 rows a tile also where 256 would leave half of the chip without a tile
-    p.small = p.direct ? rows <= 128 || (long long)n * ((rows + 255) / 256) * ((classes + 255) / 256) < 128 : rows <= 32;
-    p.bm = p.direct ? (p.small ? 128 : 256) : p.small ? 32 : 64;
-    const int bn = p.direct ? 256 : 128;
+    p.small = rows <= 32;
+    p.bm = p.small ? 32 : 64;
+    p.bn = 128;
+    if (p.direct) {                // smaller tiles where larger ones would leave half of the chip without one
+        auto tiles = [&](int m, int n_) { return (long long)n * ((rows + m - 1) / m) * ((classes + n_ - 1) / n_); };
+        p.bm = rows <= 128 || tiles(256, 256) < 128 ? 128 : 256;
+        p.bn = p.bm == 128 && tiles(128, 256) < 128 ? 128 : 256;
+    }
+    const int bn = p.bn;
     p.wave_m = p.direct ? p.bm / 2 : 32;
     p.planes = p.direct && !bf16 ? 2 : 1;
     p.parts = up_to(classes, bn) / bn;
@@ -400,12 +407,15 @@ Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
     p.ldx = up_to(features, 8);
     const int bd = p.direct ? 256 : 128;                 // columns of dx a tile
     const long long tiles = (long long)n * ((rows + p.bm - 1) / p.bm) * ((features + bd - 1) / bd);
-    p.splits = (int)std::max<long long>(1, std::min<long long>((p.direct ? 256 : 512) / std::max<long long>(1, tiles), p.piece / (p.direct ? 512 : 128)));
+    const int products = bf16 ? 1 : 3;
+    p.splits = p.direct ? best_shares(tiles, p.piece / kSlab * products, (double)lines * p.ldx * 4)
+                        : (int)std::max<long long>(1, std::min<long long>(512 / std::max<long long>(1, tiles), p.piece / 128));
     p.split_len = up_to((p.piece + p.splits - 1) / p.splits, 128);
     p.splits = (p.piece + p.split_len - 1) / p.split_len;
-    // dW of a piece with fewer tiles than compute units: the rows in shares of at least 256
+    // dW of a piece: its rows in shares where there are few tiles
     const long long dw_tiles = (long long)n * ((features + 255) / 256) * (p.piece / 256);
-    p.w_splits = p.direct ? (int)std::max<long long>(1, std::min<long long>(256 / std::max<long long>(1, dw_tiles), rows / 256)) : 1;
+    p.w_tile = dw_tiles < 128 && rows <= 512 ? 128 : 256;
+    p.w_splits = p.direct && p.w_tile == 256 ? best_shares(dw_tiles, (rows + kSlab - 1) / kSlab * products, (double)n * features * p.piece * 4) : 1;
     p.w_len = up_to((rows + p.w_splits - 1) / p.w_splits, 64);
     if (rows) p.w_splits = (rows + p.w_len - 1) / p.w_len;
     // few rows, a large W in one piece: its contraction in shares of at least 128 features, for some 4096 workgroups
@@ -538,12 +548,13 @@ template <typename T, int BM, int WM, int WN> hipError_t run_general(const LossA
 template <typename T, int PL, class Store>
 hipError_t weight_grad(const Plane3& x, const Plane3& g, const LossArgs& a, int cols, const Plan& p, const Store& store, hipStream_t s)
 {
+    if (p.w_tile == 128) return launch_direct<PL, PL, 128, 128, 2, 2, false, false>(x, g, a.n, a.features, cols, a.rows, p.w_splits, p.w_len, store, s);
     if (a.features <= 128) return launch_direct<PL, PL, 128, 256, 2, 4, false, false>(x, g, a.n, a.features, cols, a.rows, p.w_splits, p.w_len, store, s);
     return launch_direct<PL, PL, 256, 256, 2, 4, false, false>(x, g, a.n, a.features, cols, a.rows, p.w_splits, p.w_len, store, s);
 }
 
 // more rows: operands straight from memory to LDS
-template <typename T, int BM> hipError_t run_direct(const LossArgs& a, const Plan& p, hipStream_t s)
+template <typename T, int BM, int BN, int WN> hipError_t run_direct(const LossArgs& a, const Plan& p, hipStream_t s)
 {
     constexpr int PL = sizeof(T) == 4 ? 2 : 1;
     const Work k(a, p);
@@ -554,8 +565,8 @@ template <typename T, int BM> hipError_t run_direct(const LossArgs& a, const Pla
     if (PL == 2) {
         top_x = k.top; top_w = k.top + a.n;
         for (int i = 0; i < 2 * a.n && e == hipSuccess; i += 1024) { clear_kernel<<<1, 1024, 0, s>>>(k.top + i, std::min(1024, 2 * a.n - i)); e = hipGetLastError(); }
-        if (e == hipSuccess) e = find_largest(a.n, a.rows, a.features, a.x, live, k.top, s);
-        if (e == hipSuccess) e = find_largest(a.n, a.features, a.classes, a.w, Labelled{nullptr, 0}, k.top + a.n, s);
+        if (e == hipSuccess) e = find_largest(a.n, Magnitudes{(const float*)a.x.p, a.x.rep, a.x.row, a.rows, a.features, live, k.top},
+                                              Magnitudes{(const float*)a.w.p, a.w.rep, a.w.row, a.features, a.classes, {nullptr, 0}, k.top + a.n}, s);
     }
     if (e == hipSuccess) e = lay_out<T, PL>(a.n, a.rows, a.features, p.ldx, a.x, live, top_x, k.x, s);
     if (e != hipSuccess) return e;
@@ -574,17 +585,17 @@ template <typename T, int BM> hipError_t run_direct(const LossArgs& a, const Pla
     for (int c0 = 0; c0 < a.classes; c0 += step) {
         const int cols = std::min(step, a.classes - c0);
         if ((e = weights(c0, cols, false, w)) != hipSuccess) return e;
-        const Statistics<PL == 2, BM, 256, 4> stats{bias, a.bias.rep, a.labels, k.part, k.z_label, nullptr, a.rows, c0, a.classes, p.parts, 0};
-        e = launch_direct<PL, PL, BM, 256, 2, 4, true, false>(x, w, a.n, a.rows, cols, a.features, 1, a.features, stats, s);
+        const Statistics<PL == 2, BM, BN, WN> stats{bias, a.bias.rep, a.labels, k.part, k.z_label, nullptr, a.rows, c0, a.classes, p.parts, 0};
+        e = launch_direct<PL, PL, BM, BN, 2, WN, true, false>(x, w, a.n, a.rows, cols, a.features, 1, a.features, stats, s);
         if (e != hipSuccess) return e;
     }
     if ((e = join_rows(a, p, k, s)) != hipSuccess || !a.grad) return e;
     for (int i = 0; i < p.pieces; ++i) {
-        const int c0 = i * p.piece, cols = std::min(p.piece, a.classes - c0), ld = up_to(cols, 256);
+        const int c0 = i * p.piece, cols = std::min(p.piece, a.classes - c0), ld = up_to(cols, BN);
         if ((e = weights(c0, cols, p.pieces == 1, w)) != hipSuccess) return e;
         const Plane3 g{(const __bf16*)k.g, (long long)a.rows * ld, (long long)a.n * a.rows * ld, ld, a.rows, ld, nullptr};
         const Softmax<PL == 2> soft{bias, a.bias.rep, a.labels, k.norm, a.db.p ? k.sums : nullptr, a.rows, c0, a.classes, ld, p.blocks};
-        e = launch_direct<PL, PL, BM, 256, 2, 4, true, false>(x, w, a.n, a.rows, cols, a.features, 1, a.features, GradientRows<PL>{soft, (__bf16*)k.g, g.plane}, s);
+        e = launch_direct<PL, PL, BM, BN, 2, WN, true, false>(x, w, a.n, a.rows, cols, a.features, 1, a.features, GradientRows<PL>{soft, (__bf16*)k.g, g.plane}, s);
         if (e != hipSuccess) return e;
         if (a.dx.p) {
             const StoreShare<> store{k.share, a.rows, a.features, p.ldx, a.rows, a.n, i > 0, false};
@@ -617,8 +628,8 @@ hipError_t launch_loss(const LossArgs& a, hipStream_t s)
 {
     const Plan p = plan_of(a.n, a.rows, a.features, a.classes, a.bf16, a.grad);
     if (p.direct) {
-        if (a.bf16) return p.small ? run_direct<__bf16, 128>(a, p, s) : run_direct<__bf16, 256>(a, p, s);
-        return p.small ? run_direct<float, 128>(a, p, s) : run_direct<float, 256>(a, p, s);
+        if (a.bf16) return p.bm == 256 ? run_direct<__bf16, 256, 256, 4>(a, p, s) : p.bn == 256 ? run_direct<__bf16, 128, 256, 4>(a, p, s) : run_direct<__bf16, 128, 128, 2>(a, p, s);
+        return p.bm == 256 ? run_direct<float, 256, 256, 4>(a, p, s) : p.bn == 256 ? run_direct<float, 128, 256, 4>(a, p, s) : run_direct<float, 128, 128, 2>(a, p, s);
     }
     if (a.bf16) return p.small ? run_general<__bf16, 32, 1, 4>(a, p, s) : run_general<__bf16, 64, 2, 2>(a, p, s);
     return p.small ? run_general<float, 32, 1, 4>(a, p, s) : run_general<float, 64, 2, 2>(a, p, s);

@@ -26,9 +26,10 @@ Plan plan_of(int n, int rows, int in, int out, int bf16)
     p.ldx = (in + 7) / 8 * 8;
     p.ldy = (out + 7) / 8 * 8;
     p.planes = bf16 ? 1 : 3;
-    // fewer tiles than compute units: the rows in shares, of 256 rows at least, that a second launch adds
+    // few tiles: the rows in shares that a second launch adds
     const long long have = tiles(!p.direct ? 64 : p.big ? 256 : 128);
-    p.splits = (int)std::max<long long>(1, std::min<long long>(256 / have, rows / 256));
+    p.splits = p.direct ? best_shares(have, (rows + kSlab - 1) / kSlab * p.planes, (double)n * in * out * 4)
+                        : (int)std::max<long long>(1, std::min<long long>(256 / have, rows / 256));
     p.split_len = (((rows + p.splits - 1) / p.splits) + 63) / 64 * 64;
     p.splits = std::max(1, (rows + p.split_len - 1) / std::max(1, p.split_len));
     if (p.direct) {

@@ -263,22 +263,45 @@ hipError_t launch_direct(const Plane3& a, const Plane3& b, int replicas, int M, 
     return hipGetLastError();
 }
 
-// ---- laying operands out ---------------------------------------------------------------------------------------------
-// the largest finite magnitude of every replica's x, as a float's bits, joined to what top holds; rows that take no part are left out
-__global__ __launch_bounds__(256) inline void largest_kernel(const float* x, long long rep, long long row, int rows, int cols, Labelled live, unsigned* top)
+// Into how many shares a contraction of `slabs` slabs is cut: with t tiles, s shares take ceil(t s / 256) / s rounds of the 256 compute units
+// (one workgroup each), 0.85 us a slab of 256 x 256 tiles, and every share costs its bytes written and read, 5 TB/s.  At least four slabs
+// a share.  16 x 3 x 3 tiles of 72 slabs: one share 61 us, seven 35.
+inline int best_shares(long long tiles, int slabs, double share_bytes)
 {
-    const int k = blockIdx.y, chunks = (cols + 7) / 8;
-    const long long total = (long long)rows * chunks, step = (long long)gridDim.x * 256;
-    if (live.labels) live.labels += (long long)k * rows;
+    int best = 1;
+    double least = 0;
+    for (int s = 1; s <= 64 && (s == 1 || slabs / s >= 4); ++s) {
+        const double rounds = (double)((tiles * s + 255) / 256) / s, cost = rounds * slabs * 0.85e-6 + (s > 1 ? s * share_bytes * 2 / 5e12 : 0);
+        if (s == 1 || cost < 0.97 * least) { best = s; least = cost; }
+    }
+    return best;
+}
+
+// ---- laying operands out ---------------------------------------------------------------------------------------------
+// the largest finite magnitude of every replica's tensor, as a float's bits, joined to what top holds; rows that take no part are left out
+struct Magnitudes {
+    const float* x;
+    long long rep, row;
+    int rows, cols;
+    Labelled live;
+    unsigned* top;
+};
+__global__ __launch_bounds__(256) inline void largest_kernel(Magnitudes first, Magnitudes second)
+{
+    Magnitudes a = blockIdx.z ? second : first;
+    const int k = blockIdx.y, chunks = (a.cols + 7) / 8;
+    const long long total = (long long)a.rows * chunks, step = (long long)gridDim.x * 256;
+    if ((long long)blockIdx.x * 256 >= total) return;
+    if (a.live.labels) a.live.labels += (long long)k * a.rows;
     unsigned most = 0;
     for (long long at = (long long)blockIdx.x * 256 + threadIdx.x; at < total; at += step) {
         const int t = (int)(at / chunks), c = (int)(at - (long long)t * chunks) * 8;
         Chunk<float> v;
-        v.load(x + k * rep + t * row + c, live.at(t) ? cols - c : 0);
+        v.load(a.x + k * a.rep + t * a.row + c, a.live.at(t) ? a.cols - c : 0);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const unsigned a = v.a[e] & 0x7fffffffu, b = v.b[e] & 0x7fffffffu;
-            most = max(most, max(a < 0x7f800000u ? a : 0u, b < 0x7f800000u ? b : 0u));
+            const unsigned p = v.a[e] & 0x7fffffffu, q = v.b[e] & 0x7fffffffu;
+            most = max(most, max(p < 0x7f800000u ? p : 0u, q < 0x7f800000u ? q : 0u));
         }
     }
 #pragma unroll
@@ -287,7 +310,7 @@ __global__ __launch_bounds__(256) inline void largest_kernel(const float* x, lon
     if ((threadIdx.x & 63) == 0) waves[threadIdx.x / 64] = most;
     __syncthreads();
     // a maximum: the same in any order; one a workgroup, since additions to one address queue up
-    if (threadIdx.x == 0) atomicMax(top + k, max(max(waves[0], waves[1]), max(waves[2], waves[3])));
+    if (threadIdx.x == 0) atomicMax(a.top + k, max(max(waves[0], waves[1]), max(waves[2], waves[3])));
 }
 __global__ inline void clear_kernel(unsigned* p, int n) { if ((int)threadIdx.x < n) p[threadIdx.x] = 0; }
 
@@ -326,10 +349,11 @@ hipError_t lay_out(int n, int rows, int cols, int ld, const Rows& x, Labelled li
     lay_out_kernel<T, PL><<<(unsigned)((total + 255) / 256), 256, 0, s>>>((const T*)x.p, x.rep, x.row, rows, cols, ld, total, plane, live, top, out);
     return hipGetLastError();
 }
-inline hipError_t find_largest(int n, int rows, int cols, const Rows& x, Labelled live, unsigned* top, hipStream_t s)
+inline hipError_t find_largest(int n, const Magnitudes& first, const Magnitudes& second, hipStream_t s)
 {
-    const long long blocks = ((long long)rows * ((cols + 7) / 8) + 255) / 256;
-    largest_kernel<<<dim3((unsigned)std::min<long long>(blocks, std::max(8, 1024 / n)), (unsigned)n), 256, 0, s>>>((const float*)x.p, x.rep, x.row, rows, cols, live, top);
+    auto blocks = [](const Magnitudes& a) { return ((long long)a.rows * ((a.cols + 7) / 8) + 255) / 256; };
+    const long long most = std::max(blocks(first), blocks(second));
+    largest_kernel<<<dim3((unsigned)std::min<long long>(most, std::max(8, 1024 / n)), (unsigned)n, 2), 256, 0, s>>>(first, second);
     return hipGetLastError();
 }
 
