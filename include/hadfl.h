@@ -356,8 +356,9 @@ HADFL_API hadfl_status hadfl_dense_workspace(const hadfl_dense *dense, size_t *b
 HADFL_API hadfl_status hadfl_dense_grad_packed(const hadfl_dense *dense, const void *packed, const hadfl_rows *dy,
                                                const hadfl_rows *dw, const hadfl_rows *db, void *work, void *stream);
 
-/* Softmax cross entropy of a last dense layer over many classes, without its logits ever being kept: they are formed
- * a piece of the vocabulary at a time, once for the loss and once more for the gradient.  With z = x W + b,
+/* Softmax cross entropy of a last dense layer over many classes, without keeping its logits: they are formed a piece of
+ * the vocabulary at a time, once for the loss and once more for the gradient (up to 64 rows, where one piece holds the
+ * whole vocabulary, once).  A piece is at most 512 MiB, or 1024 classes.  With z = x W + b,
  *   row_loss_t = log sum_v exp(z_tv) - z_t,label(t);   loss = mean of row_loss over the replica's labelled rows.
  * A row whose label lies outside [0, n_classes) has no label: its row_loss is zero, it adds nothing to any gradient
  * (whatever its x holds), and its dx is zero.  A replica without labelled rows has loss zero and zero gradients.  A bias of
@@ -374,7 +375,8 @@ HADFL_API hadfl_status hadfl_dense_grad_packed(const hadfl_dense *dense, const v
  *   loss                  dev out, [n_replicas] floats
  *   row_loss              dev out or NULL, [n_replicas][n_rows] floats
  *   dx (t), dw (t), db    dev out, like x, w, bias; each may be NULL and is then not computed
- *   work                  dev, 256-byte aligned; hadfl_loss_workspace, grad = 1 for hadfl_loss_grad */
+ *   work                  dev, 256-byte aligned; hadfl_loss_workspace with grad = 1 serves both calls, with grad = 0
+ *                         hadfl_loss_forward alone */
 typedef struct { int32_t n_replicas, n_rows, n_features, n_classes, bf16; } hadfl_loss;
 HADFL_API hadfl_status hadfl_loss_workspace(const hadfl_loss *shape, int32_t grad, size_t *bytes);
 HADFL_API hadfl_status hadfl_loss_forward(const hadfl_loss *shape, const hadfl_rows *x, const hadfl_rows *w,

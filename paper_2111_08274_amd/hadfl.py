@@ -394,7 +394,7 @@ class _Operator:
     """Sizes, types and working memory of one operator on the current torch device.  Its tensors are torch device tensors
     [replica, row, column] (or [replica, column] for vectors) whose columns are contiguous; other strides are free.  Calls go
     to `stream` or to the current one, and the tensors have to be ready there; calls of one object share its working memory
-    and must not overlap in time.  Outputs that are not given are allocated."""
+    and must not overlap in time.  Outputs that are not given are allocated, as memory of the stream the call goes to."""
 
     def __init__(self, desc, bf16, workspace=None):
         import torch
@@ -405,14 +405,17 @@ class _Operator:
         self._structs = {}
         # the handle itself where torch offers it; the object around it takes longer to make than a kernel to launch
         self._current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
-        self.work = None
-        if workspace is not None:
-            self.work = self._bytes(workspace)
+        self._home, self._own = self._current(self.device.index), []
+        self.work = None if workspace is None else self._bytes(workspace)
 
     def _bytes(self, query):
         n = ctypes.c_size_t()
         _check(query(self._ref, ctypes.byref(n)))
-        return self.torch.empty(n.value, dtype=self.torch.uint8, device=self.device)
+        return self._keep(self.torch.empty(n.value, dtype=self.torch.uint8, device=self.device))
+
+    def _keep(self, t):
+        self._own.append(t)
+        return t
 
     def _rows(self, name, t, shape, dtype):
         """The address of the hadfl_rows of a tensor, checked; None stays None."""
@@ -439,11 +442,23 @@ class _Operator:
             raise HadflError(EINVAL, "%s must be contiguous %s %s on %s" % (name, dtype, shape, self.device))
         return t.data_ptr() or None
 
-    def _out(self, t, shape, dtype):
-        return self.torch.empty(shape, dtype=dtype, device=self.device) if t is None else t
+    def _out(self, t, shape, dtype, stream=None):
+        if t is not None:
+            return t
+        if stream is not None:
+            with self.torch.cuda.stream(stream):
+                return self.torch.empty(shape, dtype=dtype, device=self.device)
+        return self.torch.empty(shape, dtype=dtype, device=self.device)
 
-    def _stream(self, stream):
-        return self._current(self.device.index) if stream is None else stream.cuda_stream
+    def _stream(self, stream, *others):
+        """The handle of the stream a call goes to.  Away from the stream this object was made on, the allocator is told that
+        its memory (and that of the other operators that the call uses) is in use there."""
+        h = self._current(self.device.index) if stream is None else stream.cuda_stream
+        for o in (self,) + others:
+            if h != o._home:
+                for t in o._own:
+                    t.record_stream(self.torch.cuda.current_stream(self.device) if stream is None else stream)
+        return h
 
 
 class LayerNorm(_Operator):
@@ -454,12 +469,12 @@ class LayerNorm(_Operator):
         super().__init__(HadflNorm(int(n_replicas), int(n_rows), int(n_features), int(bf16), float(eps)), bf16, lib().hadfl_norm_workspace)
         self.shape, self.vector = (int(n_replicas), int(n_rows), int(n_features)), (int(n_replicas), int(n_features))
         f32 = self.torch.float32
-        self.mean = self.torch.empty(self.shape[:2], dtype=f32, device=self.device)
-        self.rstd = self.torch.empty(self.shape[:2], dtype=f32, device=self.device)
+        self.mean = self._keep(self.torch.empty(self.shape[:2], dtype=f32, device=self.device))
+        self.rstd = self._keep(self.torch.empty(self.shape[:2], dtype=f32, device=self.device))
 
     def forward(self, x, gamma, beta, y=None, stream=None):
         f32 = self.torch.float32
-        y = self._out(y, self.shape, self.dtype)
+        y = self._out(y, self.shape, self.dtype, stream)
         _check(lib().hadfl_norm_forward(self._ref, self._rows("x", x, self.shape, self.dtype), self._rows("gamma", gamma, self.vector, f32),
                                         self._rows("beta", beta, self.vector, f32), self._rows("y", y, self.shape, self.dtype),
                                         self.mean.data_ptr() or None, self.rstd.data_ptr() or None, self._stream(stream)))
@@ -468,17 +483,18 @@ class LayerNorm(_Operator):
     def backward(self, dy, x, gamma, dx=None, dgamma=None, dbeta=None, stream=None):
         """x: the tensor given to forward() or the PackedRows that holds it.  -> dx, dgamma, dbeta"""
         f32 = self.torch.float32
-        dx, dgamma, dbeta = self._out(dx, self.shape, self.dtype), self._out(dgamma, self.vector, f32), self._out(dbeta, self.vector, f32)
-        packed = None
+        dx, dgamma, dbeta = self._out(dx, self.shape, self.dtype, stream), self._out(dgamma, self.vector, f32, stream), self._out(dbeta, self.vector, f32, stream)
+        packed, others = None, ()
         if isinstance(x, PackedRows):
             if x.shape != self.shape:
                 raise HadflError(EINVAL, "the checkpoint holds %s, not %s" % (x.shape, self.shape))
+            others = (x,)
             x, packed = None, x.data.data_ptr()
         _check(lib().hadfl_norm_backward(self._ref, self._rows("dy", dy, self.shape, self.dtype), self._rows("x", x, self.shape, self.dtype),
                                          packed, self._rows("gamma", gamma, self.vector, f32), self.mean.data_ptr() or None,
                                          self.rstd.data_ptr() or None, self._rows("dx", dx, self.shape, self.dtype),
                                          self._rows("dgamma", dgamma, self.vector, f32), self._rows("dbeta", dbeta, self.vector, f32),
-                                         self.work.data_ptr(), self._stream(stream)))
+                                         self.work.data_ptr(), self._stream(stream, *others)))
         return dx, dgamma, dbeta
 
 
@@ -496,7 +512,7 @@ class PackedRows(_Operator):
         return self
 
     def unpack(self, out=None, stream=None):
-        out = self._out(out, self.shape, self.dtype)
+        out = self._out(out, self.shape, self.dtype, stream)
         _check(lib().hadfl_unpack_rows(self._ref, self.data.data_ptr(), self._rows("out", out, self.shape, self.dtype), self._stream(stream)))
         return out
 
@@ -514,11 +530,11 @@ class DenseGrad(_Operator):
         f32 = self.torch.float32
         if packed.shape != (self.n, self.rows, self.n_in):
             raise HadflError(EINVAL, "the checkpoint holds %s, not %s" % (packed.shape, (self.n, self.rows, self.n_in)))
-        dw = self._out(dw, (self.n, self.n_in, self.n_out), f32)
-        db = self._out(db, (self.n, self.n_out), f32) if bias else None
+        dw = self._out(dw, (self.n, self.n_in, self.n_out), f32, stream)
+        db = self._out(db, (self.n, self.n_out), f32, stream) if bias else None
         _check(lib().hadfl_dense_grad_packed(self._ref, packed.data.data_ptr(), self._rows("dy", dy, (self.n, self.rows, self.n_out), self.dtype),
                                              self._rows("dw", dw, (self.n, self.n_in, self.n_out), f32),
-                                             self._rows("db", db, (self.n, self.n_out), f32), self.work.data_ptr(), self._stream(stream)))
+                                             self._rows("db", db, (self.n, self.n_out), f32), self.work.data_ptr(), self._stream(stream, packed)))
         return dw, db
 
 
@@ -543,7 +559,7 @@ class ClassLoss(_Operator):
     def loss(self, x, w, labels, bias=None, loss=None, row_loss=None, stream=None):
         """-> loss [n_replicas] (mean over the labelled rows), row_loss [n_replicas, n_rows]"""
         f32 = self.torch.float32
-        loss, row_loss = self._out(loss, (self.n,), f32), self._out(row_loss, (self.n, self.rows), f32)
+        loss, row_loss = self._out(loss, (self.n,), f32, stream), self._out(row_loss, (self.n, self.rows), f32, stream)
         _check(lib().hadfl_loss_forward(*self._inputs(x, w, labels, bias, row_loss, loss), self.work.data_ptr(), self._stream(stream)))
         return loss, row_loss
 
@@ -552,10 +568,10 @@ class ClassLoss(_Operator):
         if not self.with_grad:
             raise HadflError(ESTATE, "this ClassLoss was made with grad=False")
         f32 = self.torch.float32
-        loss, row_loss = self._out(loss, (self.n,), f32), self._out(row_loss, (self.n, self.rows), f32)
-        dx = self._out(dx, (self.n, self.rows, self.features), self.dtype) if "dx" in want else None
-        dw = self._out(dw, (self.n, self.features, self.classes), self.dtype) if "dw" in want else None
-        db = self._out(db, (self.n, self.classes), f32) if "db" in want and bias is not None else None
+        loss, row_loss = self._out(loss, (self.n,), f32, stream), self._out(row_loss, (self.n, self.rows), f32, stream)
+        dx = self._out(dx, (self.n, self.rows, self.features), self.dtype, stream) if "dx" in want else None
+        dw = self._out(dw, (self.n, self.features, self.classes), self.dtype, stream) if "dw" in want else None
+        db = self._out(db, (self.n, self.classes), f32, stream) if "db" in want and bias is not None else None
         _check(lib().hadfl_loss_grad(*self._inputs(x, w, labels, bias, row_loss, loss),
                                      self._rows("dx", dx, (self.n, self.rows, self.features), self.dtype),
                                      self._rows("dw", dw, (self.n, self.features, self.classes), self.dtype),

@@ -304,6 +304,8 @@ def test_loss_over_many_classes_and_its_gradient(n, rows, d, v, bf16, bias, layo
     # the loss alone, with a plan that has no room for gradients
     alone = hadfl.ClassLoss(n, rows, d, v, bf16=bf16, grad=False).loss(c["x"], c["w"], c["y"], c["bias"])
     assert torch.equal(alone[0], loss) and torch.equal(alone[1], row)
+    alone = plan.loss(c["x"], c["w"], c["y"], c["bias"])
+    assert torch.equal(alone[0], loss) and torch.equal(alone[1], row)
 
 
 def test_each_gradient_alone_is_the_same_and_repeats_bit_for_bit():
@@ -447,6 +449,18 @@ def test_head_operators_on_a_stream_of_their_own():
     got = plan.grad(norm.forward(x, gamma, gamma, stream=s), c["w"], c["y"], c["bias"], stream=s)
     s.synchronize()
     assert all(torch.equal(p, q) for p, q in zip(want, got))
+    # made, used and dropped while another stream still runs them: their memory is not given away before it is done
+    with torch.cuda.stream(s):
+        for _ in range(20):
+            other = hadfl.ClassLoss(2, 50, 128, 1024, bf16=1)
+            packed = hadfl.PackedRows(2, 50, 128, bf16=1)
+            got = other.grad(norm.forward(packed.pack(x).unpack(), gamma, gamma), c["w"], c["y"], c["bias"])
+            del other, packed
+    junk = [torch.full((1 << 20,), float("nan"), device="cuda") for _ in range(8)]
+    s.synchronize()
+    kept = hadfl.PackedRows(2, 50, 128, bf16=1).pack(x).unpack()
+    want = plan.grad(norm.forward(kept, gamma, gamma), c["w"], c["y"], c["bias"])
+    assert all(torch.equal(p, q) for p, q in zip(want, got)) and len(junk) == 8
 
 
 def test_head_operators_replayed_from_a_graph():
