@@ -551,7 +551,7 @@ template <typename T, int BM, int WM, int WN> hipError_t run_general(const LossA
 template <typename T, int PL, class Store>
 hipError_t weight_grad(const Plane3& x, const Plane3& g, const LossArgs& a, int cols, const Plan& p, const Store& store, hipStream_t s)
 {
-    if (p.w_tile == 128) return launch_direct<PL, PL, 128, 128, 2, 2, false, false>(x, g, a.n, a.features, cols, a.rows, p.w_splits, p.w_len, store, s);
+    if (p.w_tile == 128) return launch_direct<PL, PL, 128, 128, 2, 4, false, false>(x, g, a.n, a.features, cols, a.rows, p.w_splits, p.w_len, store, s);
     if (narrow(a.features)) return launch_direct<PL, PL, 128, 256, 2, 4, false, false>(x, g, a.n, a.features, cols, a.rows, p.w_splits, p.w_len, store, s);
     return launch_direct<PL, PL, 256, 256, 2, 4, false, false>(x, g, a.n, a.features, cols, a.rows, p.w_splits, p.w_len, store, s);
 }
@@ -632,8 +632,8 @@ hipError_t launch_loss(const LossArgs& a, hipStream_t s)
 {
     const Plan p = plan_of(a.n, a.rows, a.features, a.classes, a.bf16, a.grad);
     if (p.direct) {
-        if (a.bf16) return p.bm == 256 ? run_direct<__bf16, 256, 256, 4>(a, p, s) : p.bn == 256 ? run_direct<__bf16, 128, 256, 4>(a, p, s) : run_direct<__bf16, 128, 128, 2>(a, p, s);
-        return p.bm == 256 ? run_direct<float, 256, 256, 4>(a, p, s) : p.bn == 256 ? run_direct<float, 128, 256, 4>(a, p, s) : run_direct<float, 128, 128, 2>(a, p, s);
+        if (a.bf16) return p.bm == 256 ? run_direct<__bf16, 256, 256, 4>(a, p, s) : p.bn == 256 ? run_direct<__bf16, 128, 256, 4>(a, p, s) : run_direct<__bf16, 128, 128, 4>(a, p, s);
+        return p.bm == 256 ? run_direct<float, 256, 256, 4>(a, p, s) : p.bn == 256 ? run_direct<float, 128, 256, 4>(a, p, s) : run_direct<float, 128, 128, 4>(a, p, s);
     }
     if (a.bf16) return p.small ? run_general<__bf16, 32, 1, 4>(a, p, s) : run_general<__bf16, 64, 2, 2>(a, p, s);
     return p.small ? run_general<float, 32, 1, 4>(a, p, s) : run_general<float, 64, 2, 2>(a, p, s);

@@ -57,7 +57,7 @@ template <typename T, class Store> hipError_t product(const DenseArgs& a, const 
         dy = Plane3{wy, (long long)a.rows * p.ldy, (long long)a.n * a.rows * p.ldy, p.ldy, a.rows, p.ldy, nullptr};
     }
     if (p.big) return launch_direct<1, PL, 256, 256, 2, 4, false, false>(x, dy, a.n, a.in, a.out, a.rows, p.splits, p.split_len, store, s);
-    return launch_direct<1, PL, 128, 128, 2, 2, false, false>(x, dy, a.n, a.in, a.out, a.rows, p.splits, p.split_len, store, s);
+    return launch_direct<1, PL, 128, 128, 2, 4, false, false>(x, dy, a.n, a.in, a.out, a.rows, p.splits, p.split_len, store, s);
 }
 
 template <typename T> hipError_t run(const DenseArgs& a, hipStream_t s)
