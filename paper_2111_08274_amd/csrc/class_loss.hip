@@ -96,7 +96,7 @@ template <bool EXACT, int BM, int BN, int WN> struct Statistics {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) top = __builtin_fmaxf(top, v[j][e]);          // NaNs show in the sum
             at_label<TN>(t.lane, n0, y < classes ? y : -1, [&](int j, int e) { z_label[(long long)t.rep * rows + m] = v[j][e]; });
-            top = __builtin_fmaxf(top, __shfl_xor(top, 32));
+            top = __builtin_fmaxf(top, other<32>(top));
             float sum = 0.f;
             const float base = top == -INFINITY ? 0.f : top;   // a row of -inf alone: every term is zero
             if (EXACT || b) {                                  // the difference first: a bias may be the type's lowest value
@@ -110,7 +110,7 @@ template <bool EXACT, int BM, int BN, int WN> struct Statistics {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(v[j][e], kLog2e, -base * kLog2e));
             }
-            sum += __shfl_xor(sum, 32);
+            sum += other<32>(sum);
             if (t.lane < 32) got[(t.n0 - t.bn) / (32 * TN) * BM + m - t.bm] = float2{top, sum};
         }
         __syncthreads();
@@ -272,9 +272,7 @@ template <bool EXACT> struct Softmax {
         for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                float v = column[j][e];
-#pragma unroll
-                for (int d = 1; d < 32; d *= 2) v += __shfl_xor(v, d);
+                const float v = sum_over<32>(column[j][e]);
                 const int n = t.n0 + 32 * j + 8 * (e / 4) + 4 * (t.lane >> 5) + e % 4;
                 if ((t.lane & 31) == 0 && n < ld) out[n] = v;
             }

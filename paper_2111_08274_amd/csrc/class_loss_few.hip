@@ -50,18 +50,14 @@ __global__ __launch_bounds__(256) void join_logits_kernel(const float* share, in
 #pragma unroll 4
             for (int s = 0; s < splits; ++s) v[u] += share[s * step + at];
             v[u] = c < classes ? v[u] + b : -INFINITY;
-            float top = v[u];
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) top = __builtin_fmaxf(top, __shfl_xor(top, d));
+            const float top = max_over<64>(v[u]);
             if (lane == 0) tops[tid >> 6][u] = top;
         }
         __syncthreads();
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const float top = __builtin_fmaxf(tops[2 * pair][u], tops[2 * pair + 1][u]), base = top == -INFINITY ? 0.f : top;
-            float sum = __builtin_amdgcn_exp2f((v[u] - base) * kLog2e);
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+            const float sum = sum_over<64>(__builtin_amdgcn_exp2f((v[u] - base) * kLog2e));
             if (lane == 0) sums[tid >> 6][u] = sum;
         }
         __syncthreads();

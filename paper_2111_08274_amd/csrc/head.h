@@ -154,6 +154,43 @@ __device__ __forceinline__ void store_chunk(__bf16* p, int left, const float* v)
 #pragma unroll
     for (int e = 0; e < 8; ++e) if (e < left) p[e] = (__bf16)v[e];
 }
+// The value of another lane, such that after the steps 1, 2, 4, ... N / 2 of  v = f(v, other<step>(v))  all lanes of a group of N hold f over
+// the group: within 16 lanes by moves that the arithmetic instruction does on the way (a mirror in place of an exchange: both halves hold their
+// own total by then), beyond by the exchange of lane rows; neither takes the way through LDS that a general shuffle does.
+template <int STEP> __device__ __forceinline__ float other(float v)
+{
+    const unsigned u = __builtin_bit_cast(unsigned, v);
+    if constexpr (STEP == 16) {
+        const auto w = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        return __builtin_bit_cast(float, (threadIdx.x & 16) ? w[0] : w[1]);
+    } else if constexpr (STEP == 32) {
+        const auto w = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        return __builtin_bit_cast(float, (threadIdx.x & 32) ? w[0] : w[1]);
+    } else {
+        constexpr int kMove = STEP == 1 ? 0xB1 : STEP == 2 ? 0x4E : STEP == 4 ? 0x141 : 0x140;     // quads 1032, 2301, mirrors of 8 and 16 lanes
+        return __builtin_bit_cast(float, (unsigned)__builtin_amdgcn_update_dpp(0, (int)u, kMove, 0xf, 0xf, true));
+    }
+}
+template <int N> __device__ __forceinline__ float sum_over(float v)
+{
+    if constexpr (N > 1) v += other<1>(v);
+    if constexpr (N > 2) v += other<2>(v);
+    if constexpr (N > 4) v += other<4>(v);
+    if constexpr (N > 8) v += other<8>(v);
+    if constexpr (N > 16) v += other<16>(v);
+    if constexpr (N > 32) v += other<32>(v);
+    return v;
+}
+template <int N> __device__ __forceinline__ float max_over(float v)
+{
+    if constexpr (N > 1) v = __builtin_fmaxf(v, other<1>(v));
+    if constexpr (N > 2) v = __builtin_fmaxf(v, other<2>(v));
+    if constexpr (N > 4) v = __builtin_fmaxf(v, other<4>(v));
+    if constexpr (N > 8) v = __builtin_fmaxf(v, other<8>(v));
+    if constexpr (N > 16) v = __builtin_fmaxf(v, other<16>(v));
+    if constexpr (N > 32) v = __builtin_fmaxf(v, other<32>(v));
+    return v;
+}
 // 2^e of a group from its stored byte; 255 gives infinity, whose product with the group's zeros is the NaN it stands for
 __device__ __forceinline__ float group_unit(unsigned byte) { return __builtin_bit_cast(float, byte << 23); }
 

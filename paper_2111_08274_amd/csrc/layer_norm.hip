@@ -69,15 +69,16 @@ __device__ __forceinline__ void store_row(T* row, int lane, int cols, const floa
     for (int i = 0; i < CH; ++i) store_chunk(row + column<NL>(lane, i), cols - column<NL>(lane, i), v[i]);
 }
 
-// sums of two values over the NL lanes of a row, to all of them; NL = 256: the whole workgroup, through LDS in two slots used
-// in turn, so that one barrier a sum is enough
+// sums over the NL lanes of a row, to all of them; NL = 256: the whole workgroup, through LDS in two slots used in turn, so that one barrier
+// a sum is enough
 template <int NL> struct RowSum {
     float (*slot)[4][2];
     int turn = 0;
     __device__ __forceinline__ void add(float& a, float& b)
     {
-#pragma unroll
-        for (int d = 1; d < (NL < 64 ? NL : 64); d *= 2) { a += __shfl_xor(a, d); b += __shfl_xor(b, d); }
+        constexpr int W = NL < 64 ? NL : 64;
+        a = sum_over<W>(a);
+        b = sum_over<W>(b);
         if (NL == 256) {
             const int w = threadIdx.x / 64;
             if ((threadIdx.x & 63) == 0) { slot[turn][w][0] = a; slot[turn][w][1] = b; }
@@ -86,6 +87,12 @@ template <int NL> struct RowSum {
             b = (slot[turn][0][1] + slot[turn][1][1]) + (slot[turn][2][1] + slot[turn][3][1]);
             turn ^= 1;
         }
+    }
+    __device__ __forceinline__ void add(float& a)
+    {
+        float none = 0.f;
+        if (NL == 256) add(a, none);
+        else a = sum_over<NL < 64 ? NL : 64>(a);
     }
 };
 
@@ -105,14 +112,14 @@ __global__ __launch_bounds__(256) void norm_forward_kernel(NormArgs a)
     RowSum<NL> sum{slot};
     const float inv = 1.f / (float)a.cols;
     for (; t < a.rows; t += step) {
-        float v[CH][8], m = 0.f, q = 0.f, none = 0.f;
+        float v[CH][8], m = 0.f, q = 0.f;
         next.get(v);
         if (t + step < a.rows) next.load(x + (t + step) * a.x.row, lane, a.cols);
 #pragma unroll
         for (int i = 0; i < CH; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) m += v[i][e];
-        sum.add(m, none);
+        sum.add(m);
         m *= inv;
 #pragma unroll
         for (int i = 0; i < CH; ++i)
@@ -121,7 +128,7 @@ __global__ __launch_bounds__(256) void norm_forward_kernel(NormArgs a)
                 v[i][e] = column<NL>(lane, i) + e < a.cols ? v[i][e] - m : 0.f;
                 q += v[i][e] * v[i][e];
             }
-        sum.add(q, none);
+        sum.add(q);
         const float r = 1.f / __builtin_sqrtf(q * inv + a.eps);
 #pragma unroll
         for (int i = 0; i < CH; ++i)
@@ -220,12 +227,12 @@ __global__ __launch_bounds__(256) void norm_forward_long_kernel(NormArgs a)
     const float *g = (const float*)a.gamma.p + k * a.gamma.rep, *b = (const float*)a.beta.p + k * a.beta.rep;
     RowSum<256> sum{slot};
     const float inv = 1.f / (float)a.cols;
-    float m = 0.f, q = 0.f, none = 0.f;
+    float m = 0.f, q = 0.f;
     for (int c = threadIdx.x; c < a.cols; c += 256) m += up(x[c]);
-    sum.add(m, none);
+    sum.add(m);
     m *= inv;
     for (int c = threadIdx.x; c < a.cols; c += 256) { const float v = up(x[c]) - m; q += v * v; }
-    sum.add(q, none);
+    sum.add(q);
     const float r = 1.f / __builtin_sqrtf(q * inv + a.eps);
     for (int c = threadIdx.x; c < a.cols; c += 256) y[c] = (T)((up(x[c]) - m) * r * g[c] + b[c]);
     if (threadIdx.x == 0 && a.mean) { a.mean[(long long)k * a.rows + t] = m; a.rstd[(long long)k * a.rows + t] = r; }
