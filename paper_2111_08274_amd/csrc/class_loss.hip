@@ -362,10 +362,13 @@ __global__ __launch_bounds__(256) void bias_grad_kernel(const float* sums, int b
 }
 
 // Which kernels, the piece of the vocabulary and the working memory, from the sizes alone.
-//   few rows (at most 64)   the products through registers read W as it is, 32 or 64 x 128 tiles: W is read once per pass, laying
-//                           it out first would cost as much again
-//   more                    products straight from memory to LDS; x (unlabelled rows as zeros) and a W of 32-bit or unaligned values are
-//                           laid out first
+//   few rows   the products through registers read W as it is, 32 or 64 x 128 tiles
+//   more       products straight from memory to LDS: twice to three times the rate, but x (unlabelled rows as zeros) and a W of 32-bit or
+//              unaligned values are laid out first, and there are more launches.  Rows from which that is faster, with W of E values
+//              in all: 16 + 1.0e9 / E for a bf16 W that can be read as it is (4 x 512 x 32000: at 32 rows 126 us against 149), 30 + 1.3e9 / E for
+//              one that cannot (32001 classes: at 48 rows 180 against 192; 1 x 1024 x 10007: at 160 rows 80 against 79), 90 + 2.4e9 / E for
+//              32 bits (4 x 512 x 32000: at 128 rows 541 against 593; 1 x 1024 x 10007: at 256 rows 183 against 169, at 384 211 against
+//              219); small W 200 or 400 rows later at most (1 x 256 x 2003: at 256 rows 44 against 46)
 struct Plan {
     bool direct, small;            // small: 32 rows a tile, not 64
     int bm, bn, wave_m, parts, z_splits, z_len, piece, pieces, blocks, splits, split_len, w_tile, w_splits, w_len, ldx, planes;
@@ -384,7 +387,9 @@ bool narrow(int v) { return 1.18 * up_to(v, 128) < up_to(v, 256); }
 Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
 {
     Plan p{};
-    p.direct = rows > 64 || (rows && std::min(features, classes) < 8);
+    const double values = (double)n * features * classes;
+    const double from = bf16 ? (classes % 8 == 0 ? 16 + std::min(200., 1.0e9 / values) : 30 + std::min(200., 1.3e9 / values)) : 90 + std::min(400., 2.4e9 / values);
+    p.direct = rows > from || (rows && std::min(features, classes) < 8);         // fewer values a row than a chunk: laid out
     p.small = rows <= 32;
     p.bm = p.small ? 32 : 64;
     p.bn = 128;

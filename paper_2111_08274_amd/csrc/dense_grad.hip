@@ -1,9 +1,8 @@
 // Parameter gradients of a dense layer whose input was kept in 8 bits: dW = x^T dy with x from the checkpoint, db = sum_t dy.
 // q * 2^e is exact in bf16, so a bf16 dy needs one product and a 32-bit dy, in three bf16 planes, three.  db comes from the same
 // operands as one more product, of ones (tile_product.h).
-//   short contractions or few columns   chunks of the checkpoint become bf16 in registers, on their way to LDS
-//   otherwise                           the checkpoint is laid out as bf16 first (3 bytes a value once, where every column of tiles would
-//                                       convert it again) and both operands go straight from memory to LDS
+//   less work   chunks of the checkpoint become bf16 in registers, on their way to LDS (again in every column of tiles)
+//   more        the checkpoint is laid out as bf16 first, 3 bytes a value once, and both operands go straight from memory to LDS
 #include "direct_product.h"
 
 namespace hadfl {
@@ -17,19 +16,28 @@ struct Plan {
     size_t x, y, share, total;
 };
 
+// Laying out costs 3 bytes a value of x (and 10 of a 32-bit dy, which its three planes have to win back over in x out products) and two
+// launches; the product after it runs at two to three times the rate.  Through registers / laid out, us:
+//   bf16   16 x 512 x 512, 1024 rows 30 / 31, 2048 rows 53 / 42; 4096 x 4096, 256 rows 31 / 35, 512 rows 50 / 41; 784 x 128, 16384 rows 55 / 60;
+//          8 x 784 x 130, where the larger tiles would be more than half empty, 16384 rows 153 / 191
+//   fp32   2048 x 2048, 1024 rows 49 / 54, 2048 rows 93 / 89, 8192 rows 354 / 300; 4096 x 4096, 512 rows 85 / 73; 16 x 512 x 512, 8192 rows
+//          388 / 446; 2 x 128 x 4096, 8192 rows 105 / 213
 Plan plan_of(int n, int rows, int in, int out, int bf16)
 {
     Plan p{};
-    p.direct = (rows >= 256 && in >= 96 && out >= 96) || (rows && out < 8);     // the other way takes rows of eight values at least
     auto tiles = [&](int t) { return (long long)n * ((in + t - 1) / t) * ((out + t - 1) / t); };
+    const double work = (double)n * rows * in * out;
     p.big = tiles(256) >= 192;
+    p.direct = bf16 ? work >= 4e9 && tiles(128) * 4 <= tiles(64) * 1.3 : work >= 8e9 && (p.big || (double)in * out >= 100. * (3. * in + 10. * out));
+    p.direct = p.direct || (rows && out < 8);                  // fewer values a row than a chunk: laid out
     p.ldx = (in + 7) / 8 * 8;
     p.ldy = (out + 7) / 8 * 8;
     p.planes = bf16 ? 1 : 3;
-    // few tiles: the rows in shares that a second launch adds
-    const long long have = tiles(!p.direct ? 64 : p.big ? 256 : 128);
-    p.splits = p.direct ? best_shares(have, (rows + kSlab - 1) / kSlab * p.planes, (double)n * in * out * 4)
-                        : (int)std::max<long long>(1, std::min<long long>(256 / have, rows / 256));
+    // few tiles: the rows in shares that a second launch adds, for some three workgroups a compute unit; where there is one without them, of
+    // 1024 rows at least (300 x 5000 bf16: 1024 rows in one share 19 us, in three 28; 8192 rows 150 and 112)
+    const long long have = tiles(64);
+    p.splits = p.direct ? best_shares(tiles(p.big ? 256 : 128), (rows + kSlab - 1) / kSlab * p.planes, (double)n * in * out * 4)
+                        : (int)std::max<long long>(1, std::min<long long>((768 + have - 1) / have, rows / (have < 256 ? 256 : 1024)));
     p.split_len = (((rows + p.splits - 1) / p.splits) + 63) / 64 * 64;
     p.splits = std::max(1, (rows + p.split_len - 1) / std::max(1, p.split_len));
     if (p.direct) {

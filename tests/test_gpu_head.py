@@ -228,7 +228,7 @@ def test_a_group_with_an_infinity_or_a_nan_stands_for_nans_and_no_other():
 
 # ---- a dense layer's gradient from a checkpoint ----------------------------------------------------------------------------
 DENSE = [(1, 0, 5, 9), (1, 1, 1, 1), (2, 3, 33, 7), (4, 32, 784, 128), (2, 65, 130, 257), (1, 257, 129, 120), (3, 100, 512, 512), (1, 1000, 48, 96),
-         (1, 2049, 256, 256), (2, 640, 264, 520), (1, 3000, 40, 90), (2, 1500, 97, 130), (16, 300, 520, 512)]
+         (1, 2049, 256, 256), (2, 640, 264, 520), (1, 3000, 40, 90), (2, 1500, 97, 130), (16, 300, 520, 512), (1, 2101, 2051, 2003), (1, 700, 3500, 3457)]
 
 
 @pytest.mark.parametrize("layout", ["whole", "padded", "odd"])
@@ -252,7 +252,7 @@ def test_dense_gradient_from_a_checkpoint(n, rows, i, o, bf16, layout):
 
 # ---- loss over a large vocabulary ------------------------------------------------------------------------------------------
 LOSS = [(1, 1, 1, 1), (1, 1, 64, 1000), (2, 3, 7, 5), (1, 1, 513, 4099), (4, 32, 128, 1007), (3, 33, 65, 300), (2, 100, 200, 129), (1, 257, 136, 2056),
-        (2, 130, 64, 5003), (1, 31, 1030, 256), (1, 300, 512, 1536)]
+        (2, 130, 64, 5003), (1, 31, 1030, 256), (1, 300, 512, 1536), (1, 600, 512, 1536), (2, 497, 65, 1203), (1, 530, 201, 2057), (1, 1100, 72, 300)]
 
 
 def _loss_case(n, rows, d, v, bf16, layout, bias, seed=3):
@@ -310,7 +310,7 @@ def test_loss_over_many_classes_and_its_gradient(n, rows, d, v, bf16, bias, layo
 
 def test_each_gradient_alone_is_the_same_and_repeats_bit_for_bit():
     torch = _torch()
-    for bf16, rows in ((0, 40), (1, 40), (0, 5), (1, 200)):
+    for bf16, rows in ((0, 40), (1, 40), (0, 5), (1, 200), (0, 600), (1, 600)):
         c = _loss_case(2, rows, 96, 777, bf16, "whole", True)
         plan = hadfl.ClassLoss(2, rows, 96, 777, bf16=bf16)
         whole = plan.grad(c["x"], c["w"], c["y"], c["bias"])
@@ -325,7 +325,7 @@ def test_each_gradient_alone_is_the_same_and_repeats_bit_for_bit():
 def test_replicas_without_any_label_or_row():
     torch = _torch()
     for bf16 in (0, 1):
-        for rows in (5, 70):
+        for rows in (5, 70, 600):
             c = _loss_case(2, rows, 72, 130, bf16, "whole", True)
             c["y"][1] = -1
             out = hadfl.ClassLoss(2, rows, 72, 130, bf16=bf16).grad(c["x"], c["w"], c["y"], c["bias"])
@@ -337,13 +337,30 @@ def test_replicas_without_any_label_or_row():
 
 def test_one_x_or_one_w_for_all_replicas():
     torch = _torch()
-    for bf16, rows in ((0, 20), (1, 140)):
+    for bf16, rows in ((0, 20), (1, 140), (0, 550), (1, 550)):
         c = _loss_case(3, rows, 64, 512, bf16, "whole", False)
         plan = hadfl.ClassLoss(3, rows, 64, 512, bf16=bf16)
         y = c["y"][:1].expand(3, rows).contiguous()
         x, w = c["x"][:1].expand(3, rows, 64), c["w"][:1].expand(3, 64, 512)
         a, b = plan.grad(x, w, y), plan.grad(x.contiguous(), w.contiguous(), y)
         assert all(torch.equal(p, q) for p, q in zip(a, b) if p is not None)
+
+
+@pytest.mark.parametrize("bf16,rows,d,v", [(0, 40, 64, 60000), (1, 16, 64, 90001), (0, 140, 128, 16500), (1, 80, 200, 30007)])
+def test_a_vocabulary_in_pieces(bf16, rows, d, v):
+    # 64 replicas whose logits pass what one piece holds, with one W; few rows and many
+    torch = _torch()
+    c = _loss_case(1, rows, d, v, bf16, "whole", True)
+    y = c["y"].repeat(64, 1)
+    y[63] = torch.flip(y[63], dims=[0])
+    args = c["x"].expand(64, rows, d), c["w"].expand(64, d, v), y, c["bias"].expand(64, v)
+    args[0][0].nan_to_num_(nan=0.5, posinf=0.5)
+    loss, row, dx, dw, db = hadfl.ClassLoss(64, rows, d, v, bf16=bf16).grad(*args)
+    for k in (0, 63):
+        r, b = _loss_reference(dict(x=c["x"], w=c["w"], bias=c["bias"], yh=y[k:k + 1].cpu().numpy()), 0, bf16)
+        for name, got in (("row_loss", row), ("loss", loss), ("dx", dx), ("dw", dw), ("db", db)):
+            _check(_values(got[k]), r[name], b[name], name)
+    assert all(torch.equal(o[0], o[62]) for o in (loss, row, dx, dw, db))
 
 
 def test_large_logits_and_a_label_that_is_out():
@@ -368,7 +385,7 @@ def test_large_logits_and_a_label_that_is_out():
             assert torch.isinf(row[hit]).all() and torch.isfinite(row[~hit]).all()
 
 
-@pytest.mark.parametrize("rows", [20, 100, 300])
+@pytest.mark.parametrize("rows", [20, 100, 300, 600])
 @pytest.mark.parametrize("kind", ["columns", "far apart", "outlier"])
 def test_32_bit_operands_of_uneven_magnitude(rows, kind):
     # what enters the matrix products in parts of 16 bits: features whose x and W differ by opposite powers of two, tensors of extreme
@@ -400,7 +417,7 @@ def test_a_row_whose_mask_leaves_nothing():
     # are 1 / classes but for the label's; a row of -inf alone has no softmax, and its neighbours keep theirs
     torch = _torch()
     for bf16 in (0, 1):
-        for rows in (3, 100):
+        for rows in (3, 100, 600):
             g = torch.Generator(device="cuda").manual_seed(4)
             x = torch.randn((2, rows, 32), device="cuda", generator=g).to(_dtype(bf16))
             w = torch.randn((2, 32, 500), device="cuda", generator=g).to(_dtype(bf16))
