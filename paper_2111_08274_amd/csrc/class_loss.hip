@@ -6,6 +6,8 @@
 //   3. for every piece of the vocabulary: z again, G = exp(z - max) / sum - onehot into a buffer of [rows][piece], then
 //      dx += G W^T (shares of the contraction side by side, added in a fixed order) and dW = x^T G.
 // A row without a label has G = 0 and its x is read as zeros.
+#include <cmath>
+
 #include "direct_product.h"
 
 namespace hadfl {
@@ -125,12 +127,12 @@ template <bool EXACT, int BM, int BN, int WN> struct Statistics {
 
 // The pairs of a row's tiles joined: `shares` threads a row, each its tiles in ascending order, eight loads in flight; then the
 // shares pairwise.  Where one workgroup has all rows of a replica it also takes their mean (loss, factor; else null).
-__device__ __forceinline__ void mean_of_rows(float sum, int count, float* sums, int* counts, float* loss, float* factor)
+template <int NT> __device__ __forceinline__ void mean_of_rows(float sum, int count, float* sums, int* counts, float* loss, float* factor)
 {
     __syncthreads();
     sums[threadIdx.x] = sum;
     counts[threadIdx.x] = count;
-    for (int d = 128; d > 0; d /= 2) {
+    for (int d = NT / 2; d > 0; d /= 2) {
         __syncthreads();
         if (threadIdx.x < d) { sums[threadIdx.x] += sums[threadIdx.x + d]; counts[threadIdx.x] += counts[threadIdx.x + d]; }
     }
@@ -139,12 +141,13 @@ __device__ __forceinline__ void mean_of_rows(float sum, int count, float* sums, 
         *loss = counts[0] ? sums[0] / (float)counts[0] : 0.f;
     }
 }
-__global__ __launch_bounds__(256) void row_loss_kernel(const float2* part, const float* z_label, const int32_t* labels, int rows, int classes,
+template <int NT>
+__global__ __launch_bounds__(NT) void row_loss_kernel(const float2* part, const float* z_label, const int32_t* labels, int rows, int classes,
                                                        int parts, int shares, float2* norm, float* row_loss, float* loss, float* factor)
 {
     constexpr int U = 8;
-    __shared__ float2 got[256];
-    const int per = 256 / shares, r = threadIdx.x % per, share = threadIdx.x / per, k = blockIdx.y, t = blockIdx.x * per + r;
+    __shared__ float2 got[NT];
+    const int per = NT / shares, r = threadIdx.x % per, share = threadIdx.x / per, k = blockIdx.y, t = blockIdx.x * per + r;
     const float2* src = part + (long long)k * parts * rows + t;
     float2 have{-INFINITY, 0.f};
     if (t < rows)
@@ -176,9 +179,9 @@ __global__ __launch_bounds__(256) void row_loss_kernel(const float2* part, const
         row_loss[at] = value;
     }
     if (!loss) return;
-    __shared__ float sums[256];
-    __shared__ int counts[256];
-    mean_of_rows(value, live, sums, counts, loss + k, factor + k);
+    __shared__ float sums[NT];
+    __shared__ int counts[NT];
+    mean_of_rows<NT>(value, live, sums, counts, loss + k, factor + k);
 }
 
 // a replica's mean loss and the factor 1 / (labelled rows), 0 without any
@@ -194,44 +197,47 @@ __global__ __launch_bounds__(256) void mean_loss_kernel(const float* row_loss, c
         sum += row_loss[base + t];
         count += (unsigned)labels[base + t] < (unsigned)classes;
     }
-    mean_of_rows(sum, count, sums, counts, loss + blockIdx.x, factor + blockIdx.x);
+    mean_of_rows<256>(sum, count, sums, counts, loss + blockIdx.x, factor + blockIdx.x);
 }
 
-// Few rows: G of the whole vocabulary from its logits, 64 columns a workgroup, every fourth row a wave, and db.  32-bit G takes the
+// Few rows: G of the whole vocabulary from its logits, 64 columns a workgroup, its W waves taking the rows in turn, and db.  32-bit G takes the
 // logits' place.
-template <typename T>
-__global__ __launch_bounds__(256) void gradient_columns_kernel(const float* z, const int32_t* labels, const float2* norm, int rows, int classes, int ld,
+template <typename T, int W>
+__global__ __launch_bounds__(W * 64) void gradient_columns_kernel(const float* z, const int32_t* labels, const float2* norm, int rows, int classes, int ld,
                                                                T* g, const float* factor, float* db, long long db_rep)
 {
     constexpr int U = 8;                                       // rows at a time: their loads before the first store, which may be theirs
-    __shared__ float sums[4][64];
+    __shared__ float sums[W][64];
     const int wave = threadIdx.x >> 6, c = blockIdx.x * 64 + (threadIdx.x & 63), k = blockIdx.y;
     const long long first = (long long)k * rows;
     float sum = 0.f;
-    for (int t0 = wave; t0 < rows; t0 += 4 * U) {
+    for (int t0 = wave; t0 < rows; t0 += W * U) {
         float v[U];
         float2 l[U];
         int y[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const long long t = first + min(t0 + 4 * u, rows - 1);
+            const long long t = first + min(t0 + W * u, rows - 1);
             v[u] = z[t * ld + c];
             l[u] = norm[t];
             y[u] = labels[t];
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (t0 + 4 * u >= rows) break;
+            if (t0 + W * u >= rows) break;
             const bool live = (unsigned)y[u] < (unsigned)classes;
             const float p = live && c < classes ? exp_down(v[u] - l[u].x) * (1.f / l[u].y) - (c == y[u] ? 1.f : 0.f) : 0.f;
             sum += p;
-            g[(first + t0 + 4 * u) * ld + c] = (T)p;
+            g[(first + t0 + W * u) * ld + c] = (T)p;
         }
     }
     if (!db) return;
     sums[wave][threadIdx.x & 63] = sum;
     __syncthreads();
-    if (wave == 0 && c < classes) db[k * db_rep + c] = ((sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x])) * factor[k];
+    if (wave != 0 || c >= classes) return;
+#pragma unroll
+    for (int w = 1; w < W; ++w) sum += sums[w][threadIdx.x];
+    db[k * db_rep + c] = sum * factor[k];
 }
 
 // G of a piece, unscaled, and its column sums over a wave's rows
@@ -362,13 +368,10 @@ __global__ __launch_bounds__(256) void bias_grad_kernel(const float* sums, int b
 }
 
 // Which kernels, the piece of the vocabulary and the working memory, from the sizes alone.
-//   few rows   the products through registers read W as it is, 32 or 64 x 128 tiles
+//   few rows   the products through registers read W as it is, 32 or 64 x 128 tiles, the logits' contraction in shares where there are
+//              few of them
 //   more       products straight from memory to LDS: twice to three times the rate, but x (unlabelled rows as zeros) and a W of 32-bit or
-//              unaligned values are laid out first, and there are more launches.  Rows from which that is faster, with W of E values
-//              in all: 16 + 1.0e9 / E for a bf16 W that can be read as it is (4 x 512 x 32000: at 32 rows 126 us against 149), 30 + 1.3e9 / E for
-//              one that cannot (32001 classes: at 48 rows 180 against 192; 1 x 1024 x 10007: at 160 rows 80 against 79), 90 + 2.4e9 / E for
-//              32 bits (4 x 512 x 32000: at 128 rows 541 against 593; 1 x 1024 x 10007: at 256 rows 183 against 169, at 384 211 against
-//              219); small W 200 or 400 rows later at most (1 x 256 x 2003: at 256 rows 44 against 46)
+//              unaligned values are laid out first, there are more launches, and few tiles leave most of the chip idle
 struct Plan {
     bool direct, small;            // small: 32 rows a tile, not 64
     int bm, bn, wave_m, parts, z_splits, z_len, piece, pieces, blocks, splits, split_len, w_tile, w_splits, w_len, ldx, planes;
@@ -377,19 +380,47 @@ struct Plan {
 // of G, and of a laid-out piece of W: a 32-bit W of more than one piece is laid out again for the gradient (16 x 699 x 576 x 9056: 2.36 ms
 // with 256 MiB, 2.10 with 512 and 1024; bf16 the same with each)
 constexpr long long kPieceBytes = 512ll << 20;
-constexpr long long kSharedW = 48ll << 20;
 
 int up_to(long long v, int unit) { return (int)((v + unit - 1) / unit * unit); }
 // tiles 128 wide in this direction, not 256: they are 15 to 20 % slower for the work they hold (2 x 4096 x 2048 x 65536 bf16: dx 2.14 ms
 // against 1.87, dW 2.13 against 1.86), and 256 wide ones hold up to twice the work
 bool narrow(int v) { return 1.18 * up_to(v, 128) < up_to(v, 256); }
 
+// Rows up to which W is read as it is: more where W is small, and where its features are many for its tiles.  Loss and gradients through
+// registers / laid out, us:
+//   bf16             4 x 512 x 32000, 48 rows 140 / 132; 2048 x 20000, 64 rows 99 / 102, 96 rows 123 / 107; 4096 x 10008, 128 rows 130 / 141,
+//                    192 rows 172 / 156; 2048 x 5000, 192 rows 79 / 85
+//   bf16, unaligned  16 x 256 x 10007, 128 rows 172 / 176, 192 rows 278 / 217; 8 x 200 x 4099, 192 rows 77 / 87, 256 rows 94 / 91; 4096 x 10007,
+//                    192 rows 175 / 189, 256 rows 220 / 201
+//   fp32             4 x 512 x 32000, 128 rows 482 / 550, 192 rows 690 / 669; 2048 x 20000, 192 rows 396 / 485, 256 rows 558 / 507; 8 x 200 x 4099,
+//                    256 rows 159 / 183, 384 rows 203 / 205
+double few_rows(int n, int features, int classes, int bf16)
+{
+    const double values = (double)n * features * classes, deep = std::min(250., features / ((double)n * classes / 256));
+    if (!bf16) return 165 + std::min(300., 1.6e9 / values) + 0.4 * deep;
+    return (classes % 8 ? 85 + std::min(200., 0.6e9 / values) : 16 + std::min(200., 0.7e9 / values)) + 1.2 * deep;
+}
+
+// Into how many shares the logits' contraction over few rows is cut.  A workgroup, of 128 classes, takes 12 ns a feature (bf16 W, 32 rows; 24:
+// 64 rows) or 35 (fp32; 43), three of them share a compute unit, and together they read W at 5 TB/s at best; shares cost a launch and
+// their bytes.  One row, 4096 x 10007 fp32: one share 142 us, eight 42; 2048 x 5000: 75 and 21; 512 x 32000, two: 26 and 24, and one is taken.
+int logit_shares(const Plan& p, int n, int rows, int features, int classes, int bf16)
+{
+    const double groups = (double)n * p.parts * ((rows + p.bm - 1) / p.bm), feature = (bf16 ? (p.small ? 12 : 24) : p.small ? 35 : 43) * 1e-9;
+    const double read = (double)n * features * classes * (bf16 ? 2 : 4) / 5e12;
+    int best = 1;
+    double least = 0;
+    for (int s = 1; s <= 32 && (s == 1 || features / s >= 128); ++s) {
+        const double cost = std::max(std::ceil(groups * s / 768) * features / s * feature, read) + (s > 1 ? 4e-6 + (double)n * rows * p.piece * 4 * (2 * s + 1) / 4e12 : 0);
+        if (s == 1 || cost < (best == 1 ? 0.9 : 1) * least) { best = s; least = cost; }
+    }
+    return best;
+}
+
 Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
 {
     Plan p{};
-    const double values = (double)n * features * classes;
-    const double from = bf16 ? (classes % 8 == 0 ? 16 + std::min(200., 1.0e9 / values) : 30 + std::min(200., 1.3e9 / values)) : 90 + std::min(400., 2.4e9 / values);
-    p.direct = rows > from || (rows && std::min(features, classes) < 8);         // fewer values a row than a chunk: laid out
+    p.direct = rows > few_rows(n, features, classes, bf16) || (rows && std::min(features, classes) < 8);       // fewer values a row than a chunk: laid out
     p.small = rows <= 32;
     p.bm = p.small ? 32 : 64;
     p.bn = 128;
@@ -424,11 +455,7 @@ Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
     p.w_splits = p.direct && p.w_tile == 256 ? best_shares(dw_tiles, (rows + kSlab - 1) / kSlab * products, (double)n * features * p.piece * 4) : 1;
     p.w_len = up_to((rows + p.w_splits - 1) / p.w_splits, 64);
     if (rows) p.w_splits = (rows + p.w_len - 1) / p.w_len;
-    // few rows, a large W in one piece: its contraction in shares of at least 128 features, for some 4096 workgroups
-    p.z_splits = 1;
-    const long long w_tiles = (long long)n * p.parts;
-    if (!p.direct && p.pieces == 1 && (long long)n * features * classes * (bf16 ? 2 : 4) >= kSharedW)
-        p.z_splits = (int)std::max<long long>(1, std::min<long long>(4096 / w_tiles, features / 128));
+    p.z_splits = !p.direct && p.pieces == 1 ? logit_shares(p, n, rows, features, classes, bf16) : 1;
     p.z_len = up_to((features + p.z_splits - 1) / p.z_splits, 128);
     p.z_splits = (features + p.z_len - 1) / p.z_len;
     size_t at = 0;
@@ -477,10 +504,16 @@ hipError_t join_rows(const LossArgs& a, const Plan& p, const Work& w, hipStream_
     int per = 256;                                             // rows a workgroup
     while (per > 4 && per / 2 >= a.rows) per /= 2;
     while (per > 32 && p.parts >= 2048 / per) per /= 2;
-    const bool alone = a.rows <= per;
+    int all = 4;                                               // one workgroup of 1024 for a replica's rows, sixteen pairs a thread at most: 4.6 us less
+    while (all < a.rows) all *= 2;
+    const bool large = a.rows > per && all <= 1024 && (long long)all * p.parts <= 16384, alone = large || a.rows <= per;
     if (a.rows) {
-        row_loss_kernel<<<dim3((unsigned)((a.rows + per - 1) / per), (unsigned)a.n), 256, 0, s>>>(
-            w.part, w.z_label, a.labels, a.rows, a.classes, p.parts, 256 / per, w.norm, w.row_loss, alone ? a.loss : nullptr, w.factor);
+        if (large)
+            row_loss_kernel<1024><<<dim3(1, (unsigned)a.n), 1024, 0, s>>>(w.part, w.z_label, a.labels, a.rows, a.classes, p.parts, 1024 / all, w.norm,
+                                                                          w.row_loss, a.loss, w.factor);
+        else
+            row_loss_kernel<256><<<dim3((unsigned)((a.rows + per - 1) / per), (unsigned)a.n), 256, 0, s>>>(
+                w.part, w.z_label, a.labels, a.rows, a.classes, p.parts, 256 / per, w.norm, w.row_loss, alone ? a.loss : nullptr, w.factor);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess || alone) return e;
     }
@@ -525,8 +558,9 @@ template <typename T, int BM, int WM, int WN> hipError_t run_general(const LossA
         const Source<T> w = source<T>(Rows{(T*)a.w.p + c0, a.w.rep, a.w.row}, a.features, cols);
         const Source<T> g = source<T>(Rows{k.g, (long long)a.rows * ld, ld}, a.rows, ld);            // zero beyond cols
         if (once) {
-            gradient_columns_kernel<T><<<dim3((unsigned)(ld / 64), (unsigned)a.n), 256, 0, s>>>(
-                k.z, a.labels, k.norm, a.rows, a.classes, ld, (T*)k.g, k.factor, (float*)a.db.p, a.db.rep);
+            const dim3 grid((unsigned)(ld / 64), (unsigned)a.n);
+            if (a.rows <= 64) gradient_columns_kernel<T, 4><<<grid, 256, 0, s>>>(k.z, a.labels, k.norm, a.rows, a.classes, ld, (T*)k.g, k.factor, (float*)a.db.p, a.db.rep);
+            else gradient_columns_kernel<T, 16><<<grid, 1024, 0, s>>>(k.z, a.labels, k.norm, a.rows, a.classes, ld, (T*)k.g, k.factor, (float*)a.db.p, a.db.rep);
             e = hipGetLastError();
         } else if (a.rows) {
             const Softmax<exact> soft{bias, a.bias.rep, a.labels, k.norm, a.db.p ? k.sums : nullptr, a.rows, c0, a.classes, ld, p.blocks};

@@ -41,38 +41,36 @@ __global__ __launch_bounds__(256) void join_logits_kernel(const float* share, in
     __shared__ float tops[4][4], sums[4][4];
     const int tile = blockIdx.x, k = blockIdx.y, tid = threadIdx.x, lane = tid & 63, pair = tid >> 7, c = tile * 128 + (tid & 127);
     const float b = bias && c < classes ? bias[k * bias_rep + c] : 0.f;
-    for (int m0 = 0; m0 < rows; m0 += 8) {                     // eight rows at a time, four a half of the workgroup
-        float v[4];
+    const int m0 = blockIdx.z * 8;                             // eight rows a workgroup, four a half of it
+    float v[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const long long at = ((long long)k * rows + min(m0 + 2 * u + pair, rows - 1)) * ld + c;
-            v[u] = 0.f;
+    for (int u = 0; u < 4; ++u) {
+        const long long at = ((long long)k * rows + min(m0 + 2 * u + pair, rows - 1)) * ld + c;
+        v[u] = 0.f;
 #pragma unroll 4
-            for (int s = 0; s < splits; ++s) v[u] += share[s * step + at];
-            v[u] = c < classes ? v[u] + b : -INFINITY;
-            const float top = max_over<64>(v[u]);
-            if (lane == 0) tops[tid >> 6][u] = top;
-        }
-        __syncthreads();
+        for (int s = 0; s < splits; ++s) v[u] += share[s * step + at];
+        v[u] = c < classes ? v[u] + b : -INFINITY;
+        const float top = max_over<64>(v[u]);
+        if (lane == 0) tops[tid >> 6][u] = top;
+    }
+    __syncthreads();
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const float top = __builtin_fmaxf(tops[2 * pair][u], tops[2 * pair + 1][u]), base = top == -INFINITY ? 0.f : top;
-            const float sum = sum_over<64>(__builtin_amdgcn_exp2f((v[u] - base) * kLog2e));
-            if (lane == 0) sums[tid >> 6][u] = sum;
-        }
-        __syncthreads();
+    for (int u = 0; u < 4; ++u) {
+        const float top = __builtin_fmaxf(tops[2 * pair][u], tops[2 * pair + 1][u]), base = top == -INFINITY ? 0.f : top;
+        const float sum = sum_over<64>(__builtin_amdgcn_exp2f((v[u] - base) * kLog2e));
+        if (lane == 0) sums[tid >> 6][u] = sum;
+    }
+    __syncthreads();
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int m = m0 + 2 * u + pair;
-            if (m >= rows) continue;
-            const long long line = (long long)k * rows + m;
-            z[line * ld + c] = v[u];
-            if (c < classes && labels[line] == c) z_label[line] = v[u];
-            if ((tid & 127) == 0)
-                part[((long long)k * tiles + tile) * rows + m] =
-                    float2{__builtin_fmaxf(tops[2 * pair][u], tops[2 * pair + 1][u]), sums[2 * pair][u] + sums[2 * pair + 1][u]};
-        }
-        __syncthreads();
+    for (int u = 0; u < 4; ++u) {
+        const int m = m0 + 2 * u + pair;
+        if (m >= rows) continue;
+        const long long line = (long long)k * rows + m;
+        z[line * ld + c] = v[u];
+        if (c < classes && labels[line] == c) z_label[line] = v[u];
+        if ((tid & 127) == 0)
+            part[((long long)k * tiles + tile) * rows + m] =
+                float2{__builtin_fmaxf(tops[2 * pair][u], tops[2 * pair + 1][u]), sums[2 * pair][u] + sums[2 * pair + 1][u]};
     }
 }
 
@@ -137,8 +135,8 @@ template <typename T, int TR> hipError_t weights(const LossArgs& a, const T* g, 
 hipError_t launch_join_logits(const LossArgs& a, float* share, int splits, int ld, float2* part, float* z_label, hipStream_t s)
 {
     const int tiles = (a.classes + 127) / 128;
-    join_logits_kernel<<<dim3((unsigned)tiles, (unsigned)a.n), 256, 0, s>>>(share, splits, (long long)a.n * a.rows * ld, (const float*)a.bias.p, a.bias.rep,
-                                                                            a.labels, a.rows, a.classes, ld, tiles, part, z_label, share);
+    join_logits_kernel<<<dim3((unsigned)tiles, (unsigned)a.n, (unsigned)((a.rows + 7) / 8)), 256, 0, s>>>(
+        share, splits, (long long)a.n * a.rows * ld, (const float*)a.bias.p, a.bias.rep, a.labels, a.rows, a.classes, ld, tiles, part, z_label, share);
     return hipGetLastError();
 }
 template <typename T> hipError_t launch_few_weights(const LossArgs& a, const T* g, int ld, const float* factor, hipStream_t s)
