@@ -364,7 +364,7 @@ HADFL_API hadfl_status hadfl_dense_grad_packed(const hadfl_dense *dense, const v
  * (whatever its x holds), and its dx is zero.  A replica without labelled rows has loss zero and zero gradients.  A bias of
  * -inf takes a class out.  With G = (softmax(z) - onehot(label)) / (number of labelled rows):
  *   dx = G W^T,  dW = x^T G,  db = sum_t G.
- * fp32: operands enter the matrix products in parts of 16 bits whose products are summed in 32 bits: with few rows (165 a
+ * fp32: operands enter the matrix products in parts of 16 bits whose products are summed in 32 bits: with few rows (300 a
  * replica, more the smaller w is) three bf16 parts (six products, whole for magnitudes from 2^-107 on), beyond two fp16 parts (three products) scaled by a power of two to
  * the replica's largest finite magnitude: a product is off by at most 2^-20 of itself, 2^-23.5 in the mean square, for
  * magnitudes down to 2^-29 of the largest.  bf16: softmax(z) - onehot is rounded to bf16 for the two products, db is formed before that.

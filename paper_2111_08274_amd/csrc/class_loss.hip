@@ -368,7 +368,7 @@ __global__ __launch_bounds__(256) void bias_grad_kernel(const float* sums, int b
 }
 
 // Which kernels, the piece of the vocabulary and the working memory, from the sizes alone.
-//   few rows   the products through registers read W as it is, 32 or 64 x 128 tiles, the logits' contraction in shares where there are
+//   few rows   the products through registers read W as it is, 32, 64 or 128 x 128 tiles, the logits' contraction in shares where there are
 //              few of them
 //   more       products straight from memory to LDS: twice to three times the rate, but x (unlabelled rows as zeros) and a W of 32-bit or
 //              unaligned values are laid out first, there are more launches, and few tiles leave most of the chip idle
@@ -388,17 +388,17 @@ bool narrow(int v) { return 1.18 * up_to(v, 128) < up_to(v, 256); }
 
 // Rows up to which W is read as it is: more where W is small, and where its features are many for its tiles.  Loss and gradients through
 // registers / laid out, us:
-//   bf16             4 x 512 x 32000, 48 rows 140 / 132; 2048 x 20000, 64 rows 99 / 102, 96 rows 123 / 107; 4096 x 10008, 128 rows 130 / 141,
-//                    192 rows 172 / 156; 2048 x 5000, 192 rows 79 / 85
-//   bf16, unaligned  16 x 256 x 10007, 128 rows 172 / 176, 192 rows 278 / 217; 8 x 200 x 4099, 192 rows 77 / 87, 256 rows 94 / 91; 4096 x 10007,
-//                    192 rows 175 / 189, 256 rows 220 / 201
-//   fp32             4 x 512 x 32000, 128 rows 482 / 550, 192 rows 690 / 669; 2048 x 20000, 192 rows 396 / 485, 256 rows 558 / 507; 8 x 200 x 4099,
-//                    256 rows 159 / 183, 384 rows 203 / 205
+//   bf16             4 x 512 x 32000, 64 rows 135 / 136, 96 rows 159 / 141; 2048 x 20000, 96 rows 102 / 105, 128 rows 115 / 107; 4096 x 10008,
+//                    256 rows 155 / 163, 320 rows 223 / 180; 2048 x 5000, 256 rows 79 / 86, 320 rows 93 / 91
+//   bf16, unaligned  4 x 512 x 32001, 128 rows 182 / 205, 160 rows 305 / 251; 2048 x 20011, 256 rows 165 / 187, 320 rows 246 / 204; 8 x 200 x 4099,
+//                    256 rows 82 / 89, 320 rows 97 / 88
+//   fp32             4 x 512 x 32000, 256 rows 700 / 713, 320 rows 952 / 890; 2048 x 20011, 256 rows 458 / 510, 320 rows 582 / 566; 8 x 200 x 4099,
+//                    256 rows 146 / 180, 384 rows 190 / 195
 double few_rows(int n, int features, int classes, int bf16)
 {
-    const double values = (double)n * features * classes, deep = std::min(250., features / ((double)n * classes / 256));
-    if (!bf16) return 165 + std::min(300., 1.6e9 / values) + 0.4 * deep;
-    return (classes % 8 ? 85 + std::min(200., 0.6e9 / values) : 16 + std::min(200., 0.7e9 / values)) + 1.2 * deep;
+    const double values = (double)n * features * classes, deep = std::min(125., features / ((double)n * classes / 256));
+    if (!bf16) return 300 + std::min(165., 1.0e9 / values) + 0.4 * deep;
+    return (classes % 8 ? 128 + std::min(100., 0.6e9 / values) : 30 + std::min(200., 0.7e9 / values)) + 2 * deep;
 }
 
 // Into how many shares the logits' contraction over few rows is cut.  A workgroup, of 128 classes, takes 12 ns a feature (bf16 W, 32 rows; 24:
@@ -422,7 +422,8 @@ Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
     Plan p{};
     p.direct = rows > few_rows(n, features, classes, bf16) || (rows && std::min(features, classes) < 8);       // fewer values a row than a chunk: laid out
     p.small = rows <= 32;
-    p.bm = p.small ? 32 : 64;
+    // 128 rows a tile where they hold no more than 64 do (16 x 256 x 10007 fp32, 96 rows 263 us against 290, 132 rows 419 against 410)
+    p.bm = p.small ? 32 : rows <= 64 || up_to(rows, 128) > up_to(rows, 64) ? 64 : 128;
     p.bn = 128;
     if (p.direct) {                // smaller tiles where larger ones would leave half of the chip without one
         auto tiles = [&](int m, int n_) { return (long long)n * ((rows + m - 1) / m) * ((classes + n_ - 1) / n_); };
@@ -430,7 +431,7 @@ Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
         p.bn = p.bm == 128 && tiles(128, 256) < 128 ? 128 : 256;
     }
     const int bn = p.bn;
-    p.wave_m = p.direct ? p.bm / 2 : 32;
+    p.wave_m = p.direct || p.bm == 128 ? p.bm / 2 : 32;
     p.planes = p.direct && !bf16 ? 2 : 1;
     p.parts = up_to(classes, bn) / bn;
     p.blocks = up_to(rows, p.bm) / p.wave_m;
@@ -577,8 +578,13 @@ template <typename T, int BM, int WM, int WN> hipError_t run_general(const LossA
             if ((e = launch_few_weights<T>(a, (const T*)k.g, ld, k.factor, s)) != hipSuccess) return e;
         } else if (a.dw.p) {
             const StoreTile<T> store{(T*)a.dw.p + c0, a.dw.rep, a.dw.row, k.factor, a.features, cols, nullptr, 0};
-            e = launch_product<64, 64, 2, 2, false, false>(source<T, true>(a.x, a.rows, a.features, live), g, a.n, a.features, cols, a.rows, 1,
-                                                             std::max(1, a.rows), store, s);
+            // 128 x 128 tiles where they give every compute unit four (16 x 256 x 10007 fp32, 96 rows: 246 us in all against 257), else 64 x 128 (2 x 1024 x
+            // 4099: 92 against 94)
+            const Source<T, true> xt = source<T, true>(a.x, a.rows, a.features, live);
+            if ((long long)a.n * ((a.features + 127) / 128) * ((cols + 127) / 128) >= 1024)
+                e = launch_product<128, 128, 2, 4, false, false>(xt, g, a.n, a.features, cols, a.rows, 1, std::max(1, a.rows), store, s);
+            else
+                e = launch_product<64, 128, 2, 4, false, false>(xt, g, a.n, a.features, cols, a.rows, 1, std::max(1, a.rows), store, s);
             if (e != hipSuccess) return e;
         }
     }
@@ -672,8 +678,9 @@ hipError_t launch_loss(const LossArgs& a, hipStream_t s)
         if (a.bf16) return p.bm == 256 ? run_direct<__bf16, 256, 256, 4>(a, p, s) : p.bn == 256 ? run_direct<__bf16, 128, 256, 4>(a, p, s) : run_direct<__bf16, 128, 128, 4>(a, p, s);
         return p.bm == 256 ? run_direct<float, 256, 256, 4>(a, p, s) : p.bn == 256 ? run_direct<float, 128, 256, 4>(a, p, s) : run_direct<float, 128, 128, 4>(a, p, s);
     }
-    if (a.bf16) return p.small ? run_general<__bf16, 32, 1, 4>(a, p, s) : run_general<__bf16, 64, 2, 2>(a, p, s);
-    return p.small ? run_general<float, 32, 1, 4>(a, p, s) : run_general<float, 64, 2, 2>(a, p, s);
+    if (p.bm == 128) return a.bf16 ? run_general<__bf16, 128, 2, 4>(a, p, s) : run_general<float, 128, 2, 4>(a, p, s);
+    if (a.bf16) return p.small ? run_general<__bf16, 32, 1, 4>(a, p, s) : run_general<__bf16, 64, 2, 4>(a, p, s);
+    return p.small ? run_general<float, 32, 1, 4>(a, p, s) : run_general<float, 64, 2, 4>(a, p, s);
 }
 
 }  // namespace head

@@ -11,33 +11,37 @@ namespace head {
 namespace {
 
 struct Plan {
-    bool direct, big;              // big: 256 x 256 tiles, else 128 x 128; not direct: 64 x 64
+    bool direct, big;              // big: 256 x 256 tiles, else 128 x 128; not direct: 128 x 128, else 64 x 64
     int ldx, ldy, planes, splits, split_len;
     size_t x, y, share, total;
 };
 
 // Laying out costs 3 bytes a value of x (and 10 of a 32-bit dy, which its three planes have to win back over in x out products) and two
-// launches; the product after it runs at two to three times the rate.  Through registers / laid out, us:
-//   bf16   16 x 512 x 512, 1024 rows 30 / 31, 2048 rows 53 / 42; 4096 x 4096, 256 rows 31 / 35, 512 rows 50 / 41; 784 x 128, 16384 rows 55 / 60;
-//          8 x 784 x 130, where the larger tiles would be more than half empty, 16384 rows 153 / 191
-//   fp32   2048 x 2048, 1024 rows 49 / 54, 2048 rows 93 / 89, 8192 rows 354 / 300; 4096 x 4096, 512 rows 85 / 73; 16 x 512 x 512, 8192 rows
-//          388 / 446; 2 x 128 x 4096, 8192 rows 105 / 213
+// launches; the product after it is faster where there are enough rows and tiles.  Through registers / laid out, us:
+//   bf16   16 x 512 x 512, 1024 rows 25 / 31, 2048 rows 45 / 44, 8192 rows 141 / 138; 2048 x 2048, 1024 rows 25 / 25, 2048 rows 44 / 36;
+//          4096 x 4096, 512 rows 35 / 41, 2048 rows 110 / 87; 784 x 128, 16384 rows 50 / 60; 8 x 784 x 130, where the larger tiles would be
+//          more than half empty, 16384 rows 114 / 191
+//   fp32   2048 x 2048, 2048 rows 76 / 89, 8192 rows 241 / 300; 4096 x 4096, 512 rows 65 / 73, 2048 rows 242 / 207; 16 x 1024 x 1024, 8192 rows
+//          956 / 1072; 2 x 128 x 4096, 8192 rows 105 / 213
+// Through registers 128 x 128 tiles of eight waves convert and read half of what 64 x 64 tiles do (4096 x 4096 bf16, 512 rows 35 us against 50), which
+// take few tiles (2 x 128 x 4096 fp32, 128 rows: 7 against 10).
 Plan plan_of(int n, int rows, int in, int out, int bf16)
 {
     Plan p{};
     auto tiles = [&](int t) { return (long long)n * ((in + t - 1) / t) * ((out + t - 1) / t); };
     const double work = (double)n * rows * in * out;
-    p.big = tiles(256) >= 192;
-    p.direct = bf16 ? work >= 4e9 && tiles(128) * 4 <= tiles(64) * 1.3 : work >= 8e9 && (p.big || (double)in * out >= 100. * (3. * in + 10. * out));
+    p.direct = bf16 ? rows >= 1536 && work >= 2e9 && tiles(128) >= 48 && tiles(128) * 4 <= tiles(64) * 1.3
+                    : rows >= 1024 && tiles(256) >= 192 && (double)in * out >= 250. * (3. * in + 10. * out);
     p.direct = p.direct || (rows && out < 8);                  // fewer values a row than a chunk: laid out
     p.ldx = (in + 7) / 8 * 8;
     p.ldy = (out + 7) / 8 * 8;
     p.planes = bf16 ? 1 : 3;
-    // few tiles: the rows in shares that a second launch adds, for some three workgroups a compute unit; where there is one without them, of
-    // 1024 rows at least (300 x 5000 bf16: 1024 rows in one share 19 us, in three 28; 8192 rows 150 and 112)
-    const long long have = tiles(64);
+    p.big = p.direct ? tiles(256) >= 192 : tiles(128) >= 192 || (rows >= 4096 && tiles(128) >= 100);
+    // few tiles: the rows in shares that a second launch adds, for what the compute units hold at a time; where each has a workgroup without
+    // them, of 1024 rows at least (300 x 5000 bf16: 1024 rows in one share 19 us, in three 28; 8192 rows 150 and 112)
+    const long long have = p.big ? tiles(128) : tiles(64), most = p.big && have >= 256 ? 512 : 768;
     p.splits = p.direct ? best_shares(tiles(p.big ? 256 : 128), (rows + kSlab - 1) / kSlab * p.planes, (double)n * in * out * 4)
-                        : (int)std::max<long long>(1, std::min<long long>((768 + have - 1) / have, rows / (have < 256 ? 256 : 1024)));
+                        : (int)std::max<long long>(1, std::min<long long>((most + have - 1) / have, rows / (have < 256 ? 256 : 1024)));
     p.split_len = (((rows + p.splits - 1) / p.splits) + 63) / 64 * 64;
     p.splits = std::max(1, (rows + p.split_len - 1) / std::max(1, p.split_len));
     if (p.direct) {
@@ -52,9 +56,13 @@ Plan plan_of(int n, int rows, int in, int out, int bf16)
 template <typename T, class Store> hipError_t product(const DenseArgs& a, const Plan& p, const Store& store, hipStream_t s)
 {
     constexpr int PL = sizeof(T) == 4 ? 3 : 1;
-    if (!p.direct)
-        return launch_product<64, 64, 2, 2, false, false>(SourcePacked{a.x, a.rows, a.in}, source<T>(a.dy, a.rows, a.out), a.n, a.in, a.out, a.rows,
-                                                          p.splits, std::max(1, p.split_len), store, s);
+    if (!p.direct) {
+        const SourcePacked x{a.x, a.rows, a.in};
+        const Source<T> dy = source<T>(a.dy, a.rows, a.out);
+        const int len = std::max(1, p.split_len);
+        if (p.big) return launch_product<128, 128, 2, 4, false, false>(x, dy, a.n, a.in, a.out, a.rows, p.splits, len, store, s);
+        return launch_product<64, 64, 2, 2, false, false>(x, dy, a.n, a.in, a.out, a.rows, p.splits, len, store, s);
+    }
     __bf16 *wx = (__bf16*)((char*)a.work + p.x), *wy = (__bf16*)((char*)a.work + p.y);
     hipError_t e = launch_unpack(a.n, a.rows, a.in, 1, a.x.q, Rows{wx, (long long)a.rows * p.ldx, p.ldx}, s);
     if (e != hipSuccess) return e;

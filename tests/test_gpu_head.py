@@ -346,7 +346,7 @@ def test_one_x_or_one_w_for_all_replicas():
         assert all(torch.equal(p, q) for p, q in zip(a, b) if p is not None)
 
 
-@pytest.mark.parametrize("bf16,rows,d,v", [(0, 40, 64, 60000), (1, 16, 64, 90001), (0, 140, 128, 16500), (1, 80, 200, 30007), (0, 200, 128, 16500), (1, 100, 200, 30007)])
+@pytest.mark.parametrize("bf16,rows,d,v", [(0, 40, 64, 60000), (1, 16, 64, 90001), (0, 140, 128, 16500), (1, 80, 200, 30007), (0, 200, 128, 16500), (1, 100, 200, 30007), (0, 330, 128, 16500), (1, 250, 200, 20007)])
 def test_a_vocabulary_in_pieces(bf16, rows, d, v):
     # 64 replicas whose logits pass what one piece holds, with one W; few rows and many
     torch = _torch()
