@@ -18,9 +18,9 @@ struct Plan {
 
 // Laying out costs 3 bytes a value of x (and 10 of a 32-bit dy, which its three planes have to win back over in x out products) and two
 // launches; the product after it is faster where there are enough rows and tiles.  Through registers / laid out, us:
-//   bf16   16 x 512 x 512, 1024 rows 25 / 31, 2048 rows 45 / 44, 8192 rows 141 / 138; 2048 x 2048, 1024 rows 25 / 25, 2048 rows 44 / 36;
-//          4096 x 4096, 512 rows 35 / 41, 2048 rows 110 / 87; 784 x 128, 16384 rows 50 / 60; 8 x 784 x 130, where the larger tiles would be
-//          more than half empty, 16384 rows 114 / 191
+//   bf16   packed and multiplied once, operands from memory: 16 x 512 x 512, 512 rows 33 / 33, 1024 rows 52 / 41; 2048 x 2048, 512 rows 29 / 27,
+//          1024 rows 44 / 33; 2 x 2048 x 2048, 1024 rows 51 / 54.  Again and again: 2048 x 2048, 2048 rows 44 / 36; 4096 x 4096, 2048 rows
+//          110 / 87; 784 x 128, 16384 rows 50 / 60; 8 x 784 x 130, where the larger tiles would be more than half empty, 16384 rows 114 / 191
 //   fp32   2048 x 2048, 2048 rows 76 / 89, 8192 rows 241 / 300; 4096 x 4096, 512 rows 65 / 73, 2048 rows 242 / 207; 16 x 1024 x 1024, 8192 rows
 //          956 / 1072; 2 x 128 x 4096, 8192 rows 105 / 213
 // Through registers 128 x 128 tiles of eight waves convert and read half of what 64 x 64 tiles do (4096 x 4096 bf16, 512 rows 35 us against 50), which
@@ -30,7 +30,7 @@ Plan plan_of(int n, int rows, int in, int out, int bf16)
     Plan p{};
     auto tiles = [&](int t) { return (long long)n * ((in + t - 1) / t) * ((out + t - 1) / t); };
     const double work = (double)n * rows * in * out;
-    p.direct = bf16 ? rows >= 1536 && work >= 2e9 && tiles(128) >= 48 && tiles(128) * 4 <= tiles(64) * 1.3
+    p.direct = bf16 ? rows >= 768 && work >= 2e9 && tiles(128) >= 48 && tiles(128) * 4 <= tiles(64) * 1.3
                     : rows >= 1024 && tiles(256) >= 192 && (double)in * out >= 250. * (3. * in + 10. * out);
     p.direct = p.direct || (rows && out < 8);                  // fewer values a row than a chunk: laid out
     p.ldx = (in + 7) / 8 * 8;
