@@ -1,8 +1,8 @@
 // The loss over a large vocabulary for few rows (a token, a small batch), where what counts is to stream W and dW.
-//   logits   a W of many bytes is contracted in shares, so that thousands of short workgroups stream it evenly (as one workgroup a column of
-//            tiles, the last ones to run leave most of the chip idle); the shares are added here
-//   dW       plain multiply-adds in 32 bits: a lane holds G of its classes for all rows and writes one feature after another, whole
-//            lines at a time, with no operand brought into a matrix instruction's layout
+//   logits   where W has many features for its classes it is contracted in shares (one workgroup a column of tiles would walk down all of
+//            its features: 4096 x 10007 fp32, one row, 142 us against 42); the shares are added here
+//   dW       up to eight rows by plain multiply-adds in 32 bits: a lane holds G of its classes for all rows and writes one feature after
+//            another, whole lines at a time, with no operand brought into a matrix instruction's layout
 #include "head.h"
 
 namespace hadfl {
@@ -34,7 +34,7 @@ template <> struct Four<__bf16> {
 };
 
 // Logits from the shares of their contraction, [splits][replicas][rows][ld], 128 classes a workgroup, with the bias, into [replicas][rows][ld]
-// (the first share's place), and their statistics.
+// (the first share's place), and their statistics.  Eight rows a workgroup: 128 rows x 10007 classes in eight shares 8.9 us, latency.
 __global__ __launch_bounds__(256) void join_logits_kernel(const float* share, int splits, long long step, const float* bias, long long bias_rep,
                                                           const int32_t* labels, int rows, int classes, int ld, int tiles, float2* part, float* z_label, float* z)
 {
@@ -75,9 +75,10 @@ __global__ __launch_bounds__(256) void join_logits_kernel(const float* share, in
 }
 
 // dW of 256 classes and kDepth features a workgroup: a lane holds G of four classes and all rows, and writes the classes' values of one feature
-// after another; x, transposed, from LDS, the same address for a wave.
-constexpr int kDepth = 32;
-template <typename T, int TR>
+// after another; x, transposed, from LDS, the same address for a wave.  Bound by the stores: 4 x 512 x 32000 fp32, 8 rows, 54 us = 4.8 TB/s (the
+// product on the matrix cores 67), bf16 27 us (34); at 16 rows the multiply-adds take as long as the stores, and the product is no slower.
+constexpr int kDepth = 32, TR = kFewWeights;
+template <typename T>
 __global__ __launch_bounds__(256) void few_weights_kernel(const T* x, long long x_rep, long long x_row, const int32_t* labels, const T* g, int ld, int rows,
                                                           int features, int classes, int tiles, int blocks, int total, const float* factor, T* dw,
                                                           long long dw_rep, long long dw_row)
@@ -120,28 +121,23 @@ __global__ __launch_bounds__(256) void few_weights_kernel(const T* x, long long 
     }
 }
 
-template <typename T, int TR> hipError_t weights(const LossArgs& a, const T* g, int ld, const float* factor, hipStream_t s)
+}  // namespace
+
+template <typename T> hipError_t launch_few_weights(const LossArgs& a, const T* g, int ld, const float* factor, hipStream_t s)
 {
     const int tiles = (a.classes + 255) / 256, blocks = (a.features + kDepth - 1) / kDepth;
     const long long total = (long long)a.n * tiles * blocks;
     if (total > 0x7fffff00ll) return hipErrorInvalidValue;
-    few_weights_kernel<T, TR><<<die_grid(total), 256, 0, s>>>((const T*)a.x.p, a.x.rep, a.x.row, a.labels, g, ld, a.rows, a.features, a.classes, tiles, blocks,
-                                                              (int)total, factor, (T*)a.dw.p, a.dw.rep, a.dw.row);
+    few_weights_kernel<T><<<die_grid(total), 256, 0, s>>>((const T*)a.x.p, a.x.rep, a.x.row, a.labels, g, ld, a.rows, a.features, a.classes, tiles, blocks,
+                                                          (int)total, factor, (T*)a.dw.p, a.dw.rep, a.dw.row);
     return hipGetLastError();
 }
-
-}  // namespace
-
 hipError_t launch_join_logits(const LossArgs& a, float* share, int splits, int ld, float2* part, float* z_label, hipStream_t s)
 {
     const int tiles = (a.classes + 127) / 128;
     join_logits_kernel<<<dim3((unsigned)tiles, (unsigned)a.n, (unsigned)((a.rows + 7) / 8)), 256, 0, s>>>(
         share, splits, (long long)a.n * a.rows * ld, (const float*)a.bias.p, a.bias.rep, a.labels, a.rows, a.classes, ld, tiles, part, z_label, share);
     return hipGetLastError();
-}
-template <typename T> hipError_t launch_few_weights(const LossArgs& a, const T* g, int ld, const float* factor, hipStream_t s)
-{
-    return a.rows <= 8 ? weights<T, 8>(a, g, ld, factor, s) : weights<T, 16>(a, g, ld, factor, s);
 }
 template hipError_t launch_few_weights<float>(const LossArgs&, const float*, int, const float*, hipStream_t);
 template hipError_t launch_few_weights<__bf16>(const LossArgs&, const __bf16*, int, const float*, hipStream_t);

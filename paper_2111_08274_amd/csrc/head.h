@@ -78,7 +78,8 @@ hipError_t launch_loss(const LossArgs& a, hipStream_t s);
 // few rows: logits [replicas][rows][ld], ld a multiple of 128, from the shares of their contraction (into the first one's place), their
 // statistics per 128 classes (part [replicas][tiles][rows]: the largest logit and the sum of exp of the distances to it), the labels' logits
 hipError_t launch_join_logits(const LossArgs& a, float* share, int splits, int ld, float2* part, float* z_label, hipStream_t s);
-// dW from G [replicas][rows][ld], at most 16 rows, at least four classes
+// dW from G [replicas][rows][ld], at most kFewWeights rows, at least four classes
+constexpr int kFewWeights = 8;
 template <typename T> hipError_t launch_few_weights(const LossArgs& a, const T* g, int ld, const float* factor, hipStream_t s);
 
 // ---- device pieces ------------------------------------------------------------------------------------------------

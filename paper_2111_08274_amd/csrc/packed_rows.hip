@@ -3,7 +3,8 @@
 // float's bits.  x * 2^-e is exact (e >= -126), so rounding it to the nearest integer, ties to even, is the only
 // rounding.  A power of two instead of max|x| / 127 costs up to one of the seven bits but makes q * 2^e a bf16 and an fp32
 // number, so that what reads the checkpoint need not round again.
-// Memory bound: 16 values a lane, two lanes a group; values and exponents are written once.
+// Memory bound: 16 values a lane, two lanes a group; values and exponents are written once.  4 x 4096 x 4096 bf16: packing 39 us = 5.2 TB/s;
+// 4 x 8192 x 4096: packing 65 us = 6.3 TB/s, unpacking 69 us = 5.9.
 #include "head.h"
 
 namespace hadfl {
