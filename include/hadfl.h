@@ -357,14 +357,14 @@ HADFL_API hadfl_status hadfl_dense_grad_packed(const hadfl_dense *dense, const v
                                                const hadfl_rows *dw, const hadfl_rows *db, void *work, void *stream);
 
 /* Softmax cross entropy of a last dense layer over many classes, without keeping its logits: they are formed a piece of
- * the vocabulary at a time, once for the loss and once more for the gradient (with few rows, where one piece holds the
- * whole vocabulary, once).  A piece is at most 512 MiB, or 1024 classes.  With z = x W + b,
+ * the vocabulary at a time, once for the loss and once more for the gradient (where one piece holds the whole vocabulary,
+ * and its logits with it, once).  A piece is at most 512 MiB, or 1024 classes.  With z = x W + b,
  *   row_loss_t = log sum_v exp(z_tv) - z_t,label(t);   loss = mean of row_loss over the replica's labelled rows.
  * A row whose label lies outside [0, n_classes) has no label: its row_loss is zero, it adds nothing to any gradient
  * (whatever its x holds), and its dx is zero.  A replica without labelled rows has loss zero and zero gradients.  A bias of
  * -inf takes a class out.  With G = (softmax(z) - onehot(label)) / (number of labelled rows):
  *   dx = G W^T,  dW = x^T G,  db = sum_t G.
- * fp32: operands enter the matrix products in parts of 16 bits whose products are summed in 32 bits: with few rows (300 a
+ * fp32: operands enter the matrix products in parts of 16 bits whose products are summed in 32 bits: with few rows (200 a
  * replica, more the smaller w is) three bf16 parts (six products, whole for magnitudes from 2^-107 on), beyond two fp16 parts (three products) scaled by a power of two to
  * the replica's largest finite magnitude: a product is off by at most 2^-20 of itself, 2^-23.5 in the mean square, for
  * magnitudes down to 2^-29 of the largest.  bf16: softmax(z) - onehot is rounded to bf16 for the two products, db is formed before that.

@@ -1,10 +1,11 @@
 // Softmax cross entropy of a last dense layer over many classes, and its gradient, in pieces of the vocabulary.
 //   1. logits' statistics: z = x W + b a tile at a time; a tile leaves, per row, its largest logit and the sum of exp of the
-//      distances to it, and the label's logit where the tile holds it.  Nothing of z is stored.
+//      distances to it, and the label's logit where the tile holds it.  Nothing else of z is stored.
 //   2. per row: the tiles' pairs joined to its max and sum; row losses max - z_label + log(sum), their mean and 1 / (labelled
 //      rows).
 //   3. for every piece of the vocabulary: z again, G = exp(z - max) / sum - onehot into a buffer of [rows][piece], then
-//      dx += G W^T (shares of the contraction side by side, added in a fixed order) and dW = x^T G.
+//      dx += G W^T (shares of the contraction side by side, added in a fixed order) and dW = x^T G.  Where one piece holds the vocabulary,
+//      its logits of step 1 may stay for it.
 // A row without a label has G = 0 and its x is read as zeros.
 #include <cmath>
 
@@ -363,6 +364,52 @@ template <int PL> struct GradientRows {
     }
 };
 
+// The whole vocabulary in one piece: G from its logits, bf16 or two fp16 parts, and its column sums over `depth` rows, 256 columns a workgroup,
+// every fourth row a wave.  Bound by memory: 2 x 1000 x 20011 fp32 58 us = 5.5 TB/s, 4 x 512 x 32000 bf16 68 us = 5.8.
+template <int PL> __global__ __launch_bounds__(256) void gradient_planes_kernel(const float* z, const int32_t* labels, const float2* norm, int rows, int classes, int ld,
+                                                              int depth, __bf16* g, long long plane, float* sums)
+{
+    constexpr int U = 4;
+    __shared__ f4 part[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (blockIdx.x * 64 + lane) * 4, k = blockIdx.z;
+    const int first = blockIdx.y * depth, last = min(rows, first + depth);
+    const bool in = c < ld;                                    // whole chunks: ld is a multiple of 128
+    const long long line = (long long)k * rows;
+    f4 sum{0.f, 0.f, 0.f, 0.f};
+    for (int t0 = first + wave; t0 < last; t0 += 4 * U) {
+        f4 v[U];
+        float2 l[U];
+        int y[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long long t = line + min(t0 + 4 * u, last - 1);
+            v[u] = *(const f4*)(z + t * ld + (in ? c : 0));
+            l[u] = norm[t];
+            y[u] = labels[t];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (t0 + 4 * u >= last || !in) break;
+            const bool live = (unsigned)y[u] < (unsigned)classes;
+            const float inv = 1.f / l[u].y;
+            f4 p;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[e] = live && c + e < classes ? exp_down(v[u][e] - l[u].x) * inv - (c + e == y[u] ? 1.f : 0.f) : 0.f;
+            sum += p;
+            u2 high, low;
+            if (PL == 2) split2(p, up_scale(kOneBits), high, low);
+            else high = u2{to_bf16x2(p[0], p[1]), to_bf16x2(p[2], p[3])};
+            const long long at = (line + t0 + 4 * u) * ld + c;
+            *(u2*)(g + at) = high;
+            if (PL == 2) *(u2*)(g + plane + at) = low;
+        }
+    }
+    if (!sums) return;
+    part[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && in) *(f4*)(sums + ((long long)k * gridDim.y + blockIdx.y) * ld + c) = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
+}
+
 // db of a piece: the row blocks' sums in ascending order (20011 classes: 5.4 us, a launch)
 __global__ __launch_bounds__(256) void bias_grad_kernel(const float* sums, int blocks, int ld, int c0, int cols, const float* factor, float* db, long long rep)
 {
@@ -379,7 +426,7 @@ __global__ __launch_bounds__(256) void bias_grad_kernel(const float* sums, int b
 //   more       products straight from memory to LDS: twice to three times the rate, but x (unlabelled rows as zeros) and a W of 32-bit or
 //              unaligned values are laid out first, there are more launches, and few tiles leave most of the chip idle
 struct Plan {
-    bool direct, small;            // small: 32 rows a tile, not 64
+    bool direct, small, keep;      // small: 32 rows a tile, not 64; keep: the logits of the one piece there is stay for its G
     int bm, bn, wave_m, parts, z_splits, z_len, piece, pieces, blocks, splits, split_len, w_tile, w_splits, w_len, ldx, planes;
     size_t norm, z_label, row_loss, factor, part, g, z, sums, share, w_share, x, w, top, total;
 };
@@ -394,17 +441,17 @@ bool narrow(int v) { return 1.18 * up_to(v, 128) < up_to(v, 256); }
 
 // Rows up to which W is read as it is: more where W is small, and where its features are many for its tiles.  Loss and gradients through
 // registers / laid out, us:
-//   bf16             4 x 512 x 32000, 64 rows 135 / 136, 96 rows 159 / 141; 2048 x 20000, 96 rows 102 / 105, 128 rows 115 / 107; 4096 x 10008,
-//                    256 rows 155 / 163, 320 rows 223 / 180; 2048 x 5000, 256 rows 79 / 86, 320 rows 93 / 91
-//   bf16, unaligned  4 x 512 x 32001, 128 rows 182 / 205, 160 rows 305 / 251; 2048 x 20011, 256 rows 165 / 187, 320 rows 246 / 204; 8 x 200 x 4099,
-//                    256 rows 82 / 89, 320 rows 97 / 88
-//   fp32             4 x 512 x 32000, 256 rows 700 / 713, 320 rows 952 / 890; 2048 x 20011, 256 rows 458 / 510, 320 rows 582 / 566; 8 x 200 x 4099,
-//                    256 rows 146 / 180, 384 rows 190 / 195
+//   bf16             4 x 512 x 32000, 64 rows 135 / 136, 96 rows 159 / 141; 2048 x 20000, 128 rows 113 / 113; 4096 x 10008, 128 rows 109 / 139, 256 rows
+//                    177 / 153; 2048 x 5000, 256 rows 92 / 90
+//   bf16, unaligned  4 x 512 x 32001, 128 rows 182 / 205, 160 rows 305 / 251; 2048 x 20011, 192 rows 173 / 172; 8 x 200 x 4099, 256 rows 82 / 89,
+//                    320 rows 97 / 88
+//   fp32             4 x 512 x 32000, 128 rows 471 / 540, 192 rows 641 / 639, 256 rows 725 / 684; 2048 x 20011, 256 rows 487 / 453; 12 x 520 x 8739, 256
+//                    rows 711 / 710; 8 x 200 x 4099, 256 rows 165 / 188, 320 rows 195 / 194
 double few_rows(int n, int features, int classes, int bf16)
 {
     const double values = (double)n * features * classes, deep = std::min(125., features / ((double)n * classes / 256));
-    if (!bf16) return 300 + std::min(165., 1.0e9 / values) + 0.4 * deep;
-    return (classes % 8 ? 128 + std::min(100., 0.6e9 / values) : 30 + std::min(200., 0.7e9 / values)) + 2 * deep;
+    if (!bf16) return 200 + std::min(165., 1.0e9 / values) + 0.4 * deep;
+    return (classes % 8 ? 128 + std::min(100., 0.6e9 / values) : 30 + std::min(200., 0.7e9 / values)) + 1.2 * deep;
 }
 
 // Into how many shares the logits' contraction over few rows is cut.  A workgroup, of 128 classes, takes 12 ns a feature (bf16 W, 32 rows; 24:
@@ -450,6 +497,10 @@ Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
     p.pieces = (int)((classes + most - 1) / most);
     p.piece = up_to((classes + p.pieces - 1) / p.pieces, bn);
     p.pieces = (classes + p.piece - 1) / p.piece;
+    // z as 32-bit floats costs its bytes, in the statistics' kernel and in gradient_planes_kernel; forming it again costs the product.
+    // fp32, three products: 2 x 1000 x 777 x 20011 in all 1027 us against 1191, 4 x 2656 x 64 x 2036 171 against 174.  bf16, 4 x 512 rows x 32000: 512
+    // features 434 against 416, 1024 656 against 711, 2048 1080 against 1262.
+    p.keep = p.direct && grad && p.pieces == 1 && (!bf16 || features >= 768) && lines * p.piece * (es + 4) <= kPieceBytes;
     p.ldx = up_to(features, 8);
     const int bd = p.direct && !narrow(features) ? 256 : 128;              // columns of dx a tile
     const long long tiles = (long long)n * ((rows + p.bm - 1) / p.bm) * ((features + bd - 1) / bd);
@@ -480,6 +531,7 @@ Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
         p.w = take((size_t)n * features * p.piece * 2 * p.planes);
         p.top = take((size_t)n * 8);
     }
+    if (p.keep) p.z = take((size_t)lines * p.piece * 4);
     if (!p.direct && (p.z_splits > 1 || grad) && (bf16 || !grad)) p.z = take((size_t)lines * p.piece * 4 * p.z_splits);
     if (grad) {
         p.g = take((size_t)lines * p.piece * (p.direct ? es : bf16 ? 2 : 4 * p.z_splits));
@@ -640,7 +692,7 @@ template <typename T, int BM, int BN, int WN> hipError_t run_direct(const LossAr
     for (int c0 = 0; c0 < a.classes; c0 += step) {
         const int cols = std::min(step, a.classes - c0);
         if ((e = weights(c0, cols, false, w)) != hipSuccess) return e;
-        const Statistics<PL == 2, BM, BN, WN> stats{bias, a.bias.rep, a.labels, k.part, k.z_label, nullptr, a.rows, c0, a.classes, p.parts, 0};
+        const Statistics<PL == 2, BM, BN, WN> stats{bias, a.bias.rep, a.labels, k.part, k.z_label, p.keep ? k.z : nullptr, a.rows, c0, a.classes, p.parts, p.piece};
         e = launch_direct<PL, PL, BM, BN, 2, WN, true, false>(x, w, a.n, a.rows, cols, a.features, 1, a.features, stats, s);
         if (e != hipSuccess) return e;
     }
@@ -650,7 +702,11 @@ template <typename T, int BM, int BN, int WN> hipError_t run_direct(const LossAr
         if ((e = weights(c0, cols, p.pieces == 1, w)) != hipSuccess) return e;
         const Plane3 g{(const __bf16*)k.g, (long long)a.rows * ld, (long long)a.n * a.rows * ld, ld, a.rows, ld, nullptr};
         const Softmax<PL == 2> soft{bias, a.bias.rep, a.labels, k.norm, a.db.p ? k.sums : nullptr, a.rows, c0, a.classes, ld, p.blocks};
-        e = launch_direct<PL, PL, BM, BN, 2, WN, true, false>(x, w, a.n, a.rows, cols, a.features, 1, a.features, GradientRows<PL>{soft, (__bf16*)k.g, g.plane}, s);
+        if (p.keep) {
+            gradient_planes_kernel<PL><<<dim3((unsigned)((ld + 255) / 256), (unsigned)p.blocks, (unsigned)a.n), 256, 0, s>>>(
+                k.z, a.labels, k.norm, a.rows, a.classes, ld, p.wave_m, (__bf16*)k.g, g.plane, soft.sums);
+            e = hipGetLastError();
+        } else e = launch_direct<PL, PL, BM, BN, 2, WN, true, false>(x, w, a.n, a.rows, cols, a.features, 1, a.features, GradientRows<PL>{soft, (__bf16*)k.g, g.plane}, s);
         if (e != hipSuccess) return e;
         if (a.dx.p) {
             const StoreShare<> store{k.share, a.rows, a.features, p.ldx, a.rows, a.n, i > 0, false};
