@@ -68,7 +68,7 @@ template <typename T, class Store> hipError_t product(const DenseArgs& a, const 
     if (e != hipSuccess) return e;
     const Plane3 x{wx, (long long)a.rows * p.ldx, 0, p.ldx, a.rows, p.ldx, nullptr};
     Plane3 dy{(const __bf16*)a.dy.p, a.dy.rep, 0, (int)a.dy.row, a.rows, a.out, nullptr};
-    if (PL == 3 || !chunked(a.dy, 1, a.out) || !direct_pitch(a.dy.row)) {
+    if (PL == 3 || !is_plane(a.dy, a.out)) {
         if ((e = lay_out<T, PL>(a.n, a.rows, a.out, p.ldy, a.dy, Labelled{nullptr, 0}, nullptr, wy, s)) != hipSuccess) return e;
         dy = Plane3{wy, (long long)a.rows * p.ldy, (long long)a.n * a.rows * p.ldy, p.ldy, a.rows, p.ldy, nullptr};
     }

@@ -28,7 +28,7 @@ namespace head {
 
 constexpr int kSlab = 64;
 
-struct Plane3 {                    // an operand: source rows `lines` of `cols` values, `ld` apart
+struct Plane3 {                    // an operand: source rows `lines` of `cols` values, `ld` >= cols apart
     const __bf16* p;
     long long rep, plane;
     int ld, lines, cols;
@@ -60,6 +60,9 @@ template <bool F16> __device__ __forceinline__ f16 multiply16(const bf16x8& a, c
 }
 // what the kernel's 32-bit offsets within a tile reach
 inline bool direct_pitch(long long ld) { return ld <= (1ll << 22); }
+// A bf16 tensor that is a plane as it lies: whole chunks, and rows that do not overlap (a stride of zero would), since what lies beyond a plane's
+// last row is told by its offset alone.
+inline bool is_plane(const Rows& r, long long cols) { return chunked(r, 1, cols) && direct_pitch(r.row) && r.row >= cols; }
 
 typedef __attribute__((address_space(3))) void LdsVoid;
 // 16 bytes a lane from b + off to LDS, the wave's lanes one after the other from `at` (the same in all lanes); an offset outside the

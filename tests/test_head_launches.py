@@ -1,0 +1,50 @@
+"""What the head's operators ask the GPU to launch, checked without one: the library's real launch path on a stand-in for the HIP runtime
+(tests/native/head_launches.cpp)."""
+import json
+import os
+import re
+import subprocess
+import sys
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+
+@pytest.fixture(scope="session")
+def launched(tmp_path_factory):
+    so = str(tmp_path_factory.mktemp("hip") / "head_launches.so")
+    subprocess.run(["/opt/rocm/llvm/bin/clang++", "-std=c++17", "-O1", "-shared", "-fPIC", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include",
+                    os.path.join(HERE, "native", "head_launches.cpp"), "-o", so], check=True)
+
+    def run(cases):
+        r = subprocess.run([sys.executable, os.path.join(HERE, "native", "run_head.py"), so], input=json.dumps(cases), text=True,
+                           capture_output=True, cwd=os.path.dirname(HERE), env=dict(os.environ, PYTHONPATH=os.path.dirname(HERE)))
+        assert r.returncode == 0, r.stderr[-3000:]
+        return json.loads(r.stdout)
+    return run
+
+
+def _name(launch):
+    return re.search(r"\d+([a-z_]+_kernel)", launch[0]).group(1)
+
+
+def _planes(launch):
+    """(row stride, rows, columns) of both operands of a product of planes"""
+    v = [int(q) for q in launch[7:13]]
+    return v[:3], v[3:]
+
+
+DENSE = [(1, 1000, 2048, 2048, 1), (4, 1000, 2048, 2048, 1), (1, 8200, 896, 896, 1), (1, 1100, 4104, 3592, 0)]
+
+
+def test_rows_that_overlap_are_laid_out_for_products_of_planes_in_the_dense_gradient(launched):
+    # a plane's rows end where the next begins: what lies beyond the last is told by its offset
+    cases = [dict(op="dense", n=n, rows=t, inputs=i, outputs=o, bf16=b, dy=dy) for n, t, i, o, b in DENSE
+             for dy in (None, [0, 0], [o, 0], [t * o, 0], [t * o, 16], [t * o, o - 8], [t * (o + 8), o + 8])]
+    for c, r in zip(cases, launched(cases)):
+        direct = [v for v in r["launches"] if _name(v) == "direct_kernel"]
+        assert r["status"] == 0 and direct, c
+        assert all(ld >= cols for v in direct for ld, _, cols in _planes(v)), c
+        whole = not c["dy"] or c["dy"][1] >= c["outputs"]
+        assert ("lay_out_kernel" in map(_name, r["launches"])) == (not c["bf16"] or not whole), c
