@@ -679,7 +679,7 @@ template <typename T, int BM, int BN, int WN> hipError_t run_direct(const LossAr
     if (e != hipSuccess) return e;
     const Plane3 x{k.x, (long long)a.rows * p.ldx, (long long)a.n * a.rows * p.ldx, p.ldx, a.rows, p.ldx, top_x};
     // W as it is, or laid out a piece at a time
-    const bool as_is = PL == 1 && chunked(a.w, 1, a.classes) && direct_pitch(a.w.row);
+    const bool as_is = PL == 1 && is_plane(a.w, a.classes);
     auto weights = [&](int c0, int cols, bool there, Plane3& w) -> hipError_t {
         if (as_is) { w = Plane3{(const __bf16*)a.w.p + c0, a.w.rep, 0, (int)a.w.row, a.features, cols, nullptr}; return hipSuccess; }
         const int ld = up_to(cols, 8);

@@ -58,11 +58,9 @@ template <bool F16> __device__ __forceinline__ f16 multiply16(const bf16x8& a, c
     if (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
-// what the kernel's 32-bit offsets within a tile reach
-inline bool direct_pitch(long long ld) { return ld <= (1ll << 22); }
-// A bf16 tensor that is a plane as it lies: whole chunks, and rows that do not overlap (a stride of zero would), since what lies beyond a plane's
-// last row is told by its offset alone.
-inline bool is_plane(const Rows& r, long long cols) { return chunked(r, 1, cols) && direct_pitch(r.row) && r.row >= cols; }
+// A bf16 tensor that is a plane as it lies: whole chunks, rows no farther apart than the kernel's 32-bit offsets within a tile reach, and rows that do
+// not overlap (a stride of zero would), since what lies beyond a plane's last row is told by its offset alone.
+inline bool is_plane(const Rows& r, long long cols) { return chunked(r, 1, cols) && r.row >= cols && r.row <= (1ll << 22); }
 
 typedef __attribute__((address_space(3))) void LdsVoid;
 // 16 bytes a lane from b + off to LDS, the wave's lanes one after the other from `at` (the same in all lanes); an offset outside the

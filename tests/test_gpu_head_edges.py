@@ -31,3 +31,37 @@ def test_dense_gradient_of_rows_that_overlap(n, rows, i, o, bf16, stride):
     x = torch.randn((n, rows, i), device="cuda", generator=g).to(base._dtype(bf16))
     line = torch.randn(rows * stride + n * o + 64, device="cuda", generator=g).to(base._dtype(bf16))
     _dense(n, rows, i, o, bf16, x, line.as_strided((n, rows, o), (o if n > 1 else 0, stride, 1)))
+
+
+def _loss(c, k, out, bf16, names=("row_loss", "loss", "dx", "dw", "db")):
+    """Checks replica k of what ClassLoss.grad returned against 64 bits"""
+    r, b = base._loss_reference(c, k, bf16)
+    for name, got in zip(("loss", "row_loss", "dx", "dw", "db"), out):
+        if got is not None and name in names:
+            base._check(base._values(got[k]), r[name], b[name], name)
+
+
+@pytest.mark.parametrize("rows,d,v,bf16", [(400, 200, 2056, 1), (20, 200, 2056, 1), (400, 200, 2056, 0), (20, 200, 2056, 0)])
+@pytest.mark.parametrize("stride", [0, 8])
+def test_loss_with_rows_of_w_that_overlap(rows, d, v, bf16, stride):
+    # 200 features do not fill the last 64: what lies beyond W's last row must not be taken for one.  A class whose weights are -inf
+    # is out where x is positive; its dx is 0 * inf and not looked at
+    torch = base._torch()
+    rng = np.random.default_rng(2)
+    x = base._in(rng.uniform(0.1, 1, size=(1, rows, d)), bf16, "whole")
+    line = torch.as_tensor(rng.normal(size=d * stride + v) / d).cuda().to(base._dtype(bf16))
+    y = rng.integers(0, v, size=(1, rows)).astype(np.int32)
+    for out in (False, True)[:1 + bf16]:                      # (parts of a 32-bit infinity are NaNs)
+        w = line.as_strided((1, d, v), (0, stride, 1))
+        if out:
+            line[v // 2] = float("-inf")                      # a weight of one class, or of one class a row
+        dead = torch.isinf(w[0]).any(0).cpu().numpy()
+        y[0][dead[y[0]]] = v - 1
+        c = dict(x=x, w=w, bias=None, y=torch.as_tensor(y).cuda(), yh=y)
+        got = hadfl.ClassLoss(1, rows, d, v, bf16=bf16).grad(c["x"], c["w"], c["y"])
+        if not out:
+            _loss(c, 0, got, bf16)
+        else:
+            # W with the dead classes' weights at a value that leaves exp nothing either
+            finite = dict(c, w=torch.where(torch.as_tensor(dead).cuda(), torch.full_like(w, -1e4), w))
+            _loss(finite, 0, got, bf16, ("row_loss", "loss", "dw"))

@@ -48,3 +48,15 @@ def test_rows_that_overlap_are_laid_out_for_products_of_planes_in_the_dense_grad
         assert all(ld >= cols for v in direct for ld, _, cols in _planes(v)), c
         whole = not c["dy"] or c["dy"][1] >= c["outputs"]
         assert ("lay_out_kernel" in map(_name, r["launches"])) == (not c["bf16"] or not whole), c
+
+
+@pytest.mark.parametrize("grad", [0, 1])
+def test_rows_that_overlap_are_laid_out_for_products_of_planes_in_the_loss(launched, grad):
+    cases = [dict(op="loss", n=n, rows=t, features=d, classes=v, bf16=b, grad=grad, w=w) for n, t, d, v, b in [(1, 400, 200, 2056, 1), (2, 1000, 776, 4200, 1), (1, 400, 200, 2056, 0)]
+             for w in (None, [0, 0], [v, 0], [d * v, 0], [d * v, 16], [d * v, v - 8], [d * (v + 8), v + 8])]
+    for c, r in zip(cases, launched(cases)):
+        direct = [v for v in r["launches"] if _name(v) == "direct_kernel"]
+        assert r["status"] == 0 and direct, c
+        assert all(ld >= cols for v in direct for ld, _, cols in _planes(v)), c
+        whole = not c["w"] or c["w"][1] >= c["classes"]
+        assert [_name(v) for v in r["launches"]].count("lay_out_kernel") == (1 if c["bf16"] and whole else 2), c      # x always, W where it has to be
