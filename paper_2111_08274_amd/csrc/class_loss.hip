@@ -21,6 +21,9 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // exp of a number that is not positive, off by |t| / 2 units in the last place at most: what a rounding of t itself does
 __device__ __forceinline__ float exp_down(float t) { return __builtin_amdgcn_exp2f(t * kLog2e); }
 
+// whether z * log2(e) is a float for every logit z of a row up to its largest, but for those that exp makes zero: else the difference first
+__device__ __forceinline__ bool folds(float largest) { return __builtin_fabsf(largest) <= 0x1p126f; }
+
 // logits z of a wave's block of 32 rows (lanes along m), with the bias, -inf beyond the classes; n0: the first column's class
 template <int TM, int TN>
 __device__ __forceinline__ void logits_of(const Tile<TM, TN>& t, int i, int n0, int classes, const float* bias, float (&z)[TN][16])
@@ -105,7 +108,7 @@ template <bool EXACT, int BM, int BN, int WN> struct Statistics {
             top = __builtin_fmaxf(top, other<32>(top));
             float sum = 0.f;
             const float base = top == -INFINITY ? 0.f : top;   // a row of -inf alone: every term is zero
-            if (EXACT || b) {                                  // the difference first: a bias may be the type's lowest value
+            if (EXACT || b || !folds(base)) {                  // the difference first: a bias may be the type's lowest value
 #pragma unroll
                 for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -263,7 +266,7 @@ template <bool EXACT> struct Softmax {
         const bool live = (unsigned)y < (unsigned)classes;
         const float2 l = live ? norm[(long long)t.rep * rows + m] : float2{0.f, 1.f};
         logits_of(t, i, n0, classes, bias ? bias + t.rep * bias_rep : nullptr, v);
-        if (EXACT || bias) {
+        if (EXACT || bias || !folds(l.x)) {
             const float inv = 1.f / l.y;
 #pragma unroll
             for (int j = 0; j < TN; ++j)

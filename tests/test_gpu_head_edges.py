@@ -65,3 +65,31 @@ def test_loss_with_rows_of_w_that_overlap(rows, d, v, bf16, stride):
             # W with the dead classes' weights at a value that leaves exp nothing either
             finite = dict(c, w=torch.where(torch.as_tensor(dead).cuda(), torch.full_like(w, -1e4), w))
             _loss(finite, 0, got, bf16, ("row_loss", "loss", "dw"))
+
+
+@pytest.mark.parametrize("rows,v", [(5, 300), (100, 300), (600, 1000)])
+@pytest.mark.parametrize("bf16", [0, 1])
+def test_logits_near_the_largest_float(rows, v, bf16):
+    # 2.95e38 = 0.87 of the largest float: its product with log2(e) is none.  Where z lies so far apart the softmax is one class, or
+    # an even share of those that tie
+    torch = base._torch()
+    x, w = torch.zeros((1, rows, 16), device="cuda"), torch.zeros((1, 16, v), device="cuda")
+    x[:, :, 0] = 2.0 ** 63
+    w[:, 0, 7] = w[:, 0, 9] = 2.0 ** 64 * 1.734375
+    w[:, 0, 11] = -2.0 ** 64 * 1.734375
+    low = torch.zeros_like(w)
+    low[:, 0] = -2.0 ** 64 * 1.734375                         # the same logit, far below zero, for every class
+    y = torch.full((1, rows), 7, dtype=torch.int32, device="cuda")
+    plan = hadfl.ClassLoss(1, rows, 16, v, bf16=bf16)
+    t = base._dtype(bf16)
+    loss, row, dx, dw, _ = plan.grad(x.to(t), w.to(t), y)
+    assert (row - float(np.log(2))).abs().max() < 1e-6 and (loss - float(np.log(2))).abs() < 1e-6
+    share = torch.zeros(v, device="cuda")
+    share[7], share[9] = -0.5, 0.5
+    assert torch.equal(dw[0, 0].float() / 2.0 ** 63, share) and not dw[0, 1:].any()
+    assert not dx.any()                                       # (p_7 - 1 + p_9) times the weight that 7 and 9 share
+    loss, row, dx, dw, _ = plan.grad(x.to(t), low.to(t), y)
+    assert (row - float(np.log(v))).abs().max() < 1e-5
+    even = torch.full((v,), 1.0 / v, device="cuda", dtype=torch.float64)
+    even[7] -= 1
+    assert ((dw[0, 0].double() / 2.0 ** 63 - even).abs() <= 2.0 ** -7 * even.abs()).all()
