@@ -499,6 +499,8 @@ Plan plan_of(int n, int rows, int features, int classes, int bf16, bool grad)
     most = std::max<long long>(1024, most / bn * bn);
     p.pieces = (int)((classes + most - 1) / most);
     p.piece = up_to((classes + p.pieces - 1) / p.pieces, bn);
+    // through registers a piece has eight columns at least, so that no load begins before a row or ends behind it (tile_product.h)
+    while (!p.direct && classes > p.piece && (classes - 1) % p.piece < 7) p.piece += bn;
     p.pieces = (classes + p.piece - 1) / p.piece;
     // z as 32-bit floats costs its bytes, in the statistics' kernel and in gradient_planes_kernel; forming it again costs the product.
     // fp32, three products: 2 x 1000 x 777 x 20011 in all 1027 us against 1191, 4 x 2656 x 64 x 2036 171 against 174.  bf16, 4 x 512 rows x 32000: 512

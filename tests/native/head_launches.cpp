@@ -1,6 +1,7 @@
 // Stand-in for the HIP runtime under libhadfl.so, for host-only tests of the head's operators: a launch is written down instead of run, and
 // refused as the runtime refuses it where a dimension has 2^32 threads or more.  One line a launch: the mangled kernel, the workgroups and threads of a dimension,
-// and for products of operands that lie in planes the row stride, rows and columns of both.
+// and for products of operands that lie in planes the row stride, rows and columns of both, for those through registers the columns of each that
+// is a tensor of the caller's or of the workspace.
 // Loaded ahead of libhadfl.so with RTLD_GLOBAL, so that its symbols are found first.
 #include <hip/hip_runtime.h>
 
@@ -15,6 +16,11 @@ struct Plane {                     // what direct_product.h passes as Plane3
     long long rep, plane;
     int ld, lines, cols;
     const unsigned* top;
+};
+struct Tensor {                    // tile_product.h: Source
+    const void* p;
+    long long rep, row;
+    int rows, cols;
 };
 std::map<const void*, std::string> g_names;
 std::string g_trace;
@@ -57,6 +63,12 @@ hipError_t hipLaunchKernel(const void* f, dim3 grid, dim3 block, void** args, si
             Plane p;
             std::memcpy(&p, args[i], sizeof(p));
             g_trace += " " + std::to_string(p.ld) + " " + std::to_string(p.lines) + " " + std::to_string(p.cols);
+        }
+    if (name.find("14product_kernel") != std::string::npos)
+        for (int i = name.find("14product_kernelINS0_6Source") == std::string::npos; i < 2; ++i) {
+            Tensor t;
+            std::memcpy(&t, args[i], sizeof(t));
+            g_trace += " " + std::to_string(t.cols);
         }
     g_trace += "\n";
     return hipSuccess;

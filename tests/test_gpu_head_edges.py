@@ -93,3 +93,22 @@ def test_logits_near_the_largest_float(rows, v, bf16):
     even = torch.full((v,), 1.0 / v, device="cuda", dtype=torch.float64)
     even[7] -= 1
     assert ((dw[0, 0].double() / 2.0 ** 63 - even).abs() <= 2.0 ** -7 * even.abs()).all()
+
+
+@pytest.mark.parametrize("shared", [False, True])
+def test_a_vocabulary_whose_last_piece_would_hold_three_classes(shared):
+    # 1024 replicas of 130 rows: pieces of 1024 classes would leave three for the eighth; W a full tensor, and one line for all features
+    # that ends with its last class
+    torch = base._torch()
+    n, rows, d, v = 1024, 130, 16, 7171
+    c = base._loss_case(1, rows, d, v, 0, "whole", True, seed=6)
+    c["x"].nan_to_num_(nan=0.5, posinf=0.5)
+    if shared:
+        line = torch.full((v + 8,), float("nan"), device="cuda")
+        line[:v] = c["w"][0, 0] / 4
+        c["w"] = line[:v].expand(1, d, v)
+    args = c["x"].expand(n, rows, d), c["w"].expand(n, d, v), c["y"].repeat(n, 1), c["bias"].expand(n, v)
+    out = hadfl.ClassLoss(n, rows, d, v).grad(*args)
+    one = dict(x=c["x"], w=c["w"], bias=c["bias"], yh=c["yh"])
+    _loss(one, 0, [o[:1] for o in out], 0)
+    assert all(torch.equal(o[0], o[k]) for o in out for k in (1, n - 1))

@@ -60,3 +60,18 @@ def test_rows_that_overlap_are_laid_out_for_products_of_planes_in_the_loss(launc
         assert all(ld >= cols for v in direct for ld, _, cols in _planes(v)), c
         whole = not c["w"] or c["w"][1] >= c["classes"]
         assert [_name(v) for v in r["launches"]].count("lay_out_kernel") == (1 if c["bf16"] and whole else 2), c      # x always, W where it has to be
+
+
+def test_no_operand_through_registers_has_fewer_columns_than_a_load_takes(launched):
+    # pieces of a vocabulary whose last one would hold one to eight classes; sizes of fewer than eight columns, which are laid out
+    cases = [dict(op="loss", n=1024, rows=t, features=16, classes=v, bf16=b) for b in (0, 1) for t in (30, 130) for v in list(range(7165, 7181)) + [8193, 20487, 61441, 65537, 131073]]
+    cases += [dict(op="loss", n=64, rows=40, features=64, classes=v) for v in range(58881, 58890)]
+    cases += [dict(op="loss", n=2, rows=5, features=f, classes=v, bf16=b) for f in (1, 7, 8, 9) for v in (1, 7, 8, 9) for b in (0, 1)]
+    cases += [dict(op="dense", n=2, rows=5, inputs=f, outputs=v, bf16=b) for f in (1, 7, 8, 9) for v in (1, 7, 8, 9) for b in (0, 1)]
+    pieces = set()
+    for c, r in zip(cases, launched(cases)):
+        assert r["status"] == 0, c
+        through = [v for v in r["launches"] if _name(v) == "product_kernel"]
+        assert all(int(q) >= 8 for v in through for q in v[7:]), (c, through)
+        pieces.add(sum("Gradient" in v[0] for v in through))
+    assert len(pieces) > 3
