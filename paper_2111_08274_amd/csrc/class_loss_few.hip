@@ -85,7 +85,7 @@ __global__ __launch_bounds__(256) void few_weights_kernel(const T* x, long long 
 {
     constexpr int P = TR + 4;
     __shared__ __attribute__((aligned(16))) float xs[kDepth][P];
-    const unsigned item = logical_block();
+    const unsigned item = blockIdx.y * gridDim.x + logical_block();
     if (item >= (unsigned)total) return;
     const int block = item % blocks, tile = item / blocks % tiles, k = item / blocks / tiles;
     const int tid = threadIdx.x, c = tile * 256 + (tid & 63) * 4, d0 = block * kDepth, count = min(kDepth, features - d0);
@@ -128,7 +128,7 @@ template <typename T> hipError_t launch_few_weights(const LossArgs& a, const T* 
     const int tiles = (a.classes + 255) / 256, blocks = (a.features + kDepth - 1) / kDepth;
     const long long total = (long long)a.n * tiles * blocks;
     if (total > 0x7fffff00ll) return hipErrorInvalidValue;
-    few_weights_kernel<T><<<die_grid(total), 256, 0, s>>>((const T*)a.x.p, a.x.rep, a.x.row, a.labels, g, ld, a.rows, a.features, a.classes, tiles, blocks,
+    few_weights_kernel<T><<<line_grid(die_grid(total), 256), 256, 0, s>>>((const T*)a.x.p, a.x.rep, a.x.row, a.labels, g, ld, a.rows, a.features, a.classes, tiles, blocks,
                                                           (int)total, factor, (T*)a.dw.p, a.dw.rep, a.dw.row);
     return hipGetLastError();
 }

@@ -159,7 +159,7 @@ __global__ __launch_bounds__(WM * WN * 64) void direct_kernel(Plane3 a, Plane3 b
     constexpr int kImage = LA::kBytes + LB::kBytes, IMAGES = kImage > 49152 ? 2 : kImage > 32768 ? 3 : 4, kLoads = LA::kLoads + LB::kLoads;
     __shared__ __attribute__((aligned(16))) char images[IMAGES * kImage];
 
-    const unsigned item = logical_block();
+    const unsigned item = blockIdx.y * gridDim.x + logical_block();
     if (item >= (unsigned)total) return;
     const int per = tiles_m * tiles_n, r = item / per;
     int tm_i, tn_i;
@@ -260,7 +260,7 @@ hipError_t launch_direct(const Plane3& a, const Plane3& b, int replicas, int M, 
     if (total == 0) return hipSuccess;
     if (total > 0x7fffff00ll) return hipErrorInvalidValue;
     direct_kernel<A_ALONG, B_ALONG, PA, PB, BM, BN, WM, WN, Epi>
-        <<<die_grid(total), WM * WN * 64, 0, s>>>(a, b, K, tm, tn, splits, split_len, (int)total, epi);
+        <<<line_grid(die_grid(total), WM * WN * 64), WM * WN * 64, 0, s>>>(a, b, K, tm, tn, splits, split_len, (int)total, epi);
     return hipGetLastError();
 }
 
@@ -320,7 +320,7 @@ template <typename T, int PL>
 __global__ __launch_bounds__(256) void lay_out_kernel(const T* x, long long rep, long long row, int rows, int cols, int ld, long long total, long long plane,
                                                       Labelled live, const unsigned* top, __bf16* out)
 {
-    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;          // chunk of eight
+    const long long at = line_block() * 256 + threadIdx.x;          // chunk of eight
     if (at >= total) return;
     const int chunks = ld / 8;
     const long long line = at / chunks;
@@ -347,7 +347,7 @@ hipError_t lay_out(int n, int rows, int cols, int ld, const Rows& x, Labelled li
 {
     const long long plane = (long long)n * rows * ld, total = plane / 8;
     if (total == 0) return hipSuccess;
-    lay_out_kernel<T, PL><<<(unsigned)((total + 255) / 256), 256, 0, s>>>((const T*)x.p, x.rep, x.row, rows, cols, ld, total, plane, live, top, out);
+    lay_out_kernel<T, PL><<<line_grid((total + 255) / 256, 256), 256, 0, s>>>((const T*)x.p, x.rep, x.row, rows, cols, ld, total, plane, live, top, out);
     return hipGetLastError();
 }
 inline hipError_t find_largest(int n, const Magnitudes& first, const Magnitudes& second, hipStream_t s)

@@ -19,6 +19,14 @@ inline bool chunked(const Rows& r, int bf16, long long cols)
     return ((uintptr_t)r.p & 15) == 0 && r.rep % unit == 0 && r.row % unit == 0 && cols % 8 == 0;
 }
 
+// A line of workgroups as a grid whose rows have fewer than 2^32 threads, which is what one dimension of a launch may have, and whole turns of the
+// chip's eight dies.
+inline dim3 line_grid(long long blocks, int threads)
+{
+    const long long row = std::min(blocks, 0xffffffffll / threads / tiles::kDies * tiles::kDies);
+    return dim3((unsigned)row, (unsigned)((blocks + row - 1) / row));
+}
+
 constexpr int kGroup = 32;         // values of a row that share an exponent
 inline long long packed_cols(long long cols) { return (cols + kGroup - 1) / kGroup * kGroup; }
 inline size_t align256(size_t n) { return (n + 255) / 256 * 256; }
@@ -83,6 +91,8 @@ constexpr int kFewWeights = 8;
 template <typename T> hipError_t launch_few_weights(const LossArgs& a, const T* g, int ld, const float* factor, hipStream_t s);
 
 // ---- device pieces ------------------------------------------------------------------------------------------------
+// this workgroup's place in the line of line_grid()
+__device__ __forceinline__ long long line_block() { return (long long)blockIdx.y * gridDim.x + blockIdx.x; }
 __device__ __forceinline__ float up(__bf16 v) { return (float)v; }
 __device__ __forceinline__ float up(float v) { return v; }
 // Eight consecutive values of a row, as they are in memory.  Vector accesses need no alignment of their own on this chip (a chunk

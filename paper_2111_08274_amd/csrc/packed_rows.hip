@@ -18,7 +18,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void pack_rows_kernel(const T* x, long long rep, long long row, int rows, int cols, int chunks,
                                                         long long total, int8_t* q, uint8_t* exps)
 {
-    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;          // (replica, row, chunk of 16)
+    const long long at = line_block() * 256 + threadIdx.x;          // (replica, row, chunk of 16)
     const bool live = at < total;
     const long long line = live ? at / chunks : 0;
     const int c = live ? (int)(at - line * chunks) * kLane : 0;
@@ -65,7 +65,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void unpack_rows_kernel(Packed src, int rows, int cols, int chunks, long long total, T* out,
                                                           long long rep, long long row)
 {
-    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+    const long long at = line_block() * 256 + threadIdx.x;
     if (at >= total) return;
     const long long line = at / chunks;
     const int c = (int)(at - line * chunks) * kLane;
@@ -88,7 +88,7 @@ hipError_t launch_pack(int n, int rows, int cols, int bf16, const Rows& x, void*
     const int chunks = (int)(p.cols / kLane);
     const long long total = (long long)n * rows * chunks;
     if (total == 0) return hipSuccess;
-    const unsigned grid = (unsigned)((total + 255) / 256);
+    const dim3 grid = line_grid((total + 255) / 256, 256);
     int8_t* q = const_cast<int8_t*>(p.q);
     uint8_t* e = const_cast<uint8_t*>(p.e);
     if (bf16) {
@@ -105,7 +105,7 @@ hipError_t launch_unpack(int n, int rows, int cols, int bf16, const void* packed
     const int chunks = (int)(p.cols / kLane);
     const long long total = (long long)n * rows * chunks;
     if (total == 0) return hipSuccess;
-    const unsigned grid = (unsigned)((total + 255) / 256);
+    const dim3 grid = line_grid((total + 255) / 256, 256);
     if (bf16) {
         unpack_rows_kernel<__bf16><<<grid, 256, 0, s>>>(p, rows, cols, chunks, total, (__bf16*)out.p, out.rep, out.row);
     } else {

@@ -175,7 +175,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(SA a, SB b, int K
     constexpr unsigned kBuf = PA * IA::kPlane + PB * IB::kPlane;
     __shared__ __attribute__((aligned(16))) char smem[NBUF * kBuf];
 
-    const unsigned item = logical_block();
+    const unsigned item = blockIdx.y * gridDim.x + logical_block();
     if (item >= (unsigned)total) return;
     const int tm_i = item % tiles_m, r1 = item / tiles_m, tn_i = r1 % tiles_n, r2 = r1 / tiles_n;
     Tile<TM, TN> t;
@@ -375,7 +375,7 @@ __global__ __launch_bounds__(256) void join_shares_kernel(const float* share, in
     constexpr int PER = 256 / G;
     __shared__ __attribute__((aligned(16))) float part[G][G > 1 ? PER * 8 : 8];
     const int mine = threadIdx.x % PER, group = threadIdx.x / PER;
-    const long long at = (long long)blockIdx.x * PER + mine;
+    const long long at = line_block() * PER + mine;
     f4 a = {}, b = {};
     if (at < total) {
         const float* src = share + at * 8;
@@ -410,7 +410,7 @@ hipError_t join_shares(const float* share, int splits, int replicas, int lines, 
     if (total == 0) return hipSuccess;
     auto* kernel = splits > 8 ? join_shares_kernel<T, 8> : join_shares_kernel<T, 1>;
     const int per = splits > 8 ? 32 : 256;
-    kernel<<<(unsigned)((total + per - 1) / per), 256, 0, s>>>(share, splits, all * ld, lines, cols, ld, total, live, factor, (T*)out.p, out.rep, out.row, last, last_rep);
+    kernel<<<line_grid((total + per - 1) / per, 256), 256, 0, s>>>(share, splits, all * ld, lines, cols, ld, total, live, factor, (T*)out.p, out.rep, out.row, last, last_rep);
     return hipGetLastError();
 }
 
@@ -426,7 +426,7 @@ hipError_t launch_product(const SA& a, const SB& b, int replicas, int M, int N, 
     if (total == 0) return hipSuccess;
     if (total > 0x7fffff00ll) return hipErrorInvalidValue;
     product_kernel<SA, A_ALONG, SB, B_ALONG, BM, BN, WM, WN, KS, NBUF, AHEAD, Epi>
-        <<<die_grid(total), WM * WN * 64, 0, s>>>(a, b, K, tm, tn, splits, split_len, (int)total, epi);
+        <<<line_grid(die_grid(total), WM * WN * 64), WM * WN * 64, 0, s>>>(a, b, K, tm, tn, splits, split_len, (int)total, epi);
     return hipGetLastError();
 }
 

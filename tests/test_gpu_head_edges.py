@@ -112,3 +112,42 @@ def test_a_vocabulary_whose_last_piece_would_hold_three_classes(shared):
     one = dict(x=c["x"], w=c["w"], bias=c["bias"], yh=c["yh"])
     _loss(one, 0, [o[:1] for o in out], 0)
     assert all(torch.equal(o[0], o[k]) for o in out for k in (1, n - 1))
+
+
+def test_more_rows_than_one_launch_has_threads_for():
+    # 2^24 rows of 4128 values, all the same one in memory: 2^32 threads and 2^27 more; the checkpoint's first lines and its last
+    torch = base._torch()
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 90 << 30:
+        pytest.skip("needs 72 GB of device memory")
+    n, rows, cols = 16, 1 << 20, 4128
+    x = torch.randn((1, 1, cols), device="cuda", generator=torch.Generator(device="cuda").manual_seed(0)).bfloat16()
+    one = hadfl.PackedRows(1, 1, cols, bf16=1).pack(x)
+    many = hadfl.PackedRows(n, rows, cols, bf16=1).pack(x.expand(n, rows, cols))
+    q, e = one.data[:cols], one.data[cols // 256 * 256 + 256:][:cols // 32]
+    got_q = many.data[:n * rows * cols].view(n * rows, cols)
+    got_e = many.data[n * rows * cols:][:n * rows * (cols // 32)].view(n * rows, cols // 32)
+    for t in (0, 1, 1 << 20, (1 << 23) + 5, n * rows - 1):
+        assert torch.equal(got_q[t], q) and torch.equal(got_e[t], e), t
+    assert bool((got_e == e).all())
+    del many, got_q, got_e
+    torch.cuda.empty_cache()
+
+
+def test_more_tiles_than_one_launch_has_threads_for():
+    # 2^22 rows and 2^17 classes are 2^23 tiles of 512 threads
+    torch = base._torch()
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 18 GB of device memory")
+    n, rows, d, v = 1024, 4096, 8, 131072
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x, w = torch.randn((1, rows, d), device="cuda", generator=g).bfloat16(), torch.randn((1, d, v), device="cuda", generator=g).bfloat16()
+    y = torch.randint(0, v, (1, rows), device="cuda", generator=g, dtype=torch.int32)
+    loss, row = hadfl.ClassLoss(n, rows, d, v, bf16=1, grad=False).loss(x.expand(n, rows, d), w.expand(n, d, v), y.repeat(n, 1))
+    assert bool((row == row[:1]).all()) and bool((loss == loss[0]).all())
+    some = slice(0, 64)
+    r = ref.class_loss(base._values(x[0, some]), base._values(w[0]), None, y[0, some].cpu().numpy().astype(np.int64))
+    b = ref.class_loss_bounds(r, base._values(w[0]), None, 1)
+    base._check(base._values(row[0, some]), r["row_loss"], b["row_loss"], "row_loss")
+    torch.cuda.empty_cache()

@@ -75,3 +75,21 @@ def test_no_operand_through_registers_has_fewer_columns_than_a_load_takes(launch
         assert all(int(q) >= 8 for v in through for q in v[7:]), (c, through)
         pieces.add(sum("Gradient" in v[0] for v in through))
     assert len(pieces) > 3
+
+
+def test_no_launch_has_more_threads_than_a_dimension_holds(launched):
+    # sizes within the header's limits whose workgroups, in one line, would be 2^32 threads or more
+    cases = [dict(op="pack", n=16, rows=1 << 20, features=4128, bf16=1), dict(op="pack", n=16, rows=1 << 20, features=1 << 17), dict(op="unpack", n=16, rows=1 << 20, features=1 << 17, bf16=1),
+             dict(op="loss", n=1024, rows=4096, features=8, classes=1 << 17, bf16=1, grad=0), dict(op="loss", n=16, rows=1 << 20, features=1 << 12, classes=1 << 17, bf16=1),
+             dict(op="loss", n=16, rows=1 << 20, features=1 << 12, classes=1 << 17), dict(op="loss", n=1024, rows=64, features=1 << 17, classes=1 << 20),
+             dict(op="loss", n=1024, rows=8, features=1 << 17, classes=1 << 18, bf16=1), dict(op="dense", n=1024, rows=64, inputs=1 << 16, outputs=1 << 16),
+             dict(op="dense", n=1024, rows=1 << 14, inputs=1 << 13, outputs=1 << 16, bf16=1), dict(op="norm", n=16, rows=1 << 20, features=1 << 17),
+             dict(op="norm", n=1024, rows=1 << 14, features=512)]
+    folded = 0
+    for c, r in zip(cases, launched(cases)):
+        assert r["status"] == 0, (c, r["text"])
+        for v in r["launches"]:
+            size = [int(q) for q in v[1:7]]
+            assert all(size[i] * size[i + 1] < 1 << 32 for i in (0, 2, 4)), (c, v)
+            folded += size[2] > 1 and _name(v) in ("pack_rows_kernel", "unpack_rows_kernel", "direct_kernel", "product_kernel", "few_weights_kernel", "lay_out_kernel", "join_shares_kernel")
+    assert folded > 8
