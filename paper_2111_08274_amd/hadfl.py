@@ -393,7 +393,7 @@ class Context:
 class _Operator:
     """Sizes, types and working memory of one operator on the current torch device.  Its tensors are torch device tensors
     [replica, row, column] (or [replica, column] for vectors) whose columns are contiguous; other strides are free.  Calls go
-    to `stream` or to the current one, and the tensors have to be ready there; calls of one object share its working memory
+    to `stream` or to the device's current one, and the tensors have to be ready there; calls of one object share its working memory
     and must not overlap in time.  Outputs that are not given are allocated, as memory of the stream the call goes to."""
 
     def __init__(self, desc, bf16, workspace=None):
@@ -405,6 +405,7 @@ class _Operator:
         self._structs = {}
         # the handle itself where torch offers it; the object around it takes longer to make than a kernel to launch
         self._current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+        self._device_now = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
         self._home, self._own = self._current(self.device.index), []
         self.work = None if workspace is None else self._bytes(workspace)
 
@@ -442,6 +443,12 @@ class _Operator:
             raise HadflError(EINVAL, "%s must be contiguous %s %s on %s" % (name, dtype, shape, self.device))
         return t.data_ptr() or None
 
+    def _kept(self, packed, shape):
+        """The address of a checkpoint, checked."""
+        if packed.shape != shape or packed.device != self.device:
+            raise HadflError(EINVAL, "the checkpoint holds %s on %s, not %s on %s" % (packed.shape, packed.device, shape, self.device))
+        return packed.data.data_ptr()
+
     def _out(self, t, shape, dtype, stream=None):
         if t is not None:
             return t
@@ -453,12 +460,21 @@ class _Operator:
     def _stream(self, stream, *others):
         """The handle of the stream a call goes to.  Away from the stream this object was made on, the allocator is told that
         its memory (and that of the other operators that the call uses) is in use there."""
+        if stream is not None and stream.device != self.device:
+            raise HadflError(EINVAL, "the stream is one of %s, not of %s" % (stream.device, self.device))
         h = self._current(self.device.index) if stream is None else stream.cuda_stream
         for o in (self,) + others:
             if h != o._home:
                 for t in o._own:
                     t.record_stream(self.torch.cuda.current_stream(self.device) if stream is None else stream)
         return h
+
+    def _call(self, entry, *args):
+        """A call of the library with the operator's device current, which a stream's handle does not name: the default one is 0 on all."""
+        if self._device_now() == self.device.index:
+            return _check(entry(self._ref, *args))
+        with self.torch.cuda.device(self.device):
+            return _check(entry(self._ref, *args))
 
 
 class LayerNorm(_Operator):
@@ -475,9 +491,9 @@ class LayerNorm(_Operator):
     def forward(self, x, gamma, beta, y=None, stream=None):
         f32 = self.torch.float32
         y = self._out(y, self.shape, self.dtype, stream)
-        _check(lib().hadfl_norm_forward(self._ref, self._rows("x", x, self.shape, self.dtype), self._rows("gamma", gamma, self.vector, f32),
-                                        self._rows("beta", beta, self.vector, f32), self._rows("y", y, self.shape, self.dtype),
-                                        self.mean.data_ptr() or None, self.rstd.data_ptr() or None, self._stream(stream)))
+        self._call(lib().hadfl_norm_forward, self._rows("x", x, self.shape, self.dtype), self._rows("gamma", gamma, self.vector, f32),
+                   self._rows("beta", beta, self.vector, f32), self._rows("y", y, self.shape, self.dtype),
+                   self.mean.data_ptr() or None, self.rstd.data_ptr() or None, self._stream(stream))
         return y
 
     def backward(self, dy, x, gamma, dx=None, dgamma=None, dbeta=None, stream=None):
@@ -486,15 +502,12 @@ class LayerNorm(_Operator):
         dx, dgamma, dbeta = self._out(dx, self.shape, self.dtype, stream), self._out(dgamma, self.vector, f32, stream), self._out(dbeta, self.vector, f32, stream)
         packed, others = None, ()
         if isinstance(x, PackedRows):
-            if x.shape != self.shape:
-                raise HadflError(EINVAL, "the checkpoint holds %s, not %s" % (x.shape, self.shape))
-            others = (x,)
-            x, packed = None, x.data.data_ptr()
-        _check(lib().hadfl_norm_backward(self._ref, self._rows("dy", dy, self.shape, self.dtype), self._rows("x", x, self.shape, self.dtype),
-                                         packed, self._rows("gamma", gamma, self.vector, f32), self.mean.data_ptr() or None,
-                                         self.rstd.data_ptr() or None, self._rows("dx", dx, self.shape, self.dtype),
-                                         self._rows("dgamma", dgamma, self.vector, f32), self._rows("dbeta", dbeta, self.vector, f32),
-                                         self.work.data_ptr(), self._stream(stream, *others)))
+            others, packed, x = (x,), self._kept(x, self.shape), None
+        self._call(lib().hadfl_norm_backward, self._rows("dy", dy, self.shape, self.dtype), self._rows("x", x, self.shape, self.dtype),
+                   packed, self._rows("gamma", gamma, self.vector, f32), self.mean.data_ptr() or None,
+                   self.rstd.data_ptr() or None, self._rows("dx", dx, self.shape, self.dtype),
+                   self._rows("dgamma", dgamma, self.vector, f32), self._rows("dbeta", dbeta, self.vector, f32),
+                   self.work.data_ptr(), self._stream(stream, *others))
         return dx, dgamma, dbeta
 
 
@@ -508,12 +521,12 @@ class PackedRows(_Operator):
         self.data = self._bytes(lib().hadfl_packed_bytes)
 
     def pack(self, x, stream=None):
-        _check(lib().hadfl_pack_rows(self._ref, self._rows("x", x, self.shape, self.dtype), self.data.data_ptr(), self._stream(stream)))
+        self._call(lib().hadfl_pack_rows, self._rows("x", x, self.shape, self.dtype), self.data.data_ptr(), self._stream(stream))
         return self
 
     def unpack(self, out=None, stream=None):
         out = self._out(out, self.shape, self.dtype, stream)
-        _check(lib().hadfl_unpack_rows(self._ref, self.data.data_ptr(), self._rows("out", out, self.shape, self.dtype), self._stream(stream)))
+        self._call(lib().hadfl_unpack_rows, self.data.data_ptr(), self._rows("out", out, self.shape, self.dtype), self._stream(stream))
         return out
 
 
@@ -528,13 +541,12 @@ class DenseGrad(_Operator):
     def backward(self, packed, dy, dw=None, db=None, bias=True, stream=None):
         """-> dw, db; bias=False leaves db out (None)"""
         f32 = self.torch.float32
-        if packed.shape != (self.n, self.rows, self.n_in):
-            raise HadflError(EINVAL, "the checkpoint holds %s, not %s" % (packed.shape, (self.n, self.rows, self.n_in)))
+        kept = self._kept(packed, (self.n, self.rows, self.n_in))
         dw = self._out(dw, (self.n, self.n_in, self.n_out), f32, stream)
         db = self._out(db, (self.n, self.n_out), f32, stream) if bias else None
-        _check(lib().hadfl_dense_grad_packed(self._ref, packed.data.data_ptr(), self._rows("dy", dy, (self.n, self.rows, self.n_out), self.dtype),
-                                             self._rows("dw", dw, (self.n, self.n_in, self.n_out), f32),
-                                             self._rows("db", db, (self.n, self.n_out), f32), self.work.data_ptr(), self._stream(stream, packed)))
+        self._call(lib().hadfl_dense_grad_packed, kept, self._rows("dy", dy, (self.n, self.rows, self.n_out), self.dtype),
+                   self._rows("dw", dw, (self.n, self.n_in, self.n_out), f32),
+                   self._rows("db", db, (self.n, self.n_out), f32), self.work.data_ptr(), self._stream(stream, packed))
         return dw, db
 
 
@@ -551,7 +563,7 @@ class ClassLoss(_Operator):
 
     def _inputs(self, x, w, labels, bias, row_loss, loss):
         f32, i32 = self.torch.float32, self.torch.int32
-        return (self._ref, self._rows("x", x, (self.n, self.rows, self.features), self.dtype),
+        return (self._rows("x", x, (self.n, self.rows, self.features), self.dtype),
                 self._rows("w", w, (self.n, self.features, self.classes), self.dtype), self._rows("bias", bias, (self.n, self.classes), f32),
                 self._plain("labels", labels, (self.n, self.rows), i32), self._plain("loss", loss, (self.n,), f32),
                 self._plain("row_loss", row_loss, (self.n, self.rows), f32))
@@ -560,7 +572,7 @@ class ClassLoss(_Operator):
         """-> loss [n_replicas] (mean over the labelled rows), row_loss [n_replicas, n_rows]"""
         f32 = self.torch.float32
         loss, row_loss = self._out(loss, (self.n,), f32, stream), self._out(row_loss, (self.n, self.rows), f32, stream)
-        _check(lib().hadfl_loss_forward(*self._inputs(x, w, labels, bias, row_loss, loss), self.work.data_ptr(), self._stream(stream)))
+        self._call(lib().hadfl_loss_forward, *self._inputs(x, w, labels, bias, row_loss, loss), self.work.data_ptr(), self._stream(stream))
         return loss, row_loss
 
     def grad(self, x, w, labels, bias=None, loss=None, row_loss=None, dx=None, dw=None, db=None, want=("dx", "dw", "db"), stream=None):
@@ -572,8 +584,8 @@ class ClassLoss(_Operator):
         dx = self._out(dx, (self.n, self.rows, self.features), self.dtype, stream) if "dx" in want else None
         dw = self._out(dw, (self.n, self.features, self.classes), self.dtype, stream) if "dw" in want else None
         db = self._out(db, (self.n, self.classes), f32, stream) if "db" in want and bias is not None else None
-        _check(lib().hadfl_loss_grad(*self._inputs(x, w, labels, bias, row_loss, loss),
-                                     self._rows("dx", dx, (self.n, self.rows, self.features), self.dtype),
-                                     self._rows("dw", dw, (self.n, self.features, self.classes), self.dtype),
-                                     self._rows("db", db, (self.n, self.classes), f32), self.work.data_ptr(), self._stream(stream)))
+        self._call(lib().hadfl_loss_grad, *self._inputs(x, w, labels, bias, row_loss, loss),
+                   self._rows("dx", dx, (self.n, self.rows, self.features), self.dtype),
+                   self._rows("dw", dw, (self.n, self.features, self.classes), self.dtype),
+                   self._rows("db", db, (self.n, self.classes), f32), self.work.data_ptr(), self._stream(stream))
         return loss, row_loss, dx, dw, db

@@ -1,0 +1,135 @@
+"""The binding's classes of the head's operators, on a CPU: what they pass to the library, on which device, and what they refuse.  torch's
+device side and the library are stood in for; tensors are shapes, strides and addresses."""
+import types
+
+import pytest
+
+from paper_2111_08274_amd import hadfl
+
+
+class Device:
+    def __init__(self, kind, index):
+        self.type, self.index = kind, index
+
+    def __eq__(self, other):
+        return (self.type, self.index) == (other.type, other.index)
+
+
+class Tensor:
+    def __init__(self, shape, dtype, device, requires_grad=False):
+        self.shape, self.dtype, self.device, self.requires_grad = tuple(shape), dtype, device, requires_grad
+        self.recorded = []
+
+    def stride(self):
+        out, step = [], 1
+        for s in reversed(self.shape):
+            out.append(step)
+            step *= s
+        return tuple(reversed(out))
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 1 << 20
+
+    def record_stream(self, s):
+        self.recorded.append(s)
+
+
+class Stream:
+    def __init__(self, handle, device):
+        self.cuda_stream, self.device = handle, device
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *a):
+        pass
+
+
+class Machine:
+    """Two devices; the library writes down on which of them each call came, to which stream."""
+
+    def __init__(self, monkeypatch):
+        import torch
+        self.now, self.calls, self.grad_mode = 0, [], True
+        machine = self
+
+        class Guard:
+            def __init__(self, d):
+                self.d = d if isinstance(d, int) else d.index
+
+            def __enter__(self):
+                self.before, machine.now = machine.now, self.d
+
+            def __exit__(self, *a):
+                machine.now = self.before
+
+        fake = types.ModuleType("torch")
+        fake.float32, fake.bfloat16, fake.uint8, fake.int32 = "f32", "bf16", "u8", "i32"
+        fake.device = Device
+        fake.empty = lambda shape, dtype, device: Tensor(shape if isinstance(shape, tuple) else (shape,), dtype, device)
+        fake.is_grad_enabled = lambda: machine.grad_mode
+        fake._C = types.SimpleNamespace()
+        fake.cuda = types.SimpleNamespace(current_device=lambda: machine.now, device=Guard, stream=lambda s: s,
+                                          current_stream=lambda i=None: Stream(0, Device("cuda", machine.now if i is None else i if isinstance(i, int) else i.index)))
+        real = hadfl.lib()
+        entries = {name: (lambda *a, _name=name: (machine.calls.append((_name, machine.now, a)), 0)[1])
+                   for name in hadfl.EXPORTS if name.startswith(("hadfl_norm_", "hadfl_pack", "hadfl_unpack", "hadfl_dense", "hadfl_loss"))}
+        for name in ("hadfl_norm_workspace", "hadfl_packed_bytes", "hadfl_dense_workspace", "hadfl_loss_workspace", "hadfl_last_error"):
+            entries[name] = getattr(real, name)
+        monkeypatch.setattr(hadfl, "_lib", types.SimpleNamespace(**entries))
+        monkeypatch.setitem(__import__("sys").modules, "torch", fake)
+        assert torch is not fake
+
+    def on(self, index):
+        self.now = index
+        return Device("cuda", index)
+
+
+@pytest.fixture
+def machine(monkeypatch):
+    return Machine(monkeypatch)
+
+
+def _calls(device, n=2, rows=3, f=8, v=16):
+    """One call of every kind: (operator, method, arguments)"""
+    t = lambda *s, dtype="f32": Tensor(s, dtype, device)  # noqa: E731
+    norm, kept, dense, loss = hadfl.LayerNorm(n, rows, f), hadfl.PackedRows(n, rows, f), hadfl.DenseGrad(n, rows, f, v), hadfl.ClassLoss(n, rows, f, v)
+    x, w, y, vec = t(n, rows, f), t(n, f, v), t(n, rows, dtype="i32"), t(n, f)
+    return [(norm.forward, (x, vec, vec)), (norm.backward, (x, x, vec)), (kept.pack, (x,)), (kept.unpack, ()), (norm.backward, (x, kept, vec)),
+            (dense.backward, (kept, t(n, rows, v))), (loss.loss, (x, w, y)), (loss.grad, (x, w, y))]
+
+
+def test_calls_reach_the_device_of_the_operator(machine):
+    # a stream's handle does not name its device (the default one is 0 on all): a call from a thread on another device
+    calls = _calls(machine.on(1))
+    for now in (0, 1):
+        machine.on(now)
+        for call, args in calls:
+            machine.calls.clear()
+            call(*args)
+            assert [d for _, d, _ in machine.calls] == [1] and machine.now == now, call
+
+
+def test_a_stream_of_another_device_is_refused(machine):
+    calls = _calls(machine.on(1))
+    for call, args in calls:
+        machine.calls.clear()
+        call(*args, stream=Stream(7, Device("cuda", 1)))
+        with pytest.raises(hadfl.HadflError, match="stream"):
+            call(*args, stream=Stream(7, Device("cuda", 0)))
+        assert len(machine.calls) == 1
+
+
+def test_a_checkpoint_of_another_device_or_shape_is_refused(machine):
+    kept, other = hadfl.PackedRows(2, 3, 8), hadfl.PackedRows(2, 3, 9)
+    device = machine.on(1)
+    norm, dense = hadfl.LayerNorm(2, 3, 8), hadfl.DenseGrad(2, 3, 8, 16)
+    for wrong in (kept, other):
+        with pytest.raises(hadfl.HadflError, match="checkpoint"):
+            norm.backward(Tensor((2, 3, 8), "f32", device), wrong, Tensor((2, 8), "f32", device))
+        with pytest.raises(hadfl.HadflError, match="checkpoint"):
+            dense.backward(wrong, Tensor((2, 3, 16), "f32", device))
+    assert not machine.calls
