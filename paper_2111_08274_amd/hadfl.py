@@ -390,6 +390,14 @@ class Context:
 
 
 # ---- operators of a language model's head ----------------------------------------------------------------------------
+def _int32(*values):
+    """The sizes as the library's structs hold them; ctypes would keep the low 32 bits of any number."""
+    out = [int(v) for v in values]
+    if any(not -2 ** 31 <= v < 2 ** 31 for v in out):
+        raise HadflError(EINVAL, "%s: a size must fit 32 bits" % (values,))
+    return out
+
+
 class _Operator:
     """Sizes, types and working memory of one operator on the current torch device.  Its tensors are torch device tensors
     [replica, row, column] (or [replica, column] for vectors) whose columns are contiguous; other strides are free.  Calls go
@@ -482,8 +490,9 @@ class LayerNorm(_Operator):
     forward() leaves the rows' statistics in `mean` and `rstd` for backward()."""
 
     def __init__(self, n_replicas, n_rows, n_features, bf16=0, eps=1e-5):
-        super().__init__(HadflNorm(int(n_replicas), int(n_rows), int(n_features), int(bf16), float(eps)), bf16, lib().hadfl_norm_workspace)
-        self.shape, self.vector = (int(n_replicas), int(n_rows), int(n_features)), (int(n_replicas), int(n_features))
+        n, rows, features, bf16 = _int32(n_replicas, n_rows, n_features, bf16)
+        super().__init__(HadflNorm(n, rows, features, bf16, float(eps)), bf16, lib().hadfl_norm_workspace)
+        self.shape, self.vector = (n, rows, features), (n, features)
         f32 = self.torch.float32
         self.mean = self._keep(self.torch.empty(self.shape[:2], dtype=f32, device=self.device))
         self.rstd = self._keep(self.torch.empty(self.shape[:2], dtype=f32, device=self.device))
@@ -516,8 +525,9 @@ class PackedRows(_Operator):
     writes."""
 
     def __init__(self, n_replicas, n_rows, n_features, bf16=0):
-        super().__init__(HadflPack(int(n_replicas), int(n_rows), int(n_features), int(bf16)), bf16)
-        self.shape = (int(n_replicas), int(n_rows), int(n_features))
+        n, rows, features, bf16 = _int32(n_replicas, n_rows, n_features, bf16)
+        super().__init__(HadflPack(n, rows, features, bf16), bf16)
+        self.shape = (n, rows, features)
         self.data = self._bytes(lib().hadfl_packed_bytes)
 
     def pack(self, x, stream=None):
@@ -535,8 +545,8 @@ class DenseGrad(_Operator):
     [n_replicas, n_rows, n_out]."""
 
     def __init__(self, n_replicas, n_rows, n_in, n_out, bf16=0):
-        super().__init__(HadflDense(int(n_replicas), int(n_rows), int(n_in), int(n_out), int(bf16)), bf16, lib().hadfl_dense_workspace)
-        self.n, self.rows, self.n_in, self.n_out = int(n_replicas), int(n_rows), int(n_in), int(n_out)
+        self.n, self.rows, self.n_in, self.n_out, bf16 = _int32(n_replicas, n_rows, n_in, n_out, bf16)
+        super().__init__(HadflDense(self.n, self.rows, self.n_in, self.n_out, bf16), bf16, lib().hadfl_dense_workspace)
 
     def backward(self, packed, dy, dw=None, db=None, bias=True, stream=None):
         """-> dw, db; bias=False leaves db out (None)"""
@@ -556,10 +566,9 @@ class ClassLoss(_Operator):
     n_rows] int32; a label outside [0, n_classes) marks a row that takes no part."""
 
     def __init__(self, n_replicas, n_rows, n_features, n_classes, bf16=0, grad=True):
-        desc = HadflLoss(int(n_replicas), int(n_rows), int(n_features), int(n_classes), int(bf16))
-        query = lib().hadfl_loss_workspace
-        super().__init__(desc, bf16, lambda ref, out: query(ref, int(bool(grad)), out))
-        self.n, self.rows, self.features, self.classes, self.with_grad = int(n_replicas), int(n_rows), int(n_features), int(n_classes), bool(grad)
+        self.n, self.rows, self.features, self.classes, bf16 = _int32(n_replicas, n_rows, n_features, n_classes, bf16)
+        self.with_grad, query = bool(grad), lib().hadfl_loss_workspace
+        super().__init__(HadflLoss(self.n, self.rows, self.features, self.classes, bf16), bf16, lambda ref, out: query(ref, int(self.with_grad), out))
 
     def _inputs(self, x, w, labels, bias, row_loss, loss):
         f32, i32 = self.torch.float32, self.torch.int32

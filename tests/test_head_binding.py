@@ -133,3 +133,16 @@ def test_a_checkpoint_of_another_device_or_shape_is_refused(machine):
         with pytest.raises(hadfl.HadflError, match="checkpoint"):
             dense.backward(wrong, Tensor((2, 3, 16), "f32", device))
     assert not machine.calls
+
+
+@pytest.mark.parametrize("size", [(1 << 32) + 2, -(1 << 32) + 2, 1 << 31, (1 << 64) + 2])
+def test_sizes_that_a_32_bit_field_cannot_hold_are_refused(machine, size):
+    # ctypes would keep the low 32 bits: an operator of two rows for tensors of 2^32 + 2
+    makers = [(hadfl.LayerNorm, 3), (hadfl.PackedRows, 3), (hadfl.DenseGrad, 4), (hadfl.ClassLoss, 4)]
+    for make, sizes in makers:
+        make(*[2] * sizes)
+        for i in range(sizes + 1):
+            args = [2] * sizes + [0]
+            args[i] = size
+            with pytest.raises(hadfl.HadflError, match="32 bits"):
+                make(*args)
