@@ -585,14 +585,14 @@ class ClassLoss(_Operator):
         return loss, row_loss
 
     def grad(self, x, w, labels, bias=None, loss=None, row_loss=None, dx=None, dw=None, db=None, want=("dx", "dw", "db"), stream=None):
-        """-> loss, row_loss, dx, dw, db of the mean losses; what `want` leaves out, and db without a bias, is None"""
+        """-> loss, row_loss, dx, dw, db of the mean losses; what `want` leaves out is None, and so is db where neither it nor a bias is given"""
         if not self.with_grad:
             raise HadflError(ESTATE, "this ClassLoss was made with grad=False")
         f32 = self.torch.float32
         loss, row_loss = self._out(loss, (self.n,), f32, stream), self._out(row_loss, (self.n, self.rows), f32, stream)
         dx = self._out(dx, (self.n, self.rows, self.features), self.dtype, stream) if "dx" in want else None
         dw = self._out(dw, (self.n, self.features, self.classes), self.dtype, stream) if "dw" in want else None
-        db = self._out(db, (self.n, self.classes), f32, stream) if "db" in want and bias is not None else None
+        db = self._out(db, (self.n, self.classes), f32, stream) if "db" in want and (bias is not None or db is not None) else None
         self._call(lib().hadfl_loss_grad, *self._inputs(x, w, labels, bias, row_loss, loss),
                    self._rows("dx", dx, (self.n, self.rows, self.features), self.dtype),
                    self._rows("dw", dw, (self.n, self.features, self.classes), self.dtype),

@@ -151,3 +151,13 @@ def test_more_tiles_than_one_launch_has_threads_for():
     b = ref.class_loss_bounds(r, base._values(w[0]), None, 1)
     base._check(base._values(row[0, some]), r["row_loss"], b["row_loss"], "row_loss")
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("n,rows,d,v,bf16", [(2, 5, 40, 300, 0), (2, 100, 40, 300, 1), (2, 500, 40, 1000, 0), (1, 500, 800, 2056, 1)])
+def test_db_without_a_bias(n, rows, d, v, bf16):
+    c = base._loss_case(n, rows, d, v, bf16, "whole", False)
+    db = base._out((n, v), 0, "odd")
+    out = hadfl.ClassLoss(n, rows, d, v, bf16=bf16).grad(c["x"], c["w"], c["y"], db=db.t)
+    assert out[4] is db.t and db.untouched()
+    for k in range(n):
+        _loss(c, k, out, bf16)

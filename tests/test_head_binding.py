@@ -146,3 +146,16 @@ def test_sizes_that_a_32_bit_field_cannot_hold_are_refused(machine, size):
             args[i] = size
             with pytest.raises(hadfl.HadflError, match="32 bits"):
                 make(*args)
+
+
+def test_a_db_that_is_given_is_written_without_a_bias_too(machine):
+    device = machine.on(0)
+    loss = hadfl.ClassLoss(2, 3, 8, 16)
+    t = lambda *s, dtype="f32": Tensor(s, dtype, device)  # noqa: E731
+    x, w, y, db = t(2, 3, 8), t(2, 8, 16), t(2, 3, dtype="i32"), t(2, 16)
+    for kw, is_out in ((dict(), False), (dict(db=db), True), (dict(db=db, want=("dx", "dw")), False), (dict(bias=t(2, 16)), True)):
+        machine.calls.clear()
+        out = loss.grad(x, w, y, **kw)[4]
+        passed = machine.calls[0][2][9]                       # the address of db's hadfl_rows
+        assert (out is not None) == is_out == (passed is not None), kw
+        assert "db" not in kw or out is None or out is db
