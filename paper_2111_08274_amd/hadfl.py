@@ -487,7 +487,9 @@ class _Operator:
 
 class LayerNorm(_Operator):
     """Layer norm of [n_replicas, n_rows, n_features] with gamma, beta [n_replicas, n_features] (32-bit), and its gradient.
-    forward() leaves the rows' statistics in `mean` and `rstd` for backward()."""
+    backward() takes the rows' statistics that forward() left, in `mean` and `rstd` of this object, which hold those of its last pass, or in a
+    pair of the caller's: stats=(mean, rstd), 32-bit [n_replicas, n_rows], given to both.  forward(stats=False) leaves none and keeps what is
+    there (an evaluation between a forward pass and its gradient)."""
 
     def __init__(self, n_replicas, n_rows, n_features, bf16=0, eps=1e-5):
         n, rows, features, bf16 = _int32(n_replicas, n_rows, n_features, bf16)
@@ -496,25 +498,35 @@ class LayerNorm(_Operator):
         f32 = self.torch.float32
         self.mean = self._keep(self.torch.empty(self.shape[:2], dtype=f32, device=self.device))
         self.rstd = self._keep(self.torch.empty(self.shape[:2], dtype=f32, device=self.device))
+        self._left = rows == 0                                # statistics are there
 
-    def forward(self, x, gamma, beta, y=None, stream=None):
+    def _stats(self, stats):
+        if stats is None:
+            return self.mean.data_ptr() or None, self.rstd.data_ptr() or None
+        if stats is False:
+            return None, None
+        mean, rstd = stats
+        return self._plain("mean", mean, self.shape[:2], self.torch.float32), self._plain("rstd", rstd, self.shape[:2], self.torch.float32)
+
+    def forward(self, x, gamma, beta, y=None, stream=None, stats=None):
         f32 = self.torch.float32
         y = self._out(y, self.shape, self.dtype, stream)
         self._call(lib().hadfl_norm_forward, self._rows("x", x, self.shape, self.dtype), self._rows("gamma", gamma, self.vector, f32),
-                   self._rows("beta", beta, self.vector, f32), self._rows("y", y, self.shape, self.dtype),
-                   self.mean.data_ptr() or None, self.rstd.data_ptr() or None, self._stream(stream))
+                   self._rows("beta", beta, self.vector, f32), self._rows("y", y, self.shape, self.dtype), *self._stats(stats), self._stream(stream))
+        self._left = self._left or stats is None
         return y
 
-    def backward(self, dy, x, gamma, dx=None, dgamma=None, dbeta=None, stream=None):
+    def backward(self, dy, x, gamma, dx=None, dgamma=None, dbeta=None, stream=None, stats=None):
         """x: the tensor given to forward() or the PackedRows that holds it.  -> dx, dgamma, dbeta"""
         f32 = self.torch.float32
         dx, dgamma, dbeta = self._out(dx, self.shape, self.dtype, stream), self._out(dgamma, self.vector, f32, stream), self._out(dbeta, self.vector, f32, stream)
         packed, others = None, ()
         if isinstance(x, PackedRows):
             others, packed, x = (x,), self._kept(x, self.shape), None
+        if stats is None and not self._left:
+            raise HadflError(ESTATE, "no forward() of this LayerNorm has left its statistics")
         self._call(lib().hadfl_norm_backward, self._rows("dy", dy, self.shape, self.dtype), self._rows("x", x, self.shape, self.dtype),
-                   packed, self._rows("gamma", gamma, self.vector, f32), self.mean.data_ptr() or None,
-                   self.rstd.data_ptr() or None, self._rows("dx", dx, self.shape, self.dtype),
+                   packed, self._rows("gamma", gamma, self.vector, f32), *self._stats(stats), self._rows("dx", dx, self.shape, self.dtype),
                    self._rows("dgamma", dgamma, self.vector, f32), self._rows("dbeta", dbeta, self.vector, f32),
                    self.work.data_ptr(), self._stream(stream, *others))
         return dx, dgamma, dbeta

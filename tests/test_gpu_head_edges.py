@@ -161,3 +161,20 @@ def test_db_without_a_bias(n, rows, d, v, bf16):
     assert out[4] is db.t and db.untouched()
     for k in range(n):
         _loss(c, k, out, bf16)
+
+
+def test_an_evaluation_between_a_forward_pass_and_its_gradient():
+    torch = base._torch()
+    c, other = base._norm_case(2, 9, 200, 0, "whole"), base._norm_case(2, 9, 200, 0, "whole", seed=1)
+    plan = hadfl.LayerNorm(2, 9, 200)
+    y = plan.forward(c["x"], c["gamma"], c["beta"])
+    want = plan.backward(c["dy"], c["x"], c["gamma"])
+    mine = torch.empty((2, 9), device="cuda"), torch.empty((2, 9), device="cuda")
+    seen = plan.forward(other["x"], other["gamma"], other["beta"], stats=False)
+    assert torch.equal(seen, plan.forward(other["x"], other["gamma"], other["beta"], stats=mine))
+    assert all(torch.equal(p, q) for p, q in zip(want, plan.backward(c["dy"], c["x"], c["gamma"])))
+    fresh = hadfl.LayerNorm(2, 9, 200)
+    assert torch.equal(fresh.forward(other["x"], other["gamma"], other["beta"]), seen)
+    assert all(torch.equal(p, q) for p, q in zip(fresh.backward(other["dy"], other["x"], other["gamma"]),
+                                                 plan.backward(other["dy"], other["x"], other["gamma"], stats=mine)))
+    assert torch.equal(plan.forward(c["x"], c["gamma"], c["beta"]), y)

@@ -1,5 +1,6 @@
 """The binding's classes of the head's operators, on a CPU: what they pass to the library, on which device, and what they refuse.  torch's
 device side and the library are stood in for; tensors are shapes, strides and addresses."""
+import itertools
 import types
 
 import pytest
@@ -16,9 +17,8 @@ class Device:
 
 
 class Tensor:
-    def __init__(self, shape, dtype, device, requires_grad=False):
-        self.shape, self.dtype, self.device, self.requires_grad = tuple(shape), dtype, device, requires_grad
-        self.recorded = []
+    def __init__(self, shape, dtype, device, requires_grad=False, at=1 << 20):
+        self.shape, self.dtype, self.device, self.requires_grad, self.at = tuple(shape), dtype, device, requires_grad, at
 
     def stride(self):
         out, step = [], 1
@@ -31,10 +31,10 @@ class Tensor:
         return True
 
     def data_ptr(self):
-        return 1 << 20
+        return self.at
 
     def record_stream(self, s):
-        self.recorded.append(s)
+        pass
 
 
 class Stream:
@@ -69,7 +69,8 @@ class Machine:
         fake = types.ModuleType("torch")
         fake.float32, fake.bfloat16, fake.uint8, fake.int32 = "f32", "bf16", "u8", "i32"
         fake.device = Device
-        fake.empty = lambda shape, dtype, device: Tensor(shape if isinstance(shape, tuple) else (shape,), dtype, device)
+        room = itertools.count(16 << 20, 1 << 20)
+        fake.empty = lambda shape, dtype, device: Tensor(shape if isinstance(shape, tuple) else (shape,), dtype, device, at=next(room))
         fake.is_grad_enabled = lambda: machine.grad_mode
         fake._C = types.SimpleNamespace()
         fake.cuda = types.SimpleNamespace(current_device=lambda: machine.now, device=Guard, stream=lambda s: s,
@@ -159,3 +160,31 @@ def test_a_db_that_is_given_is_written_without_a_bias_too(machine):
         passed = machine.calls[0][2][9]                       # the address of db's hadfl_rows
         assert (out is not None) == is_out == (passed is not None), kw
         assert "db" not in kw or out is None or out is db
+
+
+def test_statistics_of_the_norm_are_the_forward_pass_s_own(machine):
+    # by default the object's own; a pass that leaves none keeps the last ones; a pair of the caller's for passes in flight together
+    device = machine.on(0)
+    norm = hadfl.LayerNorm(2, 3, 8)
+    x, vec = Tensor((2, 3, 8), "f32", device), Tensor((2, 8), "f32", device)
+    mine = Tensor((2, 3), "f32", device, at=5 << 20), Tensor((2, 3), "f32", device, at=6 << 20)
+    with pytest.raises(hadfl.HadflError, match="forward") as e:
+        norm.backward(x, x, vec)
+    assert e.value.status == hadfl.ESTATE
+    norm.forward(x, vec, vec, stats=False)
+    norm.forward(x, vec, vec, stats=mine)
+    with pytest.raises(hadfl.HadflError, match="forward"):
+        norm.backward(x, x, vec)
+    norm.backward(x, x, vec, stats=mine)
+    own = norm.mean.data_ptr(), norm.rstd.data_ptr()
+    norm.forward(x, vec, vec)
+    norm.backward(x, x, vec)
+    got = [(name, a[5:7]) for name, _, a in machine.calls]
+    f, b = "hadfl_norm_forward", "hadfl_norm_backward"
+    assert got == [(f, (None, None)), (f, (5 << 20, 6 << 20)), (b, (5 << 20, 6 << 20)), (f, own), (b, own)]
+    for wrong in ((mine[0], Tensor((2, 4), "f32", device)), (Tensor((2, 3), "bf16", device), mine[1]), (mine[0], Tensor((2, 3), "f32", Device("cuda", 1)))):
+        with pytest.raises(hadfl.HadflError):
+            norm.forward(x, vec, vec, stats=wrong)
+        with pytest.raises(hadfl.HadflError):
+            norm.backward(x, x, vec, stats=wrong)
+    assert hadfl.LayerNorm(2, 0, 8).backward(Tensor((2, 0, 8), "f32", device), Tensor((2, 0, 8), "f32", device), vec)      # nothing to take from
