@@ -402,7 +402,8 @@ class _Operator:
     """Sizes, types and working memory of one operator on the current torch device.  Its tensors are torch device tensors
     [replica, row, column] (or [replica, column] for vectors) whose columns are contiguous; other strides are free.  Calls go
     to `stream` or to the device's current one, and the tensors have to be ready there; calls of one object share its working memory
-    and must not overlap in time.  Outputs that are not given are allocated, as memory of the stream the call goes to."""
+    and must not overlap in time.  Outputs that are not given are allocated, as memory of the stream the call goes to.  autograd records none of the
+    calls: a forward pass of tensors that require a gradient is refused in grad mode (an autograd.Function runs outside of it)."""
 
     def __init__(self, desc, bf16, workspace=None):
         import torch
@@ -450,6 +451,11 @@ class _Operator:
         if t.dtype != dtype or t.device != self.device or t.shape != shape or not t.is_contiguous():
             raise HadflError(EINVAL, "%s must be contiguous %s %s on %s" % (name, dtype, shape, self.device))
         return t.data_ptr() or None
+
+    def _no_graph(self, *inputs):
+        for t in inputs:
+            if t is not None and t.requires_grad and self.torch.is_grad_enabled():
+                raise HadflError(EINVAL, "an input requires a gradient, which the result would not pass on: call under torch.no_grad()")
 
     def _kept(self, packed, shape):
         """The address of a checkpoint, checked."""
@@ -510,6 +516,7 @@ class LayerNorm(_Operator):
 
     def forward(self, x, gamma, beta, y=None, stream=None, stats=None):
         f32 = self.torch.float32
+        self._no_graph(x, gamma, beta)
         y = self._out(y, self.shape, self.dtype, stream)
         self._call(lib().hadfl_norm_forward, self._rows("x", x, self.shape, self.dtype), self._rows("gamma", gamma, self.vector, f32),
                    self._rows("beta", beta, self.vector, f32), self._rows("y", y, self.shape, self.dtype), *self._stats(stats), self._stream(stream))
@@ -592,6 +599,7 @@ class ClassLoss(_Operator):
     def loss(self, x, w, labels, bias=None, loss=None, row_loss=None, stream=None):
         """-> loss [n_replicas] (mean over the labelled rows), row_loss [n_replicas, n_rows]"""
         f32 = self.torch.float32
+        self._no_graph(x, w, bias)
         loss, row_loss = self._out(loss, (self.n,), f32, stream), self._out(row_loss, (self.n, self.rows), f32, stream)
         self._call(lib().hadfl_loss_forward, *self._inputs(x, w, labels, bias, row_loss, loss), self.work.data_ptr(), self._stream(stream))
         return loss, row_loss

@@ -188,3 +188,27 @@ def test_statistics_of_the_norm_are_the_forward_pass_s_own(machine):
         with pytest.raises(hadfl.HadflError):
             norm.backward(x, x, vec, stats=wrong)
     assert hadfl.LayerNorm(2, 0, 8).backward(Tensor((2, 0, 8), "f32", device), Tensor((2, 0, 8), "f32", device), vec)      # nothing to take from
+
+
+def test_inputs_that_ask_for_a_graph_are_refused_where_a_result_would_lack_it(machine):
+    # forward passes hand out tensors that autograd would take for constants; the gradient calls give the gradients themselves
+    device = machine.on(0)
+    norm, loss, kept, dense = hadfl.LayerNorm(2, 3, 8), hadfl.ClassLoss(2, 3, 8, 16), hadfl.PackedRows(2, 3, 8), hadfl.DenseGrad(2, 3, 8, 16)
+    for which in range(4):
+        t = lambda i, *s: Tensor(s, "f32", device, requires_grad=i == which)  # noqa: E731
+        labels = Tensor((2, 3), "i32", device)
+        norm_in, loss_in = (t(0, 2, 3, 8), t(1, 2, 8), t(2, 2, 8)), (t(0, 2, 3, 8), t(1, 2, 8, 16), labels, t(2, 2, 16))
+        for call, args in ((norm.forward, norm_in), (loss.loss, loss_in)):
+            machine.grad_mode, before = True, len(machine.calls)
+            if which < 3:
+                with pytest.raises(hadfl.HadflError, match="no_grad") as e:
+                    call(*args)
+                assert e.value.status == hadfl.EINVAL and len(machine.calls) == before
+            else:
+                call(*args)
+            machine.grad_mode = False
+            call(*args)
+        machine.grad_mode = True
+        norm.backward(norm_in[0], norm_in[0], norm_in[1])
+        loss.grad(*loss_in)
+        dense.backward(kept.pack(norm_in[0]), t(0, 2, 3, 16))
