@@ -8,6 +8,7 @@
 //      its logits of step 1 may stay for it.
 // A row without a label has G = 0 and its x is read as zeros.
 #include <cmath>
+#include <type_traits>
 
 #include "direct_product.h"
 
@@ -660,7 +661,8 @@ template <typename T, int BM, int WM, int WN> hipError_t run_general(const LossA
 template <typename T, int PL, class Store>
 hipError_t weight_grad(const Plane3& x, const Plane3& g, const LossArgs& a, int cols, const Plan& p, const Store& store, hipStream_t s)
 {
-    if (p.w_tile == 128) return launch_direct<PL, PL, 128, 128, 2, 4, false, false>(x, g, a.n, a.features, cols, a.rows, p.w_splits, p.w_len, store, s);
+    if constexpr (!std::is_same_v<Store, StoreShare<>>)        // (small tiles take no shares)
+        if (p.w_tile == 128) return launch_direct<PL, PL, 128, 128, 2, 4, false, false>(x, g, a.n, a.features, cols, a.rows, p.w_splits, p.w_len, store, s);
     if (narrow(a.features)) return launch_direct<PL, PL, 128, 256, 2, 4, false, false>(x, g, a.n, a.features, cols, a.rows, p.w_splits, p.w_len, store, s);
     return launch_direct<PL, PL, 256, 256, 2, 4, false, false>(x, g, a.n, a.features, cols, a.rows, p.w_splits, p.w_len, store, s);
 }

@@ -35,6 +35,13 @@ extern "C" {
 
 void check_reset(void) { g_trace.clear(); g_last = hipSuccess; }
 const char* check_trace(void) { return g_trace.c_str(); }
+const char* check_names(void)                                  // every kernel of the library, mangled, one a line
+{
+    static std::string all;
+    all.clear();
+    for (const auto& k : g_names) all += k.second + "\n";
+    return all.c_str();
+}
 
 void** __hipRegisterFatBinary(const void*) { static void* h; return &h; }
 void __hipUnregisterFatBinary(void**) {}

@@ -7,7 +7,7 @@ import sys
 import types
 
 fake = ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)
-fake.check_trace.restype = ctypes.c_char_p
+fake.check_trace.restype = fake.check_names.restype = ctypes.c_char_p
 sys.modules["torch"] = types.ModuleType("torch")
 from paper_2111_08274_amd import hadfl  # noqa: E402
 
@@ -21,7 +21,7 @@ def rows(strides, *shape, at=AT):
 
 
 def run(c):
-    L, n, t, bf16, at = hadfl.lib(), c["n"], c["rows"], c.get("bf16", 0), c.get("at", AT)
+    L, n, t, bf16, at = hadfl.lib(), c.get("n"), c.get("rows"), c.get("bf16", 0), c.get("at", AT)
     size = ctypes.c_size_t()
     fake.check_reset()
     if c["op"] == "dense":
@@ -41,6 +41,10 @@ def run(c):
         status = L.hadfl_norm_workspace(ctypes.byref(d), ctypes.byref(size))
         status = status or L.hadfl_norm_forward(ctypes.byref(d), x, v, v, rows(None, n, t, c["features"]), AT, AT, None)
         status = status or L.hadfl_norm_backward(ctypes.byref(d), x, x, None, v, AT, AT, rows(None, n, t, c["features"]), v, v, AT, None)
+        status = status or L.hadfl_norm_backward(ctypes.byref(d), x, None, AT, v, AT, AT, rows(None, n, t, c["features"]), v, v, AT, None)
+    elif c["op"] == "kernels":
+        hadfl.lib()
+        return fake.check_names().decode().split()
     else:
         d = hadfl.HadflLoss(n, t, c["features"], c["classes"], bf16)
         grad = int(c.get("grad", 1))

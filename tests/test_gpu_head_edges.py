@@ -178,3 +178,108 @@ def test_an_evaluation_between_a_forward_pass_and_its_gradient():
     assert all(torch.equal(p, q) for p, q in zip(fresh.backward(other["dy"], other["x"], other["gamma"]),
                                                  plan.backward(other["dy"], other["x"], other["gamma"], stats=mine)))
     assert torch.equal(plan.forward(c["x"], c["gamma"], c["beta"]), y)
+
+
+# with the sizes of test_gpu_head.py these reach every kernel (test_head_launches.py)
+DENSE = [(1, 1000, 2048, 2048, 1), (6, 1001, 1288, 1544, 1), (6, 1001, 1287, 1543, 1), (1, 8200, 896, 896, 1), (1, 8199, 895, 900, 1), (1, 1101, 4104, 3592, 0),
+         (1, 1101, 4101, 3595, 0), (1, 4501, 4104, 4090, 0),
+         (31, 3588, 101, 2078, 1), (15, 631, 10, 1537, 1), (1, 9000, 40, 5, 0), (1, 9000, 40, 5, 1)]
+
+
+@pytest.mark.parametrize("layout", ["whole", "padded", "odd"])
+@pytest.mark.parametrize("n,rows,i,o,bf16", DENSE)
+def test_dense_gradient_with_operands_from_memory(n, rows, i, o, bf16, layout):
+    rng = np.random.default_rng(13)
+    x, dy = rng.normal(size=(n, rows, i)).clip(0), rng.normal(size=(n, rows, o)) * 2.0 ** rng.integers(-8, 8, size=(n, rows, 1))
+    _dense(n, rows, i, o, bf16, base._in(x, bf16, layout), base._in(dy, bf16, layout), layout)
+
+
+LOSS = [(1, 450, 776, 2500, 1), (2, 430, 1030, 2312, 1), (2, 1000, 776, 4200, 1), (2, 1000, 100, 8400, 1), (2, 1000, 500, 4203, 1), (2, 1000, 100, 8400, 0), (2, 1001, 300, 8403, 0),
+        (2, 1000, 500, 4203, 0), (2, 380, 64, 9001, 1), (2, 380, 64, 9001, 0), (1, 3000, 72, 520, 1), (1, 3000, 72, 520, 0), (1, 1175, 152, 78, 0),
+        (2, 84, 505, 124, 1), (1, 97, 325, 68, 0), (3, 39, 391, 71, 1)]
+PIECES = [(64, 500, 64, 8400, 0), (64, 500, 300, 8403, 0), (64, 500, 64, 16500, 1), (64, 500, 300, 16501, 1), (64, 180, 10, 8001, 1), (64, 32, 16, 66001, 0),
+          (8, 260, 16400, 1030, 0)]
+
+
+@pytest.mark.parametrize("layout", ["whole", "padded", "odd"])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("n,rows,d,v,bf16", LOSS)
+def test_loss_with_operands_from_memory(n, rows, d, v, bf16, bias, layout):
+    torch = base._torch()
+    c = base._loss_case(n, rows, d, v, bf16, layout, bias)
+    plan = hadfl.ClassLoss(n, rows, d, v, bf16=bf16)
+    dx, dw, db = base._out((n, rows, d), bf16, layout), base._out((n, d, v), bf16, layout), base._out((n, v), 0, layout)
+    out = plan.grad(c["x"], c["w"], c["y"], c["bias"], dx=dx.t, dw=dw.t, db=db.t if bias else None)
+    for k in range(n):
+        _loss(c, k, out, bf16)
+        dead = torch.as_tensor((c["yh"][k] < 0) | (c["yh"][k] >= v)).cuda()
+        assert not out[1][k][dead].any() and not dx.t[k][dead].any()
+    assert dx.untouched() and dw.untouched() and (not bias or db.untouched())
+    alone = plan.loss(c["x"], c["w"], c["y"], c["bias"])
+    assert torch.equal(alone[0], out[0]) and torch.equal(alone[1], out[1])
+
+
+@pytest.mark.parametrize("n,rows,d,v,bf16", PIECES)
+def test_a_vocabulary_in_pieces_of_every_kind(n, rows, d, v, bf16):
+    # replicas with one x and one W whose logits, or W's copies, pass what one piece holds
+    torch = base._torch()
+    c = base._loss_case(1, rows, d, v, bf16, "whole", True)
+    c["x"].nan_to_num_(nan=0.5, posinf=0.5)
+    y = c["y"].repeat(n, 1)
+    y[-1] = torch.flip(y[-1], dims=[0])
+    out = hadfl.ClassLoss(n, rows, d, v, bf16=bf16).grad(c["x"].expand(n, rows, d), c["w"].expand(n, d, v), y, c["bias"].expand(n, v))
+    for k in (0, n - 1):
+        _loss(dict(x=c["x"], w=c["w"], bias=c["bias"], yh=y[k:k + 1].cpu().numpy()), 0, [o[k:k + 1] for o in out], bf16)
+    assert all(torch.equal(o[0], o[n - 2]) for o in out)
+
+
+def _far(values, bf16, pitch):
+    """[1][rows][cols] as a view whose rows are `pitch` elements apart, in memory that holds zeros"""
+    torch = base._torch()
+    rows, cols = values.shape
+    t = torch.zeros(((rows - 1) * pitch + cols,), dtype=base._dtype(bf16), device="cuda").as_strided((1, rows, cols), (0, pitch, 1))
+    return t.copy_(torch.as_tensor(values)[None].to(t.dtype))
+
+
+@pytest.mark.parametrize("bf16", [0, 1])
+def test_offsets_that_pass_32_bits_in_norm_checkpoint_and_dense_gradient(bf16):
+    torch = base._torch()
+    torch.cuda.empty_cache()
+    rng = np.random.default_rng(21)
+    rows, cols, pitch = 300, 264, (1 << 24) + 8               # the last rows lie beyond 2^32 elements
+    x, dy = _far(rng.normal(size=(rows, cols)), bf16, pitch), torch.as_tensor(rng.normal(size=(1, rows, cols))).cuda().to(base._dtype(bf16))
+    gamma, near = torch.rand((1, cols), device="cuda"), x.contiguous()
+    plan = hadfl.LayerNorm(1, rows, cols, bf16=bf16)
+    y = plan.forward(near, gamma, gamma)
+    want = plan.backward(dy, near, gamma)
+    out = _far(np.zeros((rows, cols)), bf16, pitch)
+    assert torch.equal(plan.forward(x, gamma, gamma, y=out), y)
+    got = plan.backward(dy, x, gamma, dx=out)
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+    packed, same = hadfl.PackedRows(1, rows, cols, bf16=bf16).pack(x), hadfl.PackedRows(1, rows, cols, bf16=bf16).pack(near)
+    assert torch.equal(packed.unpack(out), same.unpack())
+    out.copy_(dy)
+    dense = hadfl.DenseGrad(1, rows, cols, cols, bf16=bf16)
+    assert all(torch.equal(p, q) for p, q in zip(dense.backward(packed, out), dense.backward(packed, dy)))
+    del x, out, got
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("rows,bf16", [(8, 0), (40, 0), (600, 0), (8, 1), (40, 1), (600, 1)])
+def test_offsets_that_pass_32_bits_in_the_loss(rows, bf16):
+    # W's rows as far apart as a product reads them from where they lie, and a little farther
+    torch = base._torch()
+    torch.cuda.empty_cache()
+    rng = np.random.default_rng(22)
+    d, v = 1100, 1000
+    for pitch in (1 << 22, (1 << 22) + 8):
+        w = _far(rng.normal(size=(d, v)) / 33, bf16, pitch)
+        x = torch.as_tensor(rng.normal(size=(1, rows, d))).cuda().to(w.dtype)
+        y = torch.as_tensor(rng.integers(0, v, size=(1, rows)).astype(np.int32)).cuda()
+        plan = hadfl.ClassLoss(1, rows, d, v, bf16=bf16)
+        want = plan.grad(x, w.contiguous(), y)
+        dw = _far(np.zeros((d, v)), bf16, pitch)
+        got = plan.grad(x, w, y, dw=dw)
+        assert all(torch.equal(p, q) for p, q in zip(got, want) if p is not None)
+        del w, dw, got
+        torch.cuda.empty_cache()

@@ -93,3 +93,43 @@ def test_no_launch_has_more_threads_than_a_dimension_holds(launched):
             assert all(size[i] * size[i + 1] < 1 << 32 for i in (0, 2, 4)), (c, v)
             folded += size[2] > 1 and _name(v) in ("pack_rows_kernel", "unpack_rows_kernel", "direct_kernel", "product_kernel", "few_weights_kernel", "lay_out_kernel", "join_shares_kernel")
     assert folded > 8
+
+
+def _shapes(launched):
+    """The sizes of the GPU tests, in the layouts that change a route: as they lie, and with odd strides."""
+    from tests import test_gpu_head as head
+    from tests import test_gpu_head_edges as edges
+    cases = []
+    for n, t, i, o, b in [s + (b,) for s in head.DENSE for b in (0, 1)] + edges.DENSE:
+        cases += [dict(op="dense", n=n, rows=t, inputs=i, outputs=o, bf16=b, dy=dy) for dy in (None, [t * (o + 3) + 7, o + 3])]
+    for n, t, d, v, b in [s + (b,) for s in head.LOSS for b in (0, 1)] + edges.LOSS:
+        cases += [dict(op="loss", n=n, rows=t, features=d, classes=v, bf16=b, bias=1, grad=g, w=w) for w in (None, [d * (v + 3) + 7, v + 3]) for g in (0, 1)]
+    cases += [dict(op="loss", n=n, rows=t, features=d, classes=v, bf16=b, bias=1) for n, t, d, v, b in edges.PIECES]
+    pieces = next(m for m in head.test_a_vocabulary_in_pieces.pytestmark if m.name == "parametrize").args[1]
+    cases += [dict(op="loss", n=64, rows=t, features=d, classes=v, bf16=b, bias=1) for b, t, d, v in pieces]
+    cases += [dict(op="norm", n=n, rows=t, features=f, bf16=b) for n, t, f in head.NORM for b in (0, 1)]
+    cases += [dict(op=op, n=2, rows=5, features=40, bf16=b) for op in ("pack", "unpack") for b in (0, 1)]
+    return cases
+
+
+def test_the_gpu_tests_reach_every_kernel_of_the_head(launched):
+    cases = _shapes(launched)
+    got = launched([dict(op="kernels")] + cases)
+    kernels, reached = {k for k in got[0] if "hadfl4head" in k}, set()
+    for c, r in zip(cases, got[1:]):
+        assert r["status"] == 0, (c, r["text"])
+        reached |= {v[0] for v in r["launches"]}
+    assert len(kernels) > 100 and reached <= kernels
+    assert not kernels - reached, "\n".join(sorted(kernels - reached))
+
+
+def test_the_gpu_tests_reach_planes_that_lie_in_the_callers_tensors(launched):
+    cases = _shapes(launched)
+    tiles = set()
+    for c, r in zip(cases, launched(cases)):
+        if c["op"] in ("dense", "loss") and c["bf16"]:
+            laid = [_name(v) for v in r["launches"]].count("lay_out_kernel")
+            for v in r["launches"]:
+                if _name(v) == "direct_kernel" and laid < (1 if c["op"] == "dense" else 2):
+                    tiles.add((c["op"],) + tuple(re.search(r"ELi(\d+)ELi(\d+)ELi\dELi\dEN", v[0]).groups()))
+    assert {("dense", "128", "128"), ("dense", "256", "256"), ("loss", "128", "128"), ("loss", "256", "256")} <= tiles, tiles
