@@ -345,7 +345,7 @@ HADFL_API hadfl_status hadfl_unpack_rows(const hadfl_pack *pack, const void *pac
 /* The parameter gradients of a dense layer y = x W + b whose input was kept in 8 bits:
  *   dW = x^T dy  ([n_in][n_out], the layout of a dense layer here),  db = sum_t dy,
  * x the values that the checkpoint stands for.  Products of bf16 operands on the matrix cores, sums in 32 bits; a 32-bit dy
- * enters as three bf16 parts, which hold it whole for magnitudes from 2^-107 on.
+ * enters as three bf16 parts, which hold it whole for magnitudes from 2^-107 to below 3.39e38 (a larger one, or an infinity, makes NaN).
  *   packed     dev, checkpoint of [n_replicas][n_rows][n_in]
  *   dy (t)     dev, [n_replicas][n_rows][n_out]
  *   dw         dev out, [n_replicas][n_in][n_out] floats
@@ -356,18 +356,25 @@ HADFL_API hadfl_status hadfl_dense_workspace(const hadfl_dense *dense, size_t *b
 HADFL_API hadfl_status hadfl_dense_grad_packed(const hadfl_dense *dense, const void *packed, const hadfl_rows *dy,
                                                const hadfl_rows *dw, const hadfl_rows *db, void *work, void *stream);
 
-/* Softmax cross entropy of a last dense layer over many classes, without keeping its logits: they are formed a piece of
- * the vocabulary at a time, once for the loss and once more for the gradient (where one piece holds the whole vocabulary,
- * and its logits with it, once).  A piece is at most 512 MiB, or 1024 classes.  With z = x W + b,
+/* Softmax cross entropy of a last dense layer over many classes.  Its logits are formed in the working memory, a piece of
+ * the vocabulary at a time, once for the loss and once more for the gradient; where one piece holds the whole vocabulary
+ * they may be kept there in between.  A piece is at most 512 MiB, or about a thousand classes.  The working memory holds
+ * more than that: beside a piece's gradient with respect to z its kept logits, copies of x and of a piece of w as the
+ * products take them (with many rows; reserved also where a bf16 w is read as it lies), shares of dx and dW.  A vocabulary
+ * that fits one piece can take more than its 32-bit logits would: 2 x 1000 rows x 777 features x 20011 classes, fp32,
+ * 508 MB for logits of 160; 2 x 4096 x 2048 x 65536, bf16, 931 MB for 2147.  With z = x W + b,
  *   row_loss_t = log sum_v exp(z_tv) - z_t,label(t);   loss = mean of row_loss over the replica's labelled rows.
  * A row whose label lies outside [0, n_classes) has no label: its row_loss is zero, it adds nothing to any gradient
  * (whatever its x holds), and its dx is zero.  A replica without labelled rows has loss zero and zero gradients.  A bias of
- * -inf takes a class out.  With G = (softmax(z) - onehot(label)) / (number of labelled rows):
+ * -inf takes a class out, if its w is finite.  With G = (softmax(z) - onehot(label)) / (number of labelled rows):
  *   dx = G W^T,  dW = x^T G,  db = sum_t G.
  * fp32: operands enter the matrix products in parts of 16 bits whose products are summed in 32 bits: with few rows (200 a
- * replica, more the smaller w is) three bf16 parts (six products, whole for magnitudes from 2^-107 on), beyond two fp16 parts (three products) scaled by a power of two to
- * the replica's largest finite magnitude: a product is off by at most 2^-20 of itself, 2^-23.5 in the mean square, for
- * magnitudes down to 2^-29 of the largest.  bf16: softmax(z) - onehot is rounded to bf16 for the two products, db is formed before that.
+ * replica, more the smaller w is) three bf16 parts (six products, whole for magnitudes from 2^-107 to below 3.39e38),
+ * beyond two fp16 parts (three products) scaled by a power of two to the largest finite magnitude of the replica's x (its
+ * labelled rows) or w: a product is off by at most 2^-20 of itself, 2^-23.5 in the mean square, for magnitudes down to
+ * 2^-29 of the largest; a smaller operand is off by 2^-50 of the largest.  An infinity in a 32-bit x or w makes NaN where
+ * 32-bit products would leave an infinity.  bf16: softmax(z) - onehot is rounded to bf16 for the two products, db is formed
+ * before that.
  *   x (t)                 dev, [n_replicas][n_rows][n_features]
  *   w (t)                 dev, [n_replicas][n_features][n_classes], the layout of a dense layer here
  *   bias                  dev or NULL, [n_replicas][n_classes] floats

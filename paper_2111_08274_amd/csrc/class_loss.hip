@@ -1,11 +1,11 @@
 // Softmax cross entropy of a last dense layer over many classes, and its gradient, in pieces of the vocabulary.
 //   1. logits' statistics: z = x W + b a tile at a time; a tile leaves, per row, its largest logit and the sum of exp of the
-//      distances to it, and the label's logit where the tile holds it.  Nothing else of z is stored.
+//      distances to it, the label's logit where the tile holds it, and z itself where it stays for step 3.
 //   2. per row: the tiles' pairs joined to its max and sum; row losses max - z_label + log(sum), their mean and 1 / (labelled
 //      rows).
 //   3. for every piece of the vocabulary: z again, G = exp(z - max) / sum - onehot into a buffer of [rows][piece], then
-//      dx += G W^T (shares of the contraction side by side, added in a fixed order) and dW = x^T G.  Where one piece holds the vocabulary,
-//      its logits of step 1 may stay for it.
+//      dx += G W^T (shares of the contraction side by side, added in a fixed order) and dW = x^T G.  Where one piece holds the vocabulary, the
+//      logits of step 1 stay for it: always with few rows, with more where forming them again costs more than their bytes (Plan::keep).
 // A row without a label has G = 0 and its x is read as zeros.
 #include <cmath>
 #include <type_traits>
@@ -71,8 +71,9 @@ __device__ __forceinline__ void join(float2& have, const float2& v)
 
 // The statistics of a tile: per wave and row, then joined over the WN waves that share rows.  z: the logits too (few rows), or null.
 // EXACT (32-bit operands): the distance to the largest first, then exp; else both in one multiply-add, off by 2^-24 |z| at most, which is far below
-// what bf16 operands leave of z.  128 values a lane, some 3 us a tile that no product overlaps: 2 x 4096 x 2048 x 65536 bf16 1.93 ms with the
-// product, 1140 TFLOP/s; 8 x 512 x 512 x 32000, where a tile's product is a quarter as long, 185 us, 727 TFLOP/s.
+// what bf16 operands leave of z.  128 values a lane, some 3 us a tile that no product overlaps: 2 x 4096 x 2048 x 65536 bf16 1.85 ms with the
+// product, 1190 TFLOP/s, the matrix cores busy 61 % of the time; 8 x 512 x 512 x 32000, where a tile's product is a quarter as long, 178 us, 755
+// TFLOP/s, 43 %.
 template <bool EXACT, int BM, int BN, int WN> struct Statistics {
     static constexpr bool kLaneM = true, kStaged = true, kSums = false;
     const float* bias;
@@ -250,8 +251,8 @@ __global__ __launch_bounds__(W * 64) void gradient_columns_kernel(const float* z
     db[k * db_rep + c] = sum * factor[k];
 }
 
-// G of a piece, unscaled, and its column sums over a wave's rows (EXACT: as above).  With the product 5 to 12 % slower than the statistics (2.07 ms and
-// 210 us for the sizes there): G is written.
+// G of a piece, unscaled, and its column sums over a wave's rows (EXACT: as above).  With the product 10 to 15 % slower than the statistics (2.04 ms and
+// 205 us for the sizes there): G is written.
 template <bool EXACT> struct Softmax {
     const float* bias;
     long long bias_rep;
@@ -444,13 +445,15 @@ int up_to(long long v, int unit) { return (int)((v + unit - 1) / unit * unit); }
 bool narrow(int v) { return 1.18 * up_to(v, 128) < up_to(v, 256); }
 
 // Rows up to which W is read as it is: more where W is small, and where its features are many for its tiles.  Loss and gradients through
-// registers / laid out, us:
-//   bf16             4 x 512 x 32000, 64 rows 135 / 136, 96 rows 159 / 141; 2048 x 20000, 128 rows 113 / 113; 4096 x 10008, 128 rows 109 / 139, 256 rows
-//                    177 / 153; 2048 x 5000, 256 rows 92 / 90
-//   bf16, unaligned  4 x 512 x 32001, 128 rows 182 / 205, 160 rows 305 / 251; 2048 x 20011, 192 rows 173 / 172; 8 x 200 x 4099, 256 rows 82 / 89,
-//                    320 rows 97 / 88
-//   fp32             4 x 512 x 32000, 128 rows 471 / 540, 192 rows 641 / 639, 256 rows 725 / 684; 2048 x 20011, 256 rows 487 / 453; 12 x 520 x 8739, 256
-//                    rows 711 / 710; 8 x 200 x 4099, 256 rows 165 / 188, 320 rows 195 / 194
+// registers / laid out, us (the rule's own bound in brackets):
+//   bf16             4 x 512 x 32000 (41 rows), 32 rows 107 / 128, 64 rows 130 / 136, 96 rows 155 / 139; 2048 x 20000 (78), 48 rows 84 / 79, 128 rows
+//                    111 / 92; 4096 x 10008 (172), 128 rows 106 / 107, 192 rows 143 / 117; 2048 x 5000 (224), 192 rows 67 / 68, 256 rows 77 / 71
+//   bf16, unaligned  4 x 512 x 32001 (138), 128 rows 176 / 197, 160 rows 293 / 236; 2048 x 20011 (174), 128 rows 115 / 125, 192 rows 153 / 147;
+//                    8 x 200 x 4099 (221), 256 rows 80 / 86, 320 rows 96 / 86
+//   fp32             4 x 512 x 32000 (215), 192 rows 597 / 593, 256 rows 695 / 646; 2048 x 20011 (234), 192 rows 350 / 391, 256 rows 441 / 413;
+//                    12 x 520 x 8739 (218), 192 rows 588 / 594, 256 rows 668 / 667; 8 x 200 x 4099 (353), 320 rows 161 / 169, 384 rows 180 / 177
+// Sizes alone decide, since the working memory is asked for before a W is seen: bf16 classes that are no multiple of eight stand for a W that
+// has to be copied, and a W inside rows of an odd stride is copied all the same.
 double few_rows(int n, int features, int classes, int bf16)
 {
     const double values = (double)n * features * classes, deep = std::min(125., features / ((double)n * classes / 256));

@@ -6,7 +6,7 @@
 //             ascending order: no atomics, the same bits every time.
 // Memory bound: a row is read once into registers (NL lanes, 8 * CH values a lane), both passes run there, and the next row is
 // loaded meanwhile.  16 x 4096 x 512 bf16: forward 26 us = 5.2 TB/s, backward 39.5 us = 5.1, the sums' launch 4.6; 4 x 4096 x 4096: 46 us = 5.8 and,
-// from the 8-bit checkpoint, 73 us = 4.6.  Few rows are latency: one row of 512 2.1 us.
+// from the 8-bit checkpoint, 73 us = 4.6; fp32 100 us = 5.4 and 120 us = 5.0.  Few rows are latency: one row of 512 2.1 us.
 #include "head.h"
 
 namespace hadfl {
@@ -217,7 +217,9 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(NormArgs a, float* p
     }
 }
 
-// rows longer than the registers of a workgroup hold: the row is read again for every pass
+// Rows longer than the registers of a workgroup hold: the row is read again for every pass, an element a lane and load, from the caches.  A fallback,
+// at half the rate of the kernels above and less where there are few rows for the compute units: 2 x 4096 x 8200 bf16 forward 136 us = 2.0 TB/s, backward
+// 168 (8192 columns: 43 and 69), fp32 209 and 262 (98 and 116); 1024 x 65536 bf16 224 and 235.
 template <typename T>
 __global__ __launch_bounds__(256) void norm_forward_long_kernel(NormArgs a)
 {

@@ -4,7 +4,8 @@
 // rounding.  A power of two instead of max|x| / 127 costs up to one of the seven bits but makes q * 2^e a bf16 and an fp32
 // number, so that what reads the checkpoint need not round again.
 // Memory bound: 16 values a lane, two lanes a group; values and exponents are written once.  4 x 4096 x 4096 bf16: packing 39 us = 5.2 TB/s;
-// 4 x 8192 x 4096: packing 65 us = 6.3 TB/s, unpacking 69 us = 5.9.
+// 4 x 8192 x 4096: packing 65 us = 6.3 TB/s, unpacking 69 us = 5.9; fp32: packing 114 us = 5.9, unpacking 192 us = 3.5 (a lane's four stores of 16
+// bytes lie 64 bytes from the next lane's, so each touches every line of the wave's 4 KiB).
 #include "head.h"
 
 namespace hadfl {

@@ -22,7 +22,7 @@ struct Labelled {
 
 // Three bf16 parts of a float whose sum is the float: h = bf16(x), m = bf16(x - h), l = x - h - m, both differences exact.  No scale, so
 // that products of any two magnitudes whose product is a float stay floats; l is no normal bf16 below 2^-107, where the float's lowest
-// bits go.
+// bits go.  From 3.39e38 on h rounds to infinity, and the parts of it and of an infinity hold a NaN.
 __device__ __forceinline__ void parts3(const f4& x, u2& h, u2& m, u2& l)
 {
 #pragma unroll

@@ -580,9 +580,9 @@ class DenseGrad(_Operator):
 
 
 class ClassLoss(_Operator):
-    """Softmax cross entropy of a last dense layer over many classes, the logits never kept: x [n_replicas, n_rows,
-    n_features], w [n_replicas, n_features, n_classes], bias [n_replicas, n_classes] (32-bit) or None, labels [n_replicas,
-    n_rows] int32; a label outside [0, n_classes) marks a row that takes no part."""
+    """Softmax cross entropy of a last dense layer over many classes, whose logits are formed in the working memory, a piece of the
+    vocabulary at a time: x [n_replicas, n_rows, n_features], w [n_replicas, n_features, n_classes], bias [n_replicas, n_classes]
+    (32-bit) or None, labels [n_replicas, n_rows] int32; a label outside [0, n_classes) marks a row that takes no part."""
 
     def __init__(self, n_replicas, n_rows, n_features, n_classes, bf16=0, grad=True):
         self.n, self.rows, self.features, self.classes, bf16 = _int32(n_replicas, n_rows, n_features, n_classes, bf16)

@@ -9,8 +9,8 @@ the last dense layer over the vocabulary,
     h = relu(x W1 + b1),   y = layer_norm(h; gamma, beta),   loss = cross_entropy(y W2 + b2, next token),
 
 x the fixed embedding of the last token.  A step is grouped over the replicas: what the backward pass needs of x and of h is kept in
-8 bits, the logits are never kept, and a replica that has done its local steps of the round sits the others out with rows that have
-no label.  After the local steps the library selects replicas by their versions and aggregates their rows.
+8 bits, the logits live in the loss's workspace alone, and a replica that has done its local steps of the round sits the others out with
+rows that have no label.  After the local steps the library selects replicas by their versions and aggregates their rows.
 
 Tokens are synthetic: the next token is a fixed permutation of the last one, replaced by a uniform one with probability 1/8;
 replica k sees mostly tokens of its own part of the vocabulary (shards that differ, as the method's devices do).
