@@ -1,6 +1,8 @@
 // Operators of a language model's head (layer norm, 8-bit checkpoints, loss over a large vocabulary): launch wrappers and
 // the pieces that their kernels share.
 #pragma once
+#include <algorithm>
+
 #include "hadfl_internal.h"
 #include "mfma_tiles.h"
 
