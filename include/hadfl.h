@@ -373,8 +373,8 @@ HADFL_API hadfl_status hadfl_dense_grad_packed(const hadfl_dense *dense, const v
  * beyond, and with fewer than eight features or classes, two fp16 parts (three products) scaled by a power of two to the
  * largest finite magnitude of the replica's x (its labelled rows) or w, for softmax(z) - onehot to 1: a product is off by at
  * most 2^-20 of itself, 2^-23.5 in the mean square, for magnitudes down to 2^-29 of the largest; a smaller operand is off by
- * 2^-50 of the largest.  An infinity in a 32-bit x or w makes NaN where 32-bit products would leave an infinity.  bf16: softmax(z) - onehot is rounded to bf16 for the two products, db is formed
- * before that.
+ * 2^-50 of the largest.  An infinity in a 32-bit x or w makes NaN where 32-bit products would leave an infinity.
+ * bf16: softmax(z) - onehot is rounded to bf16 for the two products, db is formed before that.
  *   x (t)                 dev, [n_replicas][n_rows][n_features]
  *   w (t)                 dev, [n_replicas][n_features][n_classes], the layout of a dense layer here
  *   bias                  dev or NULL, [n_replicas][n_classes] floats
