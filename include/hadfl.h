@@ -394,6 +394,87 @@ HADFL_API hadfl_status hadfl_loss_grad(const hadfl_loss *shape, const hadfl_rows
                                        const hadfl_rows *dx, const hadfl_rows *dw, const hadfl_rows *db,
                                        void *work, void *stream);
 
+/* ---- operators of a next-word model's layers and answers -----------------------------------------------------------
+ * As the operators of the head: grouped over replicas, without a context, on tensors of the caller, with the same limits.
+ *
+ * Which values a dropout keeps is a function of a seed, a call number and the value's place, and is drawn again by the
+ * gradient; no mask is stored.  With t = 65536 p rounded, at most 65535, the value of row r and column j of replica k is kept
+ * if the (j mod 8)-th 16-bit number of Philox4x32-10 (two to a word, the low one first) with the key (seed's low word, high
+ * word) and the counter (r, floor(j / 8) + 65536 k, call's low word, high word) is at least t; kept values are multiplied by
+ * 65536 / (65536 - t), so that the mean stays.  A dropped value is zero whatever it holds.  One call number draws the same
+ * numbers each time: a program gives every layer and step its own, or leaves the call as it is, as in a captured graph, and
+ * counts on the device.
+ *   counter    dev or NULL, 8-byte aligned: its value, read when the kernels run, is added to call (modulo 2^64) */
+typedef struct { uint64_t seed, call; const uint64_t *counter; } hadfl_draw;
+
+/* y = x kept or not, plus a residual if there is one.  The gradient with respect to x is the same call on dy without a
+ * residual; the residual's is dy.
+ *   x, residual, y (t)   dev, [n_replicas][n_rows][n_features]; residual may be NULL; y may be x or the residual (the same rows)
+ *   draw                 host, read during the call; may be NULL where nothing is dropped (65536 p rounds to 0)
+ *   p                    the probability of dropping, in [0, 1) */
+typedef struct { int32_t n_replicas, n_rows, n_features, bf16; float p; } hadfl_dropout;
+HADFL_API hadfl_status hadfl_dropout_rows(const hadfl_dropout *dropout, const hadfl_rows *x, const hadfl_rows *residual,
+                                          const hadfl_draw *draw, const hadfl_rows *y, void *stream);
+
+/* A dense layer with all that follows it in one pass, and its gradient:
+ *   z = x W + b,  y = residual + D(a(z)),  D the dropout above on [n_rows][n_out] with p = drop,
+ *   a: HADFL_ACT_NONE z;  HADFL_ACT_RELU max(z, 0), its slope at 0 is 0;  HADFL_ACT_SILU z / (1 + e^-z);
+ *      HADFL_ACT_GELU z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2.
+ * With dz = D'(dy) a'(pre), D' the same values kept:
+ *   dx = dz W^T,  dW = x^T dz,  db = sum_t dz;  the residual's gradient is dy.
+ * fp32: operands enter the products as three bf16 parts, six products, whole for magnitudes from 2^-107 to below 3.39e38; an
+ * infinity in a 32-bit operand makes NaN.  bf16: sums in 32 bits, outputs rounded once; the activation takes z before pre is
+ * rounded; dz is rounded to bf16 for the two products, db is formed before that.
+ *   x (t)               dev, [n_replicas][n_rows][n_in]
+ *   w (t)               dev, [n_replicas][n_in][n_out], the layout of a dense layer here
+ *   bias                dev or NULL, [n_replicas][n_out] floats
+ *   residual (t)        dev or NULL, [n_replicas][n_rows][n_out]; y may be the residual (the same rows) where that is not x or w
+ *   pre (t)             dev, [n_replicas][n_rows][n_out]: z, an output of the forward call (there it may be NULL) and an input of the
+ *                       gradient (not read without an activation)
+ *   packed              dev or NULL; the gradient takes x for dW from this 8-bit checkpoint (hadfl_pack_rows of [n_replicas][n_rows]
+ *                       [n_in]) instead of from x, which may then be NULL, as it may without dW; w may be NULL without dx
+ *   draw                host; may be NULL where nothing is dropped.  The gradient takes the forward call's, with the counter as it was
+ *   y (t)               dev out, [n_replicas][n_rows][n_out]
+ *   dx (t), dw (t), db  dev out, like x, w, bias; each may be NULL and is then not computed.  Outputs do not overlap inputs
+ *   work                dev, 256-byte aligned; hadfl_layer_workspace with grad = 1 serves both calls, with grad = 0 the forward
+ *                       call alone */
+typedef enum { HADFL_ACT_NONE = 0, HADFL_ACT_RELU = 1, HADFL_ACT_GELU = 2, HADFL_ACT_SILU = 3 } hadfl_activation;
+typedef struct { int32_t n_replicas, n_rows, n_in, n_out, bf16, activation; float drop; } hadfl_layer;
+HADFL_API hadfl_status hadfl_layer_workspace(const hadfl_layer *layer, int32_t grad, size_t *bytes);
+HADFL_API hadfl_status hadfl_layer_forward(const hadfl_layer *layer, const hadfl_rows *x, const hadfl_rows *w,
+                                           const hadfl_rows *bias, const hadfl_rows *residual, const hadfl_draw *draw,
+                                           const hadfl_rows *pre, const hadfl_rows *y, void *work, void *stream);
+HADFL_API hadfl_status hadfl_layer_backward(const hadfl_layer *layer, const hadfl_rows *dy, const hadfl_rows *pre,
+                                            const hadfl_rows *x, const void *packed, const hadfl_rows *w,
+                                            const hadfl_draw *draw, const hadfl_rows *dx, const hadfl_rows *dw,
+                                            const hadfl_rows *db, void *work, void *stream);
+
+/* What rows of logits say, and its gradient.  With p = softmax(z) of a row of n_classes logits:
+ *   logp_i = log p(tokens_i),  entropy = - sum_j p_j log p_j,
+ *   top, top_logp: the n_top classes of the largest logits in descending order, of equal logits the lowest first, and their log p.
+ * A logit of -inf takes a class out: its log p is -inf.  A row of nothing else has log p of -inf, entropy 0 and as top its first classes.  A row with a
+ * NaN or +inf has NaNs (top: a NaN counts as the largest).  A token outside [0, n_classes) has logp 0 and no gradient.  The gradient
+ * of logp (weighted by dlogp) and entropy (by dentropy), summed over a row's tokens, of which one may be given twice:
+ *   dz_j = sum_i dlogp_i ([tokens_i = j] - p_j) - dentropy p_j (log p_j + entropy);  zero for a row of -inf alone.
+ * Sums in 32 bits, in an order that depends on the sizes alone.
+ *   logits (t)          dev, [n_replicas][n_rows][n_classes]
+ *   tokens              dev, [n_replicas][n_rows][n_tokens] int32; n_tokens in [0, 64]; not read if 0, as logp and dlogp
+ *   logp                dev out, [n_replicas][n_rows][n_tokens] floats
+ *   entropy             dev out or NULL, [n_replicas][n_rows] floats
+ *   stats               dev, [n_replicas][n_rows][3] floats (largest logit, log of the sum of exp of the distances to it, entropy): an
+ *                       output of the forward call (there it may be NULL), an input of the gradient
+ *   top, top_logp       dev out, [n_replicas][n_rows][n_top] int32 and floats; n_top in [0, 32], at most n_classes; not written if 0
+ *   dlogp               dev, like logp;  dentropy: dev or NULL (zero), like entropy
+ *   dlogits (t)         dev out, like logits; may be the logits (the same rows)
+ *   work                dev, 256-byte aligned, the forward call's */
+typedef struct { int32_t n_replicas, n_rows, n_classes, n_tokens, n_top, bf16; } hadfl_scores;
+HADFL_API hadfl_status hadfl_scores_workspace(const hadfl_scores *scores, size_t *bytes);
+HADFL_API hadfl_status hadfl_scores_forward(const hadfl_scores *scores, const hadfl_rows *logits, const int32_t *tokens, float *logp,
+                                            float *entropy, float *stats, int32_t *top, float *top_logp, void *work, void *stream);
+HADFL_API hadfl_status hadfl_scores_backward(const hadfl_scores *scores, const hadfl_rows *logits, const int32_t *tokens,
+                                             const float *stats, const float *dlogp, const float *dentropy,
+                                             const hadfl_rows *dlogits, void *stream);
+
 HADFL_API const char *hadfl_last_error(const hadfl_ctx *ctx);   /* ctx may be NULL: error of the last failed call without a context on this thread */
 HADFL_API void hadfl_destroy(hadfl_ctx *ctx);                   /* frees host state only; NULL is a no-op */
 

@@ -6,6 +6,7 @@
 #include <type_traits>
 
 #include "kernels.h"
+#include "philox.h"
 
 // Working memory of hadfl_select_static, the selection for callers that cannot allocate device memory: the selection
 // function's values f[kMaxReplicas] (fp64), then the ascending list of the selected replicas and their weights.
@@ -16,21 +17,6 @@ static __device__ __align__(256) unsigned char scratch[kStaticScratchBytes];
 
 namespace hadfl {
 namespace {
-
-struct U4 { uint32_t x, y, z, w; };
-
-// Philox4x32-10 (Salmon et al., SC'11).
-__device__ U4 philox4x32_10(U4 c, uint32_t k0, uint32_t k1)
-{
-#pragma unroll
-    for (int r = 0; r < 10; ++r) {
-        const uint32_t lo0 = 0xD2511F53u * c.x, hi0 = __umulhi(0xD2511F53u, c.x);
-        const uint32_t lo1 = 0xCD9E8D57u * c.z, hi1 = __umulhi(0xCD9E8D57u, c.z);
-        c = U4{hi1 ^ c.y ^ k0, lo1, hi0 ^ c.w ^ k1, lo0};
-        k0 += 0x9E3779B9u; k1 += 0xBB67AE85u;
-    }
-    return c;
-}
 
 // exp(x), x in [-690, 0]: n = nearest integer to x*log2(e); r = (x - n*ln2_hi) - n*ln2_lo (two-constant
 // reduction, n*ln2_hi exact); Taylor polynomial of degree 13 by Horner; multiply by 2^n built in the exponent field.

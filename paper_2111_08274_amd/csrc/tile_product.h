@@ -164,9 +164,9 @@ __device__ __forceinline__ bf16x8 ones()
     return __builtin_bit_cast(bf16x8, (u4{one2, one2, one2, one2}));
 }
 
+// One workgroup's tile.
 template <class SA, bool A_ALONG, class SB, bool B_ALONG, int BM, int BN, int WM, int WN, int KS, int NBUF, int AHEAD, class Epi>
-__global__ __launch_bounds__(WM * WN * 64) void product_kernel(SA a, SB b, int K, int tiles_m, int tiles_n, int splits, int split_len,
-                                                               int total, Epi epi)
+__device__ __forceinline__ void product_tile(SA a, SB b, int K, int tiles_m, int tiles_n, int splits, int split_len, int total, Epi epi)
 {
     constexpr int NT = WM * WN * 64, TM = BM / WM / 32, TN = BN / WN / 32, PA = SA::kPlanes, PB = SB::kPlanes;
     typedef Image<A_ALONG, BM, KS> IA;
@@ -292,6 +292,13 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(SA a, SB b, int K
         __syncthreads();
         epi(t, smem);
     } else epi(t);
+}
+
+template <class SA, bool A_ALONG, class SB, bool B_ALONG, int BM, int BN, int WM, int WN, int KS, int NBUF, int AHEAD, class Epi>
+__global__ __launch_bounds__(WM * WN * 64) void product_kernel(SA a, SB b, int K, int tiles_m, int tiles_n, int splits, int split_len,
+                                                               int total, Epi epi)
+{
+    product_tile<SA, A_ALONG, SB, B_ALONG, BM, BN, WM, WN, KS, NBUF, AHEAD>(a, b, K, tiles_m, tiles_n, splits, split_len, total, epi);
 }
 
 // ---- epilogues that only store ---------------------------------------------------------------------------------

@@ -60,7 +60,24 @@ class HadflLoss(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("n_replicas", "n_rows", "n_features", "n_classes", "bf16")]
 
 
+class HadflDraw(ctypes.Structure):
+    _fields_ = [("seed", ctypes.c_uint64), ("call", ctypes.c_uint64), ("counter", ctypes.c_void_p)]
+
+
+class HadflDropout(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_replicas", "n_rows", "n_features", "bf16")] + [("p", ctypes.c_float)]
+
+
+class HadflLayer(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_replicas", "n_rows", "n_in", "n_out", "bf16", "activation")] + [("drop", ctypes.c_float)]
+
+
+class HadflScores(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_replicas", "n_rows", "n_classes", "n_tokens", "n_top", "bf16")]
+
+
 OPT_SIDE_STREAM, OPT_TILE_HINT = 0, 1
+ACTIVATIONS = ("none", "relu", "gelu", "silu")
 
 EXPORTS = ("hadfl_param_count", "hadfl_param_layout", "hadfl_workspace_bytes", "hadfl_init_replicas",
            "hadfl_local_steps", "hadfl_select", "hadfl_aggregate", "hadfl_step_counts", "hadfl_steps_from_times",
@@ -72,7 +89,8 @@ EXPORTS = ("hadfl_param_count", "hadfl_param_layout", "hadfl_workspace_bytes", "
            "hadfl_profile_read", "hadfl_last_error", "hadfl_destroy",
            "hadfl_norm_workspace", "hadfl_norm_forward", "hadfl_norm_backward", "hadfl_packed_bytes", "hadfl_pack_rows",
            "hadfl_unpack_rows", "hadfl_dense_workspace", "hadfl_dense_grad_packed", "hadfl_loss_workspace",
-           "hadfl_loss_forward", "hadfl_loss_grad")
+           "hadfl_loss_forward", "hadfl_loss_grad", "hadfl_dropout_rows", "hadfl_layer_workspace", "hadfl_layer_forward",
+           "hadfl_layer_backward", "hadfl_scores_workspace", "hadfl_scores_forward", "hadfl_scores_backward")
 
 _lib = None
 
@@ -134,6 +152,13 @@ def lib():
         L.hadfl_dense_grad_packed.argtypes = [vp] * 7
         L.hadfl_loss_forward.argtypes = [vp] * 9
         L.hadfl_loss_grad.argtypes = [vp] * 12
+        L.hadfl_dropout_rows.argtypes = [vp] * 6
+        L.hadfl_layer_workspace.argtypes = [vp, i32, sizep]
+        L.hadfl_layer_forward.argtypes = [vp] * 10
+        L.hadfl_layer_backward.argtypes = [vp] * 12
+        L.hadfl_scores_workspace.argtypes = [vp, sizep]
+        L.hadfl_scores_forward.argtypes = [vp] * 10
+        L.hadfl_scores_backward.argtypes = [vp] * 8
         L.hadfl_last_error.argtypes = [vp]
         L.hadfl_last_error.restype = ctypes.c_char_p
         L.hadfl_destroy.argtypes = [vp]
@@ -618,3 +643,134 @@ class ClassLoss(_Operator):
                    self._rows("dw", dw, (self.n, self.features, self.classes), self.dtype),
                    self._rows("db", db, (self.n, self.classes), f32), self.work.data_ptr(), self._stream(stream))
         return loss, row_loss, dx, dw, db
+
+
+# ---- operators of a next-word model's layers and answers --------------------------------------------------------------
+class _Drawing(_Operator):
+    """An operator that drops values: which ones is decided by seed and call, whole numbers below 2^64, and a counter, a device
+    tensor of one int64 whose value is added to call when the kernels run (one that a captured graph counts up, say)."""
+
+    def _draw(self, seed, call, counter):
+        at = None
+        if counter is not None:
+            if counter.dtype != self.torch.int64 or counter.device != self.device or counter.numel() != 1:
+                raise HadflError(EINVAL, "counter must be one int64 on %s" % (self.device,))
+            at = counter.data_ptr()
+        if not (0 <= int(seed) < 2 ** 64 and 0 <= int(call) < 2 ** 64):
+            raise HadflError(EINVAL, "seed and call must be in [0, 2^64)")
+        return ctypes.byref(HadflDraw(int(seed), int(call), at))
+
+
+class Dropout(_Drawing):
+    """Dropout of [n_replicas, n_rows, n_features] with probability p (a multiple of 2^-16, rounded to it), onto a residual if one is
+    given.  The mask is never stored: backward() with the forward pass's seed, call and counter draws it again."""
+
+    def __init__(self, n_replicas, n_rows, n_features, p, bf16=0):
+        n, rows, features, bf16 = _int32(n_replicas, n_rows, n_features, bf16)
+        super().__init__(HadflDropout(n, rows, features, bf16, float(p)), bf16)
+        self.shape = (n, rows, features)
+
+    def _run(self, x, residual, y, draw, stream, names=("x", "y")):
+        y = self._out(y, self.shape, self.dtype, stream)
+        self._call(lib().hadfl_dropout_rows, self._rows(names[0], x, self.shape, self.dtype), self._rows("residual", residual, self.shape, self.dtype),
+                   draw, self._rows(names[1], y, self.shape, self.dtype), self._stream(stream))
+        return y
+
+    def forward(self, x, residual=None, y=None, seed=0, call=0, counter=None, stream=None):
+        """y may be x or the residual"""
+        self._no_graph(x, residual)
+        return self._run(x, residual, y, self._draw(seed, call, counter), stream)
+
+    def backward(self, dy, dx=None, seed=0, call=0, counter=None, stream=None):
+        """-> dx, which may be dy; the residual's gradient is dy"""
+        return self._run(dy, None, dx, self._draw(seed, call, counter), stream, ("dy", "dx"))
+
+
+class DenseLayer(_Drawing):
+    """y = residual + dropout(activation(x w + bias)): x [n_replicas, n_rows, n_in], w [n_replicas, n_in, n_out], bias [n_replicas, n_out]
+    (32-bit) or None, residual and y [n_replicas, n_rows, n_out]; activation one of ACTIVATIONS, drop the probability of
+    dropping.  What backward() needs of the forward pass is `pre`, a tensor like y for x w + bias, and the same seed, call and counter."""
+
+    def __init__(self, n_replicas, n_rows, n_in, n_out, bf16=0, activation="none", drop=0.0, grad=True):
+        self.n, self.rows, self.n_in, self.n_out, bf16 = _int32(n_replicas, n_rows, n_in, n_out, bf16)
+        if activation not in ACTIVATIONS:
+            raise HadflError(EINVAL, "activation must be one of %s" % (ACTIVATIONS,))
+        self.with_grad, query = bool(grad), lib().hadfl_layer_workspace
+        super().__init__(HadflLayer(self.n, self.rows, self.n_in, self.n_out, bf16, ACTIVATIONS.index(activation), float(drop)), bf16,
+                         lambda ref, out: query(ref, int(self.with_grad), out))
+
+    def forward(self, x, w, bias=None, residual=None, pre=None, y=None, seed=0, call=0, counter=None, stream=None):
+        """-> y, which may be the residual; x w + bias is left in `pre` if that is given"""
+        self._no_graph(x, w, bias, residual)
+        out = (self.n, self.rows, self.n_out)
+        y = self._out(y, out, self.dtype, stream)
+        self._call(lib().hadfl_layer_forward, self._rows("x", x, (self.n, self.rows, self.n_in), self.dtype),
+                   self._rows("w", w, (self.n, self.n_in, self.n_out), self.dtype), self._rows("bias", bias, (self.n, self.n_out), self.torch.float32),
+                   self._rows("residual", residual, out, self.dtype), self._draw(seed, call, counter), self._rows("pre", pre, out, self.dtype),
+                   self._rows("y", y, out, self.dtype), self.work.data_ptr(), self._stream(stream))
+        return y
+
+    def backward(self, dy, x, w, pre=None, dx=None, dw=None, db=None, want=("dx", "dw", "db"), seed=0, call=0, counter=None, stream=None):
+        """x: the tensor given to forward() or the PackedRows that holds it (None without dw; w None without dx).  -> dx, dw, db; what
+        `want` leaves out is None.  The residual's gradient is dy."""
+        if not self.with_grad:
+            raise HadflError(ESTATE, "this DenseLayer was made with grad=False")
+        rows, weights, out = (self.n, self.rows, self.n_in), (self.n, self.n_in, self.n_out), (self.n, self.rows, self.n_out)
+        dx = self._out(dx, rows, self.dtype, stream) if "dx" in want else None
+        dw = self._out(dw, weights, self.dtype, stream) if "dw" in want else None
+        db = self._out(db, (self.n, self.n_out), self.torch.float32, stream) if "db" in want else None
+        packed, others = None, ()
+        if isinstance(x, PackedRows):
+            others, packed, x = (x,), self._kept(x, rows), None
+        self._call(lib().hadfl_layer_backward, self._rows("dy", dy, out, self.dtype), self._rows("pre", pre, out, self.dtype),
+                   self._rows("x", x, rows, self.dtype), packed, self._rows("w", w, weights, self.dtype), self._draw(seed, call, counter),
+                   self._rows("dx", dx, rows, self.dtype), self._rows("dw", dw, weights, self.dtype),
+                   self._rows("db", db, (self.n, self.n_out), self.torch.float32), self.work.data_ptr(), self._stream(stream, *others))
+        return dx, dw, db
+
+
+class TokenScores(_Operator):
+    """What logits [n_replicas, n_rows, n_classes] say: log probabilities of tokens [n_replicas, n_rows, n_tokens] int32 (one outside
+    [0, n_classes) has none: 0), entropy [n_replicas, n_rows] and the n_top largest, [n_replicas, n_rows, n_top], ties to the lowest
+    index.  backward() takes the rows' statistics that forward() left, in `stats` of this object, which holds those of its last pass, or
+    in a tensor of the caller's, 32-bit [n_replicas, n_rows, 3], given to both.  forward(stats=False) leaves none and keeps what is there."""
+
+    def __init__(self, n_replicas, n_rows, n_classes, n_tokens=1, n_top=0, bf16=0):
+        self.n, self.rows, self.classes, self.tokens, self.top, bf16 = _int32(n_replicas, n_rows, n_classes, n_tokens, n_top, bf16)
+        super().__init__(HadflScores(self.n, self.rows, self.classes, self.tokens, self.top, bf16), bf16, lib().hadfl_scores_workspace)
+        self.stats = self._keep(self.torch.empty((self.n, self.rows, 3), dtype=self.torch.float32, device=self.device))
+        self._left = self.rows == 0                           # statistics are there
+
+    def _stats(self, stats):
+        return self.stats.data_ptr() or None if stats is None else None if stats is False else self._plain("stats", stats, (self.n, self.rows, 3), self.torch.float32)
+
+    def forward(self, logits, tokens=None, logp=None, entropy=None, top=None, top_logp=None, stats=None, stream=None):
+        """-> logp (None without tokens), entropy, top (int32) and top_logp (None without alternatives)"""
+        f32, i32 = self.torch.float32, self.torch.int32
+        self._no_graph(logits)
+        given, best = (self.n, self.rows, self.tokens), (self.n, self.rows, self.top)
+        if self.tokens and tokens is None:
+            raise HadflError(EINVAL, "tokens is None")
+        logp = self._out(logp, given, f32, stream) if self.tokens else None
+        entropy = self._out(entropy, given[:2], f32, stream)
+        top, top_logp = (self._out(top, best, i32, stream), self._out(top_logp, best, f32, stream)) if self.top else (None, None)
+        self._call(lib().hadfl_scores_forward, self._rows("logits", logits, (self.n, self.rows, self.classes), self.dtype),
+                   self._plain("tokens", tokens if self.tokens else None, given, i32), self._plain("logp", logp, given, f32),
+                   self._plain("entropy", entropy, given[:2], f32), self._stats(stats), self._plain("top", top, best, i32),
+                   self._plain("top_logp", top_logp, best, f32), self.work.data_ptr(), self._stream(stream))
+        self._left = self._left or stats is None
+        return logp, entropy, top, top_logp
+
+    def backward(self, logits, tokens, dlogp, dentropy=None, dlogits=None, stats=None, stream=None):
+        """tokens, dlogp: None without tokens.  -> dlogits, which may be the logits"""
+        f32, given, rows = self.torch.float32, (self.n, self.rows, self.tokens), (self.n, self.rows, self.classes)
+        if self.tokens and (tokens is None or dlogp is None):
+            raise HadflError(EINVAL, "tokens and dlogp must be given")
+        if stats is False or (stats is None and not self._left):
+            raise HadflError(ESTATE, "no forward() of this TokenScores has left its statistics")
+        dlogits = self._out(dlogits, rows, self.dtype, stream)
+        self._call(lib().hadfl_scores_backward, self._rows("logits", logits, rows, self.dtype),
+                   self._plain("tokens", tokens if self.tokens else None, given, self.torch.int32), self._stats(stats),
+                   self._plain("dlogp", dlogp if self.tokens else None, given, f32), self._plain("dentropy", dentropy, given[:2], f32),
+                   self._rows("dlogits", dlogits, rows, self.dtype), self._stream(stream))
+        return dlogits

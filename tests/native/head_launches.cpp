@@ -65,14 +65,14 @@ hipError_t hipLaunchKernel(const void* f, dim3 grid, dim3 block, void** args, si
     const std::string& name = g_names[f];
     g_trace += name;
     for (int i = 0; i < 3; ++i) g_trace += " " + std::to_string(g[i]) + " " + std::to_string(b[i]);
-    if (name.find("13direct_kernel") != std::string::npos)
+    if (name.find("13direct_kernel") != std::string::npos || name.find("19layer_planes_kernel") != std::string::npos)
         for (int i = 0; i < 2; ++i) {
             Plane p;
             std::memcpy(&p, args[i], sizeof(p));
             g_trace += " " + std::to_string(p.ld) + " " + std::to_string(p.lines) + " " + std::to_string(p.cols);
         }
-    if (name.find("14product_kernel") != std::string::npos)
-        for (int i = name.find("14product_kernelINS0_6Source") == std::string::npos; i < 2; ++i) {
+    if (name.find("14product_kernel") != std::string::npos || name.find("20layer_product_kernel") != std::string::npos)
+        for (int i = name.find("14product_kernelINS0_6Source") == std::string::npos && name.find("20layer_product_kernel") == std::string::npos; i < 2; ++i) {
             Tensor t;
             std::memcpy(&t, args[i], sizeof(t));
             g_trace += " " + std::to_string(t.cols);
