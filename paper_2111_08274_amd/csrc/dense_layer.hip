@@ -3,7 +3,7 @@
 //              gradient where that is asked for
 //   gradient   dz = D'(dy) a'(pre) and its column sums db in one pass over dy, then dx = dz W^T and dW = x^T dz
 // bf16: dz is rounded to bf16 for the two products (2^-9 of a value, as the outputs themselves are rounded; a second part would double both
-// products); db is summed before that.  fp32: operands enter as three bf16 parts, six products (tile_product.h, direct_product.h).
+// products); db is summed before that.  fp32: operands enter as three bf16 parts, six products (tile_product.h).
 #include "direct_product.h"
 #include "layer.h"
 
@@ -15,35 +15,60 @@ using namespace head;
 namespace {
 
 // ---- epilogue -----------------------------------------------------------------------------------------------------------
-// eight 32-bit sums of columns n.. of row m to what the layer returns; a null pointer leaves its part out
+// 32-bit sums to what the layer returns, eight columns of a row at a time; a null pointer leaves its part out.
 template <typename T> struct Finish {
     const float* bias;
     long long bias_rep;
     Rows residual, pre, y;
     int rows, cols, act;
     Draws draws;
-    __device__ __forceinline__ void operator()(int k, int m, int n, unsigned long long call, float (&v)[8]) const
+    // A lane's eight columns from n, in rows m, m + step, ...: what stays the same from row to row, and where its tensors stand.
+    struct Columns {
+        const T* residual;
+        T *pre, *y;
+        long long residual_step, pre_step, y_step;
+        unsigned long long call;
+        float bias[8];
+        int k, m, n, step;
+    };
+    __device__ __forceinline__ Columns columns(int k, int m, int n, int step) const
     {
-        if (m >= rows || n >= cols) return;
-        const int left = cols - n;
-        Chunk<T> add;
-        if (residual.p) add.load((const T*)residual.p + k * residual.rep + m * residual.row + n, left);
-        if (bias) {
+        Columns c{};
+        if (residual.p) c.residual = (const T*)residual.p + k * residual.rep + m * residual.row + n;
+        if (pre.p) c.pre = (T*)pre.p + k * pre.rep + m * pre.row + n;
+        c.y = (T*)y.p + k * y.rep + m * y.row + n;
+        c.residual_step = step * residual.row; c.pre_step = step * pre.row; c.y_step = step * y.row;
+        if (bias && n < cols) {
             Chunk<float> b;
-            float w[8];
-            b.load(bias + k * bias_rep + n, left);
-            b.get(w);
-            each8([&](int e) { v[e] += w[e]; });
+            b.load(bias + k * bias_rep + n, cols - n);
+            b.get(c.bias);
         }
-        if (pre.p) store_chunk((T*)pre.p + k * pre.rep + m * pre.row + n, left, v);
-        activate8(v, act);
-        if (draws.limit) kept8(draws, call, k, m, n, [&](int e, bool kept) { v[e] = kept ? v[e] * draws.scale : 0.f; });
-        if (residual.p) {
-            float w[8];
-            add.get(w);
-            each8([&](int e) { v[e] += w[e]; });
+        c.call = draws.limit ? call_of(draws) : 0ull;
+        c.k = k; c.m = m; c.n = n; c.step = step;
+        return c;
+    }
+    // the residual of the row `ahead` steps on
+    __device__ __forceinline__ void fetch(const Columns& c, int ahead, Chunk<T>& add) const
+    {
+        if (residual.p && c.m + ahead * c.step < rows && c.n < cols) add.load(c.residual + ahead * c.residual_step, cols - c.n);
+    }
+    __device__ __forceinline__ void row(Columns& c, const Chunk<T>& add, float (&v)[8]) const
+    {
+        if (c.m < rows && c.n < cols) {
+            const int left = cols - c.n;
+            if (bias) each8([&](int e) { v[e] += c.bias[e]; });
+            if (pre.p) store_chunk(c.pre, left, v);
+            activate8(v, act);
+            if (draws.limit) kept8(draws, c.call, c.k, c.m, c.n, [&](int e, bool kept) { v[e] = kept ? v[e] * draws.scale : 0.f; });
+            if (residual.p) {
+                float w[8];
+                add.get(w);
+                each8([&](int e) { v[e] += w[e]; });
+            }
+            store_chunk(c.y, left, v);
         }
-        store_chunk((T*)y.p + k * y.rep + m * y.row + n, left, v);
+        c.m += c.step;
+        c.residual += c.residual_step; c.pre += c.pre_step; c.y += c.y_step;
     }
 };
 // only the store, rounded
@@ -52,7 +77,9 @@ template <typename T> Finish<T> store_only(const Rows& y, int rows, int cols)
     return Finish<T>{nullptr, 0, {}, {}, y, rows, cols, kNone, Draws{0, 0, 0, nullptr, 0, 1.f}};
 }
 
-// A wave's blocks of 32 rows through LDS, as floats: a lane holds four consecutive columns of a row, Finish takes eight.
+// A wave's blocks of 32 rows through LDS, as floats: a lane holds four consecutive columns of a row, Finish takes eight, the same ones in every block.
+// The blocks go through one loop: unrolled, a 256 x 256 tile's epilogue was 96 KiB of code, more than the instruction cache holds.  The residual of
+// a block is on its way while the one before is finished.
 template <typename T> struct FinishTile {
     static constexpr bool kLaneM = true, kStaged = true, kSums = false;
     template <int TN> static constexpr int pitch() { return TN * 128 + 16; }
@@ -60,25 +87,39 @@ template <typename T> struct FinishTile {
     Finish<T> finish;
     template <int TM, int TN> __device__ __forceinline__ void operator()(const Tile<TM, TN>& t, char* lds) const
     {
-        constexpr int kPitch = pitch<TN>(), kAcross = TN * 4;
+        constexpr int kPitch = pitch<TN>(), kAcross = TN * 4, kDown = 64 / kAcross, kRows = 32 / kDown;
         char* p = lds + t.wave * bytes<TN>();
-        const unsigned long long call = finish.draws.limit ? call_of(finish.draws) : 0ull;
+        const int r = t.lane / kAcross, c = t.lane % kAcross * 8;
+        auto columns = finish.columns(t.rep, t.m0 + r, t.n0 + c, kDown);
+        Chunk<T> next[kRows] = {};
 #pragma unroll
+        for (int u = 0; u < kRows; ++u) finish.fetch(columns, u, next[u]);
+#pragma unroll 1
         for (int i = 0; i < TM; ++i) {
 #pragma unroll
-            for (int j = 0; j < TN; ++j)
+            for (int b = 0; b < TM; ++b) {
+                if (b != i) continue;
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    *(f4*)(p + (t.lane & 31) * kPitch + (32 * j + 8 * q + 4 * (t.lane >> 5)) * 4) =
-                        f4{t.acc[i][j][4 * q], t.acc[i][j][4 * q + 1], t.acc[i][j][4 * q + 2], t.acc[i][j][4 * q + 3]};
+                for (int j = 0; j < TN; ++j)
 #pragma unroll
-            for (int u = 0; u < 32 * kAcross / 64; ++u) {
-                const int id = u * 64 + t.lane, r = id / kAcross, c = id % kAcross * 8;
-                const f4 a = *(const f4*)(p + r * kPitch + c * 4), b = *(const f4*)(p + r * kPitch + c * 4 + 16);
+                    for (int q = 0; q < 4; ++q)
+                        *(f4*)(p + (t.lane & 31) * kPitch + (32 * j + 8 * q + 4 * (t.lane >> 5)) * 4) =
+                            f4{t.acc[b][j][4 * q], t.acc[b][j][4 * q + 1], t.acc[b][j][4 * q + 2], t.acc[b][j][4 * q + 3]};
+            }
+            Chunk<T> now[kRows];
+#pragma unroll
+            for (int u = 0; u < kRows; ++u) {
+                now[u] = next[u];
+                if (i + 1 < TM) finish.fetch(columns, kRows + u, next[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < kRows; ++u) {
+                const char* at = p + (r + u * kDown) * kPitch + c * 4;
+                const f4 low = *(const f4*)at, high = *(const f4*)(at + 16);
                 float v[8];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
-                finish(t.rep, t.m0 + 32 * i + r, t.n0 + c, call, v);
+                for (int e = 0; e < 4; ++e) { v[e] = low[e]; v[4 + e] = high[e]; }
+                finish.row(columns, now[u], v);
             }
         }
     }
@@ -90,10 +131,94 @@ __global__ __launch_bounds__(WM * WN * 64) void layer_product_kernel(SA a, SB b,
 {
     product_tile<SA, A_ALONG, SB, B_ALONG, BM, BN, WM, WN, KS, NBUF, AHEAD>(a, b, K, tiles_m, tiles_n, splits, split_len, total, epi);
 }
-template <bool A_ALONG, bool B_ALONG, int PA, int PB, int BM, int BN, int WM, int WN, class Epi>
+// Operands in planes of bf16, straight from memory to LDS (direct_product.h: Loader), slabs of 64 k.  A wave reads the operands of a step of 16 k while it
+// multiplies the step before, across slabs too: the barrier that frees a slab's image and says that the next one has arrived lies before the slab's
+// last step, whose operands are in registers by then, so that the matrix cores have work while the first operands of the next slab are read.
+template <bool A_ALONG, bool B_ALONG, int BM, int BN, int WM, int WN, class Epi>
 __global__ __launch_bounds__(WM * WN * 64) void layer_planes_kernel(Plane3 a, Plane3 b, int K, int tiles_m, int tiles_n, int splits, int split_len, int total, Epi epi)
 {
-    direct_tile<A_ALONG, B_ALONG, PA, PB, BM, BN, WM, WN>(a, b, K, tiles_m, tiles_n, splits, split_len, total, epi);
+    constexpr int NT = WM * WN * 64, TM = BM / WM / 32, TN = BN / WN / 32, kSteps = kSlab / 16;
+    typedef Loader<A_ALONG, BM, NT> LA;
+    typedef Loader<B_ALONG, BN, NT> LB;
+    constexpr int kImage = LA::kBytes + LB::kBytes, IMAGES = kImage > 49152 ? 2 : kImage > 32768 ? 3 : 4, kLoads = LA::kLoads + LB::kLoads;
+    __shared__ __attribute__((aligned(16))) char images[IMAGES * kImage];
+    if constexpr (Epi::kStaged) static_assert(WM * WN * Epi::template bytes<TN>() <= IMAGES * kImage, "the epilogue's blocks lie in the images");
+
+    const unsigned item = blockIdx.y * gridDim.x + logical_block();
+    if (item >= (unsigned)total) return;
+    const int per = tiles_m * tiles_n, r = item / per;
+    int tm_i, tn_i;
+    place_tile(item - r * per, tiles_m, tiles_n, tm_i, tn_i);
+    Tile<TM, TN> t;
+    t.split = r % splits;
+    t.rep = r / splits;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+    t.lane = tid & 63;
+    t.wave = wave;
+    const int bm = t.bm = tm_i * BM, bn = t.bn = tn_i * BN, wm = (wave % WM) * TM * 32, wn = (wave / WM) * TN * 32;
+    t.m0 = bm + wm;
+    t.n0 = bn + wn;
+    const __bf16 *pa = a.p + t.rep * a.rep, *pb = b.p + t.rep * b.rep;
+    const int k_begin = t.split * split_len, k_end = min(K, k_begin + split_len), slabs = k_begin < k_end ? (k_end - k_begin + kSlab - 1) / kSlab : 0;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) t.acc[i][j] = f16{};
+    LA la;
+    LB lb;
+    la.init(tid, a.ld);
+    lb.init(tid, b.ld);
+
+    auto issue = [&](int slab, char* image) {
+        la.issue(a, pa, bm, k_begin + slab * kSlab, wave, image);
+        lb.issue(b, pb, bn, k_begin + slab * kSlab, wave, image + LA::kBytes);
+    };
+    bf16x8 fa[2][TM], fb[2][TN];
+    auto read = [&](const char* image, int step, int to) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) fa[to][i] = LA::read(image, wm + 32 * i, step, t.lane);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) fb[to][j] = LB::read(image + LA::kBytes, wn + 32 * j, step, t.lane);
+    };
+    auto multiply = [&](int from) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+                t.acc[i][j] = Epi::kLaneM ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[from][j], fa[from][i], t.acc[i][j], 0, 0, 0)
+                                          : __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[from][i], fb[from][j], t.acc[i][j], 0, 0, 0);
+    };
+    // Slab i + 1 is there when at most the loads of the IMAGES - 2 slabs after it are outstanding (they finish in order).
+    auto turn = [&](int i, char* image, char* next) {
+        if (i >= slabs) return;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            if (s + 1 < kSteps) read(image, s + 1, (s + 1) % 2);
+            else if (i + 1 < slabs) {
+                if (IMAGES > 2 && i + IMAGES - 1 < slabs) slab_barrier<(IMAGES - 2) * kLoads>();
+                else slab_barrier<0>();
+                if (i + IMAGES < slabs) issue(i + IMAGES, image);
+                read(next, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(s % 2);
+        }
+    };
+    static_assert(kSteps % 2 == 0, "a slab ends where the next one's first operands go");
+#pragma unroll
+    for (int i = 0; i < IMAGES; ++i)
+        if (i < slabs) issue(i, images + i * kImage);
+    if (slabs >= IMAGES) slab_barrier<(IMAGES - 1) * kLoads>();
+    else slab_barrier<0>();
+    if (slabs) read(images, 0, 0);
+    for (int i = 0; i < slabs; i += IMAGES) {
+#pragma unroll
+        for (int u = 0; u < IMAGES; ++u) turn(i + u, images + u * kImage, images + (u + 1) % IMAGES * kImage);
+    }
+    if constexpr (Epi::kStaged) {
+        __syncthreads();                                       // the images are free
+        epi(t, images);
+    } else epi(t);
 }
 
 // The shares of a contraction, [splits][replicas][rows][ld] floats, added in ascending order and finished.
@@ -112,7 +237,10 @@ __global__ __launch_bounds__(256) void finish_shares_kernel(const float* share, 
     float v[8];
 #pragma unroll
     for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
-    finish(k, t, c, finish.draws.limit ? call_of(finish.draws) : 0ull, v);
+    auto columns = finish.columns(k, t, c, 0);
+    Chunk<T> add = {};
+    finish.fetch(columns, 0, add);
+    finish.row(columns, add, v);
 }
 
 int up_to(long long v, int unit) { return (int)((v + unit - 1) / unit * unit); }
@@ -130,50 +258,74 @@ Shape cut(Shape p, int K, int splits, int unit)
     p.splits = std::max(1, (K + p.len - 1) / p.len);
     return p;
 }
-// operands in planes: products of `pairs` pairs of them
-Shape planes_shape(int n, int M, int N, int K, int pairs)
+// Tiles that there are, with what they cost in nanoseconds a k of a contraction: of a workgroup alone on its compute unit, and of each of several there
+// (`most` fit), measured over 64 to 8192 rows, 200 to 4096 inputs and outputs; and in microseconds what a tile costs beside.
+struct Choice {
+    bool planes;
+    int bm, bn, most;
+    struct { double alone, shared; } f32, bf16;
+    double tile;
+};
+constexpr Choice kChoices[] = {{false, 32, 128, 3, {23, 15}, {6.3, 5}, 3}, {false, 64, 64, 4, {25, 15.5}, {8.8, 4.9}, 3}, {false, 64, 128, 2, {28, 27}, {7.5, 7.3}, 3},
+                               {false, 128, 128, 2, {46, 46}, {10, 11}, 4}, {true, 128, 128, 1, {0, 0}, {7, 9.6}, 4}, {true, 128, 256, 1, {0, 0}, {11.5, 16}, 5},
+                               {true, 256, 256, 1, {0, 0}, {21, 28}, 8}};
+// The cheapest tiles and shares by that; `lay`: seconds to copy operands into planes first.  A share is written and read at 5 TB/s, and joining them is one more launch, 4 us.  Chosen / best of all, us:
+//   bf16  y of 16 x 1024 x 512 x 2048 47.9 / 47.7, 4096 x 1024 x 4096 38.8 / 38.8 (128 x 128 tiles 51), 8192 x 4096 x 4096 232 / 232 (315); dx of the
+//         first 39.9 / 39.7 (256 x 256 tiles 55), dW 38.5 / 38.5
+//   fp32  the same 205 / 201, 194 / 194, 1490 / 1487, 194 / 192, 191 / 191; 64 x 64 tiles take 250, 252 and 1964 of the first three
+Shape best_shape(int n, int M, int N, int K, int bf16, bool across, bool planes, bool registers, double lay)
 {
-    const int slabs = (K + kSlab - 1) / kSlab * pairs;
-    auto tiles = [&](int m, int n_) { return (long long)n * ((M + m - 1) / m) * ((N + n_ - 1) / n_); };
-    Shape p{true, 256, 256, 1, 0};
-    if (tiles(256, 256) < 192) p.bm = p.bn = 128;
-    return cut(p, K, best_shares(tiles(p.bm, p.bn), slabs, (double)n * M * N * 4), kSlab);
-}
-// operands through registers
-Shape registers_shape(int n, int M, int N, int K, int bm, int bn)
-{
-    const long long tiles = (long long)n * ((M + bm - 1) / bm) * ((N + bn - 1) / bn);
-    const int splits = (int)std::max<long long>(1, std::min<long long>(512 / std::max<long long>(1, tiles), K / 256));
-    return cut(Shape{false, bm, bn, 1, 0}, K, splits, 128);
+    Shape best{};
+    double least = -1;
+    for (const Choice& o : kChoices) {
+        if ((o.planes ? !planes : !registers) || (o.bm == 32 && (M > 32 || across))) continue;
+        const long long tiles = (long long)n * ((M + o.bm - 1) / o.bm) * ((N + o.bn - 1) / o.bn);
+        const int unit = o.planes ? kSlab : 128;
+        const double alone = bf16 ? o.bf16.alone : o.f32.alone, shared = bf16 ? o.bf16.shared : o.f32.shared;
+        for (int s = 1; s <= 64 && (s == 1 || K / s >= unit); ++s) {
+            const Shape p = cut(Shape{o.planes, o.bm, o.bn, 1, 0}, K, s, unit);
+            if (p.splits != s) continue;
+            const double each = (double)((tiles * s + 255) / 256);            // tiles of a compute unit
+            const double k = each <= o.most ? std::max(alone, each * shared) : each * shared;
+            const double cost = std::min(K, p.len) * k * 1e-9 + (each <= o.most ? 1 : each / o.most) * o.tile * 1e-6 + (o.planes ? lay : 0) + (s > 1 ? 4e-6 + (double)s * n * M * N * 8 / 5e12 : 0);
+            if (least < 0 || cost < (s > 1 && best.splits == 1 ? 0.95 : 1) * least) { best = p; least = cost; }
+        }
+    }
+    return best;
 }
 
 struct Work {                      // where things lie in the working memory
     Shape y, dx, dw;
-    int ldx, ldz, planes;
+    int ldx, ldz;
     size_t x, w, dz, sums, share, total;
     int blocks, across, depth;     // column sums: row blocks, lanes a row, rows a block
 };
-bool few(int rows, int in, int out) { return rows <= 64 && std::min(in, out) >= 8; }
-
-Work plan_of(int n, int rows, int in, int out, int bf16, bool grad)
+// Sources through registers hold eight columns at least (tile_product.h): narrower tensors are copied into rows of eight.  bf16 operands of products of
+// planes are copied where they do not lie as planes do, which shows only at the call.
+Work plan_of(int n, int rows, int in, int out, int bf16, bool grad, bool packed)
 {
     Work p{};
     p.ldx = up_to(in, 8);
     p.ldz = up_to(out, 8);
-    p.planes = bf16 ? 1 : 3;
-    const bool small = few(rows, in, out);
-    const int pairs = bf16 ? 1 : 6, bm = rows <= 32 ? 32 : 64;
+    const bool narrow = std::min(in, out) < 8;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += align256(bytes); return o; };
-    if (!small || grad) p.x = take((size_t)n * rows * p.ldx * 2 * p.planes);
-    if (!small) p.w = take((size_t)n * in * p.ldz * 2 * p.planes);
+    // rows of a size that is no multiple of eight are copied, a launch and their bytes twice
+    auto lay = [&](int lines, int cols) { return cols % 8 ? 4e-6 + (double)n * lines * cols * 4 / 4e12 : 0.; };
+    auto shape = [&](int M, int N, int K, bool across, double copies) { return best_shape(n, M, N, K, bf16, across, bf16, !bf16 || !narrow, copies); };
+    const size_t size = bf16 ? 2 : 4, x = (size_t)n * rows * p.ldx * size, w = (size_t)n * in * p.ldz * size;
     if (!grad) {
-        p.y = small ? registers_shape(n, rows, out, in, bm, 128) : planes_shape(n, rows, out, in, pairs);
+        p.y = shape(rows, out, in, false, lay(rows, in) + lay(in, out));
+        if (p.y.planes || in < 8) p.x = take(x);
+        if (p.y.planes || out < 8) p.w = take(w);
         p.share = take(share_bytes(p.y, n, rows, out));
     } else {
-        p.dx = small ? registers_shape(n, rows, in, out, bm, 128) : planes_shape(n, rows, in, out, pairs);
-        p.dw = small ? registers_shape(n, in, out, rows, 64, 64) : planes_shape(n, in, out, rows, pairs);
-        p.dz = take((size_t)n * rows * p.ldz * (small ? (bf16 ? 2 : 4) : 2 * p.planes));
+        p.dx = shape(rows, in, out, false, lay(in, out));
+        p.dw = shape(in, out, rows, true, packed ? 0. : lay(rows, in));
+        if (packed) p.x = take((size_t)n * rows * p.ldx * 2);
+        else if (p.dw.planes || in < 8) p.x = take(x);
+        if (p.dx.planes || out < 8) p.w = take(w);
+        p.dz = take((size_t)n * rows * p.ldz * size);
         p.across = 8;
         while (p.across < 64 && p.across * 8 < p.ldz) p.across *= 2;
         const long long wide = (p.ldz + p.across * 8 - 1) / (p.across * 8);
@@ -202,15 +354,14 @@ hipError_t launch_registers(const SA& a, const SB& b, int n, int M, int N, int K
         <<<line_grid(die_grid(total), WM * WN * 64), WM * WN * 64, 0, s>>>(a, b, K, tm, tn, p.splits, p.len, (int)total, epi);
     return hipGetLastError();
 }
-template <int PA, int PB, int BM, int BN, int WM, int WN, bool AA, bool BA, class Epi>
+template <int BM, int BN, int WM, int WN, bool AA, bool BA, class Epi>
 hipError_t launch_planes(const Plane3& a, const Plane3& b, int n, int M, int N, int K, const Shape& p, const Epi& epi, hipStream_t s)
 {
-    if constexpr (Epi::kStaged) static_assert(WM * WN * Epi::template bytes<BN / WN / 32>() <= 128 * 1024, "the epilogue's blocks lie in the images");
     const int tm = (M + BM - 1) / BM, tn = (N + BN - 1) / BN;
     const long long total = (long long)n * p.splits * tm * tn;
     if (total == 0) return hipSuccess;
     if (total > 0x7fffff00ll) return hipErrorInvalidValue;
-    layer_planes_kernel<AA, BA, PA, PB, BM, BN, WM, WN, Epi>
+    layer_planes_kernel<AA, BA, BM, BN, WM, WN, Epi>
         <<<line_grid(die_grid(total), WM * WN * 64), WM * WN * 64, 0, s>>>(a, b, K, tm, tn, p.splits, p.len, (int)total, epi);
     return hipGetLastError();
 }
@@ -225,55 +376,88 @@ template <typename T, class F> hipError_t whole_or_shares(const Shape& p, int n,
     finish_shares_kernel<T><<<line_grid((total + 255) / 256, 256), 256, 0, s>>>(share, p.splits, lines * ld, ld, total, finish);
     return hipGetLastError();
 }
-template <int PA, int PB, bool AA, bool BA, typename T>
-hipError_t planes_product(const Plane3& a, const Plane3& b, int n, int M, int N, int K, const Shape& p, const Finish<T>& finish, float* share, hipStream_t s)
+template <bool AA, bool BA>
+hipError_t planes_product(const Plane3& a, const Plane3& b, int n, int M, int N, int K, const Shape& p, const Finish<__bf16>& finish, float* share, hipStream_t s)
+{
+    return whole_or_shares<__bf16>(p, n, M, N, finish, share, s, [&](const auto& epi) {
+        if (p.bm == 256) return launch_planes<256, 256, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
+        if (p.bn == 256) return launch_planes<128, 256, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
+        return launch_planes<128, 128, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
+    });
+}
+template <bool AA, bool BA, typename T, class SA, class SB>
+hipError_t registers_product(const SA& a, const SB& b, int n, int M, int N, int K, const Shape& p, const Finish<T>& finish, float* share, hipStream_t s)
 {
     return whole_or_shares<T>(p, n, M, N, finish, share, s, [&](const auto& epi) {
-        if (p.bm == 256) return launch_planes<PA, PB, 256, 256, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
-        return launch_planes<PA, PB, 128, 128, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
+        if (p.bm == 128) return launch_registers<T, 128, 128, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
+        if constexpr (AA)
+            if (p.bm == 32) return launch_registers<T, 32, 128, 1, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
+        if (p.bn == 64) return launch_registers<T, 64, 64, 2, 2, AA, BA>(a, b, n, M, N, K, p, epi, s);
+        return launch_registers<T, 64, 128, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
     });
 }
 
-// a tensor [n][rows][cols] as planes: as it lies, or laid out at `at`
-template <typename T, int PL> hipError_t planes_of(const Rows& r, int n, int rows, int cols, __bf16* at, Plane3& out, hipStream_t s)
+// x [replicas][rows][cols] -> [replicas][rows][8], zero beyond cols
+template <typename T>
+__global__ __launch_bounds__(256) void widen_kernel(const T* x, long long rep, long long row, int rows, int cols, long long total, T* out)
 {
-    const int ld = up_to(cols, 8);
-    if (PL == 1 && is_plane(r, cols)) {
-        out = Plane3{(const __bf16*)r.p, r.rep, 0, (int)r.row, rows, cols, nullptr};
-        return hipSuccess;
+    const long long at = line_block() * 256 + threadIdx.x;
+    if (at >= total) return;
+    const int k = (int)(at / rows), t = (int)(at - (long long)k * rows);
+    Chunk<T> v;
+    float f[8];
+    v.load(x + k * rep + t * row, cols);
+    v.get(f);
+    store_chunk(out + at * 8, 8, f);
+}
+// A tensor [n][rows][cols] as a product takes it: as it lies, or copied to `at`.
+template <typename T> hipError_t ready(const Rows& r, int n, int rows, int cols, bool planes, void* at, Rows& out, int& width, hipStream_t s)
+{
+    out = r;
+    width = cols;
+    if (planes ? is_plane(r, cols) : cols >= 8) return hipSuccess;
+    width = up_to(cols, 8);
+    out = Rows{at, (long long)rows * width, width};
+    const long long total = (long long)n * rows;
+    if (total == 0) return hipSuccess;
+    if constexpr (sizeof(T) == 2) return lay_out<__bf16, 1>(n, rows, cols, width, r, Labelled{nullptr, 0}, nullptr, (__bf16*)at, s);
+    else {
+        widen_kernel<T><<<line_grid((total + 255) / 256, 256), 256, 0, s>>>((const T*)r.p, r.rep, r.row, rows, cols, total, (T*)at);
+        return hipGetLastError();
     }
-    out = Plane3{at, (long long)rows * ld, (long long)n * rows * ld, ld, rows, ld, nullptr};
-    return lay_out<T, PL>(n, rows, cols, ld, r, Labelled{nullptr, 0}, nullptr, at, s);
+}
+Plane3 plane(const Rows& r, int rows, int cols) { return Plane3{(const __bf16*)r.p, r.rep, 0, (int)r.row, rows, cols, nullptr}; }
+
+// C = A B of operands that are ready
+template <bool AA, bool BA, typename T, typename TA>
+hipError_t product(const Rows& a, int a_rows, int a_cols, const Rows& b, int b_rows, int b_cols, int n, int M, int N, int K, const Shape& p, const Finish<T>& finish,
+                   float* share, hipStream_t s)
+{
+    if constexpr (sizeof(T) == 2)
+        if (p.planes) return planes_product<AA, BA>(plane(a, a_rows, a_cols), plane(b, b_rows, b_cols), n, M, N, K, p, finish, share, s);
+    return registers_product<AA, BA, T>(source<TA>(a, a_rows, a_cols), source<T>(b, b_rows, b_cols), n, M, N, K, p, finish, share, s);
 }
 
 template <typename T> hipError_t forward(const LayerArgs& a, hipStream_t s)
 {
-    constexpr int PL = sizeof(T) == 4 ? 3 : 1;
     if (a.rows == 0) return hipSuccess;
-    const Work p = plan_of(a.n, a.rows, a.in, a.out, a.bf16, false);
+    const Work p = plan_of(a.n, a.rows, a.in, a.out, a.bf16, false, false);
     char* work = (char*)a.work;
-    float* share = (float*)(work + p.share);
     const Finish<T> finish{(const float*)a.bias.p, a.bias.rep, a.residual, a.pre, a.y, a.rows, a.out, a.act, a.draws};
-    if (!p.y.planes) {
-        const Source<T> x = source<T>(a.x, a.rows, a.in), w = source<T>(a.w, a.in, a.out);
-        return whole_or_shares<T>(p.y, a.n, a.rows, a.out, finish, share, s, [&](const auto& epi) {
-            if (p.y.bm == 32) return launch_registers<T, 32, 128, 1, 4, true, false>(x, w, a.n, a.rows, a.out, a.in, p.y, epi, s);
-            return launch_registers<T, 64, 128, 2, 4, true, false>(x, w, a.n, a.rows, a.out, a.in, p.y, epi, s);
-        });
-    }
-    Plane3 x, w;
-    hipError_t e = planes_of<T, PL>(a.x, a.n, a.rows, a.in, (__bf16*)(work + p.x), x, s);
-    if (e == hipSuccess) e = planes_of<T, PL>(a.w, a.n, a.in, a.out, (__bf16*)(work + p.w), w, s);
+    Rows x, w;
+    int wx, ww;
+    hipError_t e = ready<T>(a.x, a.n, a.rows, a.in, p.y.planes, work + p.x, x, wx, s);
+    if (e == hipSuccess) e = ready<T>(a.w, a.n, a.in, a.out, p.y.planes, work + p.w, w, ww, s);
     if (e != hipSuccess) return e;
-    return planes_product<PL, PL, true, false, T>(x, w, a.n, a.rows, a.out, a.in, p.y, finish, share, s);
+    return product<true, false, T, T>(x, a.rows, wx, w, a.in, ww, a.n, a.rows, a.out, a.in, p.y, finish, (float*)(work + p.share), s);
 }
 
 // ---- gradient ---------------------------------------------------------------------------------------------------------------
-// dz = D'(dy) a'(pre), eight columns a lane, as T rows (OUT = 1, [replicas][rows][ld]), three bf16 parts (3) or not stored (0), and the column
-// sums of a block's rows.  A dropped value is zero whatever dy and pre hold there.
-template <typename T, int OUT>
+// dz = D'(dy) a'(pre), eight columns a lane, into [replicas][rows][ld] if STORE, and the column sums of a block's rows.  A dropped value is zero
+// whatever dy and pre hold there.
+template <typename T, bool STORE>
 __global__ __launch_bounds__(256) void slope_kernel(const T* dy, long long yrep, long long yrow, const T* pre, long long prep, long long prow, int rows, int cols,
-                                                    int ld, int across, int depth, int act, Draws d, void* dz, long long plane, float* sums)
+                                                    int ld, int across, int depth, int act, Draws d, T* dz, float* sums)
 {
     __shared__ float part[256][9];
     const int lane = threadIdx.x % across, line = threadIdx.x / across, lines = 256 / across;
@@ -295,17 +479,7 @@ __global__ __launch_bounds__(256) void slope_kernel(const T* dy, long long yrep,
             }
             if (d.limit) kept8(d, call, k, t, c, [&](int e, bool kept) { v[e] = kept ? v[e] * d.scale : 0.f; });
             each8([&](int e) { if (c + e >= cols) v[e] = 0.f; sum[e] += v[e]; });
-            const long long to = ((long long)k * rows + t) * ld + c;
-            if constexpr (OUT == 1) store_chunk((T*)dz + to, 8, v);
-            if constexpr (OUT == 3) {
-                u2 h[2], m[2], l[2];
-                parts3(f4{v[0], v[1], v[2], v[3]}, h[0], m[0], l[0]);
-                parts3(f4{v[4], v[5], v[6], v[7]}, h[1], m[1], l[1]);
-                __bf16* out = (__bf16*)dz + to;
-                *(u4*)out = join8(h[0], h[1]);
-                *(u4*)(out + plane) = join8(m[0], m[1]);
-                *(u4*)(out + 2 * plane) = join8(l[0], l[1]);
-            }
+            if constexpr (STORE) store_chunk(dz + ((long long)k * rows + t) * ld + c, 8, v);
         }
     if (!sums) return;
     each8([&](int e) { part[threadIdx.x][e] = sum[e]; });
@@ -330,68 +504,52 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const float* sums, int
 
 template <typename T> hipError_t backward(const LayerArgs& a, hipStream_t s)
 {
-    constexpr int PL = sizeof(T) == 4 ? 3 : 1;
-    const Work p = plan_of(a.n, a.rows, a.in, a.out, a.bf16, true);
+    const Work p = plan_of(a.n, a.rows, a.in, a.out, a.bf16, true, a.packed.q);
     char* work = (char*)a.work;
     float *share = (float*)(work + p.share), *sums = (float*)(work + p.sums);
-    void* dz = work + p.dz;
-    const bool small = !p.dx.planes, products = a.dx.p || a.dw.p;
+    const bool want_dx = a.dx.p && a.rows, want_dw = a.dw.p, planes = (want_dx && p.dx.planes) || (want_dw && p.dw.planes);
     hipError_t e = hipSuccess;
-    // dz in the working memory, as the products take it; where it is dy itself only what they cannot read is laid out
-    const bool same = a.act == kNone && !a.draws.limit, there = same && (small || (PL == 1 && is_plane(a.dy, a.out)));
-    const long long plane = (long long)a.n * a.rows * p.ldz;
-    if (a.rows && ((products && !there) || a.db.p)) {
+    // dz is formed in the working memory; where it is dy itself it is read as it lies, if the products can
+    const bool there = a.act == kNone && !a.draws.limit && a.out >= 8 && (!planes || is_plane(a.dy, a.out)), form = (want_dx || want_dw) && !there;
+    if (a.rows && (form || a.db.p)) {
         const dim3 grid((unsigned)((p.ldz + p.across * 8 - 1) / (p.across * 8)), (unsigned)p.blocks, (unsigned)a.n);
-        auto* kernel = !products || there ? slope_kernel<T, 0> : small || PL == 1 ? slope_kernel<T, 1> : slope_kernel<T, PL>;
+        auto* kernel = form ? slope_kernel<T, true> : slope_kernel<T, false>;
         kernel<<<grid, 256, 0, s>>>((const T*)a.dy.p, a.dy.rep, a.dy.row, (const T*)a.pre.p, a.pre.rep, a.pre.row, a.rows, a.out, p.ldz, p.across, p.depth,
-                                    a.act, a.draws, dz, plane, a.db.p ? sums : nullptr);
+                                    a.act, a.draws, (T*)(work + p.dz), a.db.p ? sums : nullptr);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (a.db.p) {
         column_sums_kernel<<<dim3((unsigned)((a.out + 255) / 256), (unsigned)a.n), 256, 0, s>>>(sums, a.rows ? p.blocks : 0, p.ldz, a.out, (float*)a.db.p, a.db.rep);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    const Rows z = there ? a.dy : Rows{dz, (long long)a.rows * p.ldz, p.ldz};
-    const int zcols = there ? a.out : p.ldz;
-    const Finish<T> to_dx = store_only<T>(a.dx, a.rows, a.in), to_dw = store_only<T>(a.dw, a.in, a.out);
-    Rows kept{work + p.x, (long long)a.rows * p.ldx, p.ldx};   // the checkpoint's values, exact in bf16
-    if (a.dw.p && a.packed.q && a.rows && (e = launch_unpack(a.n, a.rows, a.in, 1, a.packed.q, kept, s)) != hipSuccess) return e;
-    if (small) {
-        const Source<T> g = source<T>(z, a.rows, zcols);
-        if (a.dx.p && a.rows) {
-            const Source<T> w = source<T>(a.w, a.in, a.out);
-            e = whole_or_shares<T>(p.dx, a.n, a.rows, a.in, to_dx, share, s, [&](const auto& epi) {
-                if (p.dx.bm == 32) return launch_registers<T, 32, 128, 1, 4, true, true>(g, w, a.n, a.rows, a.in, a.out, p.dx, epi, s);
-                return launch_registers<T, 64, 128, 2, 4, true, true>(g, w, a.n, a.rows, a.in, a.out, p.dx, epi, s);
-            });
-            if (e != hipSuccess) return e;
-        }
-        if (!a.dw.p) return hipSuccess;
-        return whole_or_shares<T>(p.dw, a.n, a.in, a.out, to_dw, share, s, [&](const auto& epi) {
-            if (a.packed.q) return launch_registers<T, 64, 64, 2, 2, false, false>(source<__bf16>(kept, a.rows, p.ldx), g, a.n, a.in, a.out, a.rows, p.dw, epi, s);
-            return launch_registers<T, 64, 64, 2, 2, false, false>(source<T>(a.x, a.rows, a.in), g, a.n, a.in, a.out, a.rows, p.dw, epi, s);
-        });
+    const Rows z = there ? a.dy : Rows{work + p.dz, (long long)a.rows * p.ldz, p.ldz};
+    const int wz = there ? a.out : p.ldz;
+    if (want_dx) {
+        Rows w;
+        int ww;
+        if ((e = ready<T>(a.w, a.n, a.in, a.out, p.dx.planes, work + p.w, w, ww, s)) != hipSuccess) return e;
+        e = product<true, true, T, T>(z, a.rows, wz, w, a.in, ww, a.n, a.rows, a.in, a.out, p.dx, store_only<T>(a.dx, a.rows, a.in), share, s);
+        if (e != hipSuccess) return e;
     }
-    const Plane3 g = there ? Plane3{(const __bf16*)a.dy.p, a.dy.rep, 0, (int)a.dy.row, a.rows, a.out, nullptr}
-                           : Plane3{(const __bf16*)dz, (long long)a.rows * p.ldz, plane, p.ldz, a.rows, p.ldz, nullptr};
-    if (a.dx.p && a.rows) {
-        Plane3 w;
-        if ((e = planes_of<T, PL>(a.w, a.n, a.in, a.out, (__bf16*)(work + p.w), w, s)) != hipSuccess) return e;
-        if ((e = planes_product<PL, PL, true, true, T>(g, w, a.n, a.rows, a.in, a.out, p.dx, to_dx, share, s)) != hipSuccess) return e;
+    if (!want_dw) return hipSuccess;
+    const Finish<T> to_dw = store_only<T>(a.dw, a.in, a.out);
+    if (a.packed.q) {                                          // the checkpoint's values, exact in bf16; columns beyond n_in belong to no row of dW
+        const Rows kept{work + p.x, (long long)a.rows * p.ldx, p.ldx};
+        if (a.rows && (e = launch_unpack(a.n, a.rows, a.in, 1, a.packed.q, kept, s)) != hipSuccess) return e;
+        return product<false, false, T, __bf16>(kept, a.rows, p.ldx, z, a.rows, wz, a.n, a.in, a.out, a.rows, p.dw, to_dw, share, s);
     }
-    if (!a.dw.p) return hipSuccess;
-    Plane3 x{(const __bf16*)kept.p, kept.rep, 0, p.ldx, a.rows, p.ldx, nullptr};
-    if (a.packed.q) return planes_product<1, PL, false, false, T>(x, g, a.n, a.in, a.out, a.rows, p.dw, to_dw, share, s);
-    if ((e = planes_of<T, PL>(a.x, a.n, a.rows, a.in, (__bf16*)(work + p.x), x, s)) != hipSuccess) return e;
-    return planes_product<PL, PL, false, false, T>(x, g, a.n, a.in, a.out, a.rows, p.dw, to_dw, share, s);
+    Rows x;
+    int wx;
+    if ((e = ready<T>(a.x, a.n, a.rows, a.in, p.dw.planes, work + p.x, x, wx, s)) != hipSuccess) return e;
+    return product<false, false, T, T>(x, a.rows, wx, z, a.rows, wz, a.n, a.in, a.out, a.rows, p.dw, to_dw, share, s);
 }
 
 }  // namespace
 
 size_t layer_work_bytes(int n, int rows, int in, int out, int bf16, bool grad)
 {
-    const size_t one = plan_of(n, rows, in, out, bf16, false).total;       // a workspace for the gradient serves the forward pass too
-    return grad ? std::max(one, plan_of(n, rows, in, out, bf16, true).total) : one;
+    const size_t one = plan_of(n, rows, in, out, bf16, false, false).total;       // a workspace for the gradient serves the forward pass too
+    return grad ? std::max({one, plan_of(n, rows, in, out, bf16, true, false).total, plan_of(n, rows, in, out, bf16, true, true).total}) : one;
 }
 hipError_t launch_layer_forward(const LayerArgs& a, hipStream_t s) { return a.bf16 ? forward<__bf16>(a, s) : forward<float>(a, s); }
 hipError_t launch_layer_backward(const LayerArgs& a, hipStream_t s) { return a.bf16 ? backward<__bf16>(a, s) : backward<float>(a, s); }

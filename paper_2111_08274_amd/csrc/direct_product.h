@@ -123,11 +123,6 @@ template <bool ALONG, int BR, int NT> struct Loader {
 template <int PA, int PB> struct Pairs;
 template <> struct Pairs<1, 1> { static constexpr int kCount = 1; static __device__ int a(int) { return 0; } static __device__ int b(int) { return 0; } };
 template <> struct Pairs<1, 3> { static constexpr int kCount = 3; static __device__ int a(int) { return 0; } static __device__ int b(int s) { return 2 - s; } };
-template <> struct Pairs<3, 3> {                               // (2,0) (1,1) (0,2) (1,0) (0,1) (0,0): what is left out is below 2^-24 of the product
-    static constexpr int kCount = 6;
-    static __device__ int a(int s) { return s < 3 ? 2 - s : s < 5 ? 4 - s : 0; }
-    static __device__ int b(int s) { return s < 3 ? s : s == 4; }
-};
 template <> struct Pairs<2, 2> {
     static constexpr int kCount = 3;                           // (1,0) (0,1) (0,0)
     static __device__ int a(int s) { return s == 0; }
@@ -153,9 +148,9 @@ __device__ __forceinline__ void place_tile(int at, int tiles_m, int tiles_n, int
     m = g * G + in - n * rows;
 }
 
-// One workgroup's tile.
 template <bool A_ALONG, bool B_ALONG, int PA, int PB, int BM, int BN, int WM, int WN, class Epi>
-__device__ __forceinline__ void direct_tile(Plane3 a, Plane3 b, int K, int tiles_m, int tiles_n, int splits, int split_len, int total, Epi epi)
+__global__ __launch_bounds__(WM * WN * 64) void direct_kernel(Plane3 a, Plane3 b, int K, int tiles_m, int tiles_n, int splits, int split_len,
+                                                              int total, Epi epi)
 {
     constexpr int NT = WM * WN * 64, TM = BM / WM / 32, TN = BN / WN / 32;
     typedef Loader<A_ALONG, BM, NT> LA;
@@ -255,13 +250,6 @@ __device__ __forceinline__ void direct_tile(Plane3 a, Plane3 b, int K, int tiles
         __syncthreads();                                       // the images are free
         epi(t, images);
     } else epi(t);
-}
-
-template <bool A_ALONG, bool B_ALONG, int PA, int PB, int BM, int BN, int WM, int WN, class Epi>
-__global__ __launch_bounds__(WM * WN * 64) void direct_kernel(Plane3 a, Plane3 b, int K, int tiles_m, int tiles_n, int splits, int split_len,
-                                                              int total, Epi epi)
-{
-    direct_tile<A_ALONG, B_ALONG, PA, PB, BM, BN, WM, WN>(a, b, K, tiles_m, tiles_n, splits, split_len, total, epi);
 }
 
 template <int PA, int PB, int BM, int BN, int WM, int WN, bool A_ALONG, bool B_ALONG, class Epi>

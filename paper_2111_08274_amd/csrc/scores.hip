@@ -13,6 +13,7 @@ using namespace head;
 namespace {
 
 constexpr int kList = 512;         // candidates that a workgroup ranks at once
+constexpr int kPieces = 64;        // that a wave joins
 
 __device__ __forceinline__ float exp_of(float t) { return __builtin_amdgcn_exp2f(t * kLog2); }
 // orders as the logits do, zeros of either sign alike, a NaN above all but below what stands before the first place
@@ -40,6 +41,24 @@ template <int N> __device__ __forceinline__ unsigned long long most_over(unsigne
         v = w > v ? w : v;
     }
     return v;
+}
+
+// a chunk of fewer than eight values, or none
+__device__ __forceinline__ void load_or_out(Chunk<float>& v, const float* p, int left)
+{
+    v.a = v.b = tiles::u4{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u};
+    left = here(left);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < left) { if (e < 4) v.a[e] = ((const unsigned*)p)[e]; else v.b[e - 4] = ((const unsigned*)p)[e]; }
+}
+__device__ __forceinline__ void load_or_out(Chunk<__bf16>& v, const __bf16* p, int left)
+{
+    v.a = tiles::u4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u};
+    left = here(left);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < left) v.a[e / 2] = e % 2 ? (v.a[e / 2] & 0xffffu) | (unsigned)((const unsigned short*)p)[e] << 16 : (v.a[e / 2] & 0xffff0000u) | ((const unsigned short*)p)[e];
 }
 
 struct Sums { float top, s, e; };  // m, S, E; m = -inf: nothing yet, S = 0 or NaN
@@ -103,24 +122,23 @@ __global__ __launch_bounds__(NT) void scores_kernel(const T* logits, long long r
     const int piece = (int)(at - line * pieces), k = (int)(line / rows), t = (int)(line - (long long)k * rows);
     const int tid = threadIdx.x, wave = tid / 64, begin = piece * size, n = min(size, o.classes - begin);
     const T* z = logits + k * rep + t * row;
-    Chunk<T> v[U];
+    Chunk<T> v[U];                                             // what lies outside counts as -inf
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int c = (u * NT + tid) * 8;
-        v[u].load(z + begin + (c < n ? c : 0), c < n ? n - c : 0);
+        if (c + 8 <= n) v[u].load(z + begin + c, 8);
+        else load_or_out(v[u], z + begin + c, n - c);
     }
-    // f(value, index in the piece) for what this thread holds
-    auto each = [&](auto&& f) {
+    float most[U], mine = -INFINITY;                           // NaNs show in the sum
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float x[8];
-            v[u].get(x);
-            const int c = (u * NT + tid) * 8, left = here(n - c);
-            each8([&](int e) { if (e < left) f(x[e], c + e); });
-        }
-    };
-    float mine = -INFINITY;
-    each([&](float x, int) { mine = __builtin_fmaxf(mine, x); });         // NaNs show in the sum
+    for (int u = 0; u < U; ++u) {
+        float x[8];
+        v[u].get(x);
+        most[u] = x[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) most[u] = __builtin_fmaxf(most[u], x[e]);
+        mine = __builtin_fmaxf(mine, most[u]);
+    }
     const float top_wave = max_over<64>(mine);
     if (tid == 0) count = 0;
     if (o.n_top) {
@@ -140,11 +158,17 @@ __global__ __launch_bounds__(NT) void scores_kernel(const T* logits, long long r
     for (int w = 1; w < W; ++w) top = __builtin_fmaxf(top, tops[w]);
     const float base = top == -INFINITY ? 0.f : top;
     float s = 0.f, e = 0.f;
-    each([&](float x, int) {
-        const float d = x - base, p = exp_of(d);
-        s += p;
-        e += __builtin_fmaxf(d, -1e30f) * p;                              // -inf has no weight
-    });
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float x[8];
+        v[u].get(x);
+        each8([&](int i) {
+            const float d = x[i] - base, p = exp_of(d);
+            s += p;
+            e = __builtin_fmaf(__builtin_fmaxf(d, -1e30f), p, e);         // -inf has no weight
+        });
+    }
+    const bool nans = s != s;
     s = sum_over<64>(s);
     e = sum_over<64>(e);
     if ((tid & 63) == 0) { sums[wave] = s; weighted[wave] = e; }
@@ -152,11 +176,24 @@ __global__ __launch_bounds__(NT) void scores_kernel(const T* logits, long long r
         float limit = limits[0];
 #pragma unroll
         for (int w = 1; w < W; ++w) limit = __builtin_fmaxf(limit, limits[w]);
-        each([&](float x, int i) {
-            if (x < limit) return;                                        // a NaN stays
-            const int q = atomicAdd(&count, 1);
-            if (q < kList) list[q] = place(key_of(x), begin + i);
-        });
+        // few chunks hold any: which of their values is noted in bits, the values themselves are read again
+        unsigned bits[(U + 3) / 4] = {};
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (most[u] < limit && !nans) continue;
+            float x[8];
+            v[u].get(x);
+            each8([&](int i) { bits[u / 4] |= x[i] < limit ? 0u : 1u << (8 * (u % 4) + i); });
+        }
+#pragma unroll
+        for (int w = 0; w < (U + 3) / 4; ++w)
+            while (bits[w]) {
+                const int bit = __builtin_ctz(bits[w]), i = ((4 * w + bit / 8) * NT + tid) * 8 + bit % 8;
+                bits[w] &= bits[w] - 1;
+                if (i >= n) continue;
+                const int q = atomicAdd(&count, 1);
+                if (q < kList) list[q] = place(key_of(up(z[begin + i])), begin + i);
+            }
     }
     __syncthreads();
     Sums all{top, sums[0], weighted[0]};
@@ -184,7 +221,11 @@ __global__ __launch_bounds__(NT) void scores_kernel(const T* logits, long long r
     unsigned long long last = ~0ull;
     for (int i = 0; i < o.n_top; ++i) {
         unsigned long long p = 0;
-        each([&](float x, int j) { const unsigned long long q = place(key_of(x), begin + j); p = q < last && q > p ? q : p; });
+#pragma unroll 4
+        for (int j = tid; j < n; j += NT) {
+            const unsigned long long q = place(key_of(up(z[begin + j])), begin + j);
+            p = q < last && q > p ? q : p;
+        }
         p = most_over<64>(p);
         if ((tid & 63) == 0) firsts[wave] = p;
         __syncthreads();
@@ -197,7 +238,7 @@ __global__ __launch_bounds__(NT) void scores_kernel(const T* logits, long long r
     }
 }
 
-// Rows of several pieces (at most 64): a wave a row.
+// Rows of several pieces: a wave a row, a lane a piece.
 template <typename T>
 __global__ __launch_bounds__(256) void join_scores_kernel(const T* logits, long long rep, long long row, int rows, int pieces, long long lines, Out o,
                                                           const Sums* part, const unsigned long long* best)
@@ -280,13 +321,17 @@ __global__ __launch_bounds__(256) void scores_grad_kernel(const T* logits, long 
     out[mine] = (T)sum;
 }
 
-// Threads, chunks a thread and pieces of a row.
+// Threads, chunks a thread and pieces of a row.  256 threads: workgroups at different stages share a compute unit, so loads and exponentials overlap
+// (8192 rows of 65536 bf16, five alternatives: 228 us = 4.7 TB/s, what a copy reaches, with 512 threads 287, with 1024 329).  Few logits: one
+// launch is less than a second one's 3 us, 1024 threads for rows that they hold whole, and where rows would have
+// more pieces than a wave has lanes (256 / 1024 threads: 1 x 32000 19.0 / 15.6, 1024 x 32000 27.1 /
+// 26.0, 512 x 60000 26.8 / 26.1, 1024 x 60000 38.7 / 45.7; fp32 1024 x 32000 31.8 / 31.0).
 struct Plan { int nt, u, pieces, size; };
-Plan plan_of(int classes, int bf16)
+Plan plan_of(long long lines, int classes, int bf16)
 {
     const int most = bf16 ? 8 : 4;                             // chunks a thread holds in 32 registers
     Plan p{};
-    p.nt = classes <= 256 * 8 * most ? 256 : 1024;
+    p.nt = (classes > 2048 * most && classes <= 8192 * most && (double)lines * classes <= 33e6) || classes > kPieces * 2048 * most ? 1024 : 256;
     p.pieces = (classes + p.nt * 8 * most - 1) / (p.nt * 8 * most);
     p.size = ((classes + p.pieces - 1) / p.pieces + 7) / 8 * 8;
     p.pieces = (classes + p.size - 1) / p.size;
@@ -301,7 +346,7 @@ template <typename T> hipError_t forward(const ScoreArgs& a, hipStream_t s)
     constexpr int M = sizeof(T) == 2 ? 8 : 4;
     const long long lines = (long long)a.n * a.rows;
     if (lines == 0) return hipSuccess;
-    const Plan p = plan_of(a.classes, a.bf16);
+    const Plan p = plan_of(lines, a.classes, a.bf16);
     Sums* part = (Sums*)a.work;
     unsigned long long* best = (unsigned long long*)((char*)a.work + part_bytes(p, lines));
     const Out o{a.tokens, a.logp, a.entropy, a.stats, a.top_logp, a.top, a.n_tokens, a.n_top, a.classes};
@@ -330,8 +375,8 @@ template <typename T> hipError_t backward(const ScoreArgs& a, hipStream_t s)
 
 size_t score_work_bytes(int n, int rows, int classes, int n_top, int bf16)
 {
-    const Plan p = plan_of(classes, bf16);
     const long long lines = (long long)n * rows;
+    const Plan p = plan_of(lines, classes, bf16);
     return p.pieces > 1 ? part_bytes(p, lines) + align256((size_t)lines * p.pieces * n_top * 8) : 0;
 }
 hipError_t launch_scores_forward(const ScoreArgs& a, hipStream_t s) { return a.bf16 ? forward<__bf16>(a, s) : forward<float>(a, s); }

@@ -274,7 +274,7 @@ def test_layer_gradient_against_differences():
 
 # ---- scores ----------------------------------------------------------------------------------------------------------
 SCORES = [(1, 1, 1), (2, 3, 7), (1, 2, 40), (2, 5, 300), (1, 3, 1000), (2, 3, 2050), (1, 3, 4104), (1, 2, 8193), (1, 3, 16390), (2, 1, 32001), (1, 2, 40001), (1, 2, 65536), (1, 2, 65537),
-          (1, 1, 131073), (1, 2, 300000), (40, 9, 130)]
+          (1, 1, 131073), (1, 2, 300000), (1, 1, 530001), (1, 1, 1 << 20), (40, 9, 130)]
 
 
 def _scores_case(n, rows, v, bf16, layout, tokens=3, seed=0):
@@ -327,6 +327,29 @@ def test_scores_and_their_gradient(n, rows, v, bf16, layout):
     for n_top in sorted({0, min(v, 5), min(v, 32)}):
         _check_scores(z, y, yh, n_top, bf16)
     _check_scores(z, y, yh, 0, bf16, in_place=True)
+
+
+@pytest.mark.parametrize("v", [20011, 33001, 60000])
+@pytest.mark.parametrize("bf16", [0, 1])
+def test_scores_of_many_rows(v, bf16):
+    # more logits than one launch takes whole rows of: two rows over and over, the first and the last of each against 64 bits
+    torch = _torch()
+    n, rows = 2, 1100
+    z, y, yh = _scores_case(n, 1, v, bf16, "odd")
+    plan = hadfl.TokenScores(n, rows, v, n_tokens=3, n_top=5, bf16=bf16)
+    y, yh = y.repeat(1, rows, 1), yh.repeat(rows, 1)
+    out = plan.forward(z.expand(n, rows, v), y)
+    _check_scores(z.expand(n, 2, v), y[:, :2].contiguous(), yh[:, :2], 5, bf16)
+    g, dh = torch.randn((n, 1, 3), device="cuda"), torch.randn((n, 1), device="cuda")
+    dz = plan.backward(z.expand(n, rows, v), y, g.repeat(1, rows, 1), dh.repeat(1, rows))
+    for t in out + (dz,):
+        assert bool((t == t[:, :1]).all())
+    r = [ref.scores(_values(z[k]), yh[k, :1].astype(np.int64), 5) for k in range(n)]
+    for k in range(n):
+        b = ref.scores_bounds(r[k], _values(g[k]), _values(dh[k]), bf16)
+        assert np.array_equal(out[2][k, 0].cpu().numpy(), r[k]["top"][0])
+        _check(_values(out[1][k, -1:]), r[k]["entropy"], b["entropy"], "entropy")
+        _check(_values(dz[k, -1:]), ref.scores_grad(r[k], _values(g[k]), _values(dh[k])), b["dz"], "dlogits")
 
 
 @pytest.mark.parametrize("v", [5, 32, 200, 3000, 20000, 70001, 140001])
@@ -486,7 +509,7 @@ def test_a_block_and_its_answers_against_64_bits(rows):
     want = (logp, entropy, None, lp.topk(3, -1).values, p["x"].grad, p["w1"].grad, p["b1"].grad, p["w2"].grad, p["w3"].grad)
     for i, (q, w) in enumerate(zip(got, want)):
         if w is not None:
-            assert float((q.double() - w).abs().max()) <= 1e-4 * float(w.abs().max()), i
+            assert float((q.double() - w.detach()).abs().max()) <= 1e-4 * float(w.abs().max()), i
     assert torch.equal(got[2].long(), lp.topk(3, -1).indices)
 
 
