@@ -280,7 +280,7 @@ Shape best_shape(int n, int M, int N, int K, int bf16, bool across, bool planes,
     for (const Choice& o : kChoices) {
         if ((o.planes ? !planes : !registers) || (o.bm == 32 && (M > 32 || across))) continue;
         const long long tiles = (long long)n * ((M + o.bm - 1) / o.bm) * ((N + o.bn - 1) / o.bn);
-        const int unit = o.planes ? kSlab : 128;
+        const int unit = bf16 && o.bm == 32 ? 128 : 64;                       // whole slabs of every kernel of these tiles
         const double alone = bf16 ? o.bf16.alone : o.f32.alone, shared = bf16 ? o.bf16.shared : o.f32.shared;
         for (int s = 1; s <= 64 && (s == 1 || K / s >= unit); ++s) {
             const Shape p = cut(Shape{o.planes, o.bm, o.bn, 1, 0}, K, s, unit);
@@ -343,7 +343,7 @@ template <typename T, int BM, int BN, int WM, int WN, bool AA, bool BA, class SA
 hipError_t launch_registers(const SA& a, const SB& b, int n, int M, int N, int K, const Shape& p, const Epi& epi, hipStream_t s)
 {
     constexpr bool wide = SA::kPlanes == 3 || SB::kPlanes == 3;
-    constexpr int KS = BM == 32 ? (wide ? (BA ? 64 : 32) : 128) : BN == 128 && !wide ? 64 : 32, NBUF = wide || BM == 32 ? 1 : 2, AHEAD = BM == 32 ? 2 : 1;
+    constexpr int KS = BM == 32 ? (wide ? (BA ? 64 : 32) : 128) : BN == 128 && !wide ? 64 : 32, NBUF = wide || BM == 32 ? 1 : 2, AHEAD = wide && BM != 32 ? 1 : 2;
     constexpr unsigned kLds = NBUF * (SA::kPlanes * Image<AA, BM, KS>::kPlane + SB::kPlanes * Image<BA, BN, KS>::kPlane);
     if constexpr (Epi::kStaged) static_assert(WM * WN * Epi::template bytes<BN / WN / 32>() <= kLds, "the epilogue's blocks lie in the images");
     const int tm = (M + BM - 1) / BM, tn = (N + BN - 1) / BN;
@@ -491,14 +491,21 @@ __global__ __launch_bounds__(256) void slope_kernel(const T* dy, long long yrep,
         if (col < ld) sums[((long long)k * gridDim.y + blockIdx.y) * ld + col] = v;
     }
 }
-// db: the blocks' sums in ascending order
+// db from the blocks' sums: 32 columns a workgroup, eight threads a column, each every eighth block, then the eight in order
 __global__ __launch_bounds__(256) void column_sums_kernel(const float* sums, int blocks, int ld, int cols, float* db, long long rep)
 {
-    const int c = blockIdx.x * 256 + threadIdx.x, k = blockIdx.y;
-    if (c >= cols) return;
+    __shared__ float part[8][32];
+    const int c = blockIdx.x * 32 + threadIdx.x % 32, group = threadIdx.x / 32, k = blockIdx.y;
     float v = 0.f;
+    if (c < cols) {
 #pragma unroll 8
-    for (int b = 0; b < blocks; ++b) v += sums[((long long)k * blocks + b) * ld + c];
+        for (int b = group; b < blocks; b += 8) v += sums[((long long)k * blocks + b) * ld + c];
+    }
+    part[group][threadIdx.x % 32] = v;
+    __syncthreads();
+    if (group || c >= cols) return;
+#pragma unroll
+    for (int g = 1; g < 8; ++g) v += part[g][threadIdx.x % 32];
     db[k * rep + c] = v;
 }
 
@@ -519,7 +526,7 @@ template <typename T> hipError_t backward(const LayerArgs& a, hipStream_t s)
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (a.db.p) {
-        column_sums_kernel<<<dim3((unsigned)((a.out + 255) / 256), (unsigned)a.n), 256, 0, s>>>(sums, a.rows ? p.blocks : 0, p.ldz, a.out, (float*)a.db.p, a.db.rep);
+        column_sums_kernel<<<dim3((unsigned)((a.out + 31) / 32), (unsigned)a.n), 256, 0, s>>>(sums, a.rows ? p.blocks : 0, p.ldz, a.out, (float*)a.db.p, a.db.rep);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     const Rows z = there ? a.dy : Rows{work + p.dz, (long long)a.rows * p.ldz, p.ldz};

@@ -15,7 +15,7 @@
 // being multiplied as LDS holds (256 x 256 tiles: one, 128 x 256: two, 128 x 128: three), one barrier a slab.  The LDS image is the slab itself with its 16-byte chunks exchanged within a row, so
 // that the operand reads meet every bank once (a load that writes LDS puts the chunks of a wave one after the other: the exchange is in
 // the addresses it reads from):
-//   along   the contraction runs along the source's rows: [rows][64 k], chunk c of row r at c ^ (r & 7)
+//   along   the contraction runs along the source's rows: [rows][64 k], chunk c of row r at c ^ (r / 2 & 7): two rows are the 64 banks' width
 //   across  it runs across them: [64 k][columns], chunk c of row k at c ^ 4 (k & 3); the operand read transposes
 // 256 x 256 tiles of eight waves hold 128 x 64 each: 1.5 KiB of LDS reads a matrix instruction of 32 cycles a wave.
 #pragma once
@@ -86,7 +86,7 @@ template <bool ALONG, int BR, int NT> struct Loader {
     __device__ __forceinline__ void init(int tid, int ld)
     {
         const int r = tid / kAcross, c = tid % kAcross;
-        const int from = ALONG ? c ^ (r & 7) : c ^ ((r & 3) << 2);           // kStep is a multiple of 8: the same for all its rows
+        const int from = ALONG ? c ^ (r >> 1 & 7) : c ^ ((r & 3) << 2);      // kStep is a multiple of 16 (4 across): the same for all its rows
         off = (unsigned)(r * ld + from * 8) * 2;
         step = (unsigned)(kStep * ld) * 2;
         kc = from * 8;
@@ -94,7 +94,7 @@ template <bool ALONG, int BR, int NT> struct Loader {
     // r0: the tile's first row (along) or column (across)
     __device__ __forceinline__ void issue(const Plane3& s, const __bf16* base, int r0, int k0, int wave, char* image) const
     {
-        static_assert(kStep % 8 == 0 && kLoads >= 1, "");
+        static_assert(kStep % (ALONG ? 16 : 4) == 0 && kLoads >= 1, "");
         const long long first = ALONG ? (long long)r0 * s.ld : (long long)k0 * s.ld + r0;
         const long long rest = ALONG ? (long long)(s.lines - r0 - 1) * s.ld + s.cols : (long long)(s.lines - k0 - 1) * s.ld + s.cols - r0;
         const Buffer b = buffer(same(base + first), __builtin_amdgcn_readfirstlane((unsigned)min(rest * 2, 0xffffffe0ll)));
@@ -112,7 +112,7 @@ template <bool ALONG, int BR, int NT> struct Loader {
     {
         if (ALONG) {
             const int r = r0 + (lane & 31);
-            return *(const bf16x8*)(image + r * 128 + (((ks * 2 + (lane >> 5)) ^ (lane & 7)) * 16));
+            return *(const bf16x8*)(image + r * 128 + (((ks * 2 + (lane >> 5)) ^ (lane >> 1 & 7)) * 16));
         }
         const int k = ks * 16 + (lane >> 5) * 8 + ((lane & 15) >> 2), c = r0 + ((lane >> 4) & 1) * 16 + 4 * (lane & 3);
         return lds_read_tr8(image, (unsigned)(k * BR * 2 + ((c >> 3) ^ ((k & 3) << 2)) * 16 + (c & 7) * 2), BR * 2);

@@ -651,6 +651,8 @@ class _Drawing(_Operator):
     tensor of one int64 whose value is added to call when the kernels run (one that a captured graph counts up, say)."""
 
     def _draw(self, seed, call, counter):
+        if not self.drops:
+            return None
         at = None
         if counter is not None:
             if counter.dtype != self.torch.int64 or counter.device != self.device or counter.numel() != 1:
@@ -668,7 +670,7 @@ class Dropout(_Drawing):
     def __init__(self, n_replicas, n_rows, n_features, p, bf16=0):
         n, rows, features, bf16 = _int32(n_replicas, n_rows, n_features, bf16)
         super().__init__(HadflDropout(n, rows, features, bf16, float(p)), bf16)
-        self.shape = (n, rows, features)
+        self.shape, self.drops = (n, rows, features), float(p) != 0
 
     def _run(self, x, residual, y, draw, stream, names=("x", "y")):
         y = self._out(y, self.shape, self.dtype, stream)
@@ -695,7 +697,7 @@ class DenseLayer(_Drawing):
         self.n, self.rows, self.n_in, self.n_out, bf16 = _int32(n_replicas, n_rows, n_in, n_out, bf16)
         if activation not in ACTIVATIONS:
             raise HadflError(EINVAL, "activation must be one of %s" % (ACTIVATIONS,))
-        self.with_grad, query = bool(grad), lib().hadfl_layer_workspace
+        self.with_grad, self.drops, query = bool(grad), float(drop) != 0, lib().hadfl_layer_workspace
         super().__init__(HadflLayer(self.n, self.rows, self.n_in, self.n_out, bf16, ACTIVATIONS.index(activation), float(drop)), bf16,
                          lambda ref, out: query(ref, int(self.with_grad), out))
 
