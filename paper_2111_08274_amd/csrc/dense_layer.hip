@@ -3,7 +3,7 @@
 //              gradient where that is asked for
 //   gradient   dz = D'(dy) a'(pre) and its column sums db in one pass over dy, then dx = dz W^T and dW = x^T dz
 // bf16: dz is rounded to bf16 for the two products (2^-9 of a value, as the outputs themselves are rounded; a second part would double both
-// products); db is summed before that.  fp32: operands enter as three bf16 parts, six products (tile_product.h).
+// products); db is summed before that.  fp32: operands enter as three bf16 parts, six products.
 #include "direct_product.h"
 #include "layer.h"
 
@@ -131,16 +131,20 @@ __global__ __launch_bounds__(WM * WN * 64) void layer_product_kernel(SA a, SB b,
 {
     product_tile<SA, A_ALONG, SB, B_ALONG, BM, BN, WM, WN, KS, NBUF, AHEAD>(a, b, K, tiles_m, tiles_n, splits, split_len, total, epi);
 }
-// Operands in planes of bf16, straight from memory to LDS (direct_product.h: Loader), slabs of 64 k.  A wave reads the operands of a step of 16 k while it
-// multiplies the step before, across slabs too: the barrier that frees a slab's image and says that the next one has arrived lies before the slab's
-// last step, whose operands are in registers by then, so that the matrix cores have work while the first operands of the next slab are read.
-template <bool A_ALONG, bool B_ALONG, int BM, int BN, int WM, int WN, class Epi>
+// the planes of A and B whose products are kept of three bf16 parts each, the small ones first: what is left out is below 2^-24 of the product
+constexpr int kPairA[6] = {2, 1, 0, 1, 0, 0}, kPairB[6] = {0, 1, 2, 0, 1, 0};
+
+// Operands in planes of bf16, straight from memory to LDS (direct_product.h: Loader): one plane in slabs of 64 k, or the three parts of 32-bit values in
+// slabs of 32, all planes of a slab together.  A wave reads the operands of a step of 16 k while it multiplies the step before, across slabs too: the
+// barrier that frees a slab's image and says that the next one has arrived lies before the slab's last step, whose operands are in registers by then, so
+// that the matrix cores have work while the first operands of the next slab are read.
+template <bool A_ALONG, bool B_ALONG, int PL, int BM, int BN, int WM, int WN, class Epi>
 __global__ __launch_bounds__(WM * WN * 64) void layer_planes_kernel(Plane3 a, Plane3 b, int K, int tiles_m, int tiles_n, int splits, int split_len, int total, Epi epi)
 {
-    constexpr int NT = WM * WN * 64, TM = BM / WM / 32, TN = BN / WN / 32, kSteps = kSlab / 16;
-    typedef Loader<A_ALONG, BM, NT> LA;
-    typedef Loader<B_ALONG, BN, NT> LB;
-    constexpr int kImage = LA::kBytes + LB::kBytes, IMAGES = kImage > 49152 ? 2 : kImage > 32768 ? 3 : 4, kLoads = LA::kLoads + LB::kLoads;
+    constexpr int NT = WM * WN * 64, TM = BM / WM / 32, TN = BN / WN / 32, KS = PL == 1 ? kSlab : kSlab / 2, kSteps = KS / 16;
+    typedef Loader<A_ALONG, BM, NT, KS> LA;
+    typedef Loader<B_ALONG, BN, NT, KS> LB;
+    constexpr int kImage = PL * (LA::kBytes + LB::kBytes), IMAGES = kImage > 49152 ? 2 : PL == 3 || kImage > 32768 ? 3 : 4, kLoads = PL * (LA::kLoads + LB::kLoads);
     __shared__ __attribute__((aligned(16))) char images[IMAGES * kImage];
     if constexpr (Epi::kStaged) static_assert(WM * WN * Epi::template bytes<TN>() <= IMAGES * kImage, "the epilogue's blocks lie in the images");
 
@@ -159,7 +163,7 @@ __global__ __launch_bounds__(WM * WN * 64) void layer_planes_kernel(Plane3 a, Pl
     t.m0 = bm + wm;
     t.n0 = bn + wn;
     const __bf16 *pa = a.p + t.rep * a.rep, *pb = b.p + t.rep * b.rep;
-    const int k_begin = t.split * split_len, k_end = min(K, k_begin + split_len), slabs = k_begin < k_end ? (k_end - k_begin + kSlab - 1) / kSlab : 0;
+    const int k_begin = t.split * split_len, k_end = min(K, k_begin + split_len), slabs = k_begin < k_end ? (k_end - k_begin + KS - 1) / KS : 0;
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -170,23 +174,32 @@ __global__ __launch_bounds__(WM * WN * 64) void layer_planes_kernel(Plane3 a, Pl
     lb.init(tid, b.ld);
 
     auto issue = [&](int slab, char* image) {
-        la.issue(a, pa, bm, k_begin + slab * kSlab, wave, image);
-        lb.issue(b, pb, bn, k_begin + slab * kSlab, wave, image + LA::kBytes);
+#pragma unroll
+        for (int s = 0; s < PL; ++s) la.issue(a, pa + s * a.plane, bm, k_begin + slab * KS, wave, image + s * LA::kBytes);
+#pragma unroll
+        for (int s = 0; s < PL; ++s) lb.issue(b, pb + s * b.plane, bn, k_begin + slab * KS, wave, image + PL * LA::kBytes + s * LB::kBytes);
     };
-    bf16x8 fa[2][TM], fb[2][TN];
+    bf16x8 fa[2][PL][TM], fb[2][PL][TN];
     auto read = [&](const char* image, int step, int to) {
 #pragma unroll
-        for (int i = 0; i < TM; ++i) fa[to][i] = LA::read(image, wm + 32 * i, step, t.lane);
+        for (int s = 0; s < PL; ++s) {
 #pragma unroll
-        for (int j = 0; j < TN; ++j) fb[to][j] = LB::read(image + LA::kBytes, wn + 32 * j, step, t.lane);
+            for (int i = 0; i < TM; ++i) fa[to][s][i] = LA::read(image + s * LA::kBytes, wm + 32 * i, step, t.lane);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) fb[to][s][j] = LB::read(image + PL * LA::kBytes + s * LB::kBytes, wn + 32 * j, step, t.lane);
+        }
     };
     auto multiply = [&](int from) {
 #pragma unroll
-        for (int i = 0; i < TM; ++i)
+        for (int pair = PL == 1 ? 5 : 0; pair < 6; ++pair)
 #pragma unroll
-            for (int j = 0; j < TN; ++j)
-                t.acc[i][j] = Epi::kLaneM ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[from][j], fa[from][i], t.acc[i][j], 0, 0, 0)
-                                          : __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[from][i], fb[from][j], t.acc[i][j], 0, 0, 0);
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    const bf16x8 &x = fa[from][kPairA[pair]][i], &y = fb[from][kPairB[pair]][j];
+                    t.acc[i][j] = Epi::kLaneM ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, x, t.acc[i][j], 0, 0, 0)
+                                              : __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, t.acc[i][j], 0, 0, 0);
+                }
     };
     // Slab i + 1 is there when at most the loads of the IMAGES - 2 slabs after it are outstanding (they finish in order).
     auto turn = [&](int i, char* image, char* next) {
@@ -263,32 +276,30 @@ Shape cut(Shape p, int K, int splits, int unit)
 struct Choice {
     bool planes;
     int bm, bn, most;
-    struct { double alone, shared; } f32, bf16;
+    struct { double alone, shared; } f32, bf16;                // zero: not there
     double tile;
 };
-constexpr Choice kChoices[] = {{false, 32, 128, 3, {23, 15}, {6.3, 5}, 3}, {false, 64, 64, 4, {25, 15.5}, {8.8, 4.9}, 3}, {false, 64, 128, 2, {28, 27}, {7.5, 7.3}, 3},
-                               {false, 128, 128, 2, {46, 46}, {10, 11}, 4}, {true, 128, 128, 1, {0, 0}, {7, 9.6}, 4}, {true, 128, 256, 1, {0, 0}, {11.5, 16}, 5},
+constexpr Choice kChoices[] = {{false, 32, 128, 3, {23, 15}, {6.3, 5}, 3}, {false, 64, 64, 4, {25, 15.5}, {8.8, 4.9}, 3}, {false, 64, 128, 2, {33, 28}, {7.5, 7.3}, 3},
+                               {false, 128, 128, 2, {44, 46}, {10, 11}, 4}, {true, 128, 128, 1, {0, 0}, {6, 9.6}, 4}, {true, 128, 256, 1, {73, 73}, {11.5, 16}, 5},
                                {true, 256, 256, 1, {0, 0}, {21, 28}, 8}};
-// The cheapest tiles and shares by that; `lay`: seconds to copy operands into planes first.  A share is written and read at 5 TB/s, and joining them is one more launch, 4 us.  Chosen / best of all, us:
-//   bf16  y of 16 x 1024 x 512 x 2048 47.9 / 47.7, 4096 x 1024 x 4096 38.8 / 38.8 (128 x 128 tiles 51), 8192 x 4096 x 4096 232 / 232 (315); dx of the
-//         first 39.9 / 39.7 (256 x 256 tiles 55), dW 38.5 / 38.5
-//   fp32  the same 205 / 201, 194 / 194, 1490 / 1487, 194 / 192, 191 / 191; 64 x 64 tiles take 250, 252 and 1964 of the first three
-Shape best_shape(int n, int M, int N, int K, int bf16, bool across, bool planes, bool registers, double lay)
+struct Chosen { Shape shape; double cost; };
+// The cheapest tiles and shares by that, with operands in planes or through registers.  A share is written and read at 5 TB/s, and joining them is one
+// more launch, 4 us.
+Chosen best_shape(int n, int M, int N, int K, int bf16, bool across, bool planes)
 {
-    Shape best{};
-    double least = -1;
+    Chosen best{{}, -1};
     for (const Choice& o : kChoices) {
-        if ((o.planes ? !planes : !registers) || (o.bm == 32 && (M > 32 || across))) continue;
+        const double alone = bf16 ? o.bf16.alone : o.f32.alone, shared = bf16 ? o.bf16.shared : o.f32.shared;
+        if (o.planes != planes || alone == 0 || (o.bm == 32 && (M > 32 || across))) continue;
         const long long tiles = (long long)n * ((M + o.bm - 1) / o.bm) * ((N + o.bn - 1) / o.bn);
         const int unit = bf16 && o.bm == 32 ? 128 : 64;                       // whole slabs of every kernel of these tiles
-        const double alone = bf16 ? o.bf16.alone : o.f32.alone, shared = bf16 ? o.bf16.shared : o.f32.shared;
         for (int s = 1; s <= 64 && (s == 1 || K / s >= unit); ++s) {
             const Shape p = cut(Shape{o.planes, o.bm, o.bn, 1, 0}, K, s, unit);
             if (p.splits != s) continue;
             const double each = (double)((tiles * s + 255) / 256);            // tiles of a compute unit
             const double k = each <= o.most ? std::max(alone, each * shared) : each * shared;
-            const double cost = std::min(K, p.len) * k * 1e-9 + (each <= o.most ? 1 : each / o.most) * o.tile * 1e-6 + (o.planes ? lay : 0) + (s > 1 ? 4e-6 + (double)s * n * M * N * 8 / 5e12 : 0);
-            if (least < 0 || cost < (s > 1 && best.splits == 1 ? 0.95 : 1) * least) { best = p; least = cost; }
+            const double cost = std::min(K, p.len) * k * 1e-9 + (each <= o.most ? 1 : each / o.most) * o.tile * 1e-6 + (s > 1 ? 4e-6 + (double)s * n * M * N * 8 / 5e12 : 0);
+            if (best.cost < 0 || cost < (s > 1 && best.shape.splits == 1 ? 0.95 : 1) * best.cost) best = Chosen{p, cost};
         }
     }
     return best;
@@ -297,11 +308,12 @@ Shape best_shape(int n, int M, int N, int K, int bf16, bool across, bool planes,
 struct Work {                      // where things lie in the working memory
     Shape y, dx, dw;
     int ldx, ldz;
-    size_t x, w, dz, sums, share, total;
+    size_t kept, x, w, dz, sums, share, total;
     int blocks, across, depth;     // column sums: row blocks, lanes a row, rows a block
 };
-// Sources through registers hold eight columns at least (tile_product.h): narrower tensors are copied into rows of eight.  bf16 operands of products of
-// planes are copied where they do not lie as planes do, which shows only at the call.
+// Planes of a 32-bit tensor are its three parts, 6 bytes a value, written once by one launch for x and w; a bf16 tensor is one as it lies, or copied where
+// rows of it do not start on 16 bytes or hold whole chunks of eight.  Through registers a tensor is read as it lies; sources there hold eight columns
+// at least (tile_product.h), so narrower layers take planes.
 Work plan_of(int n, int rows, int in, int out, int bf16, bool grad, bool packed)
 {
     Work p{};
@@ -310,22 +322,30 @@ Work plan_of(int n, int rows, int in, int out, int bf16, bool grad, bool packed)
     const bool narrow = std::min(in, out) < 8;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += align256(bytes); return o; };
-    // rows of a size that is no multiple of eight are copied, a launch and their bytes twice
-    auto lay = [&](int lines, int cols) { return cols % 8 ? 4e-6 + (double)n * lines * cols * 4 / 4e12 : 0.; };
-    auto shape = [&](int M, int N, int K, bool across, double copies) { return best_shape(n, M, N, K, bf16, across, bf16, !bf16 || !narrow, copies); };
-    const size_t size = bf16 ? 2 : 4, x = (size_t)n * rows * p.ldx * size, w = (size_t)n * in * p.ldz * size;
+    const double nx = (double)n * rows * p.ldx, nw = (double)n * in * p.ldz, nz = (double)n * rows * p.ldz;
+    const size_t plane = bf16 ? 2 : 6;
+    // of copying values into planes
+    auto lay = [&](int cols, double values) { return !bf16 || cols % 8 ? 2e-6 + values * (bf16 ? 4 : 10) / 4e12 : 0.; };
     if (!grad) {
-        p.y = shape(rows, out, in, false, lay(rows, in) + lay(in, out));
-        if (p.y.planes || in < 8) p.x = take(x);
-        if (p.y.planes || out < 8) p.w = take(w);
+        const Chosen r = best_shape(n, rows, out, in, bf16, false, false), q = best_shape(n, rows, out, in, bf16, false, true);
+        p.y = narrow || q.cost + lay(in, nx) + lay(out, nw) + (bf16 ? 0 : 2e-6) < r.cost ? q.shape : r.shape;
+        if (p.y.planes) { p.x = take((size_t)nx * plane); p.w = take((size_t)nw * plane); }
         p.share = take(share_bytes(p.y, n, rows, out));
     } else {
-        p.dx = shape(rows, in, out, false, lay(in, out));
-        p.dw = shape(in, out, rows, true, packed ? 0. : lay(rows, in));
-        if (packed) p.x = take((size_t)n * rows * p.ldx * 2);
-        else if (p.dw.planes || in < 8) p.x = take(x);
-        if (p.dx.planes || out < 8) p.w = take(w);
-        p.dz = take((size_t)n * rows * p.ldz * size);
+        const Chosen rx = best_shape(n, rows, in, out, bf16, false, false), rw = best_shape(n, in, out, rows, bf16, true, false);
+        const Chosen qx = best_shape(n, rows, in, out, bf16, false, true), qw = best_shape(n, in, out, rows, bf16, true, true);
+        if (bf16) {
+            p.dx = narrow || qx.cost + lay(out, nw) < rx.cost ? qx.shape : rx.shape;
+            p.dw = narrow || qw.cost + lay(packed ? 8 : in, nx) < rw.cost ? qw.shape : rw.shape;
+        } else {                                               // dz in one form for both products
+            const bool planes = narrow || qx.cost + qw.cost + lay(in, nx) + lay(out, nw) + nz * 2 / 4e12 < rx.cost + rw.cost;
+            p.dx = planes ? qx.shape : rx.shape;
+            p.dw = planes ? qw.shape : rw.shape;
+        }
+        if (packed) p.kept = take((size_t)nx * (bf16 ? 2 : 4));
+        if (p.dw.planes) p.x = take((size_t)nx * plane);
+        if (p.dx.planes) p.w = take((size_t)nw * plane);
+        p.dz = take((size_t)nz * (p.dx.planes || p.dw.planes ? plane : bf16 ? 2 : 4));
         p.across = 8;
         while (p.across < 64 && p.across * 8 < p.ldz) p.across *= 2;
         const long long wide = (p.ldz + p.across * 8 - 1) / (p.across * 8);
@@ -354,14 +374,14 @@ hipError_t launch_registers(const SA& a, const SB& b, int n, int M, int N, int K
         <<<line_grid(die_grid(total), WM * WN * 64), WM * WN * 64, 0, s>>>(a, b, K, tm, tn, p.splits, p.len, (int)total, epi);
     return hipGetLastError();
 }
-template <int BM, int BN, int WM, int WN, bool AA, bool BA, class Epi>
+template <int PL, int BM, int BN, int WM, int WN, bool AA, bool BA, class Epi>
 hipError_t launch_planes(const Plane3& a, const Plane3& b, int n, int M, int N, int K, const Shape& p, const Epi& epi, hipStream_t s)
 {
     const int tm = (M + BM - 1) / BM, tn = (N + BN - 1) / BN;
     const long long total = (long long)n * p.splits * tm * tn;
     if (total == 0) return hipSuccess;
     if (total > 0x7fffff00ll) return hipErrorInvalidValue;
-    layer_planes_kernel<AA, BA, BM, BN, WM, WN, Epi>
+    layer_planes_kernel<AA, BA, PL, BM, BN, WM, WN, Epi>
         <<<line_grid(die_grid(total), WM * WN * 64), WM * WN * 64, 0, s>>>(a, b, K, tm, tn, p.splits, p.len, (int)total, epi);
     return hipGetLastError();
 }
@@ -376,13 +396,15 @@ template <typename T, class F> hipError_t whole_or_shares(const Shape& p, int n,
     finish_shares_kernel<T><<<line_grid((total + 255) / 256, 256), 256, 0, s>>>(share, p.splits, lines * ld, ld, total, finish);
     return hipGetLastError();
 }
-template <bool AA, bool BA>
-hipError_t planes_product(const Plane3& a, const Plane3& b, int n, int M, int N, int K, const Shape& p, const Finish<__bf16>& finish, float* share, hipStream_t s)
+template <bool AA, bool BA, typename T>
+hipError_t planes_product(const Plane3& a, const Plane3& b, int n, int M, int N, int K, const Shape& p, const Finish<T>& finish, float* share, hipStream_t s)
 {
-    return whole_or_shares<__bf16>(p, n, M, N, finish, share, s, [&](const auto& epi) {
-        if (p.bm == 256) return launch_planes<256, 256, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
-        if (p.bn == 256) return launch_planes<128, 256, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
-        return launch_planes<128, 128, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
+    return whole_or_shares<T>(p, n, M, N, finish, share, s, [&](const auto& epi) {
+        if constexpr (sizeof(T) == 2) {
+            if (p.bm == 256) return launch_planes<1, 256, 256, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
+            if (p.bn == 256) return launch_planes<1, 128, 256, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
+            return launch_planes<1, 128, 128, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
+        } else return launch_planes<3, 128, 256, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
     });
 }
 template <bool AA, bool BA, typename T, class SA, class SB>
@@ -397,45 +419,53 @@ hipError_t registers_product(const SA& a, const SB& b, int n, int M, int N, int 
     });
 }
 
-// x [replicas][rows][cols] -> [replicas][rows][8], zero beyond cols
-template <typename T>
-__global__ __launch_bounds__(256) void widen_kernel(const T* x, long long rep, long long row, int rows, int cols, long long total, T* out)
+// A tensor [n][rows][cols] whose three parts go to out [3][n][rows][ld], zero beyond cols.
+struct Parts {
+    const float* x;
+    long long rep, row;
+    int rows, cols, ld;
+    long long total, plane;        // chunks of eight; values of a plane
+    __bf16* out;
+};
+Parts parts_of(const Rows& r, int n, int rows, int cols, void* out)
 {
-    const long long at = line_block() * 256 + threadIdx.x;
-    if (at >= total) return;
-    const int k = (int)(at / rows), t = (int)(at - (long long)k * rows);
-    Chunk<T> v;
-    float f[8];
-    v.load(x + k * rep + t * row, cols);
-    v.get(f);
-    store_chunk(out + at * 8, 8, f);
+    const int ld = up_to(cols, 8);
+    const long long plane = (long long)n * rows * ld;
+    return Parts{(const float*)r.p, r.rep, r.row, rows, cols, ld, plane / 8, plane, (__bf16*)out};
 }
-// A tensor [n][rows][cols] as a product takes it: as it lies, or copied to `at`.
-template <typename T> hipError_t ready(const Rows& r, int n, int rows, int cols, bool planes, void* at, Rows& out, int& width, hipStream_t s)
+__global__ __launch_bounds__(256) void parts_kernel(Parts first, Parts second)
 {
-    out = r;
-    width = cols;
-    if (planes ? is_plane(r, cols) : cols >= 8) return hipSuccess;
-    width = up_to(cols, 8);
-    out = Rows{at, (long long)rows * width, width};
-    const long long total = (long long)n * rows;
+    long long at = line_block() * 256 + threadIdx.x;
+    const bool other = at >= first.total;
+    const Parts a = other ? second : first;
+    if (other) at -= first.total;
+    if (at >= a.total) return;
+    const int chunks = a.ld / 8;
+    const long long line = at / chunks;
+    const int c = (int)(at - line * chunks) * 8, k = (int)(line / a.rows), t = (int)(line - (long long)k * a.rows);
+    Chunk<float> v;
+    u4 part[3];
+    v.load(a.x + k * a.rep + t * a.row + c, a.cols - c);
+    Source<float>::split(v, part);
+#pragma unroll
+    for (int s = 0; s < 3; ++s) *(u4*)(a.out + s * a.plane + at * 8) = part[s];
+}
+hipError_t lay_parts(const Parts& first, const Parts& second, hipStream_t s)
+{
+    const long long total = first.total + second.total;
     if (total == 0) return hipSuccess;
-    if constexpr (sizeof(T) == 2) return lay_out<__bf16, 1>(n, rows, cols, width, r, Labelled{nullptr, 0}, nullptr, (__bf16*)at, s);
-    else {
-        widen_kernel<T><<<line_grid((total + 255) / 256, 256), 256, 0, s>>>((const T*)r.p, r.rep, r.row, rows, cols, total, (T*)at);
-        return hipGetLastError();
-    }
+    parts_kernel<<<line_grid((total + 255) / 256, 256), 256, 0, s>>>(first, second);
+    return hipGetLastError();
 }
-Plane3 plane(const Rows& r, int rows, int cols) { return Plane3{(const __bf16*)r.p, r.rep, 0, (int)r.row, rows, cols, nullptr}; }
-
-// C = A B of operands that are ready
-template <bool AA, bool BA, typename T, typename TA>
-hipError_t product(const Rows& a, int a_rows, int a_cols, const Rows& b, int b_rows, int b_cols, int n, int M, int N, int K, const Shape& p, const Finish<T>& finish,
-                   float* share, hipStream_t s)
+Plane3 plane_of(const Parts& p) { return Plane3{p.out, (long long)p.rows * p.ld, p.plane, p.ld, p.rows, p.ld, nullptr}; }
+// a bf16 tensor as a plane: as it lies, or copied to `at`
+hipError_t plane_of(const Rows& r, int n, int rows, int cols, void* at, Plane3& out, hipStream_t s)
 {
-    if constexpr (sizeof(T) == 2)
-        if (p.planes) return planes_product<AA, BA>(plane(a, a_rows, a_cols), plane(b, b_rows, b_cols), n, M, N, K, p, finish, share, s);
-    return registers_product<AA, BA, T>(source<TA>(a, a_rows, a_cols), source<T>(b, b_rows, b_cols), n, M, N, K, p, finish, share, s);
+    out = Plane3{(const __bf16*)r.p, r.rep, 0, (int)r.row, rows, cols, nullptr};
+    if (is_plane(r, cols)) return hipSuccess;
+    const int ld = up_to(cols, 8);
+    out = Plane3{(const __bf16*)at, (long long)rows * ld, 0, ld, rows, ld, nullptr};
+    return lay_out<__bf16, 1>(n, rows, cols, ld, r, Labelled{nullptr, 0}, nullptr, (__bf16*)at, s);
 }
 
 template <typename T> hipError_t forward(const LayerArgs& a, hipStream_t s)
@@ -443,21 +473,28 @@ template <typename T> hipError_t forward(const LayerArgs& a, hipStream_t s)
     if (a.rows == 0) return hipSuccess;
     const Work p = plan_of(a.n, a.rows, a.in, a.out, a.bf16, false, false);
     char* work = (char*)a.work;
+    float* share = (float*)(work + p.share);
     const Finish<T> finish{(const float*)a.bias.p, a.bias.rep, a.residual, a.pre, a.y, a.rows, a.out, a.act, a.draws};
-    Rows x, w;
-    int wx, ww;
-    hipError_t e = ready<T>(a.x, a.n, a.rows, a.in, p.y.planes, work + p.x, x, wx, s);
-    if (e == hipSuccess) e = ready<T>(a.w, a.n, a.in, a.out, p.y.planes, work + p.w, w, ww, s);
-    if (e != hipSuccess) return e;
-    return product<true, false, T, T>(x, a.rows, wx, w, a.in, ww, a.n, a.rows, a.out, a.in, p.y, finish, (float*)(work + p.share), s);
+    if (!p.y.planes)
+        return registers_product<true, false, T>(source<T>(a.x, a.rows, a.in), source<T>(a.w, a.in, a.out), a.n, a.rows, a.out, a.in, p.y, finish, share, s);
+    Plane3 x, w;
+    hipError_t e;
+    if constexpr (sizeof(T) == 2) {
+        if ((e = plane_of(a.x, a.n, a.rows, a.in, work + p.x, x, s)) != hipSuccess || (e = plane_of(a.w, a.n, a.in, a.out, work + p.w, w, s)) != hipSuccess) return e;
+    } else {
+        const Parts px = parts_of(a.x, a.n, a.rows, a.in, work + p.x), pw = parts_of(a.w, a.n, a.in, a.out, work + p.w);
+        if ((e = lay_parts(px, pw, s)) != hipSuccess) return e;
+        x = plane_of(px); w = plane_of(pw);
+    }
+    return planes_product<true, false, T>(x, w, a.n, a.rows, a.out, a.in, p.y, finish, share, s);
 }
 
 // ---- gradient ---------------------------------------------------------------------------------------------------------------
-// dz = D'(dy) a'(pre), eight columns a lane, into [replicas][rows][ld] if STORE, and the column sums of a block's rows.  A dropped value is zero
-// whatever dy and pre hold there.
-template <typename T, bool STORE>
+// dz = D'(dy) a'(pre), eight columns a lane, into [replicas][rows][ld] (PARTS = 1), its three bf16 parts into such planes (3) or nowhere (0), and the
+// column sums of a block's rows.  A dropped value is zero whatever dy and pre hold there.
+template <typename T, int PARTS>
 __global__ __launch_bounds__(256) void slope_kernel(const T* dy, long long yrep, long long yrow, const T* pre, long long prep, long long prow, int rows, int cols,
-                                                    int ld, int across, int depth, int act, Draws d, T* dz, float* sums)
+                                                    int ld, int across, int depth, int act, Draws d, void* dz, long long plane, float* sums)
 {
     __shared__ float part[256][9];
     const int lane = threadIdx.x % across, line = threadIdx.x / across, lines = 256 / across;
@@ -479,7 +516,17 @@ __global__ __launch_bounds__(256) void slope_kernel(const T* dy, long long yrep,
             }
             if (d.limit) kept8(d, call, k, t, c, [&](int e, bool kept) { v[e] = kept ? v[e] * d.scale : 0.f; });
             each8([&](int e) { if (c + e >= cols) v[e] = 0.f; sum[e] += v[e]; });
-            if constexpr (STORE) store_chunk(dz + ((long long)k * rows + t) * ld + c, 8, v);
+            const long long to = ((long long)k * rows + t) * ld + c;
+            if constexpr (PARTS == 1) store_chunk((T*)dz + to, 8, v);
+            if constexpr (PARTS == 3) {
+                u2 h[2], m[2], l[2];
+                parts3(f4{v[0], v[1], v[2], v[3]}, h[0], m[0], l[0]);
+                parts3(f4{v[4], v[5], v[6], v[7]}, h[1], m[1], l[1]);
+                __bf16* out = (__bf16*)dz + to;
+                *(u4*)out = join8(h[0], h[1]);
+                *(u4*)(out + plane) = join8(m[0], m[1]);
+                *(u4*)(out + 2 * plane) = join8(l[0], l[1]);
+            }
         }
     if (!sums) return;
     each8([&](int e) { part[threadIdx.x][e] = sum[e]; });
@@ -511,44 +558,53 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const float* sums, int
 
 template <typename T> hipError_t backward(const LayerArgs& a, hipStream_t s)
 {
+    constexpr bool half = sizeof(T) == 2;
     const Work p = plan_of(a.n, a.rows, a.in, a.out, a.bf16, true, a.packed.q);
     char* work = (char*)a.work;
     float *share = (float*)(work + p.share), *sums = (float*)(work + p.sums);
     const bool want_dx = a.dx.p && a.rows, want_dw = a.dw.p, planes = (want_dx && p.dx.planes) || (want_dw && p.dw.planes);
     hipError_t e = hipSuccess;
     // dz is formed in the working memory; where it is dy itself it is read as it lies, if the products can
-    const bool there = a.act == kNone && !a.draws.limit && a.out >= 8 && (!planes || is_plane(a.dy, a.out)), form = (want_dx || want_dw) && !there;
+    const bool there = a.act == kNone && !a.draws.limit && (!planes || (half && is_plane(a.dy, a.out))), form = (want_dx || want_dw) && !there;
+    const long long plane = (long long)a.n * a.rows * p.ldz;
     if (a.rows && (form || a.db.p)) {
         const dim3 grid((unsigned)((p.ldz + p.across * 8 - 1) / (p.across * 8)), (unsigned)p.blocks, (unsigned)a.n);
-        auto* kernel = form ? slope_kernel<T, true> : slope_kernel<T, false>;
+        auto* kernel = !form ? slope_kernel<T, 0> : half || !planes ? slope_kernel<T, 1> : slope_kernel<T, half ? 1 : 3>;
         kernel<<<grid, 256, 0, s>>>((const T*)a.dy.p, a.dy.rep, a.dy.row, (const T*)a.pre.p, a.pre.rep, a.pre.row, a.rows, a.out, p.ldz, p.across, p.depth,
-                                    a.act, a.draws, (T*)(work + p.dz), a.db.p ? sums : nullptr);
+                                    a.act, a.draws, work + p.dz, plane, a.db.p ? sums : nullptr);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (a.db.p) {
         column_sums_kernel<<<dim3((unsigned)((a.out + 31) / 32), (unsigned)a.n), 256, 0, s>>>(sums, a.rows ? p.blocks : 0, p.ldz, a.out, (float*)a.db.p, a.db.rep);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
+    Rows x = a.x;
+    if (want_dw && a.packed.q) {                               // the checkpoint's values; columns beyond n_in belong to no row of dW
+        x = Rows{work + p.kept, (long long)a.rows * p.ldx, p.ldx};
+        if (a.rows && (e = launch_unpack(a.n, a.rows, a.in, half, a.packed.q, x, s)) != hipSuccess) return e;
+    }
     const Rows z = there ? a.dy : Rows{work + p.dz, (long long)a.rows * p.ldz, p.ldz};
     const int wz = there ? a.out : p.ldz;
+    const Plane3 pz{(const __bf16*)z.p, z.rep, half ? 0 : plane, (int)z.row, a.rows, wz, nullptr};
+    Plane3 px{}, pw{};
+    if constexpr (half) {
+        if (want_dw && p.dw.planes && (e = plane_of(x, a.n, a.rows, a.packed.q ? p.ldx : a.in, work + p.x, px, s)) != hipSuccess) return e;
+        if (want_dx && p.dx.planes && (e = plane_of(a.w, a.n, a.in, a.out, work + p.w, pw, s)) != hipSuccess) return e;
+    } else if (planes) {
+        const Parts none{}, fx = want_dw ? parts_of(x, a.n, a.rows, a.in, work + p.x) : none, fw = want_dx ? parts_of(a.w, a.n, a.in, a.out, work + p.w) : none;
+        if ((e = lay_parts(fx, fw, s)) != hipSuccess) return e;
+        px = plane_of(fx); pw = plane_of(fw);
+    }
     if (want_dx) {
-        Rows w;
-        int ww;
-        if ((e = ready<T>(a.w, a.n, a.in, a.out, p.dx.planes, work + p.w, w, ww, s)) != hipSuccess) return e;
-        e = product<true, true, T, T>(z, a.rows, wz, w, a.in, ww, a.n, a.rows, a.in, a.out, p.dx, store_only<T>(a.dx, a.rows, a.in), share, s);
+        const Finish<T> finish = store_only<T>(a.dx, a.rows, a.in);
+        e = p.dx.planes ? planes_product<true, true, T>(pz, pw, a.n, a.rows, a.in, a.out, p.dx, finish, share, s)
+                        : registers_product<true, true, T>(source<T>(z, a.rows, wz), source<T>(a.w, a.in, a.out), a.n, a.rows, a.in, a.out, p.dx, finish, share, s);
         if (e != hipSuccess) return e;
     }
     if (!want_dw) return hipSuccess;
-    const Finish<T> to_dw = store_only<T>(a.dw, a.in, a.out);
-    if (a.packed.q) {                                          // the checkpoint's values, exact in bf16; columns beyond n_in belong to no row of dW
-        const Rows kept{work + p.x, (long long)a.rows * p.ldx, p.ldx};
-        if (a.rows && (e = launch_unpack(a.n, a.rows, a.in, 1, a.packed.q, kept, s)) != hipSuccess) return e;
-        return product<false, false, T, __bf16>(kept, a.rows, p.ldx, z, a.rows, wz, a.n, a.in, a.out, a.rows, p.dw, to_dw, share, s);
-    }
-    Rows x;
-    int wx;
-    if ((e = ready<T>(a.x, a.n, a.rows, a.in, p.dw.planes, work + p.x, x, wx, s)) != hipSuccess) return e;
-    return product<false, false, T, T>(x, a.rows, wx, z, a.rows, wz, a.n, a.in, a.out, a.rows, p.dw, to_dw, share, s);
+    const Finish<T> finish = store_only<T>(a.dw, a.in, a.out);
+    if (p.dw.planes) return planes_product<false, false, T>(px, pz, a.n, a.in, a.out, a.rows, p.dw, finish, share, s);
+    return registers_product<false, false, T>(source<T>(x, a.rows, a.in), source<T>(z, a.rows, wz), a.n, a.in, a.out, a.rows, p.dw, finish, share, s);
 }
 
 }  // namespace

@@ -78,15 +78,23 @@ __device__ __forceinline__ const __bf16* same(const __bf16* p)
     return (const __bf16*)((unsigned long long)__builtin_amdgcn_readfirstlane((unsigned)(v >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((unsigned)v));
 }
 
-template <bool ALONG, int BR, int NT> struct Loader {
-    static constexpr int kBytes = BR * kSlab * 2, kAcross = ALONG ? 8 : BR / 8, kLoads = kBytes / 16 / NT;
+// BR rows (along) or columns (across) and KS k of an operand, by NT threads.  The exchanges above are those of KS = 64 and BR >= 128; rows of 32 k lie four
+// to the banks' width, 64 columns two.
+template <bool ALONG, int BR, int NT, int KS = kSlab> struct Loader {
+    static constexpr int kBytes = BR * KS * 2, kAcross = ALONG ? KS / 8 : BR / 8, kLoads = kBytes / 16 / NT;
     static constexpr int kStep = NT / kAcross;                 // image rows between a thread's chunks
+    static constexpr int kPeriod = ALONG ? 16 : 4;             // rows after which the exchange is the same again
+    static_assert((KS == 64 || KS == 32) && BR >= 64, "");
+    static __device__ __forceinline__ int place(int r, int c)
+    {
+        if (ALONG) return KS == 64 ? c ^ (r >> 1 & 7) : c ^ (r >> 2 & 3);
+        return BR == 64 ? c ^ ((r & 2) << 1) : c ^ ((r & 3) << 2);
+    }
     unsigned off, step;            // of this thread's first chunk, and to its next one
     int kc;                        // along: the chunk's first k
     __device__ __forceinline__ void init(int tid, int ld)
     {
-        const int r = tid / kAcross, c = tid % kAcross;
-        const int from = ALONG ? c ^ (r >> 1 & 7) : c ^ ((r & 3) << 2);      // kStep is a multiple of 16 (4 across): the same for all its rows
+        const int r = tid / kAcross, from = place(r, tid % kAcross);          // its own inverse
         off = (unsigned)(r * ld + from * 8) * 2;
         step = (unsigned)(kStep * ld) * 2;
         kc = from * 8;
@@ -94,7 +102,7 @@ template <bool ALONG, int BR, int NT> struct Loader {
     // r0: the tile's first row (along) or column (across)
     __device__ __forceinline__ void issue(const Plane3& s, const __bf16* base, int r0, int k0, int wave, char* image) const
     {
-        static_assert(kStep % (ALONG ? 16 : 4) == 0 && kLoads >= 1, "");
+        static_assert(kStep % kPeriod == 0 && kLoads >= 1, "");
         const long long first = ALONG ? (long long)r0 * s.ld : (long long)k0 * s.ld + r0;
         const long long rest = ALONG ? (long long)(s.lines - r0 - 1) * s.ld + s.cols : (long long)(s.lines - k0 - 1) * s.ld + s.cols - r0;
         const Buffer b = buffer(same(base + first), __builtin_amdgcn_readfirstlane((unsigned)min(rest * 2, 0xffffffe0ll)));
@@ -112,10 +120,10 @@ template <bool ALONG, int BR, int NT> struct Loader {
     {
         if (ALONG) {
             const int r = r0 + (lane & 31);
-            return *(const bf16x8*)(image + r * 128 + (((ks * 2 + (lane >> 5)) ^ (lane >> 1 & 7)) * 16));
+            return *(const bf16x8*)(image + r * KS * 2 + place(lane & 31, ks * 2 + (lane >> 5)) * 16);
         }
         const int k = ks * 16 + (lane >> 5) * 8 + ((lane & 15) >> 2), c = r0 + ((lane >> 4) & 1) * 16 + 4 * (lane & 3);
-        return lds_read_tr8(image, (unsigned)(k * BR * 2 + ((c >> 3) ^ ((k & 3) << 2)) * 16 + (c & 7) * 2), BR * 2);
+        return lds_read_tr8(image, (unsigned)(k * BR * 2 + place(k, c >> 3) * 16 + (c & 7) * 2), BR * 2);
     }
 };
 

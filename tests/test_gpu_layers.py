@@ -80,6 +80,13 @@ def test_probabilities_at_the_ends_of_their_range(p, limit):
 # ---- dense layer -----------------------------------------------------------------------------------------------------
 LAYER = [(1, 1, 1, 1), (1, 1, 512, 2048), (2, 3, 5, 40), (3, 33, 40, 9), (2, 17, 9, 130), (2, 64, 130, 257), (4, 32, 784, 128), (1, 5, 2048, 72), (1, 40, 2056, 130),
          (1, 65, 64, 96), (2, 200, 333, 519), (2, 300, 40, 7), (1, 700, 520, 264), (1, 300, 2048, 130), (16, 1024, 72, 768), (2, 520, 1096, 9)]
+# sizes, with the type, that between them take every tile, through registers and in planes, in one share and in several
+ROUTES = [(4, 4624, 8, 10, 1), (8, 71, 5672, 9, 1), (3, 8, 1919, 1049, 1), (16, 39, 9, 3984, 0), (32, 149, 8, 1712, 1), (1, 4120, 3131, 8, 1), (32, 33, 3701, 72, 0),
+          (8, 3648, 129, 67, 0), (4, 96, 1117, 800, 0), (3, 8, 4456, 917, 1), (4, 8056, 66, 72, 0), (4, 168, 6064, 176, 1), (2, 928, 78, 2128, 0), (3, 2096, 1992, 72, 1),
+          (8, 86, 280, 5048, 1), (1, 2890, 3030, 142, 1), (3, 1830, 71, 2097, 1), (4, 2392, 207, 1349, 0), (1, 135, 5672, 4296, 1), (2, 4288, 2744, 175, 1)]
+# and the largest tiles in several shares, some rows of whose results are looked at
+LARGE = [(1, 4096, 512, 4096, 0), (1, 2048, 16384, 1000, 1), (1, 2048, 1000, 16384, 1), (2, 16384, 1000, 1000, 1), (4, 16384, 1000, 1000, 1), (1, 4096, 1000, 16384, 1),
+         (1, 4096, 16384, 1000, 1), (1, 6000, 4096, 3000, 0)]
 OPTIONS = [("none", 0.0, False, False), ("relu", 0.0, True, False), ("gelu", 0.2, True, True), ("silu", 0.1, False, True), ("none", 0.1, True, True)]
 
 
@@ -119,6 +126,43 @@ def _check_layer(n, rows, i, o, bf16, layout, options, seed=0):
 def test_dense_layer_and_its_gradient(n, rows, i, o, bf16, layout):
     at = LAYER.index((n, rows, i, o)) + LAYOUTS.index(layout)
     _check_layer(n, rows, i, o, bf16, layout, OPTIONS[at % len(OPTIONS)])
+
+
+@pytest.mark.parametrize("n,rows,i,o,bf16", ROUTES)
+def test_dense_layer_on_every_route(n, rows, i, o, bf16):
+    at = ROUTES.index((n, rows, i, o, bf16))
+    _check_layer(n, rows, i, o, bf16, LAYOUTS[at % 2 * 2], OPTIONS[at % len(OPTIONS)], seed=at)
+
+
+@pytest.mark.parametrize("n,rows,i,o,bf16", LARGE)
+def test_large_layers(n, rows, i, o, bf16):
+    # 64 rows of y, dx and dw, the first and last among them, against 64 bits on the device; bounds as everywhere
+    torch = _torch()
+    t = _dtype(bf16)
+    g = torch.Generator(device="cuda").manual_seed(i)
+    x, w, dy, pre = (torch.randn(s, device="cuda", generator=g).to(t) for s in ((n, rows, i), (n, i, o), (n, rows, o), (n, rows, o)))
+    plan = hadfl.DenseLayer(n, rows, i, o, bf16=bf16, activation="relu")
+    y = plan.forward(x, w)
+    dx, dw, db = plan.backward(dy, x, w, pre=pre)
+    half = ref.HALF_BF16 if bf16 else ref.EPS32
+
+    def check(got, a, b, name, relu=False):
+        want, terms = a.double() @ b.double().contiguous(), a.double().abs() @ b.double().abs().contiguous()
+        err = (a.shape[1] + 16) * ref.EPS32 * terms
+        want = want.clamp(min=0) if relu else want
+        assert bool(((got.double() - want).abs() <= err + half * (want.abs() + err)).all()), name
+
+    for k in (0, n - 1):
+        some = torch.randint(0, rows, (64,), device="cuda", generator=g)
+        some[0], some[1] = 0, rows - 1
+        z = torch.where(pre[k] > 0, dy[k], torch.zeros_like(dy[k]))
+        check(y[k, some], x[k, some], w[k], "y", relu=True)
+        check(dx[k, some], z[some], w[k].t(), "dx")
+        some = torch.randint(0, i, (64,), device="cuda", generator=g)
+        some[0], some[1] = 0, i - 1
+        check(dw[k, some], x[k][:, some].t(), z, "dw")
+        want, terms = z.double().sum(0), z.double().abs().sum(0)
+        assert bool(((db[k].double() - want).abs() <= (rows + 16) * ref.EPS32 * terms).all())
 
 
 @pytest.mark.parametrize("options", OPTIONS)

@@ -72,3 +72,21 @@ def test_no_launch_has_more_threads_than_a_dimension_holds(launched):
         for v in r["launches"]:
             size = [int(q) for q in v[1:7]]
             assert all(size[i] * size[i + 1] < 1 << 32 for i in (0, 2, 4)) and size[2] < 1 << 16 and size[4] < 1 << 16, (c, v)
+
+
+def test_the_gpu_tests_reach_every_kernel_of_the_layers(launched):
+    from tests import test_gpu_layers as gpu
+    odd = lambda t, i, o: dict(x=[t * (i + 3) + 7, i + 3], w=[i * (o + 3) + 7, o + 3], y=[t * (o + 3) + 7, o + 3])  # noqa: E731
+    cases = [q for n, t, i, o in gpu.LAYER for b in (0, 1) for s in ({}, odd(t, i, o)) for q in _both(n=n, rows=t, inputs=i, outputs=o, bf16=b, **s)]
+    cases += [q for n, t, i, o, b in gpu.ROUTES + gpu.LARGE for q in _both(n=n, rows=t, inputs=i, outputs=o, bf16=b)[:3]]
+    cases += [dict(op="layer", grad=1, want=["db"], act=1, n=2, rows=5, inputs=40, outputs=40, bf16=b) for b in (0, 1)]
+    cases += [dict(op="scores", n=n, rows=t, classes=v, bf16=b, tokens=3, top=min(v, 5), grad=g) for n, t, v in gpu.SCORES + [(2, 1100, 20011), (2, 1100, 33001), (2, 1100, 60000)]
+              for b in (0, 1) for g in (0, 1)]
+    cases += [dict(op="drop", n=2, rows=5, features=40, bf16=b) for b in (0, 1)]
+    got = launched([dict(op="kernels")] + cases)
+    kernels, reached = {k for k in got[0] if "hadfl5layer" in k}, set()
+    for c, r in zip(cases, got[1:]):
+        assert r["status"] == 0, (c, r["text"])
+        reached |= {v[0] for v in r["launches"] if "hadfl5layer" in v[0]}
+    assert len(kernels) > 30 and reached <= kernels
+    assert not kernels - reached, "\n".join(sorted(kernels - reached))
