@@ -346,10 +346,11 @@ Work plan_of(int n, int rows, int in, int out, int bf16, bool grad, bool packed)
         if (p.dw.planes) p.x = take((size_t)nx * plane);
         if (p.dx.planes) p.w = take((size_t)nw * plane);
         p.dz = take((size_t)nz * (p.dx.planes || p.dw.planes ? plane : bf16 ? 2 : 4));
+        // few rows: one to a line of eight lanes, one block of them and no second launch for db
         p.across = 8;
-        while (p.across < 64 && p.across * 8 < p.ldz) p.across *= 2;
+        while (rows > 32 && p.across < 64 && p.across * 8 < p.ldz) p.across *= 2;
         const long long wide = (p.ldz + p.across * 8 - 1) / (p.across * 8);
-        p.depth = 256;
+        p.depth = rows > 32 ? 256 : 32;
         while (p.depth > 256 / p.across && (long long)n * wide * ((rows + p.depth - 1) / p.depth) < 1024) p.depth /= 2;
         p.blocks = std::max(1, (rows + p.depth - 1) / p.depth);
         p.sums = take((size_t)n * p.blocks * p.ldz * 4);
@@ -491,10 +492,11 @@ template <typename T> hipError_t forward(const LayerArgs& a, hipStream_t s)
 
 // ---- gradient ---------------------------------------------------------------------------------------------------------------
 // dz = D'(dy) a'(pre), eight columns a lane, into [replicas][rows][ld] (PARTS = 1), its three bf16 parts into such planes (3) or nowhere (0), and the
-// column sums of a block's rows.  A dropped value is zero whatever dy and pre hold there.
+// column sums of a block's rows, a line of `ld` of them a block and sums_rep apart from replica to replica: db itself where one block has all rows.  A
+// dropped value is zero whatever dy and pre hold there.
 template <typename T, int PARTS>
 __global__ __launch_bounds__(256) void slope_kernel(const T* dy, long long yrep, long long yrow, const T* pre, long long prep, long long prow, int rows, int cols,
-                                                    int ld, int across, int depth, int act, Draws d, void* dz, long long plane, float* sums)
+                                                    int ld, int across, int depth, int act, Draws d, void* dz, long long plane, float* sums, long long sums_rep)
 {
     __shared__ float part[256][9];
     const int lane = threadIdx.x % across, line = threadIdx.x / across, lines = 256 / across;
@@ -535,7 +537,7 @@ __global__ __launch_bounds__(256) void slope_kernel(const T* dy, long long yrep,
         float v = 0.f;
         for (int r = 0; r < lines; ++r) v += part[r * across + i / 8][i % 8];
         const int col = blockIdx.x * across * 8 + i;
-        if (col < ld) sums[((long long)k * gridDim.y + blockIdx.y) * ld + col] = v;
+        if (col < cols) sums[k * sums_rep + (long long)blockIdx.y * ld + col] = v;
     }
 }
 // db from the blocks' sums: 32 columns a workgroup, eight threads a column, each every eighth block, then the eight in order
@@ -571,10 +573,11 @@ template <typename T> hipError_t backward(const LayerArgs& a, hipStream_t s)
         const dim3 grid((unsigned)((p.ldz + p.across * 8 - 1) / (p.across * 8)), (unsigned)p.blocks, (unsigned)a.n);
         auto* kernel = !form ? slope_kernel<T, 0> : half || !planes ? slope_kernel<T, 1> : slope_kernel<T, half ? 1 : 3>;
         kernel<<<grid, 256, 0, s>>>((const T*)a.dy.p, a.dy.rep, a.dy.row, (const T*)a.pre.p, a.pre.rep, a.pre.row, a.rows, a.out, p.ldz, p.across, p.depth,
-                                    a.act, a.draws, work + p.dz, plane, a.db.p ? sums : nullptr);
+                                    a.act, a.draws, work + p.dz, plane, p.blocks == 1 ? (float*)a.db.p : a.db.p ? sums : nullptr,
+                                    p.blocks == 1 ? a.db.rep : (long long)p.blocks * p.ldz);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    if (a.db.p) {
+    if (a.db.p && (p.blocks > 1 || a.rows == 0)) {
         column_sums_kernel<<<dim3((unsigned)((a.out + 31) / 32), (unsigned)a.n), 256, 0, s>>>(sums, a.rows ? p.blocks : 0, p.ldz, a.out, (float*)a.db.p, a.db.rep);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }

@@ -658,9 +658,15 @@ class _Drawing(_Operator):
             if counter.dtype != self.torch.int64 or counter.device != self.device or counter.numel() != 1:
                 raise HadflError(EINVAL, "counter must be one int64 on %s" % (self.device,))
             at = counter.data_ptr()
-        if not (0 <= int(seed) < 2 ** 64 and 0 <= int(call) < 2 ** 64):
+        if not (0 <= seed < 2 ** 64 and 0 <= call < 2 ** 64):
             raise HadflError(EINVAL, "seed and call must be in [0, 2^64)")
-        return ctypes.byref(HadflDraw(int(seed), int(call), at))
+        got = self._structs.get("draw")
+        if got is None:
+            d = HadflDraw()
+            got = self._structs["draw"] = (d, ctypes.addressof(d))
+        d = got[0]
+        d.seed, d.call, d.counter = int(seed), int(call), at
+        return got[1]
 
 
 class Dropout(_Drawing):
