@@ -234,6 +234,114 @@ __global__ __launch_bounds__(WM * WN * 64) void layer_planes_kernel(Plane3 a, Pl
     } else epi(t);
 }
 
+// Few rows of a short contraction, whose time is latency: a workgroup takes 32 rows x 32 TN columns and its NW waves a share of the contraction each, in
+// slabs of 32 k that a wave stages for itself (no barrier), two in flight.  The shares are added from LDS in ascending order and finished there: one
+// launch.  One row of 512 x 2048 bf16 5.0 us in a graph (shares by workgroups and a second launch 7.3), 4 x 32 rows of 512 x 128 fp32 6.4 (8.0).
+template <class SA, class SB, bool B_ALONG, int TN, int NW, typename T>
+__global__ __launch_bounds__(NW * 64) void layer_few_kernel(SA a, SB b, int K, int tiles_m, int tiles_n, int total, Finish<T> finish)
+{
+    constexpr int PA = SA::kPlanes, PB = SB::kPlanes, KS = 32, AHEAD = 2;
+    typedef Image<true, 32, KS> IA;
+    typedef Image<B_ALONG, 32 * TN, KS> IB;
+    constexpr int NA = IA::kChunks / 64, NB = IB::kChunks / 64;
+    constexpr unsigned kWave = PA * IA::kPlane + PB * IB::kPlane, kPitch = TN * 128 + 16, kSums = NW * 32 * kPitch;
+    __shared__ __attribute__((aligned(16))) char smem[NW * kWave > kSums ? NW * kWave : kSums];
+
+    const unsigned item = blockIdx.y * gridDim.x + logical_block();
+    if (item >= (unsigned)total) return;
+    const int at_m = item % tiles_m, rest = item / tiles_m, m0 = at_m * 32, n0 = rest % tiles_n * 32 * TN, rep = rest / tiles_n;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    a.bind(rep);
+    b.bind(rep);
+    const int slabs = (K + KS - 1) / KS, per = (slabs + NW - 1) / NW, k_begin = min(wave * per * KS, K), k_end = min(K, k_begin + per * KS);
+    char* image = smem + wave * kWave;
+    f16 acc[TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[j] = f16{};
+    typename SA::Raw ra[AHEAD][NA];
+    typename SB::Raw rb[AHEAD][NB];
+    auto fetch = [&](int k0, int slot) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const int id = lane + i * 64, r = id / IB::kAcross, c = id % IB::kAcross * 8;
+            rb[slot][i] = B_ALONG ? b.load(n0 + r, k0 + c) : b.load(k0 + r, n0 + c);
+        }
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const int id = lane + i * 64;
+            ra[slot][i] = a.load(m0 + id / IA::kAcross, k0 + id % IA::kAcross * 8);
+        }
+    };
+    auto slab = [&](int k0, int slot) {
+        const bool tail_a = a.has_tail(k0, k0 + KS), tail_b = B_ALONG ? b.has_tail(k0, k0 + KS) : b.has_tail(n0, n0 + 32 * TN);
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const int id = lane + i * 64, r = id / IA::kAcross, c = id % IA::kAcross;
+            u4 p[PA];
+            a.planes(ra[slot][i], k0 + c * 8, tail_a, p);
+#pragma unroll
+            for (int s = 0; s < PA; ++s) *(u4*)(image + s * IA::kPlane + r * IA::kPitch + c * 16) = p[s];
+        }
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const int id = lane + i * 64, r = id / IB::kAcross, c = id % IB::kAcross;
+            u4 p[PB];
+            b.planes(rb[slot][i], (B_ALONG ? k0 : n0) + c * 8, tail_b, p);
+#pragma unroll
+            for (int s = 0; s < PB; ++s) *(u4*)(image + PA * IA::kPlane + s * IB::kPlane + r * IB::kPitch + c * 16) = p[s];
+        }
+        if (k0 + AHEAD * KS < k_end) fetch(k0 + AHEAD * KS, slot);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");        // this wave's stores before its reads: LDS keeps their order
+#pragma unroll
+        for (int ks = 0; ks < KS / 16; ++ks) {
+            bf16x8 fa[PA], fb[TN][PB];
+#pragma unroll
+            for (int s = 0; s < PA; ++s) fa[s] = IA::read(image + s * IA::kPlane, 0, ks, lane);
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int s = 0; s < PB; ++s) fb[j][s] = IB::read(image + PA * IA::kPlane + s * IB::kPlane, 32 * j, ks, lane);
+#pragma unroll
+            for (int pair = PA == 1 ? 5 : 0; pair < 6; ++pair)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j][kPairB[pair]], fa[kPairA[pair]], acc[j], 0, 0, 0);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (k_begin + i * KS < k_end) fetch(k_begin + i * KS, i);
+    for (int k0 = k_begin; k0 < k_end; k0 += AHEAD * KS) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (k0 + u * KS < k_end) slab(k0 + u * KS, u);
+    }
+    __syncthreads();                                           // the images are free
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            *(f4*)(smem + (wave * 32 + (lane & 31)) * kPitch + (32 * j + 8 * q + 4 * (lane >> 5)) * 4) = f4{acc[j][4 * q], acc[j][4 * q + 1], acc[j][4 * q + 2], acc[j][4 * q + 3]};
+    __syncthreads();
+    for (int id = threadIdx.x; id < 128 * TN; id += NW * 64) {
+        const int r = id / (4 * TN), c = id % (4 * TN) * 8;
+        auto columns = finish.columns(rep, m0 + r, n0 + c, 0);
+        Chunk<T> add = {};
+        finish.fetch(columns, 0, add);
+        f4 low{}, high{};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const char* at = smem + (w * 32 + r) * kPitch + c * 4;
+            low += *(const f4*)at;
+            high += *(const f4*)(at + 16);
+        }
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { v[e] = low[e]; v[4 + e] = high[e]; }
+        finish.row(columns, add, v);
+    }
+}
+
 // The shares of a contraction, [splits][replicas][rows][ld] floats, added in ascending order and finished.
 template <typename T>
 __global__ __launch_bounds__(256) void finish_shares_kernel(const float* share, int splits, long long step, int ld, long long total, Finish<T> finish)
@@ -262,6 +370,7 @@ int up_to(long long v, int unit) { return (int)((v + unit - 1) / unit * unit); }
 struct Shape {
     bool planes;                   // operands straight from memory to LDS
     int bm, bn, splits, len;
+    bool few;                      // at most 32 rows, the shares within a workgroup
 };
 size_t share_bytes(const Shape& p, int n, int M, int N) { return p.splits > 1 ? align256((size_t)p.splits * n * M * up_to(N, 8) * 4) : 0; }
 
@@ -283,18 +392,28 @@ constexpr Choice kChoices[] = {{false, 32, 128, 3, {23, 15}, {6.3, 5}, 3}, {fals
                                {false, 128, 128, 2, {44, 46}, {10, 11}, 4}, {true, 128, 128, 1, {0, 0}, {6, 9.6}, 4}, {true, 128, 256, 1, {73, 73}, {11.5, 16}, 5},
                                {true, 256, 256, 1, {0, 0}, {21, 28}, 8}};
 struct Chosen { Shape shape; double cost; };
+// Whether a product goes to layer_few_kernel: a workgroup for every compute unit at most, and no more than four slabs a wave.  us in graphs, other way /
+// this: one row bf16 of 512 x 8192 7.4 / 5.1, 1024 x 8192 7.2 / 6.5, 2048 x 2048 7.4 / 9.0; four of 512 x 2048 7.4 / 5.1, of 512 x 8192 (512 workgroups)
+// 8.0 / 8.5; fp32 512 x 8192 9.1 / 6.7, 1024 x 2048 8.3 / 9.6 (but a launch less), 2048 x 2048 10.7 / 15.3.
+constexpr int few_columns(bool bf16) { return bf16 ? 64 : 32; }       // fp32: what three planes of eight waves leave room for
+bool is_few(int n, int M, int N, int K, int bf16)
+{
+    const int columns = few_columns(bf16);
+    return M <= 64 && K <= 1024 && (long long)n * ((M + 31) / 32) * ((N + columns - 1) / columns) <= 256;
+}
 // The cheapest tiles and shares by that, with operands in planes or through registers.  A share is written and read at 5 TB/s, and joining them is one
 // more launch, 4 us.
 Chosen best_shape(int n, int M, int N, int K, int bf16, bool across, bool planes)
 {
     Chosen best{{}, -1};
+    if (!planes && !across && is_few(n, M, N, K, bf16)) return Chosen{Shape{false, 32, few_columns(bf16), 1, K, true}, 0};
     for (const Choice& o : kChoices) {
         const double alone = bf16 ? o.bf16.alone : o.f32.alone, shared = bf16 ? o.bf16.shared : o.f32.shared;
         if (o.planes != planes || alone == 0 || (o.bm == 32 && (M > 32 || across))) continue;
         const long long tiles = (long long)n * ((M + o.bm - 1) / o.bm) * ((N + o.bn - 1) / o.bn);
         const int unit = bf16 && o.bm == 32 ? 128 : 64;                       // whole slabs of every kernel of these tiles
         for (int s = 1; s <= 64 && (s == 1 || K / s >= unit); ++s) {
-            const Shape p = cut(Shape{o.planes, o.bm, o.bn, 1, 0}, K, s, unit);
+            const Shape p = cut(Shape{o.planes, o.bm, o.bn, 1, 0, false}, K, s, unit);
             if (p.splits != s) continue;
             const double each = (double)((tiles * s + 255) / 256);            // tiles of a compute unit
             const double k = each <= o.most ? std::max(alone, each * shared) : each * shared;
@@ -408,9 +527,20 @@ hipError_t planes_product(const Plane3& a, const Plane3& b, int n, int M, int N,
         } else return launch_planes<3, 128, 256, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
     });
 }
+template <bool BA, typename T, class SA, class SB>
+hipError_t launch_few(const SA& a, const SB& b, int n, int M, int N, int K, const Finish<T>& finish, hipStream_t s)
+{
+    constexpr int TN = few_columns(sizeof(T) == 2) / 32, NW = 8;
+    const int tm = (M + 31) / 32, tn = (N + 32 * TN - 1) / (32 * TN);
+    const long long total = (long long)n * tm * tn;
+    layer_few_kernel<SA, SB, BA, TN, NW, T><<<line_grid(die_grid(total), NW * 64), NW * 64, 0, s>>>(a, b, K, tm, tn, (int)total, finish);
+    return hipGetLastError();
+}
 template <bool AA, bool BA, typename T, class SA, class SB>
 hipError_t registers_product(const SA& a, const SB& b, int n, int M, int N, int K, const Shape& p, const Finish<T>& finish, float* share, hipStream_t s)
 {
+    if constexpr (AA)
+        if (p.few) return launch_few<BA, T>(a, b, n, M, N, K, finish, s);
     return whole_or_shares<T>(p, n, M, N, finish, share, s, [&](const auto& epi) {
         if (p.bm == 128) return launch_registers<T, 128, 128, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
         if constexpr (AA)

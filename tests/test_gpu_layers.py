@@ -83,7 +83,8 @@ LAYER = [(1, 1, 1, 1), (1, 1, 512, 2048), (2, 3, 5, 40), (3, 33, 40, 9), (2, 17,
 # sizes, with the type, that between them take every tile, through registers and in planes, in one share and in several
 ROUTES = [(4, 4624, 8, 10, 1), (8, 71, 5672, 9, 1), (3, 8, 1919, 1049, 1), (16, 39, 9, 3984, 0), (32, 149, 8, 1712, 1), (1, 4120, 3131, 8, 1), (32, 33, 3701, 72, 0),
           (8, 3648, 129, 67, 0), (4, 96, 1117, 800, 0), (3, 8, 4456, 917, 1), (4, 8056, 66, 72, 0), (4, 168, 6064, 176, 1), (2, 928, 78, 2128, 0), (3, 2096, 1992, 72, 1),
-          (8, 86, 280, 5048, 1), (1, 2890, 3030, 142, 1), (3, 1830, 71, 2097, 1), (4, 2392, 207, 1349, 0), (1, 135, 5672, 4296, 1), (2, 4288, 2744, 175, 1)]
+          (8, 86, 280, 5048, 1), (1, 2890, 3030, 142, 1), (3, 1830, 71, 2097, 1), (4, 2392, 207, 1349, 0), (1, 135, 5672, 4296, 1), (2, 4288, 2744, 175, 1),
+          (8, 8, 212, 3288, 1), (8, 8, 3288, 212, 1), (32, 23, 265, 288, 0), (4, 61, 300, 600, 1), (2, 50, 1000, 90, 0)]
 # and the largest tiles in several shares, some rows of whose results are looked at
 LARGE = [(1, 4096, 512, 4096, 0), (1, 2048, 16384, 1000, 1), (1, 2048, 1000, 16384, 1), (2, 16384, 1000, 1000, 1), (4, 16384, 1000, 1000, 1), (1, 4096, 1000, 16384, 1),
          (1, 4096, 16384, 1000, 1), (1, 6000, 4096, 3000, 0)]
