@@ -138,7 +138,8 @@ constexpr int kPairA[6] = {2, 1, 0, 1, 0, 0}, kPairB[6] = {0, 1, 2, 0, 1, 0};
 // slabs of 32, all planes of a slab together.  A wave reads the operands of a step of 16 k while it multiplies the step before, across slabs too: the
 // barrier that frees a slab's image and says that the next one has arrived lies before the slab's last step, whose operands are in registers by then, so
 // that the matrix cores have work while the first operands of the next slab are read.  4 x 8192 rows x 4096 x 4096 bf16 with bias and dropout onto a
-// residual: 1001 us = 1098 TFLOP/s, the matrix cores busy 58 % of the time at 1.8 to 1.9 GHz; the product alone 944, the library's 858.
+// residual: 1001 us = 1098 TFLOP/s, the matrix cores busy 57 to 58 % of the time; the product alone 944.  The library's product 858, 70 % busy, at no
+// higher clock (both 1.4 to 1.8 GHz over twelve launches in a row).
 template <bool A_ALONG, bool B_ALONG, int PL, int BM, int BN, int WM, int WN, class Epi>
 __global__ __launch_bounds__(WM * WN * 64) void layer_planes_kernel(Plane3 a, Plane3 b, int K, int tiles_m, int tiles_n, int splits, int split_len, int total, Epi epi)
 {
@@ -237,7 +238,7 @@ __global__ __launch_bounds__(WM * WN * 64) void layer_planes_kernel(Plane3 a, Pl
 
 // Few rows of a short contraction, whose time is latency: a workgroup takes 32 rows x 32 TN columns and its NW waves a share of the contraction each, in
 // slabs of 32 k that a wave stages for itself (no barrier), two in flight.  The shares are added from LDS in ascending order and finished there: one
-// launch.  One row of 512 x 2048 bf16 5.0 us in a graph (shares by workgroups and a second launch 7.3), 4 x 32 rows of 512 x 128 fp32 6.4 (8.0).
+// launch.  One row of 512 x 2048 bf16 5.0 us in a graph (shares by workgroups and a second launch 7.3), 4 x 32 rows of 512 x 128 fp32 6.4 (8.0), of 784 x 128 8.8.
 template <class SA, class SB, bool B_ALONG, int TN, int NW, typename T>
 __global__ __launch_bounds__(NW * 64) void layer_few_kernel(SA a, SB b, int K, int tiles_m, int tiles_n, int total, Finish<T> finish)
 {
@@ -403,7 +404,9 @@ bool is_few(int n, int M, int N, int K, int bf16)
     return M <= 64 && K <= 1024 && (long long)n * ((M + 31) / 32) * ((N + columns - 1) / columns) <= 256;
 }
 // The cheapest tiles and shares by that, with operands in planes or through registers.  A share is written and read at 5 TB/s, and joining them is one
-// more launch, 4 us.
+// more launch, 4 us.  us, planes / registers, the best tiles of each: fp32 y of 8192 x 4096 x 4096 1323 / 1493, 4096 x 1024 x 4096 183 / 196, 16 x 1024 x
+// 512 x 2048 221 / 200, 2 x 1001 x 777 x 1111 52 / 44; bf16 dx and dW of 8192 x 4096 x 4096 504 / 801, 16 x 1024 x 512 x 2048 129 / 145, 2 x 1001 x 777 x
+// 1111 49 / 42.  What it takes is within 5 % of the best of these but for fp32 gradients of middling sizes (2 x 1001 x 777 x 1111 88, best 79).
 Chosen best_shape(int n, int M, int N, int K, int bf16, bool across, bool planes)
 {
     Chosen best{{}, -1};
@@ -623,7 +626,8 @@ template <typename T> hipError_t forward(const LayerArgs& a, hipStream_t s)
 
 // ---- gradient ---------------------------------------------------------------------------------------------------------------
 // dz = D'(dy) a'(pre), eight columns a lane, into [replicas][rows][ld] (PARTS = 1), its three bf16 parts into such planes (3) or nowhere (0), and the
-// column sums of a block's rows (16 x 1024 x 2048 bf16 with gelu: 39.7 us = 5.1 TB/s), a line of `ld` of them a block and sums_rep apart from replica to replica: db itself where one block has all rows.  A
+// column sums of a block's rows (16 x 1024 x 2048 bf16 with gelu: 39.7 us = 5.1 TB/s), a line of `ld` of them a block and sums_rep apart
+// from replica to replica: db itself where one block has all rows.  A
 // dropped value is zero whatever dy and pre hold there.
 template <typename T, int PARTS>
 __global__ __launch_bounds__(256) void slope_kernel(const T* dy, long long yrep, long long yrow, const T* pre, long long prep, long long prow, int rows, int cols,

@@ -330,6 +330,8 @@ __global__ __launch_bounds__(256) void scores_grad_kernel(const T* logits, long 
 // launch is less than a second one's 3 us, 1024 threads for rows that they hold whole, and where rows would have
 // more pieces than a wave has lanes (256 / 1024 threads: 1 x 32000 19.0 / 15.6, 1024 x 32000 27.1 /
 // 26.0, 512 x 60000 26.8 / 26.1, 1024 x 60000 38.7 / 45.7; fp32 1024 x 32000 31.8 / 31.0).
+// A row of more pieces than one has at least 4096 classes a piece and loses at most seven of them to each piece's rounding: the last one still
+// holds as many as there are alternatives, so that every piece gives n_top of them.
 struct Plan { int nt, u, pieces, size; };
 Plan plan_of(long long lines, int classes, int bf16)
 {

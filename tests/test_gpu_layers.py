@@ -334,18 +334,18 @@ def _scores_case(n, rows, v, bf16, layout, tokens=3, seed=0):
     return _in(z, bf16, layout), _torch().as_tensor(y).cuda(), y
 
 
-def _check_scores(z, y, yh, n_top, bf16, plan=None, in_place=False, rows_of=None):
+def _check_scores(z, y, yh, n_top, bf16, plan=None, in_place=False):
     torch = _torch()
     n, rows, v = z.shape
     plan = plan or hadfl.TokenScores(n, rows, v, n_tokens=yh.shape[2], n_top=n_top, bf16=bf16)
     logp, entropy, top, top_logp = plan.forward(z, y)
     rng = np.random.default_rng(1)
     g, dh = (torch.as_tensor(rng.normal(size=s)).float().cuda() for s in (yh.shape, (n, rows)))
-    out = Inside_out = _out((n, rows, v), bf16, "odd")
-    out = (z if in_place else Inside_out.t)
+    whole = _out((n, rows, v), bf16, "odd")
+    out = z if in_place else whole.t
     zh = _values(z)
     plan.backward(z, y, g, dh, dlogits=out)
-    assert in_place or Inside_out.untouched()
+    assert in_place or whole.untouched()
     for k in range(n):
         r = ref.scores(zh[k], yh[k].astype(np.int64), n_top)
         b = ref.scores_bounds(r, _values(g[k]), _values(dh[k]), bf16)
