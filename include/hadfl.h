@@ -424,7 +424,8 @@ HADFL_API hadfl_status hadfl_dropout_rows(const hadfl_dropout *dropout, const ha
  *   dx = dz W^T,  dW = x^T dz,  db = sum_t dz;  the residual's gradient is dy.
  * fp32: operands enter the products as three bf16 parts, six products, whole for magnitudes from 2^-107 to below 3.39e38; an
  * infinity in a 32-bit operand makes NaN.  bf16: sums in 32 bits, outputs rounded once; the activation takes z before pre is
- * rounded; dz is rounded to bf16 for the two products, db is formed before that.
+ * rounded; a dz that is no bf16 value (GELU, SiLU, dropout) enters the two products as two bf16 parts, off by 2^-15 of a value at
+ * most, which doubles their operations; db is formed from it as it is.
  *   x (t)               dev, [n_replicas][n_rows][n_in]
  *   w (t)               dev, [n_replicas][n_in][n_out], the layout of a dense layer here
  *   bias                dev or NULL, [n_replicas][n_out] floats

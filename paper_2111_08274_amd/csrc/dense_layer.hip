@@ -2,8 +2,8 @@
 //   forward    one product whose epilogue does the rest on 32-bit sums, eight columns of a row at a time; pre = x W + b is left for the
 //              gradient where that is asked for
 //   gradient   dz = D'(dy) a'(pre) and its column sums db in one pass over dy, then dx = dz W^T and dW = x^T dz
-// bf16: dz is rounded to bf16 for the two products (2^-9 of a value, as the outputs themselves are rounded; a second part would double both
-// products); db is summed before that.  fp32: operands enter as three bf16 parts, six products.
+// bf16: a dz that is no bf16 value (a curved activation, a dropout's scale) enters the two products as two bf16 parts, off by 2^-15 of a value at
+// most; db is summed before that.  fp32: operands enter as three bf16 parts, six products.
 #include "direct_product.h"
 #include "layer.h"
 
@@ -131,22 +131,56 @@ __global__ __launch_bounds__(WM * WN * 64) void layer_product_kernel(SA a, SB b,
 {
     product_tile<SA, A_ALONG, SB, B_ALONG, BM, BN, WM, WN, KS, NBUF, AHEAD>(a, b, K, tiles_m, tiles_n, splits, split_len, total, epi);
 }
-// the planes of A and B whose products are kept of three bf16 parts each, the small ones first: what is left out is below 2^-24 of the product
-constexpr int kPairA[6] = {2, 1, 0, 1, 0, 0}, kPairB[6] = {0, 1, 2, 0, 1, 0};
+// f(a, b) for the planes of A and B whose products are kept, the small ones first: of three bf16 parts each what is left out is below 2^-24 of the product
+template <int PA, int PB, class F> __device__ __forceinline__ void each_pair(F&& f)
+{
+    constexpr int most = PA + PB - 2 < 2 ? PA + PB - 2 : 2;
+#pragma unroll
+    for (int sum = most; sum >= 0; --sum)
+#pragma unroll
+        for (int a = PA - 1; a >= 0; --a)
+            if (a <= sum && sum - a < PB) f(a, sum - a);
+}
 
-// Operands in planes of bf16, straight from memory to LDS (direct_product.h: Loader): one plane in slabs of 64 k, or the three parts of 32-bit values in
-// slabs of 32, all planes of a slab together.  A wave reads the operands of a step of 16 k while it multiplies the step before, across slabs too: the
+// dz as slope_kernel leaves it in two parts: planes of bf16, rows of whole chunks
+struct TwoParts {
+    static constexpr int kPlanes = 2;
+    struct Raw { Chunk<__bf16> high, low; bool in; };
+    const __bf16* p;
+    long long rep, row;
+    int rows, cols;
+    long long plane;
+    __device__ __forceinline__ void bind(int k) { p += k * rep; }
+    __device__ __forceinline__ Raw load(int r, int c) const
+    {
+        Raw v;
+        v.in = r < rows && c < cols;
+        const __bf16* at = p + (v.in ? r * row + c : 0ll);
+        v.high.load(at, 8);
+        v.low.load(at + plane, 8);
+        return v;
+    }
+    __device__ __forceinline__ bool has_tail(int, int) const { return false; }
+    __device__ __forceinline__ void planes(const Raw& v, int, bool, u4 (&out)[2]) const
+    {
+        out[0] = v.in ? v.high.a : u4{0, 0, 0, 0};
+        out[1] = v.in ? v.low.a : u4{0, 0, 0, 0};
+    }
+};
+
+// Operands in planes of bf16, straight from memory to LDS (direct_product.h: Loader): one plane each in slabs of 64 k, or two parts against one plane, or
+// three parts of 32-bit values each in slabs of 32, all planes of a slab together.  A wave reads the operands of a step of 16 k while it multiplies the step before, across slabs too: the
 // barrier that frees a slab's image and says that the next one has arrived lies before the slab's last step, whose operands are in registers by then, so
 // that the matrix cores have work while the first operands of the next slab are read.  4 x 8192 rows x 4096 x 4096 bf16 with bias and dropout onto a
 // residual: 1001 us = 1098 TFLOP/s, the matrix cores busy 57 to 58 % of the time; the product alone 944.  The library's product 858, 70 % busy, at no
 // higher clock (both 1.4 to 1.8 GHz over twelve launches in a row).
-template <bool A_ALONG, bool B_ALONG, int PL, int BM, int BN, int WM, int WN, class Epi>
+template <bool A_ALONG, bool B_ALONG, int PA, int PB, int BM, int BN, int WM, int WN, class Epi>
 __global__ __launch_bounds__(WM * WN * 64) void layer_planes_kernel(Plane3 a, Plane3 b, int K, int tiles_m, int tiles_n, int splits, int split_len, int total, Epi epi)
 {
-    constexpr int NT = WM * WN * 64, TM = BM / WM / 32, TN = BN / WN / 32, KS = PL == 1 ? kSlab : kSlab / 2, kSteps = KS / 16;
+    constexpr int NT = WM * WN * 64, TM = BM / WM / 32, TN = BN / WN / 32, KS = PA + PB == 2 ? kSlab : kSlab / 2, kSteps = KS / 16;
     typedef Loader<A_ALONG, BM, NT, KS> LA;
     typedef Loader<B_ALONG, BN, NT, KS> LB;
-    constexpr int kImage = PL * (LA::kBytes + LB::kBytes), IMAGES = kImage > 49152 ? 2 : PL == 3 || kImage > 32768 ? 3 : 4, kLoads = PL * (LA::kLoads + LB::kLoads);
+    constexpr int kImage = PA * LA::kBytes + PB * LB::kBytes, IMAGES = kImage > 49152 ? 2 : kImage > 32768 ? 3 : 4, kLoads = PA * LA::kLoads + PB * LB::kLoads;
     __shared__ __attribute__((aligned(16))) char images[IMAGES * kImage];
     if constexpr (Epi::kStaged) static_assert(WM * WN * Epi::template bytes<TN>() <= IMAGES * kImage, "the epilogue's blocks lie in the images");
 
@@ -177,31 +211,33 @@ __global__ __launch_bounds__(WM * WN * 64) void layer_planes_kernel(Plane3 a, Pl
 
     auto issue = [&](int slab, char* image) {
 #pragma unroll
-        for (int s = 0; s < PL; ++s) la.issue(a, pa + s * a.plane, bm, k_begin + slab * KS, wave, image + s * LA::kBytes);
+        for (int s = 0; s < PA; ++s) la.issue(a, pa + s * a.plane, bm, k_begin + slab * KS, wave, image + s * LA::kBytes);
 #pragma unroll
-        for (int s = 0; s < PL; ++s) lb.issue(b, pb + s * b.plane, bn, k_begin + slab * KS, wave, image + PL * LA::kBytes + s * LB::kBytes);
+        for (int s = 0; s < PB; ++s) lb.issue(b, pb + s * b.plane, bn, k_begin + slab * KS, wave, image + PA * LA::kBytes + s * LB::kBytes);
     };
-    bf16x8 fa[2][PL][TM], fb[2][PL][TN];
+    bf16x8 fa[2][PA][TM], fb[2][PB][TN];
     auto read = [&](const char* image, int step, int to) {
 #pragma unroll
-        for (int s = 0; s < PL; ++s) {
+        for (int s = 0; s < (PA > PB ? PA : PB); ++s) {
 #pragma unroll
-            for (int i = 0; i < TM; ++i) fa[to][s][i] = LA::read(image + s * LA::kBytes, wm + 32 * i, step, t.lane);
+            for (int i = 0; i < TM; ++i)
+                if (s < PA) fa[to][s][i] = LA::read(image + s * LA::kBytes, wm + 32 * i, step, t.lane);
 #pragma unroll
-            for (int j = 0; j < TN; ++j) fb[to][s][j] = LB::read(image + PL * LA::kBytes + s * LB::kBytes, wn + 32 * j, step, t.lane);
+            for (int j = 0; j < TN; ++j)
+                if (s < PB) fb[to][s][j] = LB::read(image + PA * LA::kBytes + s * LB::kBytes, wn + 32 * j, step, t.lane);
         }
     };
     auto multiply = [&](int from) {
-#pragma unroll
-        for (int pair = PL == 1 ? 5 : 0; pair < 6; ++pair)
+        each_pair<PA, PB>([&](int p, int q) {
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
                 for (int j = 0; j < TN; ++j) {
-                    const bf16x8 &x = fa[from][kPairA[pair]][i], &y = fb[from][kPairB[pair]][j];
+                    const bf16x8 &x = fa[from][p][i], &y = fb[from][q][j];
                     t.acc[i][j] = Epi::kLaneM ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, x, t.acc[i][j], 0, 0, 0)
                                               : __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, t.acc[i][j], 0, 0, 0);
                 }
+        });
     };
     // Slab i + 1 is there when at most the loads of the IMAGES - 2 slabs after it are outstanding (they finish in order).
     auto turn = [&](int i, char* image, char* next) {
@@ -303,10 +339,10 @@ __global__ __launch_bounds__(NW * 64) void layer_few_kernel(SA a, SB b, int K, i
             for (int j = 0; j < TN; ++j)
 #pragma unroll
                 for (int s = 0; s < PB; ++s) fb[j][s] = IB::read(image + PA * IA::kPlane + s * IB::kPlane, 32 * j, ks, lane);
+            each_pair<PA, PB>([&](int p, int q) {
 #pragma unroll
-            for (int pair = PA == 1 ? 5 : 0; pair < 6; ++pair)
-#pragma unroll
-                for (int j = 0; j < TN; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j][kPairB[pair]], fa[kPairA[pair]], acc[j], 0, 0, 0);
+                for (int j = 0; j < TN; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j][q], fa[p], acc[j], 0, 0, 0);
+            });
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     };
@@ -383,16 +419,19 @@ Shape cut(Shape p, int K, int splits, int unit)
     return p;
 }
 // Tiles that there are, with what they cost in nanoseconds a k of a contraction: of a workgroup alone on its compute unit, and of each of several there
-// (`most` fit), measured over 64 to 8192 rows, 200 to 4096 inputs and outputs; and in microseconds what a tile costs beside.
+// (`most` fit), measured over 64 to 8192 rows, 200 to 4096 inputs and outputs; and in microseconds what a tile costs beside.  two: one operand of bf16 in
+// two parts, for which what is not there never was the best by more than 4 % over 38 products of 24 to 8192 rows (tiles chosen: within 3 % of the best, but
+// dx of 128 x 512 x 2048, 7 %).
 struct Choice {
     bool planes;
     int bm, bn, most;
-    struct { double alone, shared; } f32, bf16;                // zero: not there
+    struct { double alone, shared; } f32, bf16, two;           // zero: not there
     double tile;
 };
-constexpr Choice kChoices[] = {{false, 32, 128, 3, {23, 15}, {6.3, 5}, 3}, {false, 64, 64, 4, {25, 15.5}, {8.8, 4.9}, 3}, {false, 64, 128, 2, {33, 28}, {7.5, 7.3}, 3},
-                               {false, 128, 128, 2, {44, 46}, {10, 11}, 4}, {true, 128, 128, 1, {0, 0}, {6, 9.6}, 4}, {true, 128, 256, 1, {73, 73}, {11.5, 16}, 5},
-                               {true, 256, 256, 1, {0, 0}, {21, 28}, 8}};
+constexpr Choice kChoices[] = {{false, 32, 128, 3, {23, 15}, {6.3, 5}, {7.5, 5.5}, 3}, {false, 64, 64, 4, {25, 15.5}, {8.8, 4.9}, {12, 6}, 3},
+                               {false, 64, 128, 2, {33, 28}, {7.5, 7.3}, {0, 0}, 3}, {false, 128, 128, 2, {44, 46}, {10, 11}, {0, 0}, 4},
+                               {true, 128, 128, 1, {0, 0}, {6, 9.6}, {16.5, 16.5}, 4}, {true, 128, 256, 1, {73, 73}, {11.5, 16}, {27, 27}, 5},
+                               {true, 256, 256, 1, {0, 0}, {21, 28}, {50, 50}, 8}};
 struct Chosen { Shape shape; double cost; };
 // Whether a product goes to layer_few_kernel: a workgroup for every compute unit at most, and no more than four slabs a wave.  us in graphs, other way /
 // this: one row bf16 of 512 x 8192 7.4 / 5.1, 1024 x 8192 7.2 / 6.5, 2048 x 2048 7.4 / 9.0; four of 512 x 2048 7.4 / 5.1, of 512 x 8192 (512 workgroups)
@@ -407,12 +446,12 @@ bool is_few(int n, int M, int N, int K, int bf16)
 // more launch, 4 us.  us, planes / registers, the best tiles of each: fp32 y of 8192 x 4096 x 4096 1323 / 1493, 4096 x 1024 x 4096 183 / 196, 16 x 1024 x
 // 512 x 2048 221 / 200, 2 x 1001 x 777 x 1111 52 / 44; bf16 dx and dW of 8192 x 4096 x 4096 504 / 801, 16 x 1024 x 512 x 2048 129 / 145, 2 x 1001 x 777 x
 // 1111 49 / 42.  What it takes is within 5 % of the best of these but for fp32 gradients of middling sizes (2 x 1001 x 777 x 1111 88, best 79).
-Chosen best_shape(int n, int M, int N, int K, int bf16, bool across, bool planes)
+Chosen best_shape(int n, int M, int N, int K, int bf16, bool across, bool planes, bool two = false)
 {
     Chosen best{{}, -1};
     if (!planes && !across && is_few(n, M, N, K, bf16)) return Chosen{Shape{false, 32, few_columns(bf16), 1, K, true}, 0};
     for (const Choice& o : kChoices) {
-        const double alone = bf16 ? o.bf16.alone : o.f32.alone, shared = bf16 ? o.bf16.shared : o.f32.shared;
+        const double alone = two ? o.two.alone : bf16 ? o.bf16.alone : o.f32.alone, shared = two ? o.two.shared : bf16 ? o.bf16.shared : o.f32.shared;
         if (o.planes != planes || alone == 0 || (o.bm == 32 && (M > 32 || across))) continue;
         const long long tiles = (long long)n * ((M + o.bm - 1) / o.bm) * ((N + o.bn - 1) / o.bn);
         const int unit = bf16 && o.bm == 32 ? 128 : 64;                       // whole slabs of every kernel of these tiles
@@ -437,7 +476,8 @@ struct Work {                      // where things lie in the working memory
 // Planes of a 32-bit tensor are its three parts, 6 bytes a value, written once by one launch for x and w; a bf16 tensor is one as it lies, or copied where
 // rows of it do not start on 16 bytes or hold whole chunks of eight.  Through registers a tensor is read as it lies; sources there hold eight columns
 // at least (tile_product.h), so narrower layers take planes.
-Work plan_of(int n, int rows, int in, int out, int bf16, bool grad, bool packed)
+// two: dz of bf16 tensors in two parts.
+Work plan_of(int n, int rows, int in, int out, int bf16, bool grad, bool packed, bool two)
 {
     Work p{};
     p.ldx = up_to(in, 8);
@@ -455,8 +495,8 @@ Work plan_of(int n, int rows, int in, int out, int bf16, bool grad, bool packed)
         if (p.y.planes) { p.x = take((size_t)nx * plane); p.w = take((size_t)nw * plane); }
         p.share = take(share_bytes(p.y, n, rows, out));
     } else {
-        const Chosen rx = best_shape(n, rows, in, out, bf16, false, false), rw = best_shape(n, in, out, rows, bf16, true, false);
-        const Chosen qx = best_shape(n, rows, in, out, bf16, false, true), qw = best_shape(n, in, out, rows, bf16, true, true);
+        const Chosen rx = best_shape(n, rows, in, out, bf16, false, false, two), rw = best_shape(n, in, out, rows, bf16, true, false, two);
+        const Chosen qx = best_shape(n, rows, in, out, bf16, false, true, two), qw = best_shape(n, in, out, rows, bf16, true, true, two);
         if (bf16) {
             p.dx = narrow || qx.cost + lay(out, nw) < rx.cost ? qx.shape : rx.shape;
             p.dw = narrow || qw.cost + lay(packed ? 8 : in, nx) < rw.cost ? qw.shape : rw.shape;
@@ -468,7 +508,7 @@ Work plan_of(int n, int rows, int in, int out, int bf16, bool grad, bool packed)
         if (packed) p.kept = take((size_t)nx * (bf16 ? 2 : 4));
         if (p.dw.planes) p.x = take((size_t)nx * plane);
         if (p.dx.planes) p.w = take((size_t)nw * plane);
-        p.dz = take((size_t)nz * (p.dx.planes || p.dw.planes ? plane : bf16 ? 2 : 4));
+        p.dz = take((size_t)nz * (two ? 4 : p.dx.planes || p.dw.planes ? plane : bf16 ? 2 : 4));
         // few rows: one to a line of eight lanes, one block of them and no second launch for db
         p.across = 8;
         while (rows > 32 && p.across < 64 && p.across * 8 < p.ldz) p.across *= 2;
@@ -486,8 +526,9 @@ Work plan_of(int n, int rows, int in, int out, int bf16, bool grad, bool packed)
 template <typename T, int BM, int BN, int WM, int WN, bool AA, bool BA, class SA, class SB, class Epi>
 hipError_t launch_registers(const SA& a, const SB& b, int n, int M, int N, int K, const Shape& p, const Epi& epi, hipStream_t s)
 {
-    constexpr bool wide = SA::kPlanes == 3 || SB::kPlanes == 3;
-    constexpr int KS = BM == 32 ? (wide ? (BA ? 64 : 32) : 128) : BN == 128 && !wide ? 64 : 32, NBUF = wide || BM == 32 ? 1 : 2, AHEAD = wide && BM != 32 ? 1 : 2;
+    constexpr int P = std::max(SA::kPlanes, SB::kPlanes);
+    constexpr bool wide = P > 1;
+    constexpr int KS = BM == 32 ? (wide ? (BA ? 64 : 32) : 128) : P == 2 || (BN == 128 && !wide) ? 64 : 32, NBUF = wide || BM == 32 ? 1 : 2, AHEAD = wide && BM != 32 ? 1 : 2;
     constexpr unsigned kLds = NBUF * (SA::kPlanes * Image<AA, BM, KS>::kPlane + SB::kPlanes * Image<BA, BN, KS>::kPlane);
     if constexpr (Epi::kStaged) static_assert(WM * WN * Epi::template bytes<BN / WN / 32>() <= kLds, "the epilogue's blocks lie in the images");
     const int tm = (M + BM - 1) / BM, tn = (N + BN - 1) / BN;
@@ -498,14 +539,14 @@ hipError_t launch_registers(const SA& a, const SB& b, int n, int M, int N, int K
         <<<line_grid(die_grid(total), WM * WN * 64), WM * WN * 64, 0, s>>>(a, b, K, tm, tn, p.splits, p.len, (int)total, epi);
     return hipGetLastError();
 }
-template <int PL, int BM, int BN, int WM, int WN, bool AA, bool BA, class Epi>
+template <int PA, int PB, int BM, int BN, int WM, int WN, bool AA, bool BA, class Epi>
 hipError_t launch_planes(const Plane3& a, const Plane3& b, int n, int M, int N, int K, const Shape& p, const Epi& epi, hipStream_t s)
 {
     const int tm = (M + BM - 1) / BM, tn = (N + BN - 1) / BN;
     const long long total = (long long)n * p.splits * tm * tn;
     if (total == 0) return hipSuccess;
     if (total > 0x7fffff00ll) return hipErrorInvalidValue;
-    layer_planes_kernel<AA, BA, PL, BM, BN, WM, WN, Epi>
+    layer_planes_kernel<AA, BA, PA, PB, BM, BN, WM, WN, Epi>
         <<<line_grid(die_grid(total), WM * WN * 64), WM * WN * 64, 0, s>>>(a, b, K, tm, tn, p.splits, p.len, (int)total, epi);
     return hipGetLastError();
 }
@@ -520,15 +561,15 @@ template <typename T, class F> hipError_t whole_or_shares(const Shape& p, int n,
     finish_shares_kernel<T><<<line_grid((total + 255) / 256, 256), 256, 0, s>>>(share, p.splits, lines * ld, ld, total, finish);
     return hipGetLastError();
 }
-template <bool AA, bool BA, typename T>
+template <bool AA, bool BA, int PA, int PB, typename T>
 hipError_t planes_product(const Plane3& a, const Plane3& b, int n, int M, int N, int K, const Shape& p, const Finish<T>& finish, float* share, hipStream_t s)
 {
     return whole_or_shares<T>(p, n, M, N, finish, share, s, [&](const auto& epi) {
         if constexpr (sizeof(T) == 2) {
-            if (p.bm == 256) return launch_planes<1, 256, 256, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
-            if (p.bn == 256) return launch_planes<1, 128, 256, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
-            return launch_planes<1, 128, 128, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
-        } else return launch_planes<3, 128, 256, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
+            if (p.bm == 256) return launch_planes<PA, PB, 256, 256, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
+            if (p.bn == 256) return launch_planes<PA, PB, 128, 256, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
+            return launch_planes<PA, PB, 128, 128, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
+        } else return launch_planes<3, 3, 128, 256, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
     });
 }
 template <bool BA, typename T, class SA, class SB>
@@ -545,12 +586,15 @@ hipError_t registers_product(const SA& a, const SB& b, int n, int M, int N, int 
 {
     if constexpr (AA)
         if (p.few) return launch_few<BA, T>(a, b, n, M, N, K, finish, s);
+    constexpr bool two = SA::kPlanes == 2 || SB::kPlanes == 2;
     return whole_or_shares<T>(p, n, M, N, finish, share, s, [&](const auto& epi) {
-        if (p.bm == 128) return launch_registers<T, 128, 128, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
         if constexpr (AA)
             if (p.bm == 32) return launch_registers<T, 32, 128, 1, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
-        if (p.bn == 64) return launch_registers<T, 64, 64, 2, 2, AA, BA>(a, b, n, M, N, K, p, epi, s);
-        return launch_registers<T, 64, 128, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
+        if constexpr (!two) {
+            if (p.bm == 128) return launch_registers<T, 128, 128, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
+            if (p.bn == 128) return launch_registers<T, 64, 128, 2, 4, AA, BA>(a, b, n, M, N, K, p, epi, s);
+        }
+        return launch_registers<T, 64, 64, 2, 2, AA, BA>(a, b, n, M, N, K, p, epi, s);
     });
 }
 
@@ -606,7 +650,7 @@ hipError_t plane_of(const Rows& r, int n, int rows, int cols, void* at, Plane3& 
 template <typename T> hipError_t forward(const LayerArgs& a, hipStream_t s)
 {
     if (a.rows == 0) return hipSuccess;
-    const Work p = plan_of(a.n, a.rows, a.in, a.out, a.bf16, false, false);
+    const Work p = plan_of(a.n, a.rows, a.in, a.out, a.bf16, false, false, false);
     char* work = (char*)a.work;
     float* share = (float*)(work + p.share);
     const Finish<T> finish{(const float*)a.bias.p, a.bias.rep, a.residual, a.pre, a.y, a.rows, a.out, a.act, a.draws};
@@ -621,12 +665,30 @@ template <typename T> hipError_t forward(const LayerArgs& a, hipStream_t s)
         if ((e = lay_parts(px, pw, s)) != hipSuccess) return e;
         x = plane_of(px); w = plane_of(pw);
     }
-    return planes_product<true, false, T>(x, w, a.n, a.rows, a.out, a.in, p.y, finish, share, s);
+    return planes_product<true, false, 1, 1, T>(x, w, a.n, a.rows, a.out, a.in, p.y, finish, share, s);
 }
 
 // ---- gradient ---------------------------------------------------------------------------------------------------------------
-// dz = D'(dy) a'(pre), eight columns a lane, into [replicas][rows][ld] (PARTS = 1), its three bf16 parts into such planes (3) or nowhere (0), and the
-// column sums of a block's rows (16 x 1024 x 2048 bf16 with gelu: 39.7 us = 5.1 TB/s), a line of `ld` of them a block and sums_rep apart
+// Two bf16 parts of a float: its sign, exponent and first eight bits, and what is left, rounded.  Both have the float's sign, and neither is zero unless
+// the float is (a value that the first part holds whole gets 2^-20 of it as its second), so that their products with an infinity are the infinity that
+// the float's product is; an infinity or a NaN is both of its parts.
+__device__ __forceinline__ void parts2(const float (&v)[8], u4& high, u4& low)
+{
+    float rest[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float top = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, v[e]) & 0xffff0000u), left = v[e] - top;
+        rest[e] = left != left ? v[e] : left == 0.f ? top * 0x1p-20f : left;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        high[e] = __builtin_bit_cast(unsigned, v[2 * e]) >> 16 | (__builtin_bit_cast(unsigned, v[2 * e + 1]) & 0xffff0000u);
+        low[e] = to_bf16x2(rest[2 * e], rest[2 * e + 1]);
+    }
+}
+
+// dz = D'(dy) a'(pre), eight columns a lane, into [replicas][rows][ld] (PARTS = 1), its two or three bf16 parts into such planes (2, 3) or nowhere (0), and
+// the column sums of a block's rows (16 x 1024 x 2048 bf16 with gelu: 39.7 us = 5.1 TB/s), a line of `ld` of them a block and sums_rep apart
 // from replica to replica: db itself where one block has all rows.  A
 // dropped value is zero whatever dy and pre hold there.
 template <typename T, int PARTS>
@@ -655,6 +717,13 @@ __global__ __launch_bounds__(256) void slope_kernel(const T* dy, long long yrep,
             each8([&](int e) { if (c + e >= cols) v[e] = 0.f; sum[e] += v[e]; });
             const long long to = ((long long)k * rows + t) * ld + c;
             if constexpr (PARTS == 1) store_chunk((T*)dz + to, 8, v);
+            if constexpr (PARTS == 2) {
+                u4 high, low;
+                parts2(v, high, low);
+                __bf16* out = (__bf16*)dz + to;
+                *(u4*)out = high;
+                *(u4*)(out + plane) = low;
+            }
             if constexpr (PARTS == 3) {
                 u2 h[2], m[2], l[2];
                 parts3(f4{v[0], v[1], v[2], v[3]}, h[0], m[0], l[0]);
@@ -693,10 +762,19 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const float* sums, int
     db[k * rep + c] = v;
 }
 
+// whether dz of bf16 tensors takes two parts: ReLU's is dy or zero
+inline bool has_two_parts(int act, unsigned drop_limit) { return drop_limit || act == kGelu || act == kSilu; }
+template <bool TWO, class S> auto parted(const TwoParts& two, const S& one)
+{
+    if constexpr (TWO) return two;
+    else return one;
+}
+
 template <typename T> hipError_t backward(const LayerArgs& a, hipStream_t s)
 {
     constexpr bool half = sizeof(T) == 2;
-    const Work p = plan_of(a.n, a.rows, a.in, a.out, a.bf16, true, a.packed.q);
+    const bool two = half && has_two_parts(a.act, a.draws.limit);
+    const Work p = plan_of(a.n, a.rows, a.in, a.out, a.bf16, true, a.packed.q, two);
     char* work = (char*)a.work;
     float *share = (float*)(work + p.share), *sums = (float*)(work + p.sums);
     const bool want_dx = a.dx.p && a.rows, want_dw = a.dw.p, planes = (want_dx && p.dx.planes) || (want_dw && p.dw.planes);
@@ -706,7 +784,7 @@ template <typename T> hipError_t backward(const LayerArgs& a, hipStream_t s)
     const long long plane = (long long)a.n * a.rows * p.ldz;
     if (a.rows && (form || a.db.p)) {
         const dim3 grid((unsigned)((p.ldz + p.across * 8 - 1) / (p.across * 8)), (unsigned)p.blocks, (unsigned)a.n);
-        auto* kernel = !form ? slope_kernel<T, 0> : half || !planes ? slope_kernel<T, 1> : slope_kernel<T, half ? 1 : 3>;
+        auto* kernel = !form ? slope_kernel<T, 0> : half ? (two ? slope_kernel<T, half ? 2 : 1> : slope_kernel<T, 1>) : planes ? slope_kernel<T, half ? 1 : 3> : slope_kernel<T, 1>;
         kernel<<<grid, 256, 0, s>>>((const T*)a.dy.p, a.dy.rep, a.dy.row, (const T*)a.pre.p, a.pre.rep, a.pre.row, a.rows, a.out, p.ldz, p.across, p.depth,
                                     a.act, a.draws, work + p.dz, plane, p.blocks == 1 ? (float*)a.db.p : a.db.p ? sums : nullptr,
                                     p.blocks == 1 ? a.db.rep : (long long)p.blocks * p.ldz);
@@ -723,7 +801,8 @@ template <typename T> hipError_t backward(const LayerArgs& a, hipStream_t s)
     }
     const Rows z = there ? a.dy : Rows{work + p.dz, (long long)a.rows * p.ldz, p.ldz};
     const int wz = there ? a.out : p.ldz;
-    const Plane3 pz{(const __bf16*)z.p, z.rep, half ? 0 : plane, (int)z.row, a.rows, wz, nullptr};
+    const Plane3 pz{(const __bf16*)z.p, z.rep, half && !two ? 0 : plane, (int)z.row, a.rows, wz, nullptr};
+    const TwoParts tz{(const __bf16*)z.p, z.rep, z.row, a.rows, wz, plane};
     Plane3 px{}, pw{};
     if constexpr (half) {
         if (want_dw && p.dw.planes && (e = plane_of(x, a.n, a.rows, a.packed.q ? p.ldx : a.in, work + p.x, px, s)) != hipSuccess) return e;
@@ -735,22 +814,33 @@ template <typename T> hipError_t backward(const LayerArgs& a, hipStream_t s)
     }
     if (want_dx) {
         const Finish<T> finish = store_only<T>(a.dx, a.rows, a.in);
-        e = p.dx.planes ? planes_product<true, true, T>(pz, pw, a.n, a.rows, a.in, a.out, p.dx, finish, share, s)
-                        : registers_product<true, true, T>(source<T>(z, a.rows, wz), source<T>(a.w, a.in, a.out), a.n, a.rows, a.in, a.out, p.dx, finish, share, s);
+        const auto w = source<T>(a.w, a.in, a.out);
+        if (half && two)
+            e = p.dx.planes ? planes_product<true, true, half ? 2 : 1, 1, T>(pz, pw, a.n, a.rows, a.in, a.out, p.dx, finish, share, s)
+                            : registers_product<true, true, T>(parted<half>(tz, source<T>(z, a.rows, wz)), w, a.n, a.rows, a.in, a.out, p.dx, finish, share, s);
+        else
+            e = p.dx.planes ? planes_product<true, true, 1, 1, T>(pz, pw, a.n, a.rows, a.in, a.out, p.dx, finish, share, s)
+                            : registers_product<true, true, T>(source<T>(z, a.rows, wz), w, a.n, a.rows, a.in, a.out, p.dx, finish, share, s);
         if (e != hipSuccess) return e;
     }
     if (!want_dw) return hipSuccess;
     const Finish<T> finish = store_only<T>(a.dw, a.in, a.out);
-    if (p.dw.planes) return planes_product<false, false, T>(px, pz, a.n, a.in, a.out, a.rows, p.dw, finish, share, s);
-    return registers_product<false, false, T>(source<T>(x, a.rows, a.in), source<T>(z, a.rows, wz), a.n, a.in, a.out, a.rows, p.dw, finish, share, s);
+    const auto sx = source<T>(x, a.rows, a.in);
+    if (half && two) {
+        if (p.dw.planes) return planes_product<false, false, 1, half ? 2 : 1, T>(px, pz, a.n, a.in, a.out, a.rows, p.dw, finish, share, s);
+        return registers_product<false, false, T>(sx, parted<half>(tz, source<T>(z, a.rows, wz)), a.n, a.in, a.out, a.rows, p.dw, finish, share, s);
+    }
+    if (p.dw.planes) return planes_product<false, false, 1, 1, T>(px, pz, a.n, a.in, a.out, a.rows, p.dw, finish, share, s);
+    return registers_product<false, false, T>(sx, source<T>(z, a.rows, wz), a.n, a.in, a.out, a.rows, p.dw, finish, share, s);
 }
 
 }  // namespace
 
-size_t layer_work_bytes(int n, int rows, int in, int out, int bf16, bool grad)
+size_t layer_work_bytes(int n, int rows, int in, int out, int bf16, int act, float drop, bool grad)
 {
-    const size_t one = plan_of(n, rows, in, out, bf16, false, false).total;       // a workspace for the gradient serves the forward pass too
-    return grad ? std::max({one, plan_of(n, rows, in, out, bf16, true, false).total, plan_of(n, rows, in, out, bf16, true, true).total}) : one;
+    const size_t one = plan_of(n, rows, in, out, bf16, false, false, false).total;       // a workspace for the gradient serves the forward pass too
+    const bool two = bf16 && has_two_parts(act, drop_limit(drop));
+    return grad ? std::max({one, plan_of(n, rows, in, out, bf16, true, false, two).total, plan_of(n, rows, in, out, bf16, true, true, two).total}) : one;
 }
 hipError_t launch_layer_forward(const LayerArgs& a, hipStream_t s) { return a.bf16 ? forward<__bf16>(a, s) : forward<float>(a, s); }
 hipError_t launch_layer_backward(const LayerArgs& a, hipStream_t s) { return a.bf16 ? backward<__bf16>(a, s) : backward<float>(a, s); }

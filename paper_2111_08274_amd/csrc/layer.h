@@ -40,7 +40,7 @@ struct LayerArgs {
     Draws draws;
     void* work;
 };
-size_t layer_work_bytes(int n, int rows, int in, int out, int bf16, bool grad);
+size_t layer_work_bytes(int n, int rows, int in, int out, int bf16, int act, float drop, bool grad);
 hipError_t launch_layer_forward(const LayerArgs& a, hipStream_t s);
 hipError_t launch_layer_backward(const LayerArgs& a, hipStream_t s);
 

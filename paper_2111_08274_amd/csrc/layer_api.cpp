@@ -50,7 +50,7 @@ hadfl_status hadfl_layer_workspace(const hadfl_layer* layer, int32_t grad, size_
     return guarded([&]() -> hadfl_status {
     const std::string text = first({check_layer(layer), bytes ? "" : "bytes is null"});
     if (!text.empty()) return bad(text);
-    *bytes = std::max<size_t>(256, layer::layer_work_bytes(layer->n_replicas, layer->n_rows, layer->n_in, layer->n_out, layer->bf16, grad != 0));
+    *bytes = std::max<size_t>(256, layer::layer_work_bytes(layer->n_replicas, layer->n_rows, layer->n_in, layer->n_out, layer->bf16, layer->activation, layer->drop, grad != 0));
     return HADFL_OK;
     });
 }
