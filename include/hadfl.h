@@ -420,7 +420,7 @@ HADFL_API hadfl_status hadfl_dropout_rows(const hadfl_dropout *dropout, const ha
  *   z = x W + b,  y = residual + D(a(z)),  D the dropout above on [n_rows][n_out] with p = drop,
  *   a: HADFL_ACT_NONE z;  HADFL_ACT_RELU max(z, 0), its slope at 0 is 0;  HADFL_ACT_SILU z / (1 + e^-z);
  *      HADFL_ACT_GELU z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2.
- * With dz = D'(dy) a'(pre), D' the same values kept:
+ * With dz = D'(dy) a'(pre), D' the same values kept, and zero where ReLU is off, whatever dy holds there:
  *   dx = dz W^T,  dW = x^T dz,  db = sum_t dz;  the residual's gradient is dy.
  * fp32: operands enter the products as three bf16 parts, six products, whole for magnitudes from 2^-107 to below 3.39e38; an
  * infinity in a 32-bit operand makes NaN.  bf16: sums in 32 bits, outputs rounded once; the activation takes z before pre is

@@ -690,7 +690,7 @@ __device__ __forceinline__ void parts2(const float (&v)[8], u4& high, u4& low)
 // dz = D'(dy) a'(pre), eight columns a lane, into [replicas][rows][ld] (PARTS = 1), its two or three bf16 parts into such planes (2, 3) or nowhere (0), and
 // the column sums of a block's rows (16 x 1024 x 2048 bf16 with gelu: 39.7 us = 5.1 TB/s), a line of `ld` of them a block and sums_rep apart
 // from replica to replica: db itself where one block has all rows.  A
-// dropped value is zero whatever dy and pre hold there.
+// dropped value is zero whatever dy and pre hold there, one that ReLU has switched off whatever dy holds.
 template <typename T, int PARTS>
 __global__ __launch_bounds__(256) void slope_kernel(const T* dy, long long yrep, long long yrow, const T* pre, long long prep, long long prow, int rows, int cols,
                                                     int ld, int across, int depth, int act, Draws d, void* dz, long long plane, float* sums, long long sums_rep)
@@ -709,7 +709,7 @@ __global__ __launch_bounds__(256) void slope_kernel(const T* dy, long long yrep,
             in.get(v);
             if (act != kNone) {
                 at.get(z);
-                if (act == kRelu) each8([&](int e) { v[e] *= slope(z[e], kRelu); });
+                if (act == kRelu) each8([&](int e) { v[e] = relu_slope(v[e], z[e]); });
                 else if (act == kGelu) each8([&](int e) { v[e] *= slope(z[e], kGelu); });
                 else each8([&](int e) { v[e] *= slope(z[e], kSilu); });
             }

@@ -81,12 +81,12 @@ __device__ __forceinline__ float activate(float z, int act)
     if (act == kSilu) return z * sigmoid(z);
     return z;
 }
-// The activation's derivative: with E = e^-t, s = 1 / (1 + E) and 1 - s = E s, which loses nothing where s is almost one.  Where E would leave the
-// floats the curved ones are straight.
+// What ReLU passes on of v: nothing where it is off, whatever v holds.
+__device__ __forceinline__ float relu_slope(float v, float z) { return z > 0.f ? v : z == z ? 0.f : z; }
+// The curved activations' derivative: with E = e^-t, s = 1 / (1 + E) and 1 - s = E s, which loses nothing where s is almost one.  Where E would leave the
+// floats they are straight.
 __device__ __forceinline__ float slope(float z, int act)
 {
-    if (act == kRelu) return z > 0.f ? 1.f : z == z ? 0.f : z;
-    if (act == kNone) return 1.f;
     const float most = act == kSilu ? 80.f : 10.f;
     z = z > most ? most : z < -most ? -most : z;
     const float t = act == kSilu ? z : kGeluA * z * __builtin_fmaf(kGeluB * z, z, 1.f), along = act == kSilu ? z : kGeluA * z * __builtin_fmaf(3.f * kGeluB * z, z, 1.f);
