@@ -22,6 +22,9 @@ import json
 
 import numpy as np
 
+LOGITS = 1 << 28                   # that answers hold at once: 1 GiB of floats
+COLUMNS = 1 << 17                  # of a dense layer
+
 
 class Head:
     """Parameters of all replicas in rows [n, row_stride] (views into them), their gradients and the operators' plans."""
@@ -115,9 +118,18 @@ class Head:
         for i in range(self.blocks):
             a = self.up.forward(h, self.weights("u%d" % i), p["a%d" % i])
             h = hadfl.DenseLayer(self.n, self.batch, 2 * self.hidden, self.hidden, self.bf16, grad=False).forward(a, self.weights("v%d" % i), p["c%d" % i], residual=h)
-        y = self.norm.forward(h, p["gamma"], p["beta"], stats=False)
-        logits = hadfl.DenseLayer(self.n, self.batch, self.hidden, self.vocab, self.bf16, grad=False).forward(y, self.weights("w2"), p["b2"])
-        return hadfl.TokenScores(self.n, self.batch, self.vocab, n_tokens=tokens.shape[2], n_top=top, bf16=self.bf16).forward(logits, tokens)
+        y, w2 = self.norm.forward(h, p["gamma"], p["beta"], stats=False), self.weights("w2")
+        rows = max(1, min(self.batch, LOGITS // (self.n * self.vocab)))       # of the batch, whose logits are there at once
+        columns = -(-self.vocab // -(-self.vocab // COLUMNS))
+        outs = []
+        for at in range(0, max(1, self.batch), rows):
+            x, given = y[:, at:at + rows], tokens[:, at:at + rows].contiguous()
+            logits = self.torch.empty((self.n, x.shape[1], self.vocab), dtype=self.dtype, device=y.device)
+            for c in range(0, self.vocab, columns):
+                z = logits[:, :, c:c + columns]
+                hadfl.DenseLayer(self.n, x.shape[1], self.hidden, z.shape[2], self.bf16, grad=False).forward(x, w2[:, :, c:c + columns], p["b2"][:, c:c + columns], y=z)
+            outs.append(hadfl.TokenScores(self.n, x.shape[1], self.vocab, n_tokens=tokens.shape[2], n_top=top, bf16=self.bf16).forward(logits, given))
+        return outs[0] if len(outs) == 1 else tuple(None if q[0] is None else self.torch.cat(q, 1) for q in zip(*outs))
 
     def update(self, lr):
         self.rows.sub_(self.grads, alpha=lr)
