@@ -9,10 +9,10 @@ the last dense layer over the vocabulary,
     h = relu(x W1 + b1),   y = layer_norm(h; gamma, beta),   loss = cross_entropy(y W2 + b2, next token),
 
 x the fixed embedding of the last token.  With --blocks, h passes as many blocks h <- h + D(gelu(h U + a) V + c) before the norm, with --drop D
-drops values (and of x too), other ones in every step.  After the rounds the aggregated model answers tokens that it was not trained on: log
-probabilities of the right next ones, entropies and alternatives, from its logits.  A step is grouped over the replicas: what the backward pass needs of x and of h is kept in
-8 bits, the logits live in the loss's workspace alone, and a replica that has done its local steps of the round sits the others out with
-rows that have no label.  After the local steps the library selects replicas by their versions and aggregates their rows.
+drops values (and of x too), other ones in every step.  A step is grouped over the replicas: what the backward pass needs of x and of h
+is kept in 8 bits, the logits live in the loss's workspace alone, and a replica that has done its local steps of the round sits the others
+out with rows that have no label.  After the rounds the aggregated model answers freshly drawn tokens of the training distribution, whose
+right next ones have no noise: their log probabilities, entropies and alternatives, from its logits.  After the local steps the library selects replicas by their versions and aggregates their rows.
 
 Tokens are synthetic: the next token is a fixed permutation of the last one, replaced by a uniform one with probability 1/8;
 replica k sees mostly tokens of its own part of the vocabulary (shards that differ, as the method's devices do).
