@@ -696,8 +696,8 @@ class Dropout(_Drawing):
 
 class DenseLayer(_Drawing):
     """y = residual + dropout(activation(x w + bias)): x [n_replicas, n_rows, n_in], w [n_replicas, n_in, n_out], bias [n_replicas, n_out]
-    (32-bit) or None, residual and y [n_replicas, n_rows, n_out]; activation one of ACTIVATIONS, drop the probability of
-    dropping.  What backward() needs of the forward pass is `pre`, a tensor like y for x w + bias, and the same seed, call and counter."""
+    (32-bit) or None, residual and y [n_replicas, n_rows, n_out]; activation one of ACTIVATIONS ("gelu" is the tanh form, z (1 +
+    tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2, not the one of the error function), drop the probability of dropping.  What backward() needs of the forward pass is `pre`, a tensor like y for x w + bias, and the same seed, call and counter."""
 
     def __init__(self, n_replicas, n_rows, n_in, n_out, bf16=0, activation="none", drop=0.0, grad=True):
         self.n, self.rows, self.n_in, self.n_out, bf16 = _int32(n_replicas, n_rows, n_in, n_out, bf16)
