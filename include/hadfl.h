@@ -425,7 +425,7 @@ HADFL_API hadfl_status hadfl_dropout_rows(const hadfl_dropout *dropout, const ha
  * fp32: operands enter the products as three bf16 parts, six products, whole for magnitudes from 2^-107 to below 3.39e38; an
  * infinity in a 32-bit operand makes NaN.  bf16: sums in 32 bits, outputs rounded once; the activation takes z before pre is
  * rounded; a dz that is no bf16 value (GELU, SiLU, dropout) enters the two products as two bf16 parts, off by 2^-15 of a value at
- * most, which doubles their operations; db is formed from it as it is.
+ * most from 2^-111 on, which doubles their operations; db is formed from it as it is.
  *   x (t)               dev, [n_replicas][n_rows][n_in]
  *   w (t)               dev, [n_replicas][n_in][n_out], the layout of a dense layer here
  *   bias                dev or NULL, [n_replicas][n_out] floats
@@ -438,7 +438,9 @@ HADFL_API hadfl_status hadfl_dropout_rows(const hadfl_dropout *dropout, const ha
  *   y (t)               dev out, [n_replicas][n_rows][n_out]
  *   dx (t), dw (t), db  dev out, like x, w, bias; each may be NULL and is then not computed.  Outputs do not overlap inputs
  *   work                dev, 256-byte aligned; hadfl_layer_workspace with grad = 1 serves both calls, with grad = 0 the forward
- *                       call alone */
+ *                       call alone.  It holds x and w as the products of large layers take them (reserved also where bf16 tensors
+ *                       are read as they lie: 403 MB for the forward call of 4 x 8192 x 4096 x 4096), for the gradient dz, and shares
+ *                       of the products; layers whose calls follow one another may have one, as large as the largest asks for */
 typedef enum { HADFL_ACT_NONE = 0, HADFL_ACT_RELU = 1, HADFL_ACT_GELU = 2, HADFL_ACT_SILU = 3 } hadfl_activation;
 typedef struct { int32_t n_replicas, n_rows, n_in, n_out, bf16, activation; float drop; } hadfl_layer;
 HADFL_API hadfl_status hadfl_layer_workspace(const hadfl_layer *layer, int32_t grad, size_t *bytes);

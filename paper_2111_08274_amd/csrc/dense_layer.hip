@@ -3,7 +3,7 @@
 //              gradient where that is asked for
 //   gradient   dz = D'(dy) a'(pre) and its column sums db in one pass over dy, then dx = dz W^T and dW = x^T dz
 // bf16: a dz that is no bf16 value (a curved activation, a dropout's scale) enters the two products as two bf16 parts, off by 2^-15 of a value at
-// most; db is summed before that.  fp32: operands enter as three bf16 parts, six products.
+// most (from 2^-111 on, where the second part is a normal number); db is summed before that.  fp32: operands enter as three bf16 parts, six products.
 #include "direct_product.h"
 #include "layer.h"
 

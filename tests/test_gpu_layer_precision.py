@@ -103,3 +103,16 @@ def test_infinite_operands_of_a_bf16_gradient(rows):
         dx, dw, db = plan.backward(dy, x.clamp(-1, 1), w.clamp(-1, 1).abs(), pre=pre, call=call)
         assert bool((dx[0, 3] == float("inf")).all()) and bool((dw[0, :5, 4] == float("inf")).all()) and db[0, 4] == float("inf")
         assert bool(torch.isfinite(dx[0, :3]).all()) and bool(torch.isfinite(dw[0, :, 5:]).all())
+
+
+@pytest.mark.parametrize("rows", [20, 300])
+def test_small_and_large_magnitudes_of_a_bf16_gradient(rows):
+    # the second part is no smaller than a normal number, the first no larger than the largest: bounds as everywhere
+    n, i, o = 2, 96, 136
+    for e, f in ((-100, 80), (90, -70)):
+        c = _layer_case(n, rows, i, o, 1, "whole", seed=7)
+        dy, x, w = c["dy"] * 2.0 ** e, c["x"] * 2.0 ** f, c["w"] * 2.0 ** f
+        dx, dw, db = hadfl.DenseLayer(n, rows, i, o, bf16=1, activation="silu", drop=0.1).backward(dy, x, w, pre=c["pre"], seed=SEED, call=CALL)
+        want, bound = _grad(_values(dy), _values(c["pre"]), _values(x), _values(w), "silu", 0.1, SEED, CALL)
+        for name, got in (("db", db), ("dx", dx), ("dw", dw)):
+            _check(_values(got), want[name], bound[name], name)
