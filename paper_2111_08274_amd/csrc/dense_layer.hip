@@ -173,7 +173,8 @@ struct TwoParts {
 // barrier that frees a slab's image and says that the next one has arrived lies before the slab's last step, whose operands are in registers by then, so
 // that the matrix cores have work while the first operands of the next slab are read.  4 x 8192 rows x 4096 x 4096 bf16 with bias and dropout onto a
 // residual: 1001 us = 1098 TFLOP/s, the matrix cores busy 57 to 58 % of the time; the product alone 944.  The library's product 858, 70 % busy, at no
-// higher clock (both 1.4 to 1.8 GHz over twelve launches in a row).
+// higher clock (both 1.4 to 1.8 GHz over twelve launches in a row).  Two parts against one plane: dx of 16 x 1024 x 512 x 2048 71 us, dW 63 (of one part
+// 44 and 40): an operand read for two products, the matrix cores busy 45 and 55 % of the time.
 template <bool A_ALONG, bool B_ALONG, int PA, int PB, int BM, int BN, int WM, int WN, class Epi>
 __global__ __launch_bounds__(WM * WN * 64) void layer_planes_kernel(Plane3 a, Plane3 b, int K, int tiles_m, int tiles_n, int splits, int split_len, int total, Epi epi)
 {
@@ -690,7 +691,7 @@ __device__ __forceinline__ void parts2(const float (&v)[8], u4& high, u4& low)
 }
 
 // dz = D'(dy) a'(pre), eight columns a lane, into [replicas][rows][ld] (PARTS = 1), its two or three bf16 parts into such planes (2, 3) or nowhere (0), and
-// the column sums of a block's rows (16 x 1024 x 2048 bf16 with gelu: 39.7 us = 5.1 TB/s), a line of `ld` of them a block and sums_rep apart
+// the column sums of a block's rows (16 x 1024 x 2048 bf16 with gelu, two parts: 48 us = 5.6 TB/s), a line of `ld` of them a block and sums_rep apart
 // from replica to replica: db itself where one block has all rows.  A
 // dropped value is zero whatever dy and pre hold there, one that ReLU has switched off whatever dy holds.
 template <typename T, int PARTS>
@@ -764,7 +765,8 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const float* sums, int
     db[k * rep + c] = v;
 }
 
-// whether dz of bf16 tensors takes two parts: ReLU's is dy or zero
+// Whether dz of bf16 tensors takes two parts: ReLU's is dy or zero.  Rounded to one, dz adds an error of 1.6e-3 of their norm to dx and dW, as much as their
+// own rounding; two parts add none that shows, and cost twice the operations (dx and dW of 8192 x 4096 x 4096 866 us, of one part 469).
 inline bool has_two_parts(int act, unsigned drop_limit) { return drop_limit || act == kGelu || act == kSilu; }
 template <bool TWO, class S> auto parted(const TwoParts& two, const S& one)
 {
