@@ -116,3 +116,19 @@ def test_small_and_large_magnitudes_of_a_bf16_gradient(rows):
         want, bound = _grad(_values(dy), _values(c["pre"]), _values(x), _values(w), "silu", 0.1, SEED, CALL)
         for name, got in (("db", db), ("dx", dx), ("dw", dw)):
             _check(_values(got), want[name], bound[name], name)
+
+
+def test_a_bf16_gradient_of_no_rows_repeats_and_of_each_alone():
+    torch = _torch()
+    for i, o in ((96, 136), (3, 136), (96, 5), (512, 2048)):
+        plan = hadfl.DenseLayer(2, 0, i, o, bf16=1, activation="gelu", drop=0.2)
+        t = lambda *s: torch.randn(s, device="cuda").bfloat16()  # noqa: E731
+        dx, dw, db = plan.backward(t(2, 0, o), t(2, 0, i), t(2, i, o), pre=t(2, 0, o))
+        assert dx.shape == (2, 0, i) and not dw.any() and not db.any()
+        for rows in (1, 40, 300):
+            c = _layer_case(2, rows, i, o, 1, "odd", seed=3)
+            plan = hadfl.DenseLayer(2, rows, i, o, bf16=1, activation="gelu", drop=0.2)
+            whole = plan.backward(c["dy"], c["x"], c["w"], pre=c["pre"], seed=1)
+            for k, name in enumerate(("dx", "dw", "db")):
+                got = plan.backward(c["dy"], c["x"] if name == "dw" else None, c["w"] if name == "dx" else None, pre=c["pre"], want=(name,), seed=1)
+                assert torch.equal(got[k], whole[k])
